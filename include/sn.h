@@ -442,6 +442,184 @@ int32_t sn_adamw_step(void *W, int64_t ldw, const void *G, int64_t ldg, int32_t 
                       void *workspace, size_t workspace_bytes, sn_stream stream);
 
 /* ------------------------------------------------------------------------ */
+/* Token log probabilities: what the last stage answers with and learns from. */
+/*                                                                            */
+/* Z (N x V) holds a row of logits per token, scale c > 0 the inverse         */
+/* temperature.  With m = max z, x = c (z - m), S = sum e^x and L = log S:    */
+/*   log p_j = x_j - L,   H = -sum_j p_j log p_j                              */
+/* logp[i] is log p of the row's given token tok[i]; tok[i] = -1 marks a row  */
+/* without one (padding): logp 0, and no gradient flows through it.           */
+/* A logit of -inf is a forbidden token: p = 0, log p = -inf, 0 log 0 = 0.    */
+/* A row whose logits are all -inf has p = 0 throughout: logp -inf, H 0,      */
+/* stats (-inf, -inf).  A row that holds NaN or +inf has no distribution:     */
+/* logp, entropy, stats, top_logp and gradients are NaN, top_id -1.           */
+/* Sums are float32; scale lies in [2^-20, 2^20], V < 2^31.                   */
+/* ------------------------------------------------------------------------ */
+
+/* Largest number of alternatives a call reports for a row. */
+#define SN_MAX_TOP 64
+
+/* sn_token_logprobs
+ *
+ *   Z         N x V logits (dt), row stride ldz >= V
+ *   tok       int32[N] given tokens, or NULL: logp is not written (may be NULL).
+ *             Ids outside [-1, V) are clamped and reported in bit 0 of *err_flag
+ *   logp      float[N], log p of the given tokens
+ *   entropy   float[N], H
+ *   stats     float[2 N], the rows' (m, L): what the backward call reads.
+ *             log sum_j e^(c z_j) = c m + L
+ *   n_top     alternatives per row, 0 <= n_top <= min(V, SN_MAX_TOP)
+ *   top_logp, top_id   N x n_top (contiguous, float and int32; unused when
+ *             n_top == 0): the largest logits' log p and ids, in descending
+ *             order, the lower id first among equals
+ * Outputs may not overlap Z, tok or each other.  Errors: NULL, SHAPE, DTYPE,
+ * ALIGN, ALIAS, UNSUPPORTED (n_top > SN_MAX_TOP), HIP. */
+int32_t sn_token_logprobs(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
+                          double scale, const int32_t *tok, float *logp, float *entropy,
+                          float *stats, int32_t n_top, float *top_logp, int32_t *top_id,
+                          int32_t *err_flag, sn_stream stream);
+
+/* sn_token_logprobs_backward: for given gradients gl of logp and gh of the
+ * entropy,  dZ_j = c (gl (d_jt - p_j) - gh p_j (log p_j + H)).
+ *
+ *   Z, N, V, ldz, dt, scale, tok   as in the forward call
+ *   stats, entropy   as the forward call wrote them (entropy may be NULL when
+ *             g_entropy is)
+ *   g_logp    float[N] or NULL (0); needs tok
+ *   g_entropy float[N] or NULL (0)
+ *   dZ        N x V gradient (dt), row stride lddz >= V.  May be Z itself (same
+ *             pointer and stride), else may not overlap an input
+ * A row whose gradients are both 0 (or whose token is -1, with g_entropy 0)
+ * gets zeros and its logits are not read.  Errors: NULL, SHAPE, DTYPE, ALIGN,
+ * ALIAS, HIP. */
+int32_t sn_token_logprobs_backward(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
+                                   double scale, const int32_t *tok, const float *stats,
+                                   const float *entropy, const float *g_logp,
+                                   const float *g_entropy, void *dZ, int64_t lddz,
+                                   int32_t *err_flag, sn_stream stream);
+
+/* sn_token_loss: log probabilities and gradient in one call, where the weights
+ * are known before it: the loss is -sum_i weight[i] logp[i] and
+ *   dZ[i, j] = weight[i] c (p_j - d_jt).
+ *
+ *   Z, N, V, ldz, dt, scale   as above
+ *   tok       int32[N] given tokens, as above (required)
+ *   weight    float[N], or NULL: 1
+ *   logp      float[N] (unweighted)
+ *   dZ        N x V (dt), row stride lddz >= V; may be Z itself, as above
+ * A row of weight 0 or without a token gets zeros, whatever its logits.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, HIP. */
+int32_t sn_token_loss(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt, double scale,
+                      const int32_t *tok, const float *weight, float *logp, void *dZ,
+                      int64_t lddz, int32_t *err_flag, sn_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Root-mean-square norm with the residual's addition.                        */
+/*                                                                            */
+/*   h = x + r,   y = h w / sqrt(mean_j h_j^2 + eps)                          */
+/* over rows of d columns, in float32; h is rounded to dt where it is stored, */
+/* and y is made from the sum before that rounding.                           */
+/* ------------------------------------------------------------------------ */
+
+/* sn_rmsnorm
+ *
+ *   X         N x d (dt), row stride ldx >= d
+ *   R         N x d residual (dt), row stride ldr >= d, or NULL: h = x
+ *   w         d gains (dt), or NULL: 1
+ *   eps       finite, >= 0
+ *   H         N x d (dt), row stride ldh >= d, receives h; or NULL.  May be X or
+ *             R itself (same pointer and stride), else may not overlap an input
+ *   Y         N x d (dt), row stride ldy >= d; may not overlap anything
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, HIP. */
+int32_t sn_rmsnorm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *R,
+                   int64_t ldr, const void *w, double eps, void *H, int64_t ldh, void *Y,
+                   int64_t ldy, sn_stream stream);
+
+/* sn_rmsnorm_quant: sn_rmsnorm with y in 8 bits (e4m3: sign, 4 exponent, 3
+ * mantissa bits, largest value 448, no infinities), y ~ q s:
+ *
+ *   group     0: one scale per row; 128: one for each 128 columns (the last
+ *             ones may be fewer)
+ *   Q         N x d bytes, row stride ldq >= d; may not overlap anything
+ *   S         float scales, N x (group ? ceil(d / 128) : 1), row stride lds:
+ *             s = max(max |y|, 2^-100) / 448 over the scale's columns
+ * q is y / s rounded to nearest even.  Columns of a scale that hold a NaN are
+ * NaN throughout, and so is their scale.  Other arguments and errors as
+ * sn_rmsnorm, and UNSUPPORTED for another group. */
+int32_t sn_rmsnorm_quant(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
+                         const void *R, int64_t ldr, const void *w, double eps, void *H,
+                         int64_t ldh, int32_t group, void *Q, int64_t ldq, float *S, int64_t lds,
+                         sn_stream stream);
+
+/* Workspace bytes of sn_rmsnorm_backward (0 if invalid; needed with gw only). */
+size_t sn_rmsnorm_backward_workspace_bytes(int64_t N, int64_t d, int32_t dt);
+
+/* sn_rmsnorm_backward: with u = dy w and rho = 1 / sqrt(mean h^2 + eps),
+ *   dX = rho u - h rho^3 mean(u h) + dH,      gw += sum over rows of dy h rho.
+ *
+ *   H         N x d, the forward call's h (dt; without a residual its X)
+ *   dY        N x d gradient of y (dt; of the 8-bit form: of the values q s)
+ *   w         d gains (dt), or NULL: 1
+ *   dH        N x d gradient that flows into h from elsewhere (dt), or NULL: 0
+ *   dX        N x d (dt), the gradient of X and of R alike; may be dY or dH
+ *             itself (same pointer and stride), else may not overlap an input
+ *   gw        d float32, ACCUMULATED into, or NULL
+ *   workspace sn_rmsnorm_backward_workspace_bytes(N, d, dt) bytes, 256-byte
+ *             aligned; may be NULL without gw
+ * Deterministic: rows are added in a fixed order, float32 within a workgroup
+ * and float64 over workgroups.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS,
+ * WORKSPACE, HIP. */
+int32_t sn_rmsnorm_backward(const void *H, int64_t N, int64_t d, int64_t ldh, int32_t dt,
+                            const void *dY, int64_t lddy, const void *w, double eps,
+                            const void *dH, int64_t lddh, void *dX, int64_t lddx, float *gw,
+                            void *workspace, size_t workspace_bytes, sn_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Global gradient norm and clipping (before the optimizer steps).            */
+/*                                                                            */
+/*   sumsq = sum of g^2 over every element of every tensor                    */
+/*   g <- g * f,  f = 1 where sqrt(sumsq) <= max_norm, else max_norm / sqrt   */
+/* Two calls: where a model is cut into stages or shards, the sums are added  */
+/* over the ranks between them.                                               */
+/* ------------------------------------------------------------------------ */
+
+/* One gradient: rows x cols, row stride ld >= cols (elements), element type
+ * dt.  A tensor without gaps may be given as one row; cols < 2^40, rows < 2^31. */
+typedef struct sn_tensor {
+  void *data;
+  int64_t rows, cols, ld;
+  int32_t dt;
+} sn_tensor;
+
+/* Workspace bytes of sn_grad_sumsq for these tensors (a HOST array; 0 if
+ * invalid).  Only the shapes are read. */
+size_t sn_grad_sumsq_workspace_bytes(int32_t count, const sn_tensor *grads);
+
+/* sn_grad_sumsq: *sumsq = sum of squares, in float64.
+ *   grads     HOST array of count >= 0 tensors of any of the dtypes, mixed;
+ *             tensors without elements are skipped, none gives 0
+ *   sumsq     device double (8-byte aligned), written
+ *   workspace sn_grad_sumsq_workspace_bytes(count, grads) bytes, 256-byte aligned
+ * Deterministic.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, WORKSPACE, HIP. */
+int32_t sn_grad_sumsq(int32_t count, const sn_tensor *grads, double *sumsq, void *workspace,
+                      size_t workspace_bytes, sn_stream stream);
+
+/* sn_grad_clip
+ *   grads     HOST array of count >= 0 tensors, as above
+ *   out       HOST array of count tensors of the same rows, cols and dtypes that
+ *             receive the products, or NULL: in place (each out[i] is grads[i]
+ *             itself or overlaps no gradient).  In place, nothing is written
+ *             when the factor is 1
+ *   sumsq     device double: sn_grad_sumsq's, or the ranks' sum of them
+ *   max_norm  >= 0 (+inf: never scales)
+ *   norm      device float or NULL, receives sqrt(*sumsq)
+ * The factor follows IEEE arithmetic: an infinite norm gives 0 (and NaN for
+ * infinite gradients), a NaN norm makes every gradient NaN.  No two outputs may
+ * overlap.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, HIP. */
+int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out,
+                     const double *sumsq, double max_norm, float *norm, sn_stream stream);
+
+/* ------------------------------------------------------------------------ */
 /* Diagnostics.                                                               */
 /* ------------------------------------------------------------------------ */
 

@@ -18,7 +18,9 @@ the output dtype with round-to-nearest-even:
 The subspace update of Section 4.5 (off-subspace loss, accumulation matrix,
 Riemannian gradient, QR retraction) is in ``grassmann``; the modified AdamW
 step of Section 5 in ``adamw``; the trainable low-rank token table of
-Section 4.3.1 in ``embed``.
+Section 4.3.1 in ``embed``.  What a training step needs around them is in
+``logprobs`` (token log probabilities and their gradients), ``rmsnorm`` and
+``clip`` (gradient norm and clipping).
 
 ``exact`` holds the same operations in exact rational arithmetic
 (``fractions.Fraction``) for brute-force checks on tiny inputs.
@@ -26,8 +28,8 @@ Section 4.3.1 in ``embed``.
 from .bf16 import decode_bf16, encode_bf16, round_bf16, round_f32, round_to
 from .codec import (compress, decompress, grad_compress, grad_decompress,
                     project_weights, default_positions)
-from . import adamw, embed, grassmann
+from . import adamw, clip, embed, grassmann, logprobs, rmsnorm
 
 __all__ = ["decode_bf16", "encode_bf16", "round_bf16", "round_f32", "round_to",
            "compress", "decompress", "grad_compress", "grad_decompress",
-           "project_weights", "default_positions", "grassmann", "adamw", "embed"]
+           "project_weights", "default_positions", "grassmann", "adamw", "embed", "logprobs", "rmsnorm", "clip"]

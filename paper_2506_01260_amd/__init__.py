@@ -24,11 +24,24 @@ built the first call raises ``RuntimeError``.
     U2 = sn_grassmann_step(basis, state, eta)        # every few hundred iterations
 
     sn_adamw_step(W2, grad, M, V, t, lr, weight_decay=wd)   # modified AdamW (Sec. 5)
+
+    Y, H = sn_rmsnorm(X, w, residual=R)              # a block's norm, H = X + R
+    Q, S, H = sn_rmsnorm_quant(X, w, residual=R)     # the same with Y in 8 bits
+    dX = sn_rmsnorm_backward(H, dY, w, dH=dH, gw=gw) # gw += the gain's gradient
+
+    logp, dZ = sn_token_loss(logits, tok, weight=wt) # the last stage's loss and gradient
+    r = sn_token_logprobs(logits, tok, n_top=5)      # scoring: r.logp, r.entropy, r.top_id, ...
+    dZ = sn_token_logprobs_backward(logits, r.stats, r.entropy, tok, g_logp=gl)
+
+    total = sn_grad_sumsq(grads)                     # float64; add it over the ranks
+    norm = sn_grad_clip(grads, total, max_norm)      # in place, before the optimizer steps
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -50,6 +63,14 @@ _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
 _SZ = ctypes.c_size_t
+
+class _Tensor(ctypes.Structure):
+    """sn_tensor of include/sn.h."""
+    _fields_ = [("data", _P), ("rows", _I64), ("cols", _I64), ("ld", _I64), ("dt", _I32)]
+
+
+_F64 = ctypes.c_double
+_TENSORS = ctypes.POINTER(_Tensor)
 
 _SIGNATURES = {
     "sn_basis_packed_bytes": (_SZ, [_I64, _I64, _I32]),
@@ -85,6 +106,20 @@ _SIGNATURES = {
     "sn_adamw_step": (_I32, [_P, _I64, _P, _I64, _I32, _P, _P, _I64, _I64, _I64, _I64,
                              ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                              ctypes.c_double, _I32, _P, _SZ, _P]),
+    "sn_token_logprobs": (_I32, [_P, _I64, _I64, _I64, _I32, _F64, _P, _P, _P, _P, _I32, _P, _P,
+                                 _P, _P]),
+    "sn_token_logprobs_backward": (_I32, [_P, _I64, _I64, _I64, _I32, _F64, _P, _P, _P, _P, _P, _P,
+                                          _I64, _P, _P]),
+    "sn_token_loss": (_I32, [_P, _I64, _I64, _I64, _I32, _F64, _P, _P, _P, _P, _I64, _P, _P]),
+    "sn_rmsnorm": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _I64, _P, _F64, _P, _I64, _P, _I64, _P]),
+    "sn_rmsnorm_quant": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _I64, _P, _F64, _P, _I64, _I32, _P,
+                                _I64, _P, _I64, _P]),
+    "sn_rmsnorm_backward_workspace_bytes": (_SZ, [_I64, _I64, _I32]),
+    "sn_rmsnorm_backward": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _I64, _P, _F64, _P, _I64, _P,
+                                   _I64, _P, _P, _SZ, _P]),
+    "sn_grad_sumsq_workspace_bytes": (_SZ, [_I32, _TENSORS]),
+    "sn_grad_sumsq": (_I32, [_I32, _TENSORS, _P, _P, _SZ, _P]),
+    "sn_grad_clip": (_I32, [_I32, _TENSORS, _TENSORS, _P, _F64, _P, _P]),
     "sn_status_string": (ctypes.c_char_p, [_I32]),
     "sn_last_error": (ctypes.c_char_p, []),
     "sn_version": (ctypes.c_char_p, []),
@@ -708,6 +743,336 @@ def sn_adamw_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, V: torch.Te
                                workspace.data_ptr() if need else None, need,
                                _stream(stream)))
     return W
+
+
+# ---------------------------------------------------------------------------
+# token log probabilities, norms, gradient clipping
+# ---------------------------------------------------------------------------
+def _on(stream, *tensors):
+    """The context that a call allocates in: memory for work on `stream` comes from
+    that stream's pool, so that it is not given away while the work runs.  Every
+    tensor has to lie on the current device, where the call launches."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != dev:
+            raise SnError(2, f"a tensor lies on {t.device}, the current device is {dev}")
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _vec(t, name, n, dtype=torch.float32):
+    """Pointer of a contiguous device vector of n values (None stays None)."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or \
+            (n > 1 and t.stride(0) != 1):
+        raise SnError(2, f"{name} must be a contiguous {dtype} device vector of length {n}")
+    return t.data_ptr()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class TokenLogprobs(NamedTuple):
+    """What sn_token_logprobs returns; float32 device tensors (top_id: int32)."""
+    logp: Optional[torch.Tensor]      # (N,) log p of the given tokens; None without tokens
+    entropy: torch.Tensor             # (N,)
+    stats: torch.Tensor               # (N, 2): largest logit, log of the sum (for the backward)
+    top_logp: Optional[torch.Tensor]  # (N, n_top), descending; None with n_top = 0
+    top_id: Optional[torch.Tensor]    # (N, n_top)
+
+
+def _tokens(tok, name, n):
+    if tok is None:
+        raise SnError(1, f"{name} is required")
+    return _ids(tok, name, n)
+
+
+def sn_token_logprobs(Z: torch.Tensor, tok=None, n_top: int = 0, scale: float = 1.0,
+                      err_flag=None, stream=None) -> TokenLogprobs:
+    """Log probabilities of the tokens tok (-1: none in this row) under the logits
+    Z (N x V) times scale, each row's entropy, and its n_top largest logits."""
+    native = _native()
+    if native is not None:
+        r = native.token_logprobs(Z, tok, n_top, scale, err_flag, stream)
+        if r is not None:
+            return TokenLogprobs(*r)
+    zp, N, V, ldz = _mat(Z, "Z")
+    dt, n_top = _dt(Z), int(n_top)
+    tok_ptr = _ids(tok, "tok", N)
+    with _on(stream, Z, tok, err_flag):
+        def new(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=Z.device)
+        logp = None if tok is None else new(N)
+        entropy, stats = new(N), new(N, 2)
+        top_logp = top_id = None
+        if n_top > 0:
+            top_logp, top_id = new(N, n_top), new(N, n_top, dtype=torch.int32)
+        flag, own = _id_flag(err_flag, Z.device)
+        _check(lib().sn_token_logprobs(zp, N, V, ldz, dt, float(scale), tok_ptr, _ptr(logp),
+                                       entropy.data_ptr(), stats.data_ptr(), n_top, _ptr(top_logp),
+                                       _ptr(top_id), _ptr(flag), _stream(stream)))
+        _id_check(own, err_flag, "sn_token_logprobs")
+    return TokenLogprobs(logp, entropy, stats, top_logp, top_id)
+
+
+def _dlogits(Z, out):
+    """(gradient's tensor, pointer, row stride) of a call on logits."""
+    if out is None:
+        out = torch.empty(Z.shape, dtype=Z.dtype, device=Z.device)
+    _out_shape(out, Z.shape, "out")
+    if out.dtype != Z.dtype:
+        raise SnError(3, f"out must be {Z.dtype}, as Z")
+    op, _, _, ld = _mat(out, "out")
+    return out, op, ld
+
+
+def sn_token_logprobs_backward(Z: torch.Tensor, stats: torch.Tensor, entropy=None, tok=None,
+                               g_logp=None, g_entropy=None, scale: float = 1.0, out=None,
+                               err_flag=None, stream=None) -> torch.Tensor:
+    """dZ from the gradients of logp and entropy, with the forward call's stats and
+    entropy; out may be Z."""
+    native = _native()
+    if native is not None:
+        dZ = native.token_logprobs_backward(Z, stats, entropy, tok, g_logp, g_entropy, scale, out,
+                                            err_flag, stream)
+        if dZ is not None:
+            return dZ
+    zp, N, V, ldz = _mat(Z, "Z")
+    dt = _dt(Z)
+    if not stats.is_cuda or stats.dtype != torch.float32 or tuple(stats.shape) != (N, 2) or \
+            not stats.is_contiguous():
+        raise SnError(2, f"stats must be a contiguous float32 device tensor of shape {(N, 2)}")
+    args = (_ids(tok, "tok", N), stats.data_ptr(), _vec(entropy, "entropy", N),
+            _vec(g_logp, "g_logp", N), _vec(g_entropy, "g_entropy", N))
+    with _on(stream, Z, stats, entropy, tok, g_logp, g_entropy, out, err_flag):
+        out, op, ldo = _dlogits(Z, out)
+        flag, own = _id_flag(err_flag, Z.device)
+        _check(lib().sn_token_logprobs_backward(zp, N, V, ldz, dt, float(scale), *args, op, ldo,
+                                                _ptr(flag), _stream(stream)))
+        _id_check(own, err_flag, "sn_token_logprobs_backward")
+    return out
+
+
+def sn_token_loss(Z: torch.Tensor, tok: torch.Tensor, weight=None, scale: float = 1.0, out=None,
+                  err_flag=None, stream=None):
+    """(logp, dZ): the tokens' log probabilities, and the gradient of the loss
+    -sum weight logp for the logits; out (dZ) may be Z."""
+    native = _native()
+    if native is not None:
+        r = native.token_loss(Z, tok, weight, scale, out, err_flag, stream)
+        if r is not None:
+            return r
+    zp, N, V, ldz = _mat(Z, "Z")
+    dt = _dt(Z)
+    args = (_tokens(tok, "tok", N), _vec(weight, "weight", N))
+    with _on(stream, Z, tok, weight, out, err_flag):
+        out, op, ldo = _dlogits(Z, out)
+        logp = torch.empty(N, dtype=torch.float32, device=Z.device)
+        flag, own = _id_flag(err_flag, Z.device)
+        _check(lib().sn_token_loss(zp, N, V, ldz, dt, float(scale), *args, logp.data_ptr(), op,
+                                   ldo, _ptr(flag), _stream(stream)))
+        _id_check(own, err_flag, "sn_token_loss")
+    return logp, out
+
+
+def _same_as(X, *tensors, shape=True):
+    """Tensors of X's dtype (and shape); None passes."""
+    for name, t in tensors:
+        if t is None:
+            continue
+        if t.dtype != X.dtype:
+            raise SnError(3, f"{name} must be {X.dtype}, as the input")
+        if shape:
+            _out_shape(t, X.shape, name)
+
+
+def _gains(w, X, d):
+    if w is not None and w.dtype != X.dtype:
+        raise SnError(3, f"w must be {X.dtype}, as the input")
+    return _vec(w, "w", d, X.dtype)
+
+
+def _norm_inputs(X, w, residual, resid_out):
+    """(X, N, d, ldx, dt, R, ldr, w) of a norm call, and its H: resid_out, a new
+    tensor where there is a residual, or X itself (None to the library)."""
+    xp, N, d, ldx = _mat(X, "X")
+    dt = _dt(X)
+    _same_as(X, ("residual", residual), ("resid_out", resid_out))
+    rp = ldr = 0
+    if residual is not None:
+        rp, _, _, ldr = _mat(residual, "residual")
+        if resid_out is None:
+            resid_out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+    hp = ldh = 0
+    if resid_out is not None:
+        hp, _, _, ldh = _mat(resid_out, "resid_out")
+    return (xp, N, d, ldx, dt, rp or None, ldr, _gains(w, X, d)), resid_out, hp or None, ldh
+
+
+def sn_rmsnorm(X: torch.Tensor, w=None, residual=None, eps: float = 1e-6, out=None,
+               resid_out=None, stream=None):
+    """(Y, H): H = X + residual (X itself without one) and Y = H w / rms(H).
+    resid_out may be X or residual."""
+    native = _native()
+    if native is not None:
+        r = native.rmsnorm(X, w, residual, eps, out, resid_out, stream)
+        if r is not None:
+            return r
+    with _on(stream, X, w, residual, out, resid_out):
+        args, H, hp, ldh = _norm_inputs(X, w, residual, resid_out)
+        if out is None:
+            out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        _same_as(X, ("out", out))
+        yp, _, _, ldy = _mat(out, "out")
+        _check(lib().sn_rmsnorm(*args, float(eps), hp, ldh, yp, ldy, _stream(stream)))
+    return out, X if H is None else H
+
+
+def sn_rmsnorm_quant(X: torch.Tensor, w=None, residual=None, eps: float = 1e-6, group: int = 0,
+                     out=None, scales=None, resid_out=None, stream=None):
+    """(Q, S, H): sn_rmsnorm with Y ~ Q S in 8 bits (torch.float8_e4m3fn), one scale
+    per row (group 0) or per 128 columns (group 128)."""
+    native = _native()
+    if native is not None:
+        r = native.rmsnorm_quant(X, w, residual, eps, group, out, scales, resid_out, stream)
+        if r is not None:
+            return r
+    if group not in (0, 128):
+        raise SnError(8, "group must be 0 or 128")
+    with _on(stream, X, w, residual, out, scales, resid_out):
+        args, H, hp, ldh = _norm_inputs(X, w, residual, resid_out)
+        N, d = X.shape
+        if out is None:
+            out = torch.empty(X.shape, dtype=torch.float8_e4m3fn, device=X.device)
+        _out_shape(out, X.shape, "out")
+        if scales is None:
+            scales = torch.empty((N, -(-d // group) if group else 1), dtype=torch.float32,
+                                 device=X.device)
+        _out_shape(scales, (N, -(-d // group) if group else 1), "scales")
+        if out.dtype != torch.float8_e4m3fn or scales.dtype != torch.float32:
+            raise SnError(3, "out must be float8_e4m3fn and scales float32")
+        qp, _, _, ldq = _mat(out, "out")
+        sp, _, _, lds = _mat(scales, "scales")
+        _check(lib().sn_rmsnorm_quant(*args, float(eps), hp, ldh, int(group), qp, ldq, sp, lds,
+                                      _stream(stream)))
+    return out, scales, X if H is None else H
+
+
+def sn_rmsnorm_backward_workspace_bytes(N: int, d: int, dt: int) -> int:
+    return lib().sn_rmsnorm_backward_workspace_bytes(N, d, dt)
+
+
+def sn_rmsnorm_backward(H: torch.Tensor, dY: torch.Tensor, w=None, dH=None, eps: float = 1e-6,
+                        gw=None, out=None, workspace=None, stream=None) -> torch.Tensor:
+    """dX, the gradient of the norm's input (and residual) from dY and, where h goes
+    on as the residual stream, dH; gw (float32) += the gain's gradient.  out may be
+    dY or dH."""
+    native = _native()
+    if native is not None:
+        dX = native.rmsnorm_backward(H, dY, w, dH, eps, gw, out, workspace, stream)
+        if dX is not None:
+            return dX
+    hp, N, d, ldh = _mat(H, "H")
+    dt = _dt(H)
+    _same_as(H, ("dY", dY), ("dH", dH))
+    yp, _, _, lddy = _mat(dY, "dY")
+    rp = lddh = 0
+    if dH is not None:
+        rp, _, _, lddh = _mat(dH, "dH")
+    gp = _vec(gw, "gw", d)
+    with _on(stream, H, dY, w, dH, gw, out, workspace):
+        if out is None:
+            out = torch.empty(H.shape, dtype=H.dtype, device=H.device)
+        _same_as(H, ("out", out))
+        op, _, _, ldo = _mat(out, "out")
+        need = sn_rmsnorm_backward_workspace_bytes(N, d, dt) if gw is not None else 0
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=H.device)
+        ws, have = _workspace(workspace, need)
+        _check(lib().sn_rmsnorm_backward(hp, N, d, ldh, dt, yp, lddy, _gains(w, H, d), float(eps),
+                                         rp or None, lddh, op, ldo, gp, ws, have, _stream(stream)))
+    return out
+
+
+def _workspace(t, need):
+    """(pointer, bytes) of a call's workspace; (None, 0) where none is needed."""
+    if not need:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous() or t.numel() * t.element_size() < need:
+        raise SnError(9, f"workspace needs {need} contiguous device bytes")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _tensors(ts, name):
+    """sn_tensor array of a list of device tensors: vectors, matrices with any row
+    stride, and tensors of any shape without gaps."""
+    arr = (_Tensor * max(1, len(ts)))()
+    for i, t in enumerate(ts):
+        if not t.is_cuda:
+            raise SnError(2, f"{name}[{i}] must be a device tensor")
+        if t.is_contiguous():
+            arr[i] = _Tensor(t.data_ptr() if t.numel() else None, 1, t.numel(), t.numel(), _dt(t))
+        else:
+            ptr, rows, cols, ld = _mat(t if t.dim() != 1 else t[:, None], f"{name}[{i}]")
+            arr[i] = _Tensor(ptr, rows, cols, ld, _dt(t))
+    return arr
+
+
+def sn_grad_sumsq(grads, out=None, workspace=None, stream=None) -> torch.Tensor:
+    """Sum of the squares of every value of every tensor of the list, one float64
+    device value (out: float64, one value)."""
+    native = _native()
+    if native is not None:
+        r = native.grad_sumsq(grads, out, workspace, stream)
+        if r is not None:
+            return r
+    grads = list(grads)
+    arr = _tensors(grads, "grads")
+    with _on(stream, *grads, out, workspace):
+        if out is None:
+            out = torch.empty(1, dtype=torch.float64, device="cuda")
+        need = lib().sn_grad_sumsq_workspace_bytes(len(grads), arr)
+        if workspace is None:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        ws, have = _workspace(workspace, max(need, 1))
+        _check(lib().sn_grad_sumsq(len(grads), arr, _vec(out, "out", 1, torch.float64), ws, have,
+                                   _stream(stream)))
+    return out
+
+
+def sn_grad_clip(grads, sumsq: torch.Tensor, max_norm: float, out=None, norm=None,
+                 stream=None) -> torch.Tensor:
+    """Scale the gradients by min(1, max_norm / sqrt(sumsq)), in place or into the
+    tensors of the list out (same shapes and dtypes); returns the norm (float32,
+    one value)."""
+    native = _native()
+    if native is not None:
+        r = native.grad_clip(grads, sumsq, max_norm, out, norm, stream)
+        if r is not None:
+            return r
+    grads = list(grads)
+    arr = _tensors(grads, "grads")
+    outs = arr_out = None
+    if out is not None:
+        outs = list(out)
+        if len(outs) != len(grads):
+            raise SnError(2, f"out must hold {len(grads)} tensors, got {len(outs)}")
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            _out_shape(o, g.shape, f"out[{i}]")
+        # a gradient without gaps whose output has some is taken as a matrix too
+        arr_out = _tensors(outs, "out")
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            if arr[i].rows != arr_out[i].rows:
+                for a, t in ((arr, g), (arr_out, o)):
+                    ptr, rows, cols, ld = _mat(t if t.dim() != 1 else t[:, None], f"tensor {i}")
+                    a[i] = _Tensor(ptr, rows, cols, ld, _dt(t))
+    with _on(stream, *grads, *(outs or ()), sumsq, norm):
+        if norm is None:
+            norm = torch.empty(1, dtype=torch.float32, device="cuda")
+        _check(lib().sn_grad_clip(len(grads), arr, arr_out, _vec(sumsq, "sumsq", 1, torch.float64),
+                                  float(max_norm), _vec(norm, "norm", 1), _stream(stream)))
+    return norm
 
 
 def sn_version() -> str:

@@ -5,9 +5,12 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <exception>
+#include <vector>
 
 #include "sn_internal.h"
 
@@ -74,6 +77,7 @@ Span span(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t es) {
 bool overlap(Span a, Span b) { return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi; }
 
 constexpr int64_t kMaxDim = int64_t(1) << 31;  // rows, columns and strides stay below 2^31
+constexpr int64_t kMaxElems = int64_t(1) << 40;  // elements of the tensors of a clipping call
 
 int32_t check_basis(const void *basis, int64_t d, int64_t k, int32_t dt) {
   if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
@@ -734,6 +738,430 @@ int32_t sn_project_weights_multi(const void *basis, int64_t d, int64_t k, int32_
       return st;
   }
   return ok();
+}
+
+}  // extern "C"
+
+// ---- token log probabilities, norms, gradient clipping ---------------------
+
+namespace {
+
+int32_t check_rows(const char *name, int64_t n, int64_t cols, int64_t ld) {
+  if (n < 0 || n >= kMaxDim || cols < 1 || cols >= kMaxDim)
+    return fail(SN_ERR_SHAPE, "%s: %lld x %lld out of range", name, (long long)n, (long long)cols);
+  if (ld < cols || ld >= kMaxDim)
+    return fail(SN_ERR_SHAPE, "%s: the row stride must be >= the columns", name);
+  return SN_OK;
+}
+
+int32_t check_scale(double scale) {
+  if (!(scale >= 0x1p-20 && scale <= 0x1p20))
+    return fail(SN_ERR_SHAPE, "scale must lie in [2^-20, 2^20]");
+  return SN_OK;
+}
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// The buffers of a call, for the checks that no output overlaps another buffer.
+struct Buffers {
+  static constexpr int kMost = 12;
+  Span in[kMost], out[kMost];
+  int ins = 0, outs = 0;
+  void read(Span s) { in[ins++] = s; }
+  void write(Span s) { out[outs++] = s; }
+  int32_t check(const char *call) const {
+    for (int i = 0; i < outs; ++i) {
+      for (int j = 0; j < ins; ++j)
+        if (overlap(out[i], in[j])) return fail(SN_ERR_ALIAS, "%s: an output overlaps an input", call);
+      for (int j = 0; j < i; ++j)
+        if (overlap(out[i], out[j])) return fail(SN_ERR_ALIAS, "%s: two outputs overlap", call);
+    }
+    return SN_OK;
+  }
+};
+
+// What the calls on logits share.
+int32_t check_logits(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt, double scale,
+                     const int32_t *tok) {
+  if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
+  int32_t st = check_rows("Z", N, V, ldz);
+  if (st || (st = check_scale(scale))) return st;
+  if (N == 0) return SN_OK;
+  if (!Z) return fail(SN_ERR_NULL, "Z is NULL");
+  if (!elem_aligned(Z, dt)) return fail(SN_ERR_ALIGN, "Z not aligned to its element size");
+  if (!aligned(tok, 4)) return fail(SN_ERR_ALIGN, "tok not 4-byte aligned");
+  return SN_OK;
+}
+
+int32_t check_dlogits(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt, void *dZ,
+                      int64_t lddz, Buffers &b) {
+  if (lddz < V || lddz >= kMaxDim) return fail(SN_ERR_SHAPE, "lddz must be >= V");
+  if (N == 0) return SN_OK;
+  if (!dZ) return fail(SN_ERR_NULL, "dZ is NULL");
+  if (!elem_aligned(dZ, dt)) return fail(SN_ERR_ALIGN, "dZ not aligned to its element size");
+  b.write(span(dZ, N, V, lddz, elem_size(dt)));
+  if (dZ != Z || lddz != ldz) b.read(span(Z, N, V, ldz, elem_size(dt)));
+  return SN_OK;
+}
+
+// H, X, R and w of the norm's forward calls; adds them to the buffers.
+int32_t check_norm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *R,
+                   int64_t ldr, const void *w, double eps, void *H, int64_t ldh, Buffers &b) {
+  if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
+  int32_t st = check_rows("X", N, d, ldx);
+  if (st || (R && (st = check_rows("R", N, d, ldr))) || (H && (st = check_rows("H", N, d, ldh))))
+    return st;
+  if (!(eps >= 0.0 && eps <= 3.0e38)) return fail(SN_ERR_SHAPE, "eps must be finite and >= 0");
+  if (N == 0) return SN_OK;
+  if (!X) return fail(SN_ERR_NULL, "X is NULL");
+  if (!elem_aligned(X, dt) || !elem_aligned(R, dt) || !elem_aligned(w, dt) || !elem_aligned(H, dt))
+    return fail(SN_ERR_ALIGN, "X, R, w or H not aligned to its element size");
+  const size_t es = elem_size(dt);
+  const bool on_x = H == X && ldh == ldx, on_r = H == R && ldh == ldr;
+  if (H) b.write(span(H, N, d, ldh, es));
+  if (!H || !on_x) b.read(span(X, N, d, ldx, es));
+  if (R && (!H || !on_r)) b.read(span(R, N, d, ldr, es));
+  b.read(span(w, 1, d, d, es));
+  return SN_OK;
+}
+
+sn::NormArgs norm_args(const void *X, int64_t N, int64_t d, int64_t ldx, const void *R,
+                       int64_t ldr, const void *w, double eps, void *H, int64_t ldh) {
+  sn::NormArgs a = {};
+  a.X = X;
+  a.R = R;
+  a.w = w;
+  a.N = N;
+  a.d = d;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.inv_d = static_cast<float>(1.0 / static_cast<double>(d));
+  a.eps = static_cast<float>(eps);
+  a.H = H;
+  a.ldh = ldh;
+  return a;
+}
+
+// The tensors of a clipping call as the kernels take them (rows without gaps as
+// one row), checked; spans of those with elements go to `reads` where given.
+int32_t clip_tensors(int32_t count, const sn_tensor *grads, const sn_tensor *out, bool shapes_only,
+                     std::vector<sn::ClipTensor> &t) {
+  if (count < 0) return fail(SN_ERR_SHAPE, "count must be >= 0");
+  if (count > 0 && !grads) return fail(SN_ERR_NULL, "grads is NULL");
+  t.reserve(static_cast<size_t>(count));
+  int64_t total = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    const sn_tensor &g = grads[i];
+    if (!dtype_ok(g.dt)) return fail(SN_ERR_DTYPE, "grads[%d]: unknown dtype %d", i, g.dt);
+    if (g.rows < 0 || g.rows >= kMaxDim || g.cols < 0 || g.cols >= kMaxElems)
+      return fail(SN_ERR_SHAPE, "grads[%d]: %lld x %lld out of range", i, (long long)g.rows,
+                  (long long)g.cols);
+    if (out && (out[i].rows != g.rows || out[i].cols != g.cols))
+      return fail(SN_ERR_SHAPE, "out[%d] has another shape than grads[%d]", i, i);
+    if (out && out[i].dt != g.dt)
+      return fail(SN_ERR_DTYPE, "out[%d] has another dtype than grads[%d]", i, i);
+    if (g.rows == 0 || g.cols == 0) continue;
+    // rows < 2^31 and cols < 2^40: compared without their product
+    if (g.cols > (kMaxElems - 1) / g.rows || (total += g.rows * g.cols) >= kMaxElems)
+      return fail(SN_ERR_SHAPE, "2^40 or more elements");
+    const int64_t ldo = out ? out[i].ld : g.ld;
+    if (g.rows > 1 && (g.ld < g.cols || g.ld >= kMaxElems || ldo < g.cols || ldo >= kMaxElems))
+      return fail(SN_ERR_SHAPE, "tensor %d: the row stride must be >= the columns", i);
+    sn::ClipTensor c = {};
+    c.g = g.data;
+    c.out = out ? out[i].data : g.data;
+    if (!shapes_only) {
+      if (!c.g || !c.out) return fail(SN_ERR_NULL, "tensor %d is NULL", i);
+      if (!elem_aligned(c.g, g.dt) || !elem_aligned(c.out, g.dt))
+        return fail(SN_ERR_ALIGN, "tensor %d not aligned to its element size", i);
+    }
+    const bool gaps = g.rows > 1 && (g.ld != g.cols || ldo != g.cols);
+    c.rows = gaps ? g.rows : 1;
+    c.cols = gaps ? g.cols : g.rows * g.cols;
+    c.ldg = gaps ? g.ld : c.cols;
+    c.ldo = gaps ? ldo : c.cols;
+    c.f32 = g.dt == SN_F32;
+    t.push_back(c);
+  }
+  return SN_OK;
+}
+
+Span clip_span(const sn::ClipTensor &c, bool out) {
+  return span(out ? c.out : c.g, c.rows, c.cols, out ? c.ldo : c.ldg, c.f32 ? 4 : 2);
+}
+
+// No output may overlap another tensor's gradient or output: with the spans in
+// order of their starts, each output against the span before it.
+int32_t check_clip_alias(const std::vector<sn::ClipTensor> &t) {
+  struct Item {
+    Span s;
+    bool out;
+  };
+  std::vector<Item> v;
+  v.reserve(2 * t.size());
+  for (const sn::ClipTensor &c : t) {
+    const bool same = c.out == c.g && c.ldo == c.ldg;
+    v.push_back({clip_span(c, true), true});
+    if (!same) v.push_back({clip_span(c, false), false});
+  }
+  std::sort(v.begin(), v.end(), [](const Item &a, const Item &b) { return a.s.lo < b.s.lo; });
+  uintptr_t any = 0, outs = 0;  // the furthest end of a span, of an output's span
+  for (const Item &x : v) {
+    if (x.s.lo < (x.out ? any : outs))
+      return fail(SN_ERR_ALIAS, "an output overlaps another gradient or output");
+    any = x.s.hi > any ? x.s.hi : any;
+    if (x.out) outs = x.s.hi > outs ? x.s.hi : outs;
+  }
+  return SN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t sn_token_logprobs(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
+                          double scale, const int32_t *tok, float *logp, float *entropy,
+                          float *stats, int32_t n_top, float *top_logp, int32_t *top_id,
+                          int32_t *err_flag, sn_stream stream) {
+  int32_t st = check_logits(Z, N, V, ldz, dt, scale, tok);
+  if (st) return st;
+  if (n_top < 0 || n_top > V) return fail(SN_ERR_SHAPE, "need 0 <= n_top <= V");
+  if (n_top > SN_MAX_TOP) return fail(SN_ERR_UNSUPPORTED, "n_top > SN_MAX_TOP");
+  if (N == 0) return ok();
+  if (!entropy || !stats || (tok && !logp) || (n_top && (!top_logp || !top_id)))
+    return fail(SN_ERR_NULL, "an output is NULL");
+  if (!aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 4) || !aligned(top_logp, 4) ||
+      !aligned(top_id, 4))
+    return fail(SN_ERR_ALIGN, "an output is not 4-byte aligned");
+  Buffers b;
+  b.read(span(Z, N, V, ldz, elem_size(dt)));
+  if (tok) {
+    b.read(span(tok, 1, N, N, 4));
+    b.write(span(logp, 1, N, N, 4));
+  }
+  b.write(span(entropy, 1, N, N, 4));
+  b.write(span(stats, N, 2, 2, 4));
+  if (n_top) {
+    b.write(span(top_logp, N, n_top, n_top, 4));
+    b.write(span(top_id, N, n_top, n_top, 4));
+  }
+  if ((st = b.check("sn_token_logprobs"))) return st;
+  const sn::LogprobsArgs a = {Z,       N,     V,     ldz,      static_cast<float>(scale),
+                              tok,     tok ? logp : nullptr, entropy, stats,
+                              n_top,   top_logp, top_id, err_flag};
+  return hip_status(sn::launch_logprobs(dt, a, static_cast<hipStream_t>(stream)),
+                    "sn_token_logprobs launch");
+}
+
+int32_t sn_token_logprobs_backward(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
+                                   double scale, const int32_t *tok, const float *stats,
+                                   const float *entropy, const float *g_logp,
+                                   const float *g_entropy, void *dZ, int64_t lddz,
+                                   int32_t *err_flag, sn_stream stream) {
+  Buffers b;
+  int32_t st = check_logits(Z, N, V, ldz, dt, scale, tok);
+  if (st || (st = check_dlogits(Z, N, V, ldz, dt, dZ, lddz, b))) return st;
+  if (N == 0) return ok();
+  if (!stats || (g_logp && !tok) || (g_entropy && !entropy))
+    return fail(SN_ERR_NULL, "stats, tok with g_logp and entropy with g_entropy are required");
+  if (!aligned(stats, 4) || !aligned(entropy, 4) || !aligned(g_logp, 4) || !aligned(g_entropy, 4))
+    return fail(SN_ERR_ALIGN, "a float input is not 4-byte aligned");
+  b.read(span(stats, N, 2, 2, 4));
+  b.read(span(tok, 1, N, N, 4));
+  b.read(span(entropy, 1, N, N, 4));
+  b.read(span(g_logp, 1, N, N, 4));
+  b.read(span(g_entropy, 1, N, N, 4));
+  if ((st = b.check("sn_token_logprobs_backward"))) return st;
+  const sn::LogprobsGradArgs a = {Z,      N,         V,  ldz,  static_cast<float>(scale), tok, stats,
+                                  entropy, g_logp, g_entropy, dZ, lddz, err_flag};
+  return hip_status(sn::launch_logprobs_grad(dt, a, static_cast<hipStream_t>(stream)),
+                    "sn_token_logprobs_backward launch");
+}
+
+int32_t sn_token_loss(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt, double scale,
+                      const int32_t *tok, const float *weight, float *logp, void *dZ,
+                      int64_t lddz, int32_t *err_flag, sn_stream stream) {
+  Buffers b;
+  int32_t st = check_logits(Z, N, V, ldz, dt, scale, tok);
+  if (st || (st = check_dlogits(Z, N, V, ldz, dt, dZ, lddz, b))) return st;
+  if (N == 0) return ok();
+  if (!tok || !logp) return fail(SN_ERR_NULL, "tok or logp is NULL");
+  if (!aligned(weight, 4) || !aligned(logp, 4))
+    return fail(SN_ERR_ALIGN, "weight or logp is not 4-byte aligned");
+  // logp is written while rows are still read: not over Z, in place or not
+  b.read(span(tok, 1, N, N, 4));
+  b.read(span(weight, 1, N, N, 4));
+  b.write(span(logp, 1, N, N, 4));
+  if ((st = b.check("sn_token_loss"))) return st;
+  const sn::LossArgs a = {Z,      N,    V,  ldz,  static_cast<float>(scale), tok,
+                          weight, logp, dZ, lddz, err_flag};
+  return hip_status(sn::launch_loss(dt, a, static_cast<hipStream_t>(stream)),
+                    "sn_token_loss launch");
+}
+
+int32_t sn_rmsnorm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *R,
+                   int64_t ldr, const void *w, double eps, void *H, int64_t ldh, void *Y,
+                   int64_t ldy, sn_stream stream) {
+  Buffers b;
+  int32_t st = check_norm(X, N, d, ldx, dt, R, ldr, w, eps, H, ldh, b);
+  if (st || (st = check_rows("Y", N, d, ldy))) return st;
+  if (N == 0) return ok();
+  if (!Y) return fail(SN_ERR_NULL, "Y is NULL");
+  if (!elem_aligned(Y, dt)) return fail(SN_ERR_ALIGN, "Y not aligned to its element size");
+  const Span y = span(Y, N, d, ldy, elem_size(dt));
+  b.write(y);
+  if ((st = b.check("sn_rmsnorm"))) return st;
+  sn::NormArgs a = norm_args(X, N, d, ldx, R, ldr, w, eps, H, ldh);
+  a.Y = Y;
+  a.ldy = ldy;
+  return hip_status(sn::launch_rmsnorm(dt, a, static_cast<hipStream_t>(stream)),
+                    "sn_rmsnorm launch");
+}
+
+int32_t sn_rmsnorm_quant(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
+                         const void *R, int64_t ldr, const void *w, double eps, void *H,
+                         int64_t ldh, int32_t group, void *Q, int64_t ldq, float *S, int64_t lds,
+                         sn_stream stream) {
+  Buffers b;
+  int32_t st = check_norm(X, N, d, ldx, dt, R, ldr, w, eps, H, ldh, b);
+  if (st || (st = check_rows("Q", N, d, ldq))) return st;
+  if (group < 0) return fail(SN_ERR_SHAPE, "group must be >= 0");
+  if (group != 0 && group != 128) return fail(SN_ERR_UNSUPPORTED, "group must be 0 or 128");
+  const int64_t scales = group ? sn::ceil_div(d, group) : 1;
+  if ((st = check_rows("S", N, scales, lds))) return st;
+  if (N == 0) return ok();
+  if (!Q || !S) return fail(SN_ERR_NULL, "Q or S is NULL");
+  if (!aligned(S, 4)) return fail(SN_ERR_ALIGN, "S is not 4-byte aligned");
+  b.write(span(Q, N, d, ldq, 1));
+  b.write(span(S, N, scales, lds, 4));
+  if ((st = b.check("sn_rmsnorm_quant"))) return st;
+  sn::NormArgs a = norm_args(X, N, d, ldx, R, ldr, w, eps, H, ldh);
+  a.Y = Q;
+  a.ldy = ldq;
+  a.S = S;
+  a.lds = lds;
+  a.group = group;
+  return hip_status(sn::launch_rmsnorm(dt, a, static_cast<hipStream_t>(stream)),
+                    "sn_rmsnorm_quant launch");
+}
+
+size_t sn_rmsnorm_backward_workspace_bytes(int64_t N, int64_t d, int32_t dt) {
+  if (!dtype_ok(dt) || N < 1 || N >= kMaxDim || d < 1 || d >= kMaxDim) return 0;
+  return sn::rmsnorm_grad_workspace_bytes(dt, N, d);
+}
+
+int32_t sn_rmsnorm_backward(const void *H, int64_t N, int64_t d, int64_t ldh, int32_t dt,
+                            const void *dY, int64_t lddy, const void *w, double eps,
+                            const void *dH, int64_t lddh, void *dX, int64_t lddx, float *gw,
+                            void *workspace, size_t workspace_bytes, sn_stream stream) {
+  if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
+  int32_t st = check_rows("H", N, d, ldh);
+  if (st || (st = check_rows("dY", N, d, lddy)) || (st = check_rows("dX", N, d, lddx)) ||
+      (dH && (st = check_rows("dH", N, d, lddh))))
+    return st;
+  if (!(eps >= 0.0 && eps <= 3.0e38)) return fail(SN_ERR_SHAPE, "eps must be finite and >= 0");
+  if (N == 0) return ok();
+  if (!H || !dY || !dX) return fail(SN_ERR_NULL, "H, dY or dX is NULL");
+  if (!elem_aligned(H, dt) || !elem_aligned(dY, dt) || !elem_aligned(w, dt) ||
+      !elem_aligned(dH, dt) || !elem_aligned(dX, dt))
+    return fail(SN_ERR_ALIGN, "a matrix or w not aligned to its element size");
+  if (!aligned(gw, 4)) return fail(SN_ERR_ALIGN, "gw is not 4-byte aligned");
+  const size_t es = elem_size(dt);
+  Buffers b;
+  b.write(span(dX, N, d, lddx, es));
+  b.read(span(H, N, d, ldh, es));
+  b.read(span(w, 1, d, d, es));
+  if (dX != dY || lddx != lddy) b.read(span(dY, N, d, lddy, es));
+  if (dH && (dX != dH || lddx != lddh)) b.read(span(dH, N, d, lddh, es));
+  if (gw) {
+    const size_t need = sn::rmsnorm_grad_workspace_bytes(dt, N, d);
+    if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+    b.write(span(gw, 1, d, d, 4));
+    b.write(bytes_span(workspace, need));
+  }
+  if ((st = b.check("sn_rmsnorm_backward"))) return st;
+  sn::NormGradArgs a = {};
+  a.H = H;
+  a.dY = dY;
+  a.w = w;
+  a.dH = dH;
+  a.N = N;
+  a.d = d;
+  a.ldh = ldh;
+  a.lddy = lddy;
+  a.lddh = lddh;
+  a.inv_d = static_cast<float>(1.0 / static_cast<double>(d));
+  a.eps = static_cast<float>(eps);
+  a.dX = dX;
+  a.lddx = lddx;
+  return hip_status(
+      sn::launch_rmsnorm_grad(dt, a, gw, workspace, static_cast<hipStream_t>(stream)),
+      "sn_rmsnorm_backward launch");
+}
+
+size_t sn_grad_sumsq_workspace_bytes(int32_t count, const sn_tensor *grads) {
+  try {
+    std::vector<sn::ClipTensor> t;
+    if (clip_tensors(count, grads, nullptr, true, t)) return 0;
+    const int64_t units = sn::clip_units(t.data(), static_cast<int32_t>(t.size()));
+    return sn::align256(static_cast<size_t>(units > 0 ? units : 1) * sizeof(double));
+  } catch (const std::exception &) {
+    fail(SN_ERR_WORKSPACE, "out of host memory");
+    return 0;
+  }
+}
+
+int32_t sn_grad_sumsq(int32_t count, const sn_tensor *grads, double *sumsq, void *workspace,
+                      size_t workspace_bytes, sn_stream stream) {
+  try {
+    std::vector<sn::ClipTensor> t;
+    int32_t st = clip_tensors(count, grads, nullptr, false, t);
+    if (st) return st;
+    if (!sumsq) return fail(SN_ERR_NULL, "sumsq is NULL");
+    if (!aligned(sumsq, 8)) return fail(SN_ERR_ALIGN, "sumsq is not 8-byte aligned");
+    const int32_t n = static_cast<int32_t>(t.size());
+    const int64_t units = sn::clip_units(t.data(), n);
+    const size_t need = sn::align256(static_cast<size_t>(units > 0 ? units : 1) * sizeof(double));
+    if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+    const Span ws = bytes_span(workspace, need), to = bytes_span(sumsq, 8);
+    if (overlap(ws, to)) return fail(SN_ERR_ALIAS, "sumsq overlaps the workspace");
+    for (const sn::ClipTensor &c : t)
+      if (overlap(clip_span(c, false), ws) || overlap(clip_span(c, false), to))
+        return fail(SN_ERR_ALIAS, "a gradient overlaps the workspace or sumsq");
+    return hip_status(
+        sn::launch_sumsq(t.data(), n, sumsq, workspace, static_cast<hipStream_t>(stream)),
+        "sn_grad_sumsq launch");
+  } catch (const std::exception &) {
+    return fail(SN_ERR_WORKSPACE, "out of host memory");
+  }
+}
+
+int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out,
+                     const double *sumsq, double max_norm, float *norm, sn_stream stream) {
+  try {
+    std::vector<sn::ClipTensor> t;
+    int32_t st = clip_tensors(count, grads, out, false, t);
+    if (st) return st;
+    if (!sumsq) return fail(SN_ERR_NULL, "sumsq is NULL");
+    if (!aligned(sumsq, 8) || !aligned(norm, 4))
+      return fail(SN_ERR_ALIGN, "sumsq or norm is not aligned to its element size");
+    if (!(max_norm >= 0.0)) return fail(SN_ERR_SHAPE, "max_norm must be >= 0");
+    if ((st = check_clip_alias(t))) return st;
+    const Span from = bytes_span(sumsq, 8), to = bytes_span(norm, norm ? 4 : 0);
+    if (overlap(from, to)) return fail(SN_ERR_ALIAS, "norm overlaps sumsq");
+    bool in_place = true;
+    for (const sn::ClipTensor &c : t) {
+      const Span g = clip_span(c, false), o = clip_span(c, true);
+      if (overlap(o, from) || overlap(g, to) || overlap(o, to))
+        return fail(SN_ERR_ALIAS, "a tensor overlaps sumsq or norm");
+      in_place = in_place && c.out == c.g && c.ldo == c.ldg;
+    }
+    return hip_status(sn::launch_clip(t.data(), static_cast<int32_t>(t.size()), in_place, sumsq,
+                                      max_norm, norm, static_cast<hipStream_t>(stream)),
+                      "sn_grad_clip launch");
+  } catch (const std::exception &) {
+    return fail(SN_ERR_WORKSPACE, "out of host memory");
+  }
 }
 
 const char *sn_status_string(int32_t status) {

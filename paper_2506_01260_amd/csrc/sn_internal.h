@@ -266,6 +266,87 @@ hipError_t launch_project_mfma_segs(const PackLayout &L, const void *packed, con
 hipError_t launch_project_mfma(const PackLayout &L, const void *packed, void *W, int64_t m,
                                int64_t ldw, void *ws, hipStream_t s);
 
+// ---- token log probabilities ----------------------------------------------------
+struct LogprobsArgs {
+  const void *Z;
+  int64_t N, V, ldz;
+  float scale;
+  const int32_t *tok;  // NULL: logp is not written
+  float *logp, *entropy, *stats;
+  int n_top;
+  float *top_logp;
+  int32_t *top_id, *err_flag;
+};
+struct LogprobsGradArgs {
+  const void *Z;
+  int64_t N, V, ldz;
+  float scale;
+  const int32_t *tok;
+  const float *stats, *entropy, *g_logp, *g_entropy;  // either gradient may be NULL
+  void *dZ;
+  int64_t lddz;
+  int32_t *err_flag;
+};
+struct LossArgs {
+  const void *Z;
+  int64_t N, V, ldz;
+  float scale;
+  const int32_t *tok;
+  const float *weight;  // NULL: 1
+  float *logp;
+  void *dZ;
+  int64_t lddz;
+  int32_t *err_flag;
+};
+hipError_t launch_logprobs(int dt, const LogprobsArgs &a, hipStream_t s);
+hipError_t launch_logprobs_grad(int dt, const LogprobsGradArgs &a, hipStream_t s);
+hipError_t launch_loss(int dt, const LossArgs &a, hipStream_t s);
+
+// ---- root-mean-square norm --------------------------------------------------------
+struct NormArgs {
+  const void *X, *R, *w;  // R, w may be NULL
+  int64_t N, d, ldx, ldr;
+  float inv_d, eps;
+  void *H;  // may be NULL
+  int64_t ldh;
+  void *Y;  // dt, or 8 bits with the scales S (group 0: one per row)
+  int64_t ldy;
+  float *S;
+  int64_t lds;
+  int group;
+};
+struct NormGradArgs {
+  const void *H, *dY, *w, *dH;  // w, dH may be NULL
+  int64_t N, d, ldh, lddy, lddh;
+  float inv_d, eps;
+  void *dX;
+  int64_t lddx;
+  float *part;  // the gain gradient's parts, or NULL
+};
+hipError_t launch_rmsnorm(int dt, const NormArgs &a, hipStream_t s);
+size_t rmsnorm_grad_workspace_bytes(int dt, int64_t N, int64_t d);
+hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipStream_t s);
+
+// ---- gradient norm and clipping ---------------------------------------------------
+struct ClipTensor {
+  const void *g;
+  void *out;
+  int64_t rows, cols, ldg, ldo;  // one row where the rows lie without gaps
+  int32_t f32;
+};
+constexpr int kClipTensors = 64;
+struct ClipTable {  // a kernel argument: below 4 KB
+  int n = 0;
+  uint32_t unit0[kClipTensors];
+  ClipTensor t[kClipTensors];
+};
+static_assert(sizeof(ClipTable) <= 3968, "kernel arguments stay below 4 KB");
+int64_t clip_units(const ClipTensor *t, int32_t count);
+hipError_t launch_sumsq(const ClipTensor *t, int32_t count, double *sumsq, void *ws,
+                        hipStream_t s);
+hipError_t launch_clip(const ClipTensor *t, int32_t count, bool in_place, const double *sumsq,
+                       double max_norm, float *norm, hipStream_t s);
+
 // Record a message for sn_last_error() on the calling thread; returns st.
 int32_t set_error(int32_t st, const char *fmt, ...);
 // sn_project_weights' checks of everything but the workspace (SN_OK or the

@@ -1,0 +1,477 @@
+// Root-mean-square norm with the residual's addition, N x d:
+//   h = x + r,   y = h w / sqrt(mean h^2 + eps)
+// h is rounded to dt where it is stored; y is made from the 32-bit sum.  The
+// 8-bit form writes q = y / s in e4m3 (largest value 448) with one float32 scale
+// s = max |y| / 448 for a row or for each 128 columns of it.  Backward, from the
+// stored h, u = dy w and rho = 1 / sqrt(mean h^2 + eps):
+//   dx = rho u - h rho^3 mean(u h) + dh,    gw += sum over rows of dy h rho.
+//
+// Memory-bound: each operand passes once, the row staying in registers between
+// its sums and its outputs.  R threads hold a row in K pieces each; with R = 64
+// a wave has a row of its own and no barrier.
+#include "sn_internal.h"
+#include "sn_rows.h"
+
+namespace sn {
+
+namespace {
+
+constexpr float kF8Max = 448.0f;
+constexpr uint32_t kTiny = 0x0D800000u;  // 2^-100, the least maximum a scale is made from
+
+// a piece of a row that may be absent (NULL) or end inside the piece
+template <typename T>
+__device__ __forceinline__ void get(const T *row, int64_t c0, int64_t d,
+                                    float (&x)[Piece<T>::E]) {
+  if (c0 + Piece<T>::E <= d)
+    Piece<T>::unpack(load_piece(row + c0), x);
+  else
+    load_part(row, c0, d, 0.0f, x);
+}
+template <typename T>
+__device__ __forceinline__ void put(T *row, int64_t c0, int64_t d,
+                                    const float (&x)[Piece<T>::E]) {
+  if (c0 + Piece<T>::E <= d)
+    store_piece(row + c0, Piece<T>::pack(x));
+  else
+    store_part(row, c0, d, x);
+}
+
+__device__ __forceinline__ uint32_t f8x4(float a, float b, float c, float d) {
+  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true));
+}
+
+// E values of a row in 8 bits
+template <int E>
+__device__ __forceinline__ void put8(uint8_t *row, int64_t c0, int64_t d, const float (&q)[E]) {
+  uint32_t w[E / 4];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) w[i] = f8x4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+  if (c0 + E <= d) {
+    __builtin_memcpy(row + c0, w, E);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (c0 + i < d) row[c0 + i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+// largest |y| as its bits: as whole numbers they are ordered, a NaN above all
+__device__ __forceinline__ uint32_t abs_bits(float y) { return __float_as_uint(y) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
+#pragma unroll
+  for (int m = LANES / 2; m; m >>= 1) v = umax(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), m)));
+  return v;
+}
+__device__ __forceinline__ float scale_of(uint32_t bits) {
+  return __uint_as_float(umax(bits, kTiny)) / kF8Max;
+}
+// y / s within e4m3's range (a NaN stays one)
+__device__ __forceinline__ float to_range(float y, float inv) {
+  const float q = y * inv;
+  return q > kF8Max ? kF8Max : q < -kF8Max ? -kF8Max : q;
+}
+
+enum { kOut = 0, kOut8Row = 1, kOut8Group = 2 };
+constexpr int kGroup = 128;  // columns of a scale in the grouped form
+
+// R threads per row, NT / R rows in a workgroup at a time.
+template <typename T, int R, int K, int NT, int OUT>
+__global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
+  constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
+  static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
+  __shared__ float red[W];
+  __shared__ uint32_t redu[W];
+  const int tr = threadIdx.x % R;
+  const T *w = static_cast<const T *>(a.w);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / R; i < a.N;
+       i += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+    const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
+    float h[K][E], ss = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+      get(X, c0, a.d, h[k]);
+    }
+    if (Rs) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float r[E];
+        get(Rs, static_cast<int64_t>(tr + k * R) * E, a.d, r);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[k][e] += r[e];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) ss = fmaf(h[k][e], h[k][e], ss);
+    ss = group_sum<W>(ss, red);
+    if (a.H) {
+      T *H = static_cast<T *>(a.H) + i * a.ldh;
+#pragma unroll
+      for (int k = 0; k < K; ++k) put(H, static_cast<int64_t>(tr + k * R) * E, a.d, h[k]);
+    }
+    const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+    uint32_t big[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+      float g[E];
+      if (w) get(w, c0, a.d, g);
+      big[k] = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        h[k][e] *= rho;
+        if (w) h[k][e] *= g[e];
+        if constexpr (OUT != kOut) big[k] = umax(big[k], abs_bits(h[k][e]));
+      }
+      if constexpr (OUT == kOut) put(static_cast<T *>(a.Y) + i * a.ldy, c0, a.d, h[k]);
+    }
+    if constexpr (OUT == kOut8Row) {
+      uint32_t m = big[0];
+#pragma unroll
+      for (int k = 1; k < K; ++k) m = umax(m, big[k]);
+      m = lanes_umax<64>(m);
+      if constexpr (W > 1) {
+        if ((tr & 63) == 0) redu[tr >> 6] = m;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) big[k] = m;
+      if (tr == 0) a.S[i * a.lds] = scale_of(m);
+    } else if constexpr (OUT == kOut8Group) {
+      constexpr int L = kGroup / E;  // lanes of a scale
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        big[k] = lanes_umax<L>(big[k]);
+        const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+        if (tr % L == 0 && c0 < a.d) a.S[i * a.lds + c0 / kGroup] = scale_of(big[k]);
+      }
+    }
+    if constexpr (OUT != kOut) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const float inv = 1.0f / scale_of(big[k]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[k][e] = to_range(h[k][e], inv);
+        put8<E>(static_cast<uint8_t *>(a.Y) + i * a.ldy, static_cast<int64_t>(tr + k * R) * E, a.d,
+                h[k]);
+      }
+    }
+    if constexpr (W > 1) {
+      if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
+    }
+  }
+}
+
+// Rows longer than the registers hold: two or three passes over them.
+template <typename T, int OUT>
+__global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
+  constexpr int E = Piece<T>::E, NT = 1024, W = NT / 64;
+  __shared__ float red[W];
+  __shared__ uint32_t redu[W];
+  const T *w = static_cast<const T *>(a.w);
+  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
+    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+    const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
+    float h[E], r[E], ss = 0.0f;
+    auto sum = [&](int64_t c0) {
+      get(X, c0, a.d, h);
+      if (Rs) {
+        get(Rs, c0, a.d, r);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[e] += r[e];
+      }
+    };
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      sum(c0);
+#pragma unroll
+      for (int e = 0; e < E; ++e) ss = fmaf(h[e], h[e], ss);
+    }
+    ss = group_sum<W>(ss, red);
+    const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+    auto norm = [&](int64_t c0) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] *= rho;
+      if (w) {
+        get(w, c0, a.d, r);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[e] *= r[e];
+      }
+    };
+    uint32_t m = 0;
+    if constexpr (OUT == kOut8Row) {
+      for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+        sum(c0);
+        norm(c0);
+#pragma unroll
+        for (int e = 0; e < E; ++e) m = umax(m, abs_bits(h[e]));
+      }
+      m = lanes_umax<64>(m);
+      if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
+      if (threadIdx.x == 0) a.S[i * a.lds] = scale_of(m);
+    }
+    // whole waves stay in the loop, so that the lanes of a scale are all there
+    for (int64_t b = 0; b < a.d; b += NT * E) {
+      const int64_t c0 = b + threadIdx.x * E;
+      sum(c0);
+      if (a.H) put(static_cast<T *>(a.H) + i * a.ldh, c0, a.d, h);
+      norm(c0);
+      if constexpr (OUT == kOut) {
+        put(static_cast<T *>(a.Y) + i * a.ldy, c0, a.d, h);
+      } else {
+        if constexpr (OUT == kOut8Group) {
+          constexpr int L = kGroup / E;
+          m = 0;
+#pragma unroll
+          for (int e = 0; e < E; ++e) m = umax(m, abs_bits(h[e]));
+          m = lanes_umax<L>(m);
+          if (threadIdx.x % L == 0 && c0 < a.d) a.S[i * a.lds + c0 / kGroup] = scale_of(m);
+        }
+        const float inv = 1.0f / scale_of(m);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[e] = to_range(h[e], inv);
+        put8<E>(static_cast<uint8_t *>(a.Y) + i * a.ldy, c0, a.d, h);
+      }
+    }
+    if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
+  }
+}
+
+// Backward.  A workgroup takes the rows blockIdx.x, + gridDim.x, ... and keeps its
+// part of the gain's gradient in registers; the parts are summed by gain_kernel.
+template <typename T, int R, int K, int NT>
+__global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
+  constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
+  static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
+  __shared__ float red[2][W];
+  const int tr = threadIdx.x % R;
+  const T *w = static_cast<const T *>(a.w);
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / R;
+  float gw[K][E] = {};
+  for (int64_t i = first; i < a.N; i += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const T *H = static_cast<const T *>(a.H) + i * a.ldh;
+    const T *dY = static_cast<const T *>(a.dY) + i * a.lddy;
+    const T *dH = a.dH ? static_cast<const T *>(a.dH) + i * a.lddh : nullptr;
+    float h[K][E], u[K][E], ss = 0.0f, uh = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+      get(H, c0, a.d, h[k]);
+      get(dY, c0, a.d, u[k]);
+    }
+    float g[E];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (w) get(w, static_cast<int64_t>(tr + k * R) * E, a.d, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        ss = fmaf(h[k][e], h[k][e], ss);
+        uh = fmaf(w ? u[k][e] * g[e] : u[k][e], h[k][e], uh);
+      }
+    }
+    ss = group_sum<W>(ss, red[0]);
+    uh = group_sum<W>(uh, red[1]);
+    const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+    const float f = rho * rho * rho * (uh * a.inv_d);
+    T *dX = static_cast<T *>(a.dX) + i * a.lddx;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+      float o[E];
+      if (dH)
+        get(dH, c0, a.d, o);
+      else
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.0f;
+      if (w) get(w, c0, a.d, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        gw[k][e] = fmaf(u[k][e] * h[k][e], rho, gw[k][e]);
+        o[e] += fmaf(w ? u[k][e] * g[e] : u[k][e], rho, -h[k][e] * f);
+      }
+      put(dX, c0, a.d, o);
+    }
+    if constexpr (W > 1) {
+      if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
+    }
+  }
+  if (a.part && first < a.N) {
+    float *part = a.part + first * a.d;  // the first row's number names the part
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (c0 + e < a.d) part[c0 + e] = gw[k][e];
+    }
+  }
+}
+
+// Rows longer than the registers hold: the part of the gain's gradient is kept
+// in the workspace between the workgroup's rows.
+template <typename T>
+__global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a) {
+  constexpr int E = Piece<T>::E, NT = 1024, W = NT / 64;
+  __shared__ float red[2][W];
+  const T *w = static_cast<const T *>(a.w);
+  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
+    const T *H = static_cast<const T *>(a.H) + i * a.ldh;
+    const T *dY = static_cast<const T *>(a.dY) + i * a.lddy;
+    const T *dH = a.dH ? static_cast<const T *>(a.dH) + i * a.lddh : nullptr;
+    float h[E], u[E], g[E], ss = 0.0f, uh = 0.0f;
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      get(H, c0, a.d, h);
+      get(dY, c0, a.d, u);
+      if (w) get(w, c0, a.d, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        ss = fmaf(h[e], h[e], ss);
+        uh = fmaf(w ? u[e] * g[e] : u[e], h[e], uh);
+      }
+    }
+    ss = group_sum<W>(ss, red[0]);
+    uh = group_sum<W>(uh, red[1]);
+    const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+    const float f = rho * rho * rho * (uh * a.inv_d);
+    float *part = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      float o[E] = {};
+      get(H, c0, a.d, h);
+      get(dY, c0, a.d, u);
+      if (dH) get(dH, c0, a.d, o);
+      if (w) get(w, c0, a.d, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (part && c0 + e < a.d)
+          part[c0 + e] = fmaf(u[e] * h[e], rho, i == blockIdx.x ? 0.0f : part[c0 + e]);
+        o[e] += fmaf(w ? u[e] * g[e] : u[e], rho, -h[e] * f);
+      }
+      put(static_cast<T *>(a.dX) + i * a.lddx, c0, a.d, o);
+    }
+    if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
+  }
+}
+
+// gw[c] += sum over the parts, in float64 and in a fixed order: 16 waves take
+// every 16th part of 64 columns, then the waves in order.
+constexpr int kGainWaves = 16;
+__global__ __launch_bounds__(64 * kGainWaves) void gain_kernel(const float *__restrict__ part,
+                                                               int64_t parts, int64_t d,
+                                                               float *__restrict__ gw) {
+  __shared__ double red[kGainWaves][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+  double s = 0.0;
+  if (c < d) {
+#pragma unroll 8
+    for (int64_t b = w; b < parts; b += kGainWaves) s += static_cast<double>(part[b * d + c]);
+  }
+  red[w][lane] = s;
+  __syncthreads();
+  if (w != 0 || c >= d) return;
+#pragma unroll
+  for (int i = 1; i < kGainWaves; ++i) s += red[i][lane];
+  gw[c] = static_cast<float>(static_cast<double>(gw[c]) + s);
+}
+
+// pieces of a row; R * K of them are held by R threads in K pieces each
+int64_t pieces_of(int dt, int64_t d) { return ceil_div(d, dt == 0 ? 4 : 8); }
+
+template <typename T, int OUT>
+hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
+  const int64_t n = ceil_div(a.d, Piece<T>::E);
+  const auto grid = [&](int rows) {
+    const int64_t g = ceil_div(a.N, rows);
+    return static_cast<unsigned>(g < (1 << 20) ? g : 1 << 20);
+  };
+  if (n <= 64)
+    rmsnorm_kernel<T, 64, 1, 256, OUT><<<grid(4), 256, 0, s>>>(a);
+  else if (n <= 128)
+    rmsnorm_kernel<T, 64, 2, 256, OUT><<<grid(4), 256, 0, s>>>(a);
+  else if (n <= 256)
+    rmsnorm_kernel<T, 64, 4, 256, OUT><<<grid(4), 256, 0, s>>>(a);
+  else if (n <= 512)
+    rmsnorm_kernel<T, 256, 2, 256, OUT><<<grid(1), 256, 0, s>>>(a);
+  else if (n <= 1024)
+    rmsnorm_kernel<T, 256, 4, 256, OUT><<<grid(1), 256, 0, s>>>(a);
+  else if (n <= 4096)
+    rmsnorm_kernel<T, 1024, 4, 1024, OUT><<<grid(1), 1024, 0, s>>>(a);
+  else
+    rmsnorm_long_kernel<T, OUT><<<grid(1), 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_norm_out(const NormArgs &a, hipStream_t s) {
+  if (!a.S) return launch_norm_t<T, kOut>(a, s);
+  return a.group ? launch_norm_t<T, kOut8Group>(a, s) : launch_norm_t<T, kOut8Row>(a, s);
+}
+
+// Workgroups of the backward, two for each of the 256 CUs (each leaves a part of
+// d values), or a part for each row where they are few.
+constexpr int64_t kGradGroups = 512;
+
+struct GradPlan {
+  int rows;       // rows of a workgroup at a time
+  int64_t grid, parts;
+};
+GradPlan grad_plan(int dt, int64_t N, int64_t d) {
+  GradPlan p;
+  p.rows = pieces_of(dt, d) <= 128 ? 4 : 1;
+  p.grid = ceil_div(N, p.rows) < kGradGroups ? ceil_div(N, p.rows) : kGradGroups;
+  p.parts = p.grid * p.rows < N ? p.grid * p.rows : N;
+  return p;
+}
+
+template <typename T>
+hipError_t launch_grad_t(int dt, const NormGradArgs &a, hipStream_t s) {
+  const int64_t n = ceil_div(a.d, Piece<T>::E);
+  const unsigned g = static_cast<unsigned>(grad_plan(dt, a.N, a.d).grid);
+  if (n <= 64)
+    rmsnorm_grad_kernel<T, 64, 1, 256><<<g, 256, 0, s>>>(a);
+  else if (n <= 128)
+    rmsnorm_grad_kernel<T, 64, 2, 256><<<g, 256, 0, s>>>(a);
+  else if (n <= 256)
+    rmsnorm_grad_kernel<T, 256, 1, 256><<<g, 256, 0, s>>>(a);
+  else if (n <= 512)
+    rmsnorm_grad_kernel<T, 256, 2, 256><<<g, 256, 0, s>>>(a);
+  else if (n <= 1024)
+    rmsnorm_grad_kernel<T, 512, 2, 512><<<g, 512, 0, s>>>(a);
+  else if (n <= 2048)
+    rmsnorm_grad_kernel<T, 1024, 2, 1024><<<g, 1024, 0, s>>>(a);
+  else
+    rmsnorm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm(int dt, const NormArgs &a, hipStream_t s) {
+  return dt == 0 ? launch_norm_out<float>(a, s) : launch_norm_out<bf16_t>(a, s);
+}
+
+size_t rmsnorm_grad_workspace_bytes(int dt, int64_t N, int64_t d) {
+  return align256(static_cast<size_t>(grad_plan(dt, N, d).parts) * d * sizeof(float));
+}
+
+hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipStream_t s) {
+  a.part = gw ? static_cast<float *>(ws) : nullptr;
+  const hipError_t e = dt == 0 ? launch_grad_t<float>(dt, a, s) : launch_grad_t<bf16_t>(dt, a, s);
+  if (e != hipSuccess || !gw) return e;
+  gain_kernel<<<static_cast<unsigned>(ceil_div(a.d, 64)), 64 * kGainWaves, 0, s>>>(
+      a.part, grad_plan(dt, a.N, a.d).parts, a.d, gw);
+  return hipGetLastError();
+}
+
+}  // namespace sn

@@ -1,0 +1,117 @@
+// Row pieces and reductions shared by the kernels that work along rows of any
+// length and alignment (gfx950 only).
+#pragma once
+
+#include "sn_device.h"
+
+namespace sn {
+
+// A piece: 16 bytes of a row, 8 bf16 or 4 floats, one load or store of a lane.
+// Rows may start at any element (odd strides): the pointer types below promise
+// the element's alignment only, and gfx950 loads and stores 16 bytes at any
+// such address in one instruction.
+typedef uint32_t piece_b16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t piece_b32 __attribute__((ext_vector_type(4), aligned(4)));
+
+template <typename T> struct Piece;
+
+template <> struct Piece<bf16_t> {
+  static constexpr int E = 8;
+  typedef piece_b16 mem;
+  static __device__ __forceinline__ void unpack(u32x4 v, float (&x)[E]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = bf_lo(w[i]);
+      x[2 * i + 1] = bf_hi(w[i]);
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&x)[E]) {
+    return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                 pack_bf16x2(x[6], x[7])};
+  }
+};
+
+template <> struct Piece<float> {
+  static constexpr int E = 4;
+  typedef piece_b32 mem;
+  static __device__ __forceinline__ void unpack(u32x4 v, float (&x)[E]) {
+    const f32x4 f = __builtin_bit_cast(f32x4, v);
+    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&x)[E]) {
+    return __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
+  }
+};
+
+// NT: non-temporal, for data that nothing reads again soon.
+template <typename T, bool NT = false>
+__device__ __forceinline__ u32x4 load_piece(const T *p) {
+  auto q = reinterpret_cast<const typename Piece<T>::mem *>(p);
+  if constexpr (NT) return __builtin_nontemporal_load(q);
+  return *q;
+}
+template <typename T, bool NT = false>
+__device__ __forceinline__ void store_piece(T *p, u32x4 v) {
+  auto q = reinterpret_cast<typename Piece<T>::mem *>(p);
+  if constexpr (NT)
+    __builtin_nontemporal_store(static_cast<typename Piece<T>::mem>(v), q);
+  else
+    *q = v;
+}
+
+// The elements c0 .. c0 + E - 1 of a row of n: those at or past n read as `fill`
+// and are not written.
+template <typename T>
+__device__ __forceinline__ void load_part(const T *row, int64_t c0, int64_t n, float fill,
+                                          float (&x)[Piece<T>::E]) {
+#pragma unroll
+  for (int i = 0; i < Piece<T>::E; ++i) x[i] = c0 + i < n ? to_f32(row[c0 + i]) : fill;
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T *row, int64_t c0, int64_t n,
+                                           const float (&x)[Piece<T>::E]) {
+#pragma unroll
+  for (int i = 0; i < Piece<T>::E; ++i)
+    if (c0 + i < n) row[c0 + i] = from_f32<T>(x[i]);
+}
+
+// ---- reductions: every lane / thread gets the result ------------------------
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+  return v;
+}
+
+// Sums / maxima over a workgroup of W waves; red: W floats of LDS that no
+// thread uses between the caller's last barrier and the call, nor after it
+// before the next barrier.  One barrier.  The waves are added in order.
+template <int W>
+__device__ __forceinline__ float group_sum(float v, float *red) {
+  v = wave_sum(v);
+  if constexpr (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) v += red[i];
+  return v;
+}
+template <int W>
+__device__ __forceinline__ float group_max(float v, float *red) {
+  v = wave_max(v);
+  if constexpr (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) v = fmaxf(v, red[i]);
+  return v;
+}
+
+}  // namespace sn

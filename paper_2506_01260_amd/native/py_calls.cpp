@@ -18,8 +18,12 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <initializer_list>
+#include <vector>
 
 #include "sn.h"
 
@@ -30,7 +34,10 @@ namespace {
   X(sn_project_weights) X(sn_project_weights_workspace_bytes) X(sn_project_weights_multi)     \
   X(sn_project_weights_multi_workspace_bytes) X(sn_grassmann_accumulate)                      \
   X(sn_grassmann_workspace_bytes) X(sn_embed_lowrank_forward) X(sn_embed_lowrank_backward)    \
-  X(sn_embed_lowrank_workspace_bytes) X(sn_adamw_step) X(sn_adamw_workspace_bytes)
+  X(sn_embed_lowrank_workspace_bytes) X(sn_adamw_step) X(sn_adamw_workspace_bytes)            \
+  X(sn_token_logprobs) X(sn_token_logprobs_backward) X(sn_token_loss) X(sn_rmsnorm)           \
+  X(sn_rmsnorm_quant) X(sn_rmsnorm_backward) X(sn_rmsnorm_backward_workspace_bytes)           \
+  X(sn_grad_sumsq) X(sn_grad_sumsq_workspace_bytes) X(sn_grad_clip)
 
 struct Calls {
 #define X(f) decltype(&::f) f = nullptr;
@@ -512,6 +519,346 @@ SN_FAST(adamw_step) {
   });
 }
 
+// ---- token log probabilities, norms, gradient clipping ----------------------
+// These take calls on the current stream only (stream None), with every tensor on
+// the current device.
+
+const at::Tensor *here(PyObject *o) {
+  const at::Tensor *t = plain(o);
+  return t && t->get_device() == c10::hip::current_device() ? t : nullptr;
+}
+
+bool mat_here(PyObject *o, Mat &m) { return here(o) && mat(o, m); }
+
+bool sn_type(at::ScalarType t) { return t == at::kFloat || t == at::kBFloat16; }
+int32_t dt_of(at::ScalarType t) { return t == at::kFloat ? SN_F32 : SN_BF16; }
+
+// A contiguous vector of n values (absent: None).
+bool vec(PyObject *o, at::ScalarType type, int64_t n, void *&p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor *t = here(o);
+  if (!t || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n ||
+      (n > 1 && t->stride(0) != 1))
+    return false;
+  p = t->data_ptr();
+  return true;
+}
+
+bool number(PyObject *o, double &v) {
+  if (PyFloat_CheckExact(o)) {
+    v = PyFloat_AS_DOUBLE(o);
+    return true;
+  }
+  int64_t i;
+  if (!int_of(o, i)) return false;
+  v = static_cast<double>(i);
+  return true;
+}
+
+at::Tensor make(PyObject *like, at::ScalarType type, at::IntArrayRef shape) {
+  return at::empty(shape, THPVariable_Unpack(like).options().dtype(type).requires_grad(false));
+}
+
+// The output argument of the given type and shape, or a new matrix.
+bool output_here(PyObject *o, PyObject *like, at::ScalarType type, int64_t rows, int64_t cols,
+                 Mat &m, at::Tensor &t) {
+  return (o == Py_None || here(o)) && output(o, like, type, rows, cols, m, t);
+}
+
+PyObject *wrap(PyObject *o, at::Tensor &made) {
+  return made.defined() ? THPVariable_Wrap(std::move(made)) : given(o);
+}
+
+bool failed(int32_t status) {
+  if (status == SN_OK) return false;
+  Py_XDECREF(PyObject_CallFunction(g_check, "i", status));
+  return PyErr_Occurred() != nullptr;
+}
+
+// A tuple of new references; none of them if one is missing.
+PyObject *tuple_of(std::initializer_list<PyObject *> items) {
+  PyObject *r = PyTuple_New(static_cast<Py_ssize_t>(items.size()));
+  Py_ssize_t i = 0;
+  bool whole = r != nullptr;
+  for (PyObject *o : items) {
+    whole = whole && o;
+    if (r) PyTuple_SET_ITEM(r, i++, o);
+    else Py_XDECREF(o);
+  }
+  if (!whole) Py_CLEAR(r);
+  return r;
+}
+
+bool tokens(PyObject *o, int64_t n, const int32_t *&p) {
+  return o == Py_None ? (p = nullptr, true) : here(o) && ids(o, true, n, p);
+}
+bool flag_here(PyObject *o, int32_t *&p) { return (o == Py_None || here(o)) && flag(o, p); }
+
+// (Z, tok, n_top, scale, err_flag, stream)
+SN_FAST(token_logprobs) {
+  return guarded(n, 6, [&](bool &taken) -> PyObject * {
+    Mat z;
+    const int32_t *tok;
+    int32_t *err;
+    int64_t top;
+    double scale;
+    sn_stream s;
+    if (a[5] != Py_None || !mat_here(a[0], z) || !sn_type(z.type) || !tokens(a[1], z.rows, tok) ||
+        !int_of(a[2], top) || top < 0 || top > SN_MAX_TOP || !number(a[3], scale) ||
+        !flag_here(a[4], err) || !stream(a[5], s))
+      SN_LEAVE;
+    const int64_t N = z.rows;
+    at::Tensor lp, h = make(a[0], at::kFloat, {N}), st = make(a[0], at::kFloat, {N, 2}), tl, ti;
+    const bool given_tok = a[1] != Py_None;
+    if (given_tok) lp = make(a[0], at::kFloat, {N});
+    if (top) {
+      tl = make(a[0], at::kFloat, {N, top});
+      ti = make(a[0], at::kInt, {N, top});
+    }
+    float *lpp = given_tok ? lp.data_ptr<float>() : nullptr, *hp = h.data_ptr<float>();
+    float *sp = st.data_ptr<float>(), *tlp = top ? tl.data_ptr<float>() : nullptr;
+    int32_t *tip = top ? ti.data_ptr<int32_t>() : nullptr;
+    if (failed(launch([&] {
+          return g_lib.sn_token_logprobs(z.p, N, z.cols, z.ld, dt_of(z.type), scale, tok, lpp, hp,
+                                         sp, static_cast<int32_t>(top), tlp, tip, err, s);
+        })))
+      return nullptr;
+    return tuple_of({wrap(Py_None, lp), wrap(Py_None, h), wrap(Py_None, st), wrap(Py_None, tl),
+                     wrap(Py_None, ti)});
+  });
+}
+
+// (Z, stats, entropy, tok, g_logp, g_entropy, scale, out, err_flag, stream)
+SN_FAST(token_logprobs_backward) {
+  return guarded(n, 10, [&](bool &taken) -> PyObject * {
+    Mat z, stats, out;
+    const int32_t *tok;
+    int32_t *err;
+    double scale;
+    void *ent, *gl, *gh;
+    sn_stream s;
+    at::Tensor made;
+    if (a[9] != Py_None || !mat_here(a[0], z) || !sn_type(z.type) || !mat_here(a[1], stats) ||
+        stats.type != at::kFloat || stats.rows != z.rows || stats.cols != 2 || stats.ld != 2 ||
+        !vec(a[2], at::kFloat, z.rows, ent) || !tokens(a[3], z.rows, tok) ||
+        !vec(a[4], at::kFloat, z.rows, gl) || !vec(a[5], at::kFloat, z.rows, gh) ||
+        !number(a[6], scale) || !flag_here(a[8], err) || !stream(a[9], s) ||
+        !output_here(a[7], a[0], z.type, z.rows, z.cols, out, made))
+      SN_LEAVE;
+    const int32_t st = launch([&] {
+      return g_lib.sn_token_logprobs_backward(
+          z.p, z.rows, z.cols, z.ld, dt_of(z.type), scale, tok, static_cast<float *>(stats.p),
+          static_cast<float *>(ent), static_cast<float *>(gl), static_cast<float *>(gh), out.p,
+          out.ld, err, s);
+    });
+    return finish(st, a[7], made);
+  });
+}
+
+// (Z, tok, weight, scale, out, err_flag, stream)
+SN_FAST(token_loss) {
+  return guarded(n, 7, [&](bool &taken) -> PyObject * {
+    Mat z, out;
+    const int32_t *tok;
+    int32_t *err;
+    double scale;
+    void *w;
+    sn_stream s;
+    at::Tensor made;
+    if (a[6] != Py_None || a[1] == Py_None || !mat_here(a[0], z) || !sn_type(z.type) ||
+        !tokens(a[1], z.rows, tok) || !vec(a[2], at::kFloat, z.rows, w) || !number(a[3], scale) ||
+        !flag_here(a[5], err) || !stream(a[6], s) ||
+        !output_here(a[4], a[0], z.type, z.rows, z.cols, out, made))
+      SN_LEAVE;
+    at::Tensor lp = make(a[0], at::kFloat, {z.rows});
+    float *lpp = lp.data_ptr<float>();
+    if (failed(launch([&] {
+          return g_lib.sn_token_loss(z.p, z.rows, z.cols, z.ld, dt_of(z.type), scale, tok,
+                                     static_cast<float *>(w), lpp, out.p, out.ld, err, s);
+        })))
+      return nullptr;
+    return tuple_of({wrap(Py_None, lp), wrap(a[4], made)});
+  });
+}
+
+// What the norm's forward calls share: X, w, residual, eps, resid_out.
+struct Norm {
+  Mat x, r, h;
+  void *w = nullptr;
+  double eps = 0.0;
+  at::Tensor made;  // H, where it is new
+};
+bool norm(PyObject *X, PyObject *w, PyObject *res, PyObject *eps, PyObject *H, Norm &c) {
+  if (!mat_here(X, c.x) || !sn_type(c.x.type) || !vec(w, c.x.type, c.x.cols, c.w) ||
+      !number(eps, c.eps))
+    return false;
+  if (res != Py_None && (!mat_here(res, c.r) || c.r.type != c.x.type || c.r.rows != c.x.rows ||
+                         c.r.cols != c.x.cols))
+    return false;
+  if (res == Py_None && H == Py_None) return true;
+  return output_here(H, X, c.x.type, c.x.rows, c.x.cols, c.h, c.made);
+}
+// the call's H: what was made or given, or X
+PyObject *norm_h(PyObject *X, PyObject *H, Norm &c) {
+  return wrap(H == Py_None ? X : H, c.made);
+}
+
+// (X, w, residual, eps, out, resid_out, stream)
+SN_FAST(rmsnorm) {
+  return guarded(n, 7, [&](bool &taken) -> PyObject * {
+    Norm c;
+    Mat y;
+    sn_stream s;
+    at::Tensor made;
+    if (a[6] != Py_None || !norm(a[0], a[1], a[2], a[3], a[5], c) || !stream(a[6], s) ||
+        !output_here(a[4], a[0], c.x.type, c.x.rows, c.x.cols, y, made))
+      SN_LEAVE;
+    if (failed(launch([&] {
+          return g_lib.sn_rmsnorm(c.x.p, c.x.rows, c.x.cols, c.x.ld, dt_of(c.x.type), c.r.p, c.r.ld,
+                                  c.w, c.eps, c.h.p, c.h.ld, y.p, y.ld, s);
+        })))
+      return nullptr;
+    return tuple_of({wrap(a[4], made), norm_h(a[0], a[5], c)});
+  });
+}
+
+// (X, w, residual, eps, group, out, scales, resid_out, stream)
+SN_FAST(rmsnorm_quant) {
+  return guarded(n, 9, [&](bool &taken) -> PyObject * {
+    Norm c;
+    Mat q, sc;
+    int64_t group;
+    sn_stream s;
+    at::Tensor qmade, smade;
+    if (a[8] != Py_None || !int_of(a[4], group) || (group != 0 && group != 128) ||
+        !norm(a[0], a[1], a[2], a[3], a[7], c) || !stream(a[8], s))
+      SN_LEAVE;
+    const int64_t scales = group ? (c.x.cols + group - 1) / group : 1;
+    if (!output_here(a[5], a[0], at::kFloat8_e4m3fn, c.x.rows, c.x.cols, q, qmade) ||
+        !output_here(a[6], a[0], at::kFloat, c.x.rows, scales, sc, smade))
+      SN_LEAVE;
+    if (failed(launch([&] {
+          return g_lib.sn_rmsnorm_quant(c.x.p, c.x.rows, c.x.cols, c.x.ld, dt_of(c.x.type), c.r.p,
+                                        c.r.ld, c.w, c.eps, c.h.p, c.h.ld,
+                                        static_cast<int32_t>(group), q.p, q.ld,
+                                        static_cast<float *>(sc.p), sc.ld, s);
+        })))
+      return nullptr;
+    return tuple_of({wrap(a[5], qmade), wrap(a[6], smade), norm_h(a[0], a[7], c)});
+  });
+}
+
+// (H, dY, w, dH, eps, gw, out, workspace, stream)
+SN_FAST(rmsnorm_backward) {
+  return guarded(n, 9, [&](bool &taken) -> PyObject * {
+    Mat h, dy, dh, out;
+    void *w, *gw, *ws = nullptr;
+    double eps;
+    sn_stream s;
+    size_t bytes = 0;
+    at::Tensor made, wmade;
+    if (a[8] != Py_None || !mat_here(a[0], h) || !sn_type(h.type) || !mat_here(a[1], dy) ||
+        dy.type != h.type || dy.rows != h.rows || dy.cols != h.cols ||
+        !vec(a[2], h.type, h.cols, w) ||
+        (a[3] != Py_None && (!mat_here(a[3], dh) || dh.type != h.type || dh.rows != h.rows ||
+                             dh.cols != h.cols)) ||
+        !number(a[4], eps) || !vec(a[5], at::kFloat, h.cols, gw) || !stream(a[8], s))
+      SN_LEAVE;
+    const int32_t dt = dt_of(h.type);
+    const size_t need = gw ? g_lib.sn_rmsnorm_backward_workspace_bytes(h.rows, h.cols, dt) : 0;
+    if (a[7] != Py_None) {
+      const at::Tensor *t = here(a[7]);
+      if (!t || t->scalar_type() != at::kByte || !t->is_contiguous()) SN_LEAVE;
+    }
+    if (need && !workspace(a[7], a[0], need, ws, bytes, wmade)) SN_LEAVE;
+    if (!output_here(a[6], a[0], h.type, h.rows, h.cols, out, made)) SN_LEAVE;
+    const int32_t st = launch([&] {
+      return g_lib.sn_rmsnorm_backward(h.p, h.rows, h.cols, h.ld, dt, dy.p, dy.ld, w, eps, dh.p,
+                                       dh.ld, out.p, out.ld, static_cast<float *>(gw), ws, bytes,
+                                       s);
+    });
+    return finish(st, a[6], made);
+  });
+}
+
+// The tensors of a list, each without gaps.
+bool tensors(PyObject *o, std::vector<sn_tensor> &v) {
+  if (!PyList_CheckExact(o)) return false;
+  const Py_ssize_t count = PyList_GET_SIZE(o);
+  v.resize(static_cast<size_t>(count));
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    const at::Tensor *t = here(PyList_GET_ITEM(o, i));
+    if (!t || !sn_type(t->scalar_type()) || !t->is_contiguous()) return false;
+    const int64_t e = t->numel();
+    v[static_cast<size_t>(i)] = {e ? t->data_ptr() : nullptr, 1, e, e, dt_of(t->scalar_type())};
+  }
+  return true;
+}
+
+// (grads, out, workspace, stream)
+SN_FAST(grad_sumsq) {
+  return guarded(n, 4, [&](bool &taken) -> PyObject * {
+    std::vector<sn_tensor> g;
+    void *to, *ws;
+    size_t bytes;
+    sn_stream s;
+    at::Tensor made, wmade;
+    if (a[3] != Py_None || !tensors(a[0], g) || g.empty() || !stream(a[3], s) ||
+        !vec(a[1], at::kDouble, 1, to))
+      SN_LEAVE;
+    PyObject *like = PyList_GET_ITEM(a[0], 0);
+    const int32_t count = static_cast<int32_t>(g.size());
+    const size_t need = g_lib.sn_grad_sumsq_workspace_bytes(count, g.data());
+    if (need == 0) SN_LEAVE;
+    if (a[2] != Py_None) {
+      const at::Tensor *t = here(a[2]);
+      if (!t || t->scalar_type() != at::kByte || !t->is_contiguous()) SN_LEAVE;
+    }
+    if (!workspace(a[2], like, need, ws, bytes, wmade)) SN_LEAVE;
+    if (!to) {
+      made = make(like, at::kDouble, {1});
+      to = made.data_ptr();
+    }
+    const int32_t st = launch([&] {
+      return g_lib.sn_grad_sumsq(count, g.data(), static_cast<double *>(to), ws, bytes, s);
+    });
+    return finish(st, a[1], made);
+  });
+}
+
+// (grads, sumsq, max_norm, out, norm, stream)
+SN_FAST(grad_clip) {
+  return guarded(n, 6, [&](bool &taken) -> PyObject * {
+    std::vector<sn_tensor> g, out;
+    void *from, *to;
+    double most;
+    sn_stream s;
+    at::Tensor made;
+    if (a[5] != Py_None || !tensors(a[0], g) || g.empty() || a[1] == Py_None ||
+        !vec(a[1], at::kDouble, 1, from) || !number(a[2], most) || !stream(a[5], s) ||
+        !vec(a[4], at::kFloat, 1, to))
+      SN_LEAVE;
+    if (a[3] != Py_None) {
+      if (!tensors(a[3], out) || out.size() != g.size()) SN_LEAVE;
+      for (size_t i = 0; i < g.size(); ++i)
+        if (THPVariable_Unpack(PyList_GET_ITEM(a[0], static_cast<Py_ssize_t>(i))).sizes() !=
+            THPVariable_Unpack(PyList_GET_ITEM(a[3], static_cast<Py_ssize_t>(i))).sizes())
+          SN_LEAVE;
+    }
+    if (!to) {
+      made = make(PyList_GET_ITEM(a[0], 0), at::kFloat, {1});
+      to = made.data_ptr();
+    }
+    const int32_t st = launch([&] {
+      return g_lib.sn_grad_clip(static_cast<int32_t>(g.size()), g.data(),
+                                out.empty() ? nullptr : out.data(), static_cast<double *>(from),
+                                most, static_cast<float *>(to), s);
+    });
+    return finish(st, a[4], made);
+  });
+}
+
 // bind(addresses: dict of entry point -> address, check: status check)
 SN_FAST(bind) {
   if (n != 2 || !PyDict_Check(a[0])) {
@@ -544,6 +891,14 @@ PyMethodDef g_methods[] = {SN_METHOD(bind),
                            SN_METHOD(embed_lowrank_forward),
                            SN_METHOD(embed_lowrank_backward),
                            SN_METHOD(adamw_step),
+                           SN_METHOD(token_logprobs),
+                           SN_METHOD(token_logprobs_backward),
+                           SN_METHOD(token_loss),
+                           SN_METHOD(rmsnorm),
+                           SN_METHOD(rmsnorm_quant),
+                           SN_METHOD(rmsnorm_backward),
+                           SN_METHOD(grad_sumsq),
+                           SN_METHOD(grad_clip),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods,
                         nullptr,               nullptr,  nullptr, nullptr};

@@ -1,0 +1,416 @@
+"""GPU parity of the token log probabilities, their backward and the loss call
+through the binding against the float64 oracle.
+
+Tolerances (u = 2^-24, the rounding of a float32 operation).  For a row of V
+logits with differences x = c (z - m), L = log S and a = E_p |x|:
+  * S is a float32 sum of at most V / 64 terms per thread and a tree of 10 more
+    levels, its terms e^x wrong by 2 ulp of the exponential and 2 |x| u of its
+    argument:  dS / S <= u (V / 64 + 16 + 2 a) =: u s
+  * log p = x - L:      u (4 + 2 |x| + 2 |L| + s)
+  * H = L - E_p x:      u (4 + 2 |L| + s (1 + a) + 4 E_p x^2)
+  * backward, stats and H rounded once to float32:
+    c p (|gl| + |gh| (|log p| + H)) u (16 + 4 |log p| + 4 |x| + 4 |L|) + 4 u |gl| c d_jt
+  * loss: |w| c p u (16 + 4 |x| + s) + 4 u |w| c d_jt
+and for bf16 gradients half an ulp more (2^-8 of the value, its own rounding
+included).  Probabilities below 2^-120 may be 0.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01260_amd as sn
+from gpu_helpers import host, log
+from oracle import logprobs as orc
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+TINY = 2.0 ** -120
+INF = float("inf")
+
+
+def _logits(seed, n, v, dtype, pad=0, std=3.0):
+    """n x v logits as a view with `pad` more columns to a row."""
+    g = torch.Generator().manual_seed(seed)
+    full = (torch.randn(n, v + pad, generator=g) * std).to(DT[dtype]).cuda()
+    return full[:, :v]
+
+
+def _tokens(seed, n, v, padded=0.2):
+    r = np.random.default_rng(seed)
+    tok = r.integers(0, v, n)
+    tok[r.random(n) < padded] = -1
+    return tok
+
+
+def _bounds(Z, lp, scale):
+    """(x, |x|, s, L, a, E_p x^2) of the tolerances above."""
+    V = Z.shape[1]
+    with np.errstate(invalid="ignore"):
+        x = scale * (Z - Z.max(1, keepdims=True))
+    x = np.where(np.isfinite(x), x, 0.0)
+    p = np.where(np.isfinite(lp), np.exp(lp), 0.0)
+    a = (p * np.abs(x)).sum(1)
+    L = -(np.where(np.isfinite(lp), lp, 0.0) - x).max(1)
+    s = V / 64 + 16 + 2 * a
+    return np.abs(x), s, np.abs(L), a, (p * x * x).sum(1)
+
+
+def _near(got, ref, tol, what):
+    got, ref = np.asarray(got, np.float64), np.asarray(ref, np.float64)
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    with np.errstate(over="ignore"):  # a value past float32's range is an infinity there
+        ref = np.where(np.isfinite(ref.astype(np.float32)), ref, ref.astype(np.float32))
+    fine = np.isfinite(ref)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), what
+    assert np.array_equal(got[~fine & ~np.isnan(ref)], ref[~fine & ~np.isnan(ref)]), what
+    err = np.abs(got - ref)[fine]
+    tol = np.broadcast_to(tol, ref.shape)[fine]
+    if err.size:
+        k = int(np.argmax(err - tol))
+        assert (err <= tol).all(), f"{what}: {err[k]:.3g} over {tol[k]:.3g}"
+        log(f"  {what}: ok, at most {float(np.max(err / np.maximum(tol, 1e-300))):.2g} of the bound")
+
+
+def _check_forward(Z, tok, n_top, scale, what):
+    zh = host(Z)
+    n = len(zh)
+    r = sn.sn_token_logprobs(Z, torch.tensor(tok, dtype=torch.int32).cuda(), n_top=n_top, scale=scale)
+    logp, H, stats, top_logp, top_id = orc.token_logprobs(zh, tok, n_top, scale)
+    lp = orc.log_p(zh, scale)
+    ax, s, L, a, x2 = _bounds(zh, lp, scale)
+    axt = np.where(tok >= 0, ax[np.arange(n), np.maximum(tok, 0)], 0)
+    _near(host(r.logp), logp, U * (4 + 2 * axt + 2 * L + s), f"{what} logp")
+    _near(host(r.entropy), H, U * (4 + 2 * L + s * (1 + a) + 4 * x2), f"{what} entropy")
+    _near(host(r.stats[:, 0]), stats[:, 0], 0.0, f"{what} stats m")
+    _near(host(r.stats[:, 1]), stats[:, 1], U * (4 + 2 * L + s), f"{what} stats L")
+    if n_top:
+        assert np.array_equal(r.top_id.cpu().numpy(), top_id), f"{what} top_id"
+        with np.errstate(invalid="ignore"):
+            axj = np.take_along_axis(ax, np.maximum(top_id, 0), 1)
+        _near(host(r.top_logp), top_logp, U * (4 + 2 * axj + (2 * L + s)[:, None]), f"{what} top")
+    else:
+        assert r.top_logp is None and r.top_id is None
+
+
+SHAPES = [(1, 1), (1, 2), (3, 7), (5, 64), (4, 257), (2, 1000), (7, 2049), (3, 4097), (2, 16385),
+          (1, 50257), (2, 32000), (1, 128256)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", SHAPES)
+def test_forward_matches_oracle(dtype, n, v):
+    log(f"[logprobs] {dtype} {n} x {v}")
+    for n_top, scale, pad in ((0, 1.0, 0), (min(v, 5), 0.7, 3), (min(v, 64), 1.25, 1)):
+        Z = _logits(n + v + n_top, n, v, dtype, pad)
+        _check_forward(Z, _tokens(v, n, v), n_top, scale, f"top {n_top} pad {pad}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows(dtype):
+    log(f"[logprobs many rows] {dtype}")
+    for n, v, n_top in ((3001, 33, 4), (2100, 520, 3)):
+        _check_forward(_logits(v, n, v, dtype), _tokens(n, n, v), n_top, 1.0, f"{n} x {v}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [9, 700, 5000])
+def test_ties_forbidden_and_empty_rows(dtype, v):
+    """Equal logits in every order, forbidden ones, a row with nothing allowed, the
+    type's lowest value, zeros of both signs."""
+    log(f"[logprobs special rows] {dtype} V={v}")
+    Z = _logits(v, 12, v, dtype).clone()
+    low = torch.finfo(Z.dtype).min
+    Z[0] = 1.5                                  # all equal
+    Z[1] = torch.round(Z[1])                    # many ties
+    Z[2, 1:] = -INF                             # one allowed
+    Z[3] = -INF                                 # none
+    Z[4] = low                                  # all the lowest value
+    Z[5, ::2] = low
+    Z[6, ::3] = -INF
+    Z[7] = torch.arange(v).flip(0).to(Z.dtype) / 64.0   # descending
+    Z[8] = torch.arange(v).to(Z.dtype) / 64.0           # ascending
+    Z[9] = -0.0
+    Z[9, ::2] = 0.0
+    Z[10, :] = -INF
+    Z[10, v // 2:] = low
+    Z[11] = torch.finfo(Z.dtype).max
+    Z[11, 0] = low
+    tok = np.array([v - 1, 0, 0, 1, 2, 1, 1, -1, v - 1, 3, 0, 0])
+    for n_top in (1, 5, min(v, 64)):
+        _check_forward(Z, tok, n_top, 1.0, f"top {n_top}")
+
+
+def test_rows_without_a_distribution():
+    """NaN or +inf: NaN everywhere and ids of -1; the rows beside it are untouched."""
+    log("[logprobs NaN]")
+    for dtype in ("f32", "bf16"):
+        for bad in (float("nan"), -float("nan"), INF):
+            Z = _logits(3, 5, 3000, dtype).clone()
+            Z[1, 2999] = bad
+            Z[3, 0] = bad
+            _check_forward(Z, np.array([1, 2, 3, 4, 5]), 6, 1.0, f"{dtype} {bad}")
+            r = sn.sn_token_logprobs(Z)
+            assert r.logp is None and bool(torch.isnan(r.entropy[[1, 3]]).all())
+
+
+def test_offsets_past_two_to_the_31():
+    """More than 2^31 logits in one matrix: the last rows."""
+    log("[logprobs 2^31]")
+    n, v = 17200, 128256
+    Z = torch.zeros(n, v, dtype=torch.bfloat16, device="cuda")
+    Z[-3:] = _logits(1, 3, v, "bf16")
+    tok = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    tok[-3:] = torch.tensor([0, 77, v - 1], dtype=torch.int32)
+    r = sn.sn_token_logprobs(Z, tok, n_top=2)
+    ref = orc.token_logprobs(host(Z[-3:]), tok[-3:].cpu().numpy(), 2)
+    assert np.abs(host(r.logp[-3:]) - ref[0]).max() < 1e-3
+    assert np.array_equal(r.top_id[-3:].cpu().numpy(), ref[4])
+    assert r.top_id[0].tolist() == [0, 1] and float(r.logp[0]) == 0.0
+    logp, dZ = sn.sn_token_loss(Z, tok, out=Z)
+    assert torch.equal(logp, r.logp) or float((logp - r.logp).abs().max()) < 1e-4
+    assert float(dZ[:-3].abs().max()) == 0.0
+    assert abs(float(dZ[-1].double().sum())) < 2e-2 and float(dZ[-1, v - 1]) < -0.5
+
+
+def _round(tol, ref, dtype):
+    return tol + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else 0.0) + TINY
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", SHAPES + [(300, 130)])
+def test_backward_matches_oracle(dtype, n, v):
+    log(f"[logprobs backward] {dtype} {n} x {v}")
+    rng = np.random.default_rng(v)
+    for scale, pad, use in ((1.0, 0, "le"), (0.7, 3, "l"), (1.25, 1, "e")):
+        Z = _logits(v + pad, n, v, dtype, pad)
+        zh, tok = host(Z), _tokens(v, n, v)
+        gl = rng.standard_normal(n).astype(np.float32) if "l" in use else None
+        gh = rng.standard_normal(n).astype(np.float32) if "e" in use else None
+        _, H, stats, _, _ = orc.token_logprobs(zh, tok, 0, scale)
+        dev = lambda a: None if a is None else torch.tensor(a, dtype=torch.float32).cuda()  # noqa: E731
+        out = torch.full((n, v + pad), 9.0, dtype=Z.dtype, device="cuda")[:, :v]
+        got = sn.sn_token_logprobs_backward(Z, dev(stats), dev(H), torch.tensor(tok, dtype=torch.int32).cuda(),
+                                            g_logp=dev(gl), g_entropy=dev(gh), scale=scale, out=out)
+        assert got is out
+        ref = orc.token_logprobs_backward(zh, tok, gl, gh, scale)
+        lp = orc.log_p(zh, scale)
+        ax, s, L, a, _ = _bounds(zh, lp, scale)
+        gla = np.zeros(n) if gl is None else np.where(tok >= 0, np.abs(gl), 0)
+        gha = np.zeros(n) if gh is None else np.abs(gh)
+        p = np.exp(lp)
+        tol = scale * p * (gla[:, None] + gha[:, None] * (np.abs(lp) + H[:, None])) * U * \
+            (16 + 4 * np.abs(lp) + 4 * ax + 4 * L[:, None])
+        hit = np.arange(v)[None] == tok[:, None]
+        tol = tol + 4 * U * scale * gla[:, None] * hit
+        _near(host(got), ref, _round(tol, ref, dtype), f"{use} scale {scale} pad {pad}")
+        # in place, the same bits
+        Zc = Z.clone()
+        same = sn.sn_token_logprobs_backward(Zc, dev(stats), dev(H), torch.tensor(tok, dtype=torch.int32).cuda(),
+                                             g_logp=dev(gl), g_entropy=dev(gh), scale=scale, out=Zc)
+        assert same is Zc and torch.equal(Zc, out)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", SHAPES + [(700, 130)])
+def test_loss_matches_oracle(dtype, n, v):
+    log(f"[loss] {dtype} {n} x {v}")
+    rng = np.random.default_rng(v)
+    for scale, pad, weighted in ((1.0, 0, True), (0.7, 3, False), (1.25, 1, True)):
+        Z = _logits(v + pad, n, v, dtype, pad)
+        zh, tok = host(Z), _tokens(v, n, v)
+        w = rng.random(n).astype(np.float32) if weighted else None
+        if weighted and n > 2:
+            w[1] = 0.0
+        tk = torch.tensor(tok, dtype=torch.int32).cuda()
+        wd = None if w is None else torch.tensor(w).cuda()
+        out = torch.full((n, v + pad), 9.0, dtype=Z.dtype, device="cuda")[:, :v]
+        logp, got = sn.sn_token_loss(Z, tk, weight=wd, scale=scale, out=out)
+        assert got is out
+        ref_lp, ref = orc.token_loss(zh, tok, w, scale)
+        lp = orc.log_p(zh, scale)
+        ax, s, L, a, _ = _bounds(zh, lp, scale)
+        wa = np.where(tok >= 0, np.ones(n) if w is None else w, 0.0)[:, None]
+        axt = np.where(tok >= 0, ax[np.arange(n), np.maximum(tok, 0)], 0)
+        _near(host(logp), ref_lp, U * (4 + 2 * axt + 2 * L + s), "logp")
+        hit = np.arange(v)[None] == tok[:, None]
+        tol = wa * scale * U * (np.exp(lp) * (16 + 4 * ax + s[:, None]) + 4 * hit)
+        _near(host(got), ref, _round(tol, ref, dtype), f"dZ scale {scale} pad {pad}")
+        Zc = Z.clone()
+        lp2, same = sn.sn_token_loss(Zc, tk, weight=wd, scale=scale, out=Zc)
+        assert same is Zc and torch.equal(Zc, out) and torch.equal(lp2, logp)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_special_rows(dtype):
+    """Forbidden logits get no gradient, an empty row only the given token's, a NaN
+    row NaN; a row that nothing flows into is 0 whatever it holds."""
+    log(f"[gradients of special rows] {dtype}")
+    v = 600
+    Z = _logits(2, 6, v, dtype).clone()
+    Z[0, ::2] = -INF
+    Z[1] = -INF
+    Z[2, 5] = float("nan")
+    Z[3, 5] = float("nan")
+    Z[4] = torch.finfo(Z.dtype).min
+    Z[5, 0] = INF
+    tok = np.array([1, 3, 4, -1, 7, 2])
+    tk = torch.tensor(tok, dtype=torch.int32).cuda()
+    w = np.array([0.5, 0.25, 1.0, 1.0, 2.0, 0.0], np.float32)
+    logp, dZ = sn.sn_token_loss(Z, tk, weight=torch.tensor(w).cuda())
+    ref_lp, ref = orc.token_loss(host(Z), tok, w)
+    _near(host(dZ), ref, _round(1e-6 * np.ones_like(ref), ref, dtype), "loss dZ")
+    _near(host(logp), ref_lp, 1e-5, "loss logp")
+    r = sn.sn_token_logprobs(Z, tk)
+    gl, gh = -w, np.array([0.1, 0.2, 0.3, 0.0, 0.4, 0.0], np.float32)
+    got = sn.sn_token_logprobs_backward(Z, r.stats, r.entropy, tk, g_logp=torch.tensor(gl).cuda(),
+                                        g_entropy=torch.tensor(gh).cuda())
+    ref = orc.token_logprobs_backward(host(Z), tok, gl, gh)
+    _near(host(got), ref, _round(1e-6 * np.ones_like(ref), ref, dtype), "backward dZ")
+    assert float(got[3].abs().max()) == 0.0 and float(dZ[5].abs().max()) == 0.0
+
+
+def test_gradient_against_differences():
+    """<dZ, v> against central differences of sum gl logp + gh H along v (float32
+    outputs: 1e-6 / step, the third derivative times step^2 / 6)."""
+    log("[gradient against differences]")
+    n, v, scale, step = 6, 901, 0.8, 2.0 ** -6
+    Z = _logits(9, n, v, "f32")
+    tk = torch.tensor(_tokens(4, n, v, 0.0), dtype=torch.int32).cuda()
+    g = torch.Generator().manual_seed(1)
+    gl, gh, dv = (torch.randn(s, generator=g).cuda() for s in (n, n, (n, v)))
+
+    def f(z):
+        r = sn.sn_token_logprobs(z, tk, scale=scale)
+        return float((gl.double() * r.logp.double() + gh.double() * r.entropy.double()).sum())
+
+    r = sn.sn_token_logprobs(Z, tk, scale=scale)
+    d = sn.sn_token_logprobs_backward(Z, r.stats, r.entropy, tk, g_logp=gl, g_entropy=gh, scale=scale)
+    want = (f(Z + step * dv) - f(Z - step * dv)) / (2 * step)
+    have = float((d.double() * dv.double()).sum())
+    log(f"  {have:.6f} against {want:.6f}")
+    assert abs(have - want) <= 2e-3 * max(1.0, abs(want))
+    _, d = sn.sn_token_loss(Z, tk, weight=gl, scale=scale)
+    gh.zero_()
+    want = -(f(Z + step * dv) - f(Z - step * dv)) / (2 * step)
+    have = float((d.double() * dv.double()).sum())
+    assert abs(have - want) <= 2e-3 * max(1.0, abs(want))
+
+
+def test_ids_out_of_range_are_clamped_and_reported():
+    log("[ids]")
+    Z = _logits(5, 4, 100, "bf16")
+    tk = torch.tensor([5, 100, -2, -1], dtype=torch.int32).cuda()
+    fixed = torch.tensor([5, 99, 0, -1], dtype=torch.int32).cuda()
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    a = sn.sn_token_logprobs(Z, tk, err_flag=flag)
+    assert int(flag) == 1
+    assert torch.equal(a.logp, sn.sn_token_logprobs(Z, fixed).logp)
+    flag.zero_()
+    x = sn.sn_token_loss(Z, tk, err_flag=flag)
+    y = sn.sn_token_loss(Z, fixed)
+    assert int(flag) == 1 and torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+    flag.zero_()
+    gl = torch.ones(4, device="cuda")
+    x = sn.sn_token_logprobs_backward(Z, a.stats, tok=tk, g_logp=gl, err_flag=flag)
+    assert int(flag) == 1
+    assert torch.equal(x, sn.sn_token_logprobs_backward(Z, a.stats, tok=fixed, g_logp=gl))
+    sn.set_check_ids(True)
+    try:
+        for call in (lambda: sn.sn_token_logprobs(Z, tk), lambda: sn.sn_token_loss(Z, tk)):
+            with pytest.raises(sn.SnError) as e:
+                call()
+            assert e.value.status == sn.SN_ERR_INDEX
+        sn.sn_token_logprobs(Z, fixed)
+    finally:
+        sn.set_check_ids(False)
+
+
+def test_refusals_streams_and_empty():
+    log("[refusals]")
+    Z = _logits(5, 4, 100, "bf16")
+    tk = torch.zeros(4, dtype=torch.int32, device="cuda")
+    stats = torch.zeros(4, 2, device="cuda")
+    ones = torch.ones(4, device="cuda")
+    for status, call in (
+            (2, lambda: sn.sn_token_logprobs(Z, tk[:3])),
+            (2, lambda: sn.sn_token_logprobs(Z, tk, n_top=101)),
+            (8, lambda: sn.sn_token_logprobs(Z, tk, n_top=65)),
+            (2, lambda: sn.sn_token_logprobs(Z, tk, n_top=-1)),
+            (2, lambda: sn.sn_token_logprobs(Z, tk, scale=0.0)),
+            (2, lambda: sn.sn_token_logprobs(Z, tk, scale=float("nan"))),
+            (2, lambda: sn.sn_token_logprobs(Z.t(), tk)),
+            (2, lambda: sn.sn_token_logprobs(Z.cpu(), tk)),
+            (3, lambda: sn.sn_token_logprobs(Z.half(), tk)),
+            (2, lambda: sn.sn_token_logprobs(Z, tk.long())),
+            (1, lambda: sn.sn_token_loss(Z, None)),
+            (2, lambda: sn.sn_token_loss(Z, tk, weight=ones[:2])),
+            (3, lambda: sn.sn_token_loss(Z, tk, out=Z.float())),
+            (2, lambda: sn.sn_token_loss(Z, tk, out=Z[:2])),
+            (1, lambda: sn.sn_token_logprobs_backward(Z, stats, g_logp=ones)),
+            (1, lambda: sn.sn_token_logprobs_backward(Z, stats, g_entropy=ones)),
+            (2, lambda: sn.sn_token_logprobs_backward(Z, stats[:2], tok=tk, g_logp=ones)),
+            (2, lambda: sn.sn_token_logprobs_backward(Z, stats.t().contiguous(), tok=tk, g_logp=ones))):
+        with pytest.raises(sn.SnError) as e:
+            call()
+        assert e.value.status == status, e.value
+    wide = torch.zeros(4, 150, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(sn.SnError) as e:
+        sn.sn_token_loss(wide[:, :100], tk, out=wide[:, 20:120])
+    assert e.value.status == 5
+    # n_top = V, on a stream of its own
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    r = sn.sn_token_logprobs(Z[:, :64], tk, n_top=64, stream=s)
+    logp, dZ = sn.sn_token_loss(Z, tk, stream=s)
+    s.synchronize()
+    assert torch.equal(r.top_id, sn.sn_token_logprobs(Z[:, :64], tk, n_top=64).top_id)
+    assert torch.equal(dZ, sn.sn_token_loss(Z, tk)[1])
+    none = Z[:0]
+    r = sn.sn_token_logprobs(none, tk[:0], n_top=3)
+    assert r.logp.shape == (0,) and r.top_id.shape == (0, 3)
+    assert sn.sn_token_loss(none, tk[:0])[1].shape == (0, 100)
+
+
+def test_deterministic_and_in_a_graph():
+    log("[logprobs graph]")
+    Z = _logits(8, 50, 5001, "bf16")
+    tk = torch.tensor(_tokens(1, 50, 5001), dtype=torch.int32).cuda()
+    out = torch.empty_like(Z)
+    keep = {}
+
+    def step():
+        r = sn.sn_token_logprobs(Z, tk, n_top=7)
+        keep["r"] = r
+        keep["loss"] = sn.sn_token_loss(Z, tk, out=out)
+        keep["d"] = sn.sn_token_logprobs_backward(Z, r.stats, r.entropy, tk, g_logp=r.logp,
+                                                  g_entropy=r.entropy)
+
+    def bits():
+        r = keep["r"]
+        return [t.clone() for t in (*r, keep["loss"][0], out, keep["d"])]
+
+    step()
+    want = bits()
+    step()
+    for x, y in zip(want, bits()):
+        assert torch.equal(x, y)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in (*keep["r"], keep["loss"][0], out, keep["d"]):
+            t.fill_(3)
+        sn.sn_token_logprobs(Z[:3], n_top=1)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(want, bits()):
+            assert torch.equal(x, y)
