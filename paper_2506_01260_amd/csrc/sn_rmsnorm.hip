@@ -19,21 +19,26 @@ namespace {
 constexpr float kF8Max = 448.0f;
 constexpr uint32_t kTiny = 0x0D800000u;  // 2^-100, the least maximum a scale is made from
 
-// a piece of a row that may be absent (NULL) or end inside the piece
-template <typename T>
-__device__ __forceinline__ void get(const T *row, int64_t c0, int64_t d,
-                                    float (&x)[Piece<T>::E]) {
-  if (c0 + Piece<T>::E <= d)
-    Piece<T>::unpack(load_piece(row + c0), x);
-  else
-    load_part(row, c0, d, 0.0f, x);
+// The piece at column c0 of a row of d: 0 past the row's end.  WHOLE: d is a
+// multiple of the piece, so that a piece lies in the row or past it.
+template <typename T, bool WHOLE = false>
+__device__ __forceinline__ u32x4 get(const T *row, int64_t c0, int64_t d) {
+  constexpr int E = Piece<T>::E;
+  if (WHOLE ? c0 < d : c0 + E <= d) return load_piece(row + c0);
+  if constexpr (!WHOLE) {
+    if (c0 < d) {
+      float x[E];
+      load_part(row, c0, d, 0.0f, x);
+      return Piece<T>::pack(x);  // exact: the values are T's own
+    }
+  }
+  return u32x4{0, 0, 0, 0};
 }
-template <typename T>
-__device__ __forceinline__ void put(T *row, int64_t c0, int64_t d,
-                                    const float (&x)[Piece<T>::E]) {
-  if (c0 + Piece<T>::E <= d)
+template <typename T, bool WHOLE = false>
+__device__ __forceinline__ void put(T *row, int64_t c0, int64_t d, const float (&x)[Piece<T>::E]) {
+  if (WHOLE ? c0 < d : c0 + Piece<T>::E <= d)
     store_piece(row + c0, Piece<T>::pack(x));
-  else
+  else if (!WHOLE)
     store_part(row, c0, d, x);
 }
 
@@ -43,14 +48,14 @@ __device__ __forceinline__ uint32_t f8x4(float a, float b, float c, float d) {
 }
 
 // E values of a row in 8 bits
-template <int E>
+template <int E, bool WHOLE = false>
 __device__ __forceinline__ void put8(uint8_t *row, int64_t c0, int64_t d, const float (&q)[E]) {
   uint32_t w[E / 4];
 #pragma unroll
   for (int i = 0; i < E / 4; ++i) w[i] = f8x4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
-  if (c0 + E <= d) {
+  if (WHOLE ? c0 < d : c0 + E <= d) {
     __builtin_memcpy(row + c0, w, E);
-  } else {
+  } else if (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < E; ++i)
       if (c0 + i < d) row[c0 + i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i % 4)));
@@ -78,59 +83,67 @@ __device__ __forceinline__ float to_range(float y, float inv) {
 enum { kOut = 0, kOut8Row = 1, kOut8Group = 2 };
 constexpr int kGroup = 128;  // columns of a scale in the grouped form
 
-// R threads per row, NT / R rows in a workgroup at a time.
-template <typename T, int R, int K, int NT, int OUT>
+// R threads per row, NT / R rows in a workgroup at a time.  The row's number is
+// the same for a whole wave, so that the rows' addresses are scalars.
+template <typename T, int R, int K, int NT, int OUT, bool WHOLE>
 __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
   constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
   static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
   __shared__ float red[W];
   __shared__ uint32_t redu[W];
-  const int tr = threadIdx.x % R;
+  const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
+  const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
   const T *w = static_cast<const T *>(a.w);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / R; i < a.N;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + sub; i < a.N;
        i += static_cast<int64_t>(gridDim.x) * ROWS) {
     const T *X = static_cast<const T *>(a.X) + i * a.ldx;
-    const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
+    u32x4 in[K], more[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) in[k] = get<T, WHOLE>(X, c + k * R * E, d);
+    if (a.R) {
+      const T *Rs = static_cast<const T *>(a.R) + i * a.ldr;
+#pragma unroll
+      for (int k = 0; k < K; ++k) more[k] = get<T, WHOLE>(Rs, c + k * R * E, d);
+    }
     float h[K][E], ss = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
-      get(X, c0, a.d, h[k]);
-    }
-    if (Rs) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
+      Piece<T>::unpack(in[k], h[k]);
+      if (a.R) {
         float r[E];
-        get(Rs, static_cast<int64_t>(tr + k * R) * E, a.d, r);
+        Piece<T>::unpack(more[k], r);
 #pragma unroll
         for (int e = 0; e < E; ++e) h[k][e] += r[e];
       }
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < E; ++e) ss = fmaf(h[k][e], h[k][e], ss);
+    }
     ss = group_sum<W>(ss, red);
     if (a.H) {
       T *H = static_cast<T *>(a.H) + i * a.ldh;
 #pragma unroll
-      for (int k = 0; k < K; ++k) put(H, static_cast<int64_t>(tr + k * R) * E, a.d, h[k]);
+      for (int k = 0; k < K; ++k) put<T, WHOLE>(H, c + k * R * E, d, h[k]);
     }
     const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
     uint32_t big[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
-      float g[E];
-      if (w) get(w, c0, a.d, g);
-      big[k] = 0;
+      const int c0 = c + k * R * E;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        h[k][e] *= rho;
-        if (w) h[k][e] *= g[e];
-        if constexpr (OUT != kOut) big[k] = umax(big[k], abs_bits(h[k][e]));
+      for (int e = 0; e < E; ++e) h[k][e] *= rho;
+      if (w) {
+        float g[E];
+        Piece<T>::unpack(get<T, WHOLE>(w, c0, d), g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[k][e] *= g[e];
       }
-      if constexpr (OUT == kOut) put(static_cast<T *>(a.Y) + i * a.ldy, c0, a.d, h[k]);
+      if constexpr (OUT == kOut) {
+        put<T, WHOLE>(static_cast<T *>(a.Y) + i * a.ldy, c0, d, h[k]);
+      } else {
+        big[k] = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) big[k] = umax(big[k], abs_bits(h[k][e]));
+      }
     }
     if constexpr (OUT == kOut8Row) {
       uint32_t m = big[0];
@@ -138,31 +151,31 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
       for (int k = 1; k < K; ++k) m = umax(m, big[k]);
       m = lanes_umax<64>(m);
       if constexpr (W > 1) {
-        if ((tr & 63) == 0) redu[tr >> 6] = m;
+        if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
       }
 #pragma unroll
       for (int k = 0; k < K; ++k) big[k] = m;
-      if (tr == 0) a.S[i * a.lds] = scale_of(m);
+      if (c == 0) a.S[i * a.lds] = scale_of(m);
     } else if constexpr (OUT == kOut8Group) {
       constexpr int L = kGroup / E;  // lanes of a scale
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         big[k] = lanes_umax<L>(big[k]);
-        const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
-        if (tr % L == 0 && c0 < a.d) a.S[i * a.lds + c0 / kGroup] = scale_of(big[k]);
+        const int c0 = c + k * R * E;
+        if (c0 % kGroup == 0 && c0 < d) a.S[i * a.lds + c0 / kGroup] = scale_of(big[k]);
       }
     }
     if constexpr (OUT != kOut) {
+      uint8_t *Q = static_cast<uint8_t *>(a.Y) + i * a.ldy;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const float inv = 1.0f / scale_of(big[k]);
 #pragma unroll
         for (int e = 0; e < E; ++e) h[k][e] = to_range(h[k][e], inv);
-        put8<E>(static_cast<uint8_t *>(a.Y) + i * a.ldy, static_cast<int64_t>(tr + k * R) * E, a.d,
-                h[k]);
+        put8<E, WHOLE>(Q, c + k * R * E, d, h[k]);
       }
     }
     if constexpr (W > 1) {
@@ -183,9 +196,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
     const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
     float h[E], r[E], ss = 0.0f;
     auto sum = [&](int64_t c0) {
-      get(X, c0, a.d, h);
+      Piece<T>::unpack(get(X, c0, a.d), h);
       if (Rs) {
-        get(Rs, c0, a.d, r);
+        Piece<T>::unpack(get(Rs, c0, a.d), r);
 #pragma unroll
         for (int e = 0; e < E; ++e) h[e] += r[e];
       }
@@ -201,7 +214,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) h[e] *= rho;
       if (w) {
-        get(w, c0, a.d, r);
+        Piece<T>::unpack(get(w, c0, a.d), r);
 #pragma unroll
         for (int e = 0; e < E; ++e) h[e] *= r[e];
       }
@@ -250,34 +263,48 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
 
 // Backward.  A workgroup takes the rows blockIdx.x, + gridDim.x, ... and keeps its
 // part of the gain's gradient in registers; the parts are summed by gain_kernel.
-template <typename T, int R, int K, int NT>
+// Everything of a row is loaded before its sums are joined, and stays as loaded
+// (16 bytes a piece) until it is used: at d = 8192 bf16 registers for two
+// workgroups of 8 waves on a CU instead of one.
+template <typename T, int R, int K, int NT, bool WHOLE>
 __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
   constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
   static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
   __shared__ float red[2][W];
-  const int tr = threadIdx.x % R;
+  const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
+  const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
   const T *w = static_cast<const T *>(a.w);
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / R;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   float gw[K][E] = {};
   for (int64_t i = first; i < a.N; i += static_cast<int64_t>(gridDim.x) * ROWS) {
     const T *H = static_cast<const T *>(a.H) + i * a.ldh;
     const T *dY = static_cast<const T *>(a.dY) + i * a.lddy;
-    const T *dH = a.dH ? static_cast<const T *>(a.dH) + i * a.lddh : nullptr;
-    float h[K][E], u[K][E], ss = 0.0f, uh = 0.0f;
+    u32x4 hp[K], yp[K], dp[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
-      get(H, c0, a.d, h[k]);
-      get(dY, c0, a.d, u[k]);
+      hp[k] = get<T, WHOLE>(H, c + k * R * E, d);
+      yp[k] = get<T, WHOLE>(dY, c + k * R * E, d);
     }
-    float g[E];
+    if (a.dH) {
+      const T *dH = static_cast<const T *>(a.dH) + i * a.lddh;
+#pragma unroll
+      for (int k = 0; k < K; ++k) dp[k] = get<T, WHOLE>(dH, c + k * R * E, d);
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k) dp[k] = u32x4{0, 0, 0, 0};
+    }
+    float h[E], y[E], g[E], ss = 0.0f, uh = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[e] = 1.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (w) get(w, static_cast<int64_t>(tr + k * R) * E, a.d, g);
+      Piece<T>::unpack(hp[k], h);
+      Piece<T>::unpack(yp[k], y);
+      if (w) Piece<T>::unpack(get<T, WHOLE>(w, c + k * R * E, d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        ss = fmaf(h[k][e], h[k][e], ss);
-        uh = fmaf(w ? u[k][e] * g[e] : u[k][e], h[k][e], uh);
+        ss = fmaf(h[e], h[e], ss);
+        uh = fmaf(y[e] * g[e], h[e], uh);
       }
     }
     ss = group_sum<W>(ss, red[0]);
@@ -287,20 +314,18 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
     T *dX = static_cast<T *>(a.dX) + i * a.lddx;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+      const int c0 = c + k * R * E;
       float o[E];
-      if (dH)
-        get(dH, c0, a.d, o);
-      else
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.0f;
-      if (w) get(w, c0, a.d, g);
+      Piece<T>::unpack(hp[k], h);
+      Piece<T>::unpack(yp[k], y);
+      Piece<T>::unpack(dp[k], o);
+      if (w) Piece<T>::unpack(get<T, WHOLE>(w, c0, d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        gw[k][e] = fmaf(u[k][e] * h[k][e], rho, gw[k][e]);
-        o[e] += fmaf(w ? u[k][e] * g[e] : u[k][e], rho, -h[k][e] * f);
+        gw[k][e] = fmaf(y[e] * h[e], rho, gw[k][e]);
+        o[e] += fmaf(y[e] * g[e], rho, -h[e] * f);
       }
-      put(dX, c0, a.d, o);
+      put<T, WHOLE>(dX, c0, d, o);
     }
     if constexpr (W > 1) {
       if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
@@ -310,10 +335,10 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
     float *part = a.part + first * a.d;  // the first row's number names the part
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t c0 = static_cast<int64_t>(tr + k * R) * E;
+      const int c0 = c + k * R * E;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (c0 + e < a.d) part[c0 + e] = gw[k][e];
+        if (c0 + e < d) part[c0 + e] = gw[k][e];
     }
   }
 }
@@ -331,9 +356,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
     const T *dH = a.dH ? static_cast<const T *>(a.dH) + i * a.lddh : nullptr;
     float h[E], u[E], g[E], ss = 0.0f, uh = 0.0f;
     for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
-      get(H, c0, a.d, h);
-      get(dY, c0, a.d, u);
-      if (w) get(w, c0, a.d, g);
+      Piece<T>::unpack(get(H, c0, a.d), h);
+      Piece<T>::unpack(get(dY, c0, a.d), u);
+      if (w) Piece<T>::unpack(get(w, c0, a.d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         ss = fmaf(h[e], h[e], ss);
@@ -347,10 +372,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
     float *part = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
     for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
       float o[E] = {};
-      get(H, c0, a.d, h);
-      get(dY, c0, a.d, u);
-      if (dH) get(dH, c0, a.d, o);
-      if (w) get(w, c0, a.d, g);
+      Piece<T>::unpack(get(H, c0, a.d), h);
+      Piece<T>::unpack(get(dY, c0, a.d), u);
+      if (dH) Piece<T>::unpack(get(dH, c0, a.d), o);
+      if (w) Piece<T>::unpack(get(w, c0, a.d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (part && c0 + e < a.d)
@@ -388,7 +413,7 @@ __global__ __launch_bounds__(64 * kGainWaves) void gain_kernel(const float *__re
 // pieces of a row; R * K of them are held by R threads in K pieces each
 int64_t pieces_of(int dt, int64_t d) { return ceil_div(d, dt == 0 ? 4 : 8); }
 
-template <typename T, int OUT>
+template <typename T, int OUT, bool WHOLE>
 hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
   const auto grid = [&](int rows) {
@@ -396,17 +421,17 @@ hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
     return static_cast<unsigned>(g < (1 << 20) ? g : 1 << 20);
   };
   if (n <= 64)
-    rmsnorm_kernel<T, 64, 1, 256, OUT><<<grid(4), 256, 0, s>>>(a);
+    rmsnorm_kernel<T, 64, 1, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
   else if (n <= 128)
-    rmsnorm_kernel<T, 64, 2, 256, OUT><<<grid(4), 256, 0, s>>>(a);
+    rmsnorm_kernel<T, 64, 2, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
   else if (n <= 256)
-    rmsnorm_kernel<T, 64, 4, 256, OUT><<<grid(4), 256, 0, s>>>(a);
+    rmsnorm_kernel<T, 64, 4, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
   else if (n <= 512)
-    rmsnorm_kernel<T, 256, 2, 256, OUT><<<grid(1), 256, 0, s>>>(a);
+    rmsnorm_kernel<T, 256, 2, 256, OUT, WHOLE><<<grid(1), 256, 0, s>>>(a);
   else if (n <= 1024)
-    rmsnorm_kernel<T, 256, 4, 256, OUT><<<grid(1), 256, 0, s>>>(a);
-  else if (n <= 4096)
-    rmsnorm_kernel<T, 1024, 4, 1024, OUT><<<grid(1), 1024, 0, s>>>(a);
+    rmsnorm_kernel<T, 512, 2, 512, OUT, WHOLE><<<grid(1), 512, 0, s>>>(a);
+  else if (n <= 2048)
+    rmsnorm_kernel<T, 1024, 2, 1024, OUT, WHOLE><<<grid(1), 1024, 0, s>>>(a);
   else
     rmsnorm_long_kernel<T, OUT><<<grid(1), 1024, 0, s>>>(a);
   return hipGetLastError();
@@ -414,8 +439,14 @@ hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_norm_out(const NormArgs &a, hipStream_t s) {
-  if (!a.S) return launch_norm_t<T, kOut>(a, s);
-  return a.group ? launch_norm_t<T, kOut8Group>(a, s) : launch_norm_t<T, kOut8Row>(a, s);
+  if (a.d % Piece<T>::E == 0) {
+    if (!a.S) return launch_norm_t<T, kOut, true>(a, s);
+    return a.group ? launch_norm_t<T, kOut8Group, true>(a, s)
+                   : launch_norm_t<T, kOut8Row, true>(a, s);
+  }
+  if (!a.S) return launch_norm_t<T, kOut, false>(a, s);
+  return a.group ? launch_norm_t<T, kOut8Group, false>(a, s)
+                 : launch_norm_t<T, kOut8Row, false>(a, s);
 }
 
 // Workgroups of the backward, two for each of the 256 CUs (each leaves a part of
@@ -434,25 +465,31 @@ GradPlan grad_plan(int dt, int64_t N, int64_t d) {
   return p;
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 hipError_t launch_grad_t(int dt, const NormGradArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
   const unsigned g = static_cast<unsigned>(grad_plan(dt, a.N, a.d).grid);
   if (n <= 64)
-    rmsnorm_grad_kernel<T, 64, 1, 256><<<g, 256, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 64, 1, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 128)
-    rmsnorm_grad_kernel<T, 64, 2, 256><<<g, 256, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 64, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 256)
-    rmsnorm_grad_kernel<T, 256, 1, 256><<<g, 256, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 256, 1, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 512)
-    rmsnorm_grad_kernel<T, 256, 2, 256><<<g, 256, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 256, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 1024)
-    rmsnorm_grad_kernel<T, 512, 2, 512><<<g, 512, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 512, 2, 512, WHOLE><<<g, 512, 0, s>>>(a);
   else if (n <= 2048)
-    rmsnorm_grad_kernel<T, 1024, 2, 1024><<<g, 1024, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 1024, 2, 1024, WHOLE><<<g, 1024, 0, s>>>(a);
   else
     rmsnorm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_grad_d(int dt, const NormGradArgs &a, hipStream_t s) {
+  return a.d % Piece<T>::E == 0 ? launch_grad_t<T, true>(dt, a, s)
+                                : launch_grad_t<T, false>(dt, a, s);
 }
 
 }  // namespace
@@ -467,7 +504,7 @@ size_t rmsnorm_grad_workspace_bytes(int dt, int64_t N, int64_t d) {
 
 hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipStream_t s) {
   a.part = gw ? static_cast<float *>(ws) : nullptr;
-  const hipError_t e = dt == 0 ? launch_grad_t<float>(dt, a, s) : launch_grad_t<bf16_t>(dt, a, s);
+  const hipError_t e = dt == 0 ? launch_grad_d<float>(dt, a, s) : launch_grad_d<bf16_t>(dt, a, s);
   if (e != hipSuccess || !gw) return e;
   gain_kernel<<<static_cast<unsigned>(ceil_div(a.d, 64)), 64 * kGainWaves, 0, s>>>(
       a.part, grad_plan(dt, a.N, a.d).parts, a.d, gw);
