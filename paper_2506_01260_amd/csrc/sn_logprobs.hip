@@ -32,17 +32,15 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // z - m is no difference of infinities where every logit is -inf.
 struct Running {
   float best = -INFINITY;  // largest logit seen
-  int64_t at = 0;          // the piece that first held it
   float m = -FLT_MAX, s = 0.0f, t = 0.0f;  // sum e^x, sum e^x (z - m)
 
   template <int E, bool ENT>
-  __device__ __forceinline__ void add(const float (&z)[E], int64_t piece, float c2) {
+  __device__ __forceinline__ void add(const float (&z)[E], float c2) {
     float top = z[0];
 #pragma unroll
     for (int i = 1; i < E; ++i) top = fmaxf(top, z[i]);
     if (top > best) {
       best = top;
-      at = piece;
       const float mn = fmaxf(top, -FLT_MAX), d = fmaxf(m - mn, kFar), cr = exp2_fast(d * c2);
       if constexpr (ENT) t = cr * fmaf(s, d, t);
       s *= cr;
@@ -61,39 +59,40 @@ struct Running {
 template <typename T, int NT, bool ENT>
 __device__ __forceinline__ Running scan_row(const T *row, int64_t V, float c2) {
   constexpr int E = Piece<T>::E, U = 4;
-  const int64_t full = V / E;
+  const int full = static_cast<int>(V / E), tid = threadIdx.x;
   Running r;
-  int64_t p = threadIdx.x;
-  r.at = p;
   float z[E];
-  for (; p + (U - 1) * NT < full; p += U * NT) {
+  int b = 0;
+  for (; b + U * NT <= full; b += U * NT) {
     u32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_piece(row + (p + u * NT) * E);
+    for (int u = 0; u < U; ++u) v[u] = load_own(row, b + u * NT);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       Piece<T>::unpack(v[u], z);
-      r.add<E, ENT>(z, p + u * NT, c2);
+      r.add<E, ENT>(z, c2);
     }
   }
-  for (; p < full; p += NT) {
-    Piece<T>::unpack(load_piece(row + p * E), z);
-    r.add<E, ENT>(z, p, c2);
+  for (; b + tid < full; b += NT) {
+    Piece<T>::unpack(load_own(row, b), z);
+    r.add<E, ENT>(z, c2);
   }
-  if (p * E < V) {  // the row's last, short piece
-    load_part(row, p * E, V, -INFINITY, z);
-    r.add<E, ENT>(z, p, c2);
+  if (b + tid == full && V % E != 0) {  // the row's last, short piece
+    load_part(row, static_cast<int64_t>(full) * E, V, -INFINITY, z);
+    r.add<E, ENT>(z, c2);
   }
   return r;
 }
 
 // ---- the largest logits --------------------------------------------------------
-// A 64-bit key orders logits by value, the lower index (or piece) first among
-// equals: the value's bits made ascending, then the complement of the index.
+// A float's bits made ascending as a whole number (-0 counts as 0).
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+// A 64-bit key orders logits by value, the lower index first among equals.
 __device__ __forceinline__ uint64_t order_key(float v, uint32_t index) {
-  const uint32_t b = __float_as_uint(v + 0.0f);  // -0 counts as 0
-  const uint32_t o = b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-  return (static_cast<uint64_t>(o) << 32) | (0xFFFFFFFFu - index);
+  return (static_cast<uint64_t>(ordered(v)) << 32) | (0xFFFFFFFFu - index);
 }
 __device__ __forceinline__ float key_value(uint64_t k) {
   const uint32_t o = static_cast<uint32_t>(k >> 32);
@@ -103,77 +102,105 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) {
   return 0xFFFFFFFFu - static_cast<uint32_t>(k);
 }
 
-__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int mask) {
-  return __shfl_xor(static_cast<unsigned long long>(v), mask);
-}
-// one step of a bitonic network over the wave: lane and lane ^ j exchange
-__device__ __forceinline__ uint64_t exchange(uint64_t k, int j, bool larger) {
-  const uint64_t o = lane_xor(k, j);
-  return (o > k) == larger ? o : k;
-}
-// the wave's 64 keys in descending order
-__device__ __forceinline__ uint64_t sort64(uint64_t k, int lane) {
+// Candidates a workgroup keeps for a row: the n largest and those equal to the
+// last of the thread maxima that bound them (about n of them but for rows of
+// many equal logits, which take the pass over the row below instead).
+constexpr int kCandidates = 256;
+
+template <int NT>
+struct TopLds {
+  uint32_t best[NT];  // the threads' largest logits, ordered()
+  uint16_t sel[NT];   // threads that may hold one of the n largest
+  uint64_t cand[kCandidates];
+  uint32_t sels, cands;
+};
+
+// The largest bound that at least n of the threads' maxima reach (0 if fewer
+// threads have a piece), built from its highest bit down: the same in each wave.
+template <int NT>
+__device__ __forceinline__ uint32_t nth_best(const uint32_t (&best)[NT], int n) {
+  constexpr int P = NT / 64;
+  const int lane = threadIdx.x & 63;
+  uint32_t v[P], bound = 0;
 #pragma unroll
-  for (int n = 2; n <= 64; n <<= 1)
+  for (int i = 0; i < P; ++i) v[i] = best[64 * i + lane];
+  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+    int count = 0;
 #pragma unroll
-    for (int j = n >> 1; j; j >>= 1) k = exchange(k, j, ((lane & j) == 0) == ((lane & n) == 0));
-  return k;
-}
-// the 64 largest of two descending lists, descending
-__device__ __forceinline__ uint64_t merge64(uint64_t a, uint64_t b, int lane) {
-  const uint64_t o = lane_xor(b, 63);
-  uint64_t k = o > a ? o : a;
-#pragma unroll
-  for (int j = 32; j; j >>= 1) k = exchange(k, j, (lane & j) == 0);
-  return k;
-}
-// the W waves' lists merged: list[0] at the end (a barrier included)
-template <int W>
-__device__ __forceinline__ void merge_waves(uint64_t k, uint64_t (*list)[64], int lane, int wave) {
-  list[wave][lane] = k;
-  __syncthreads();
-#pragma unroll
-  for (int h = 1; h < W; h <<= 1) {
-    if ((wave & (2 * h - 1)) == 0) {
-      k = merge64(k, list[wave + h][lane], lane);
-      list[wave][lane] = k;
-    }
-    __syncthreads();
+    for (int i = 0; i < P; ++i) count += __popcll(__ballot(v[i] >= (bound | bit)));
+    if (count >= n) bound |= bit;
+    if (count == n) break;  // exactly n reach it: no higher bound is needed
   }
+  return bound;
 }
 
-// The n largest logits of a row, after scan_row by the same threads.  Those of
-// each thread's first largest piece are ordered first: a logit outside the n
-// threads that come first is smaller than n others, so only these threads'
-// pieces are read again, and of them only logits not below the n-th thread's
-// largest are kept.  The keys are in list[0] at the end.
-template <typename T, int NT>
-__device__ __forceinline__ void top_row(const T *row, int64_t V, const Running &r, int n,
-                                        uint64_t (*list)[64]) {
-  constexpr int E = Piece<T>::E, W = NT / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t pieces = (V + E - 1) / E;
-  uint64_t k = threadIdx.x < pieces ? order_key(r.best, static_cast<uint32_t>(r.at)) : 0;
-  merge_waves<W>(sort64(k, lane), list, lane, wave);
-  const uint64_t least = list[0][n - 1];
-  k = 0;
-  for (int j = wave; j < n; j += W) {
-    const uint64_t thread = list[0][j];
-    if (thread == 0) break;  // fewer threads than n have a piece
-    for (int64_t p = key_index(thread) % NT + NT * (lane / E);; p += NT * (64 / E)) {
-      const int64_t i = p * E + lane % E;
-      uint64_t mine = 0;
-      if (i < V) {
-        const float v = to_f32(row[i]);
-        if (order_key(v, static_cast<uint32_t>(p)) >= least)
-          mine = order_key(v, static_cast<uint32_t>(i));
-      }
-      if (__ballot(i < V) == 0) break;
-      if (__ballot(mine != 0)) k = merge64(k, sort64(mine, lane), lane);
-    }
+__device__ __forceinline__ uint64_t wave_max(uint64_t k) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) {
+    const uint64_t o = __shfl_xor(static_cast<unsigned long long>(k), m);
+    k = o > k ? o : k;
   }
-  __syncthreads();  // list[0] has been read
-  merge_waves<W>(k, list, lane, wave);
+  return k;
+}
+
+// The n largest logits of a row, by the threads that scanned it: put(rank, key)
+// is called once for each rank below n.  A logit below the n-th largest of the
+// threads' maxima has n others above it, so only the pieces of threads whose
+// maximum reaches that bound are read again, and only logits that reach it are
+// candidates; each one's rank is the number of candidates above it.
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<NT> &lds, F &&put) {
+  constexpr int E = Piece<T>::E;
+  const uint32_t pieces = static_cast<uint32_t>((V + E - 1) / E), each = (pieces + NT - 1) / NT;
+  const uint32_t bound = nth_best<NT>(lds.best, n);
+  const uint32_t mine = lds.best[threadIdx.x];
+  if (mine != 0 && mine >= bound) lds.sel[atomicAdd(&lds.sels, 1u)] = threadIdx.x;
+  __syncthreads();
+  const uint32_t all = lds.sels * each;
+  for (uint32_t q = threadIdx.x; q < all; q += NT) {
+    const uint32_t k = q / each, p = lds.sel[k] + (q - k * each) * NT;
+    if (p >= pieces) continue;
+    const int64_t c0 = static_cast<int64_t>(p) * E;
+    float z[E];
+    if (c0 + E <= V)
+      Piece<T>::unpack(load_piece(row + c0), z);
+    else
+      load_part(row, c0, V, -INFINITY, z);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (c0 + e < V && ordered(z[e]) >= bound) {
+        const uint32_t at = atomicAdd(&lds.cands, 1u);
+        if (at < kCandidates) lds.cand[at] = order_key(z[e], static_cast<uint32_t>(c0 + e));
+      }
+  }
+  __syncthreads();
+  const uint32_t count = lds.cands;
+  if (count <= kCandidates) {
+    for (uint32_t i = threadIdx.x; i < count; i += NT) {
+      const uint64_t k = lds.cand[i];
+      int rank = 0;
+      for (uint32_t j = 0; j < count; ++j) rank += lds.cand[j] > k;
+      if (rank < n) put(rank, k);
+    }
+    return;
+  }
+  // many equal logits: the next largest by a pass over the row each
+  uint64_t last = ~0ull;
+  for (int r = 0; r < n; ++r) {
+    uint64_t k = 0;
+    for (int64_t c = threadIdx.x; c < V; c += NT) {
+      const uint64_t o = order_key(to_f32(row[c]), static_cast<uint32_t>(c));
+      k = o < last && o > k ? o : k;
+    }
+    k = wave_max(k);
+    __syncthreads();  // the candidates before have been read
+    if ((threadIdx.x & 63) == 0) lds.cand[threadIdx.x >> 6] = k;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) k = lds.cand[i] > k ? lds.cand[i] : k;
+    if (threadIdx.x == 0) put(r, k);
+    last = k;
+  }
 }
 
 // ---- kernels ---------------------------------------------------------------------
@@ -182,40 +209,48 @@ template <typename T, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobsArgs a) {
   constexpr int W = NT / 64;
   __shared__ float red[3][W];
-  __shared__ uint64_t list[TOP ? W : 1][64];
+  __shared__ TopLds<TOP ? NT : 64> lds;
   const float c2 = a.scale * kLog2e;
-  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
-    const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
-    const Running r = scan_row<T, NT, true>(row, a.V, c2);
-    const float m = group_max<W>(r.m, red[0]);
-    const float d = fmaxf(r.m - m, kFar), cr = exp2_fast(d * c2);
-    const float s = group_sum<W>(r.s * cr, red[1]);
-    const float t = group_sum<W>(cr * fmaf(r.s, d, r.t), red[2]);
-    const float L = logf(s);  // -inf: nothing is allowed; NaN: a logit is NaN or +inf
-    if constexpr (TOP) top_row<T, NT>(row, a.V, r, a.n_top, list);
-    if (threadIdx.x == 0) {
-      if (a.logp) {
-        const int32_t tok = a.tok[i];
-        float lp = 0.0f;
-        if (tok != -1) {
-          const float z = to_f32(row[clamp_id(tok, a.V, a.err_flag, 1)]);
-          lp = s > 0.0f ? fmaf(z - m, a.scale, -L) : L;
-        }
-        a.logp[i] = lp;
+  const int64_t i = group_number();
+  if (i >= a.N) return;
+  const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
+  const Running r = scan_row<T, NT, true>(row, a.V, c2);
+  if constexpr (TOP) {
+    // 0, below every logit's, for a thread without a piece
+    lds.best[threadIdx.x] = static_cast<int64_t>(threadIdx.x) * Piece<T>::E < a.V ? ordered(r.best) : 0;
+    if (threadIdx.x == 0) lds.sels = lds.cands = 0;
+    if constexpr (W == 1) __syncthreads();
+  }
+  const float m = group_max<W>(r.m, red[0]);
+  const float d = fmaxf(r.m - m, kFar), cr = exp2_fast(d * c2);
+  const float s = group_sum<W>(r.s * cr, red[1]);
+  const float t = group_sum<W>(cr * fmaf(r.s, d, r.t), red[2]);
+  const float L = logf(s);  // -inf: nothing is allowed; NaN: a logit is NaN or +inf
+  if (threadIdx.x == 0) {
+    if (a.logp) {
+      const int32_t tok = a.tok[i];
+      float lp = 0.0f;
+      if (tok != -1) {
+        const float z = to_f32(row[clamp_id(tok, a.V, a.err_flag, 1)]);
+        lp = s > 0.0f ? fmaf(z - m, a.scale, -L) : L;
       }
-      a.entropy[i] = s == 0.0f ? 0.0f : L - a.scale * t / s;
-      a.stats[2 * i] = s > 0.0f ? m : L;
-      a.stats[2 * i + 1] = L;
+      a.logp[i] = lp;
     }
-    if constexpr (TOP) {
-      if (threadIdx.x < a.n_top) {
-        const uint64_t k = list[0][threadIdx.x];
-        const int64_t o = i * a.n_top + threadIdx.x;
-        a.top_logp[o] = s > 0.0f ? fmaf(key_value(k) - m, a.scale, -L) : L;
-        a.top_id[o] = s != s ? -1 : static_cast<int32_t>(key_index(k));
-      }
+    a.entropy[i] = s == 0.0f ? 0.0f : L - a.scale * t / s;
+    a.stats[2 * i] = s > 0.0f ? m : L;
+    a.stats[2 * i + 1] = L;
+  }
+  if constexpr (TOP) {
+    const int64_t o = i * a.n_top;
+    if (s == s) {
+      top_row<T, NT>(row, a.V, a.n_top, lds, [&](int rank, uint64_t k) {
+        a.top_logp[o + rank] = s > 0.0f ? fmaf(key_value(k) - m, a.scale, -L) : L;
+        a.top_id[o + rank] = static_cast<int32_t>(key_index(k));
+      });
+    } else if (threadIdx.x < a.n_top) {
+      a.top_logp[o + threadIdx.x] = s;
+      a.top_id[o + threadIdx.x] = -1;
     }
-    if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
   }
 }
 
@@ -234,141 +269,211 @@ struct RowGrad {
   }
 };
 
-// A unit is kPieces pieces of each of 256 threads in one row.
+// A unit is kGradPieces pieces of each of 256 threads in one row.
 constexpr int kGradPieces = 4;
 
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, int64_t per_row,
                                                             int64_t units) {
   constexpr int E = Piece<T>::E, U = kGradPieces;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t i = unit / per_row, first = (unit - i * per_row) * (256 * U) + threadIdx.x;
-    const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
-    T *out = static_cast<T *>(a.dZ) + i * a.lddz;
-    const int32_t tok = a.tok ? a.tok[i] : -1;
-    int64_t t = -1;
-    RowGrad g;
-    g.gl = 0.0f;
-    if (tok != -1) {
-      t = clamp_id(tok, a.V, a.err_flag, 1);
-      g.gl = a.g_logp ? a.g_logp[i] : 0.0f;
-    }
-    g.gh = a.g_entropy ? a.g_entropy[i] : 0.0f;
-    const float hit = a.scale * g.gl;
-    const bool none = g.gl == 0.0f && g.gh == 0.0f;  // a row that nothing flows into
+  const int full = static_cast<int>(a.V / E);
+  const int64_t unit = group_number();
+  if (unit >= units) return;
+  const int64_t i = unit / per_row;
+  const int base = static_cast<int>(unit - i * per_row) * (256 * U), first = base + threadIdx.x;
+  const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
+  T *out = static_cast<T *>(a.dZ) + i * a.lddz;
+  const int32_t tok = a.tok ? a.tok[i] : -1;
+  int t = -1;
+  RowGrad g;
+  g.gl = 0.0f;
+  if (tok != -1) {
+    t = static_cast<int>(clamp_id(tok, a.V, a.err_flag, 1));
+    g.gl = a.g_logp ? a.g_logp[i] : 0.0f;
+  }
+  g.gh = a.g_entropy ? a.g_entropy[i] : 0.0f;
+  const float hit = a.scale * g.gl;
+  const bool none = g.gl == 0.0f && g.gh == 0.0f;  // a row that nothing flows into
+  if (!none) {
+    g.m = a.stats[2 * i];
+    g.L = a.stats[2 * i + 1];
+    g.H = g.gh != 0.0f ? a.entropy[i] : 0.0f;
+    g.c = a.scale;
+    if (g.L != g.L) g.gl = g.L;
+  }
+  const int tp = t < 0 ? -1 : t / E, te = t - tp * E;  // the given token's piece
+  u32x4 v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    v[u] = u32x4{0, 0, 0, 0};
+    if (!none && first + u * 256 < full)
+      v[u] = load_own<T, true>(row, base + u * 256);
+  }
+  float z[E];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int p = first + u * 256;
+    if (p >= full) break;
     if (!none) {
-      g.m = a.stats[2 * i];
-      g.L = a.stats[2 * i + 1];
-      g.H = g.gh != 0.0f ? a.entropy[i] : 0.0f;
-      g.c = a.scale;
-      if (g.L != g.L) g.gl = g.L;
-    }
-    u32x4 v[U];
-    if (!none) {
+      Piece<T>::unpack(v[u], z);
+      g.apply(z);
+      if (p == tp) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if ((first + u * 256 + 1) * E <= a.V)
-          v[u] = load_piece<T, true>(row + (first + u * 256) * E);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t c0 = (first + u * 256) * E;
-      if (c0 >= a.V) break;
-      const bool whole = c0 + E <= a.V;
-      float z[E] = {};
-      if (!none) {
-        if (whole)
-          Piece<T>::unpack(v[u], z);
-        else
-          load_part(row, c0, a.V, 0.0f, z);
-        g.apply(z);
-        if (t >= c0 && t < c0 + E) {
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (t == c0 + e) z[e] += hit;
-        }
+        for (int e = 0; e < E; ++e) z[e] += e == te ? hit : 0.0f;
       }
-      if (whole)
-        store_piece<T, true>(out + c0, Piece<T>::pack(z));
-      else
-        store_part(out, c0, a.V, z);
+      v[u] = Piece<T>::pack(z);
     }
+    store_own<T, true>(out, base + u * 256, v[u]);
+  }
+  // the row's last, short piece
+  if (a.V % E != 0 && full >= first && full < first + 256 * U && (full - first) % 256 == 0) {
+    const int64_t c0 = static_cast<int64_t>(full) * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = 0.0f;
+    if (!none) {
+      load_part(row, c0, a.V, 0.0f, z);
+      g.apply(z);
+      if (full == tp) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] += e == te ? hit : 0.0f;
+      }
+    }
+    store_part(out, c0, a.V, z);
   }
 }
 
-// log p of the given token and w c (p - d) in one call: two passes over the row.
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void loss_kernel(LossArgs a) {
+// log p of the given token and w c (p - d) in one call.  A thread keeps its first
+// K pieces of the row in registers between the sums and the gradient; what a longer
+// row has beyond them is read a second time, the last read first (the Infinity
+// Cache still holds most of it).
+template <typename T, int NT, int K, int WAVES>
+__global__ __launch_bounds__(NT, WAVES) void loss_kernel(LossArgs a) {
   constexpr int E = Piece<T>::E, W = NT / 64;
+  static_assert(K % 4 == 0, "the pieces beyond the kept ones go in fours");
   __shared__ float red[2][W];
   const float c2 = a.scale * kLog2e;
-  const int64_t full = a.V / E;
-  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
-    const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
-    T *out = static_cast<T *>(a.dZ) + i * a.lddz;
-    const int32_t tok = a.tok[i];
-    int64_t t = -1;
-    float w = 0.0f, m = 0.0f, f = 0.0f;
-    if (tok != -1) {
-      t = clamp_id(tok, a.V, a.err_flag, 1);
-      w = a.weight ? a.weight[i] : 1.0f;
-      const float zt = to_f32(row[t]);
-      const Running r = scan_row<T, NT, false>(row, a.V, c2);
-      m = group_max<W>(r.m, red[0]);
-      const float s = group_sum<W>(r.s * exp2_fast(fmaxf(r.m - m, kFar) * c2), red[1]);
-      const float L = logf(s);
-      if (threadIdx.x == 0) a.logp[i] = s > 0.0f ? fmaf(zt - m, a.scale, -L) : L;
-      f = s == 0.0f ? 0.0f : w * a.scale / s;
-    } else if (threadIdx.x == 0) {
-      a.logp[i] = 0.0f;
+  const int full = static_cast<int>(a.V / E), tid = threadIdx.x;
+  const bool tail = a.V % E != 0 && full % NT == tid;  // holds the row's last, short piece
+  const int64_t i = group_number();
+  if (i >= a.N) return;
+  const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
+  T *out = static_cast<T *>(a.dZ) + i * a.lddz;
+  const auto at = [&](int p) { return static_cast<int64_t>(p) * E; };
+  const int32_t tok = a.tok[i];
+  int t = -1;
+  float w = 0.0f;
+  if (tok != -1) {
+    t = static_cast<int>(clamp_id(tok, a.V, a.err_flag, 1));
+    w = a.weight ? a.weight[i] : 1.0f;
+  }
+  u32x4 kept[K];
+  float z[E], last[E], m = 0.0f, f = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) last[e] = 0.0f;
+  if (tok != -1) {
+    const float zt = to_f32(row[t]);
+    Running r;
+    for (int b = K * NT; b < full; b += 4 * NT) {
+      u32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u] = u32x4{0, 0, 0, 0};
+        if (b + u * NT + tid < full) v[u] = load_own(row, b + u * NT);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (b + u * NT + tid < full) {
+          Piece<T>::unpack(v[u], z);
+          r.add<E, false>(z, c2);
+        }
     }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      kept[k] = u32x4{0, 0, 0, 0};
+      if (k * NT + tid < full) kept[k] = load_own(row, k * NT);
+    }
+    if (tail) load_part(row, at(full), a.V, -INFINITY, last);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (k * NT + tid < full) {
+        Piece<T>::unpack(kept[k], z);
+        r.add<E, false>(z, c2);
+      }
+    if (tail) r.add<E, false>(last, c2);
+    m = group_max<W>(r.m, red[0]);
+    const float s = group_sum<W>(r.s * exp2_fast(fmaxf(r.m - m, kFar) * c2), red[1]);
+    const float L = logf(s);
+    if (tid == 0) a.logp[i] = s > 0.0f ? fmaf(zt - m, a.scale, -L) : L;
+    f = s == 0.0f ? 0.0f : w * a.scale / s;
+  } else if (tid == 0) {
+    a.logp[i] = 0.0f;
+  }
+  if (w == 0.0f) {
+    for (int b = 0; b + tid < full; b += NT) store_own<T, true>(out, b, u32x4{0, 0, 0, 0});
+#pragma unroll
+    for (int e = 0; e < E; ++e) last[e] = 0.0f;
+    if (tail) store_part(out, at(full), a.V, last);
+  } else {
     const float hit = w * a.scale;
-    const bool none = w == 0.0f;
-    auto finish = [&](float (&z)[E], int64_t c0) {
+    const int tp = t / E, te = t - tp * E;  // the given token's piece
+    const auto finish = [&](float (&x)[E], int p) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) z[e] = f * exp2_fast((z[e] - m) * c2);
-      if (t >= c0 && t < c0 + E) {
+      for (int e = 0; e < E; ++e) x[e] = f * exp2_fast((x[e] - m) * c2);
+      if (p == tp) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (t == c0 + e) z[e] -= hit;
+        for (int e = 0; e < E; ++e) x[e] -= e == te ? hit : 0.0f;
       }
     };
-    int64_t p = threadIdx.x;
-    float z[E] = {};
-    if (none) {
-      for (; p < full; p += NT) store_piece<T, true>(out + p * E, u32x4{0, 0, 0, 0});
-      if (p * E < a.V) store_part(out, p * E, a.V, z);
-    } else {
-      for (; p < full; p += NT) {
-        Piece<T>::unpack(load_piece(row + p * E), z);
-        finish(z, p * E);
-        store_piece<T, true>(out + p * E, Piece<T>::pack(z));
-      }
-      if (p * E < a.V) {
-        load_part(row, p * E, a.V, 0.0f, z);
-        finish(z, p * E);
-        store_part(out, p * E, a.V, z);
-      }
+    const auto write = [&](u32x4 v, int base) {
+      Piece<T>::unpack(v, z);
+      finish(z, base + tid);
+      store_own<T, true>(out, base, Piece<T>::pack(z));
+    };
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (k * NT + tid < full) write(kept[k], k * NT);
+    if (tail) {
+      finish(last, full);
+      store_part(out, at(full), a.V, last);
     }
-    if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
+    for (int b = (full - 1) / (4 * NT) * (4 * NT); b >= K * NT; b -= 4 * NT) {
+      u32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u] = u32x4{0, 0, 0, 0};
+        if (b + u * NT + tid < full) v[u] = load_own(row, b + u * NT);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (b + u * NT + tid < full) write(v[u], b + u * NT);
+    }
   }
 }
 
-unsigned grid_of(int64_t n) { return static_cast<unsigned>(n < (1 << 20) ? n : 1 << 20); }
+template <typename T, int NT>
+hipError_t launch_logprobs_nt(const LogprobsArgs &a, hipStream_t s) {
+  if (a.n_top)
+    logprobs_kernel<T, NT, true><<<groups_grid(a.N), NT, 0, s>>>(a);
+  else
+    logprobs_kernel<T, NT, false><<<groups_grid(a.N), NT, 0, s>>>(a);
+  return hipGetLastError();
+}
 
+// Threads of a row: a wave up to 8 pieces for each lane; else 1024 where the rows
+// are fewer than the CUs, 256 where there are more of them than workgroups of
+// 1024 that run at a time.
 template <typename T>
 hipError_t launch_logprobs_t(const LogprobsArgs &a, hipStream_t s) {
-  if (a.n_top)
-    logprobs_kernel<T, 256, true><<<grid_of(a.N), 256, 0, s>>>(a);
-  else
-    logprobs_kernel<T, 256, false><<<grid_of(a.N), 256, 0, s>>>(a);
-  return hipGetLastError();
+  const int64_t pieces = ceil_div(a.V, Piece<T>::E);
+  if (pieces <= 512) return launch_logprobs_nt<T, 64>(a, s);
+  if (a.N <= 512 && pieces > 1024) return launch_logprobs_nt<T, 1024>(a, s);
+  return launch_logprobs_nt<T, 256>(a, s);
 }
 
 template <typename T>
 hipError_t launch_grad_t(const LogprobsGradArgs &a, hipStream_t s) {
   const int64_t per_row = ceil_div(a.V, Piece<T>::E * 256 * kGradPieces), units = per_row * a.N;
-  logprobs_grad_kernel<T><<<grid_of(units), 256, 0, s>>>(a, per_row, units);
+  logprobs_grad_kernel<T><<<groups_grid(units), 256, 0, s>>>(a, per_row, units);
   return hipGetLastError();
 }
 
@@ -382,12 +487,24 @@ hipError_t launch_logprobs_grad(int dt, const LogprobsGradArgs &a, hipStream_t s
   return dt == 0 ? launch_grad_t<float>(a, s) : launch_grad_t<bf16_t>(a, s);
 }
 
-hipError_t launch_loss(int dt, const LossArgs &a, hipStream_t s) {
-  if (dt == 0)
-    loss_kernel<float, 512><<<grid_of(a.N), 512, 0, s>>>(a);
+namespace {
+template <typename T>
+hipError_t launch_loss_t(const LossArgs &a, hipStream_t s) {
+  const int64_t pieces = ceil_div(a.V, Piece<T>::E);
+  if (pieces <= 256)
+    loss_kernel<T, 64, 4, 6><<<groups_grid(a.N), 64, 0, s>>>(a);
+  else if (pieces <= 1024)
+    loss_kernel<T, 256, 4, 6><<<groups_grid(a.N), 256, 0, s>>>(a);
+  else if (pieces <= 4096)
+    loss_kernel<T, 512, 8, 6><<<groups_grid(a.N), 512, 0, s>>>(a);
   else
-    loss_kernel<bf16_t, 512><<<grid_of(a.N), 512, 0, s>>>(a);
+    loss_kernel<T, 1024, 8, 8><<<groups_grid(a.N), 1024, 0, s>>>(a);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_loss(int dt, const LossArgs &a, hipStream_t s) {
+  return dt == 0 ? launch_loss_t<float>(a, s) : launch_loss_t<bf16_t>(a, s);
 }
 
 }  // namespace sn

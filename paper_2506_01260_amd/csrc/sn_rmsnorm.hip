@@ -20,19 +20,27 @@ constexpr float kF8Max = 448.0f;
 constexpr uint32_t kTiny = 0x0D800000u;  // 2^-100, the least maximum a scale is made from
 
 // The piece at column c0 of a row of d: 0 past the row's end.  WHOLE: d is a
-// multiple of the piece, so that a piece lies in the row or past it.
+// multiple of the piece, so that a piece lies in the row or past it.  Else the
+// row's last piece is the one that ends with the row, shifted: one load, as for
+// the others (element by element it was another round trip to memory, and a
+// backward of width 1601 took a quarter longer).
 template <typename T, bool WHOLE = false>
 __device__ __forceinline__ u32x4 get(const T *row, int64_t c0, int64_t d) {
   constexpr int E = Piece<T>::E;
-  if (WHOLE ? c0 < d : c0 + E <= d) return load_piece(row + c0);
-  if constexpr (!WHOLE) {
-    if (c0 < d) {
-      float x[E];
-      load_part(row, c0, d, 0.0f, x);
-      return Piece<T>::pack(x);  // exact: the values are T's own
-    }
+  if (c0 >= d) return u32x4{0, 0, 0, 0};
+  if (WHOLE || c0 + E <= d) return load_piece(row + c0);
+  if (d < E) {
+    float x[E];
+    load_part(row, c0, d, 0.0f, x);
+    return Piece<T>::pack(x);  // exact: the values are T's own
   }
-  return u32x4{0, 0, 0, 0};
+  const u32x4 v = load_piece(row + d - E);
+  const int bits = static_cast<int>(c0 - (d - E)) * 8 * static_cast<int>(sizeof(T));  // 16 .. 112
+  uint64_t lo = v.x | static_cast<uint64_t>(v.y) << 32, hi = v.z | static_cast<uint64_t>(v.w) << 32;
+  lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+  hi = bits < 64 ? hi >> bits : 0;
+  return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32),
+               static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 template <typename T, bool WHOLE = false>
 __device__ __forceinline__ void put(T *row, int64_t c0, int64_t d, const float (&x)[Piece<T>::E]) {
@@ -94,92 +102,88 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
   const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
   const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
   const T *w = static_cast<const T *>(a.w);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + sub; i < a.N;
-       i += static_cast<int64_t>(gridDim.x) * ROWS) {
-    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
-    u32x4 in[K], more[K];
+  const int64_t i = group_number() * ROWS + sub;
+  if (i >= a.N) return;
+  const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+  u32x4 in[K], more[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) in[k] = get<T, WHOLE>(X, c + k * R * E, d);
+  for (int k = 0; k < K; ++k) in[k] = get<T, WHOLE>(X, c + k * R * E, d);
+  if (a.R) {
+    const T *Rs = static_cast<const T *>(a.R) + i * a.ldr;
+#pragma unroll
+    for (int k = 0; k < K; ++k) more[k] = get<T, WHOLE>(Rs, c + k * R * E, d);
+  }
+  float h[K][E], ss = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    Piece<T>::unpack(in[k], h[k]);
     if (a.R) {
-      const T *Rs = static_cast<const T *>(a.R) + i * a.ldr;
+      float r[E];
+      Piece<T>::unpack(more[k], r);
 #pragma unroll
-      for (int k = 0; k < K; ++k) more[k] = get<T, WHOLE>(Rs, c + k * R * E, d);
+      for (int e = 0; e < E; ++e) h[k][e] += r[e];
     }
-    float h[K][E], ss = 0.0f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      Piece<T>::unpack(in[k], h[k]);
-      if (a.R) {
-        float r[E];
-        Piece<T>::unpack(more[k], r);
+    for (int e = 0; e < E; ++e) ss = fmaf(h[k][e], h[k][e], ss);
+  }
+  ss = group_sum<W>(ss, red);
+  if (a.H) {
+    T *H = static_cast<T *>(a.H) + i * a.ldh;
 #pragma unroll
-        for (int e = 0; e < E; ++e) h[k][e] += r[e];
-      }
+    for (int k = 0; k < K; ++k) put<T, WHOLE>(H, c + k * R * E, d, h[k]);
+  }
+  const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+  uint32_t big[K];
 #pragma unroll
-      for (int e = 0; e < E; ++e) ss = fmaf(h[k][e], h[k][e], ss);
+  for (int k = 0; k < K; ++k) {
+    const int c0 = c + k * R * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[k][e] *= rho;
+    if (w) {
+      float g[E];
+      Piece<T>::unpack(get<T, WHOLE>(w, c0, d), g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[k][e] *= g[e];
     }
-    ss = group_sum<W>(ss, red);
-    if (a.H) {
-      T *H = static_cast<T *>(a.H) + i * a.ldh;
+    if constexpr (OUT == kOut) {
+      put<T, WHOLE>(static_cast<T *>(a.Y) + i * a.ldy, c0, d, h[k]);
+    } else {
+      big[k] = 0;
 #pragma unroll
-      for (int k = 0; k < K; ++k) put<T, WHOLE>(H, c + k * R * E, d, h[k]);
+      for (int e = 0; e < E; ++e) big[k] = umax(big[k], abs_bits(h[k][e]));
     }
-    const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
-    uint32_t big[K];
+  }
+  if constexpr (OUT == kOut8Row) {
+    uint32_t m = big[0];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c0 = c + k * R * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) h[k][e] *= rho;
-      if (w) {
-        float g[E];
-        Piece<T>::unpack(get<T, WHOLE>(w, c0, d), g);
-#pragma unroll
-        for (int e = 0; e < E; ++e) h[k][e] *= g[e];
-      }
-      if constexpr (OUT == kOut) {
-        put<T, WHOLE>(static_cast<T *>(a.Y) + i * a.ldy, c0, d, h[k]);
-      } else {
-        big[k] = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) big[k] = umax(big[k], abs_bits(h[k][e]));
-      }
-    }
-    if constexpr (OUT == kOut8Row) {
-      uint32_t m = big[0];
-#pragma unroll
-      for (int k = 1; k < K; ++k) m = umax(m, big[k]);
-      m = lanes_umax<64>(m);
-      if constexpr (W > 1) {
-        if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
-      }
-#pragma unroll
-      for (int k = 0; k < K; ++k) big[k] = m;
-      if (c == 0) a.S[i * a.lds] = scale_of(m);
-    } else if constexpr (OUT == kOut8Group) {
-      constexpr int L = kGroup / E;  // lanes of a scale
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        big[k] = lanes_umax<L>(big[k]);
-        const int c0 = c + k * R * E;
-        if (c0 % kGroup == 0 && c0 < d) a.S[i * a.lds + c0 / kGroup] = scale_of(big[k]);
-      }
-    }
-    if constexpr (OUT != kOut) {
-      uint8_t *Q = static_cast<uint8_t *>(a.Y) + i * a.ldy;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const float inv = 1.0f / scale_of(big[k]);
-#pragma unroll
-        for (int e = 0; e < E; ++e) h[k][e] = to_range(h[k][e], inv);
-        put8<E, WHOLE>(Q, c + k * R * E, d, h[k]);
-      }
-    }
+    for (int k = 1; k < K; ++k) m = umax(m, big[k]);
+    m = lanes_umax<64>(m);
     if constexpr (W > 1) {
-      if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
+      if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) big[k] = m;
+    if (c == 0) a.S[i * a.lds] = scale_of(m);
+  } else if constexpr (OUT == kOut8Group) {
+    constexpr int L = kGroup / E;  // lanes of a scale
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      big[k] = lanes_umax<L>(big[k]);
+      const int c0 = c + k * R * E;
+      if (c0 % kGroup == 0 && c0 < d) a.S[i * a.lds + c0 / kGroup] = scale_of(big[k]);
+    }
+  }
+  if constexpr (OUT != kOut) {
+    uint8_t *Q = static_cast<uint8_t *>(a.Y) + i * a.ldy;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const float inv = 1.0f / scale_of(big[k]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[k][e] = to_range(h[k][e], inv);
+      put8<E, WHOLE>(Q, c + k * R * E, d, h[k]);
     }
   }
 }
@@ -191,73 +195,72 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
   __shared__ float red[W];
   __shared__ uint32_t redu[W];
   const T *w = static_cast<const T *>(a.w);
-  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
-    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
-    const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
-    float h[E], r[E], ss = 0.0f;
-    auto sum = [&](int64_t c0) {
-      Piece<T>::unpack(get(X, c0, a.d), h);
-      if (Rs) {
-        Piece<T>::unpack(get(Rs, c0, a.d), r);
+  const int64_t i = group_number();
+  if (i >= a.N) return;
+  const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+  const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
+  float h[E], r[E], ss = 0.0f;
+  auto sum = [&](int64_t c0) {
+    Piece<T>::unpack(get(X, c0, a.d), h);
+    if (Rs) {
+      Piece<T>::unpack(get(Rs, c0, a.d), r);
 #pragma unroll
-        for (int e = 0; e < E; ++e) h[e] += r[e];
-      }
-    };
+      for (int e = 0; e < E; ++e) h[e] += r[e];
+    }
+  };
+  for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+    sum(c0);
+#pragma unroll
+    for (int e = 0; e < E; ++e) ss = fmaf(h[e], h[e], ss);
+  }
+  ss = group_sum<W>(ss, red);
+  const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+  auto norm = [&](int64_t c0) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] *= rho;
+    if (w) {
+      Piece<T>::unpack(get(w, c0, a.d), r);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] *= r[e];
+    }
+  };
+  uint32_t m = 0;
+  if constexpr (OUT == kOut8Row) {
     for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
       sum(c0);
+      norm(c0);
 #pragma unroll
-      for (int e = 0; e < E; ++e) ss = fmaf(h[e], h[e], ss);
+      for (int e = 0; e < E; ++e) m = umax(m, abs_bits(h[e]));
     }
-    ss = group_sum<W>(ss, red);
-    const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
-    auto norm = [&](int64_t c0) {
+    m = lanes_umax<64>(m);
+    if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
+    __syncthreads();
 #pragma unroll
-      for (int e = 0; e < E; ++e) h[e] *= rho;
-      if (w) {
-        Piece<T>::unpack(get(w, c0, a.d), r);
-#pragma unroll
-        for (int e = 0; e < E; ++e) h[e] *= r[e];
-      }
-    };
-    uint32_t m = 0;
-    if constexpr (OUT == kOut8Row) {
-      for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
-        sum(c0);
-        norm(c0);
+    for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
+    if (threadIdx.x == 0) a.S[i * a.lds] = scale_of(m);
+  }
+  // whole waves stay in the loop, so that the lanes of a scale are all there
+  for (int64_t b = 0; b < a.d; b += NT * E) {
+    const int64_t c0 = b + threadIdx.x * E;
+    sum(c0);
+    if (a.H) put(static_cast<T *>(a.H) + i * a.ldh, c0, a.d, h);
+    norm(c0);
+    if constexpr (OUT == kOut) {
+      put(static_cast<T *>(a.Y) + i * a.ldy, c0, a.d, h);
+    } else {
+      if constexpr (OUT == kOut8Group) {
+        constexpr int L = kGroup / E;
+        m = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) m = umax(m, abs_bits(h[e]));
+        m = lanes_umax<L>(m);
+        if (threadIdx.x % L == 0 && c0 < a.d) a.S[i * a.lds + c0 / kGroup] = scale_of(m);
       }
-      m = lanes_umax<64>(m);
-      if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
-      __syncthreads();
+      const float inv = 1.0f / scale_of(m);
 #pragma unroll
-      for (int j = 0; j < W; ++j) m = umax(m, redu[j]);
-      if (threadIdx.x == 0) a.S[i * a.lds] = scale_of(m);
+      for (int e = 0; e < E; ++e) h[e] = to_range(h[e], inv);
+      put8<E>(static_cast<uint8_t *>(a.Y) + i * a.ldy, c0, a.d, h);
     }
-    // whole waves stay in the loop, so that the lanes of a scale are all there
-    for (int64_t b = 0; b < a.d; b += NT * E) {
-      const int64_t c0 = b + threadIdx.x * E;
-      sum(c0);
-      if (a.H) put(static_cast<T *>(a.H) + i * a.ldh, c0, a.d, h);
-      norm(c0);
-      if constexpr (OUT == kOut) {
-        put(static_cast<T *>(a.Y) + i * a.ldy, c0, a.d, h);
-      } else {
-        if constexpr (OUT == kOut8Group) {
-          constexpr int L = kGroup / E;
-          m = 0;
-#pragma unroll
-          for (int e = 0; e < E; ++e) m = umax(m, abs_bits(h[e]));
-          m = lanes_umax<L>(m);
-          if (threadIdx.x % L == 0 && c0 < a.d) a.S[i * a.lds + c0 / kGroup] = scale_of(m);
-        }
-        const float inv = 1.0f / scale_of(m);
-#pragma unroll
-        for (int e = 0; e < E; ++e) h[e] = to_range(h[e], inv);
-        put8<E>(static_cast<uint8_t *>(a.Y) + i * a.ldy, c0, a.d, h);
-      }
-    }
-    if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
   }
 }
 
@@ -416,10 +419,7 @@ int64_t pieces_of(int dt, int64_t d) { return ceil_div(d, dt == 0 ? 4 : 8); }
 template <typename T, int OUT, bool WHOLE>
 hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
-  const auto grid = [&](int rows) {
-    const int64_t g = ceil_div(a.N, rows);
-    return static_cast<unsigned>(g < (1 << 20) ? g : 1 << 20);
-  };
+  const auto grid = [&](int rows) { return groups_grid(ceil_div(a.N, rows)); };
   if (n <= 64)
     rmsnorm_kernel<T, 64, 1, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
   else if (n <= 128)
@@ -449,18 +449,18 @@ hipError_t launch_norm_out(const NormArgs &a, hipStream_t s) {
                  : launch_norm_t<T, kOut8Row, false>(a, s);
 }
 
-// Workgroups of the backward, two for each of the 256 CUs (each leaves a part of
-// d values), or a part for each row where they are few.
-constexpr int64_t kGradGroups = 512;
-
+// Workgroups of the backward: four of 256 threads for each of the 256 CUs, two of
+// 512 or 1024 (each leaves a part of d values), or a part for each row where they
+// are few.
 struct GradPlan {
   int rows;       // rows of a workgroup at a time
   int64_t grid, parts;
 };
 GradPlan grad_plan(int dt, int64_t N, int64_t d) {
+  const int64_t n = pieces_of(dt, d), most = n <= 512 ? 1024 : 512;
   GradPlan p;
-  p.rows = pieces_of(dt, d) <= 128 ? 4 : 1;
-  p.grid = ceil_div(N, p.rows) < kGradGroups ? ceil_div(N, p.rows) : kGradGroups;
+  p.rows = n <= 128 ? 4 : 1;
+  p.grid = ceil_div(N, p.rows) < most ? ceil_div(N, p.rows) : most;
   p.parts = p.grid * p.rows < N ? p.grid * p.rows : N;
   return p;
 }

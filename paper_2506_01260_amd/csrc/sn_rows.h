@@ -60,6 +60,31 @@ __device__ __forceinline__ void store_piece(T *p, u32x4 v) {
     *q = v;
 }
 
+// The same for piece `base` + threadIdx.x of a row, base the same in all threads.
+template <typename T, bool NT = false>
+__device__ __forceinline__ u32x4 load_own(const T *row, int base) {
+  const auto b = reinterpret_cast<const char *>(row + static_cast<int64_t>(base) * Piece<T>::E);
+  return load_piece<T, NT>(reinterpret_cast<const T *>(b + 16u * threadIdx.x));
+}
+template <typename T, bool NT = false>
+__device__ __forceinline__ void store_own(T *row, int base, u32x4 v) {
+  const auto b = reinterpret_cast<char *>(row + static_cast<int64_t>(base) * Piece<T>::E);
+  store_piece<T, NT>(reinterpret_cast<T *>(b + 16u * threadIdx.x), v);
+}
+
+// Workgroups numbered over two grid dimensions, one of which holds fewer than 2^32
+// threads: one row (or part of one) each.  A loop over rows inside the kernel made
+// the compiler keep the addresses and comparisons of the whole unrolled body in
+// registers across it, up to 190 of them for 60.
+constexpr int64_t kGridX = 1 << 20;
+__device__ __forceinline__ int64_t group_number() {
+  return static_cast<int64_t>(blockIdx.y) * kGridX + blockIdx.x;
+}
+inline dim3 groups_grid(int64_t n) {
+  return dim3(static_cast<unsigned>(n < kGridX ? n : kGridX),
+              static_cast<unsigned>((n + kGridX - 1) / kGridX));
+}
+
 // The elements c0 .. c0 + E - 1 of a row of n: those at or past n read as `fill`
 // and are not written.
 template <typename T>
