@@ -84,6 +84,40 @@ __device__ __forceinline__ Running scan_row(const T *row, int64_t V, float c2) {
   return r;
 }
 
+// The threads' statistics joined over a workgroup of W waves (m and s in every
+// thread, t too with ENT): over each wave, then over the waves in order.  red: 3 W
+// floats of LDS.  One barrier.
+template <int W, bool ENT>
+__device__ __forceinline__ Running join(Running r, float *red, float c2) {
+  const auto rescale = [&](float m, float &s, float &t, float to) {
+    const float d = fmaxf(m - to, kFar), cr = exp2_fast(d * c2);
+    if constexpr (ENT) t = cr * fmaf(s, d, t);
+    s *= cr;
+  };
+  const float m = wave_max(r.m);
+  rescale(r.m, r.s, r.t, m);
+  r.m = m;
+  r.s = wave_sum(r.s);
+  if constexpr (ENT) r.t = wave_sum(r.t);
+  if constexpr (W == 1) return r;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane == 0) {
+    red[wave] = r.m;
+    red[W + wave] = r.s;
+    if constexpr (ENT) red[2 * W + wave] = r.t;
+  }
+  __syncthreads();
+  // lane i of each wave takes wave i's: again a reduction over a wave
+  const bool has = lane < W;
+  Running g;
+  if (has) {
+    g.m = red[lane];
+    g.s = red[W + lane];
+    if constexpr (ENT) g.t = red[2 * W + lane];
+  }
+  return join<1, ENT>(g, red, c2);
+}
+
 // ---- the largest logits --------------------------------------------------------
 // A float's bits made ascending as a whole number (-0 counts as 0).
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -102,9 +136,8 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) {
   return 0xFFFFFFFFu - static_cast<uint32_t>(k);
 }
 
-// Candidates a workgroup keeps for a row: the n largest and those equal to the
-// last of the thread maxima that bound them (about n of them but for rows of
-// many equal logits, which take the pass over the row below instead).
+// Candidates a workgroup keeps for a row: little more than n of them reach the
+// bound, but for rows of many equal logits (which take n passes instead).
 constexpr int kCandidates = 256;
 
 template <int NT>
@@ -115,16 +148,19 @@ struct TopLds {
   uint32_t sels, cands;
 };
 
-// The largest bound that at least n of the threads' maxima reach (0 if fewer
-// threads have a piece), built from its highest bit down: the same in each wave.
-template <int NT>
+// The largest bound that n of 64 P groups' largest logits reach (0 if fewer have
+// any), built from its highest bit down to bit LOW: the same in each wave.
+template <int NT, int P, int LOW>
 __device__ __forceinline__ uint32_t nth_best(const uint32_t (&best)[NT], int n) {
-  constexpr int P = NT / 64;
   const int lane = threadIdx.x & 63;
   uint32_t v[P], bound = 0;
 #pragma unroll
-  for (int i = 0; i < P; ++i) v[i] = best[64 * i + lane];
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+  for (int i = 0; i < P; ++i) {
+    v[i] = best[64 * i + lane];
+#pragma unroll
+    for (int j = i + P; j < NT / 64; j += P) v[i] = max(v[i], best[64 * j + lane]);
+  }
+  for (uint32_t bit = 0x80000000u; bit >= 1u << LOW; bit >>= 1) {
     int count = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) count += __popcll(__ballot(v[i] >= (bound | bit)));
@@ -152,7 +188,11 @@ template <typename T, int NT, typename F>
 __device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<NT> &lds, F &&put) {
   constexpr int E = Piece<T>::E;
   const uint32_t pieces = static_cast<uint32_t>((V + E - 1) / E), each = (pieces + NT - 1) / NT;
-  const uint32_t bound = nth_best<NT>(lds.best, n);
+  // Groups of threads, at least four to a logit asked for: nearly as good a bound as
+  // the threads' own.  A bf16 logit's order lies in the upper 16 bits.
+  constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
+  const uint32_t bound = NT == 64 || n <= 16 ? nth_best<NT, 1, LOW>(lds.best, n)
+                                             : nth_best<NT, NT == 64 ? 1 : 4, LOW>(lds.best, n);
   const uint32_t mine = lds.best[threadIdx.x];
   if (mine != 0 && mine >= bound) lds.sel[atomicAdd(&lds.sels, 1u)] = threadIdx.x;
   __syncthreads();
@@ -208,23 +248,21 @@ __device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<N
 template <typename T, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobsArgs a) {
   constexpr int W = NT / 64;
-  __shared__ float red[3][W];
+  __shared__ float red[3 * W];
   __shared__ TopLds<TOP ? NT : 64> lds;
   const float c2 = a.scale * kLog2e;
   const int64_t i = group_number();
   if (i >= a.N) return;
   const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
-  const Running r = scan_row<T, NT, true>(row, a.V, c2);
+  Running r = scan_row<T, NT, true>(row, a.V, c2);
   if constexpr (TOP) {
     // 0, below every logit's, for a thread without a piece
     lds.best[threadIdx.x] = static_cast<int64_t>(threadIdx.x) * Piece<T>::E < a.V ? ordered(r.best) : 0;
     if (threadIdx.x == 0) lds.sels = lds.cands = 0;
     if constexpr (W == 1) __syncthreads();
   }
-  const float m = group_max<W>(r.m, red[0]);
-  const float d = fmaxf(r.m - m, kFar), cr = exp2_fast(d * c2);
-  const float s = group_sum<W>(r.s * cr, red[1]);
-  const float t = group_sum<W>(cr * fmaf(r.s, d, r.t), red[2]);
+  r = join<W, true>(r, red, c2);
+  const float m = r.m, s = r.s, t = r.t;
   const float L = logf(s);  // -inf: nothing is allowed; NaN: a logit is NaN or +inf
   if (threadIdx.x == 0) {
     if (a.logp) {
@@ -350,7 +388,7 @@ template <typename T, int NT, int K, int WAVES>
 __global__ __launch_bounds__(NT, WAVES) void loss_kernel(LossArgs a) {
   constexpr int E = Piece<T>::E, W = NT / 64;
   static_assert(K % 4 == 0, "the pieces beyond the kept ones go in fours");
-  __shared__ float red[2][W];
+  __shared__ float red[3 * W];
   const float c2 = a.scale * kLog2e;
   const int full = static_cast<int>(a.V / E), tid = threadIdx.x;
   const bool tail = a.V % E != 0 && full % NT == tid;  // holds the row's last, short piece
@@ -400,8 +438,9 @@ __global__ __launch_bounds__(NT, WAVES) void loss_kernel(LossArgs a) {
         r.add<E, false>(z, c2);
       }
     if (tail) r.add<E, false>(last, c2);
-    m = group_max<W>(r.m, red[0]);
-    const float s = group_sum<W>(r.s * exp2_fast(fmaxf(r.m - m, kFar) * c2), red[1]);
+    r = join<W, false>(r, red, c2);
+    m = r.m;
+    const float s = r.s;
     const float L = logf(s);
     if (tid == 0) a.logp[i] = s > 0.0f ? fmaf(zt - m, a.scale, -L) : L;
     f = s == 0.0f ? 0.0f : w * a.scale / s;
@@ -465,7 +504,9 @@ hipError_t launch_logprobs_nt(const LogprobsArgs &a, hipStream_t s) {
 template <typename T>
 hipError_t launch_logprobs_t(const LogprobsArgs &a, hipStream_t s) {
   const int64_t pieces = ceil_div(a.V, Piece<T>::E);
-  if (pieces <= 512) return launch_logprobs_nt<T, 64>(a, s);
+  // (a wave's 64 lanes bound up to 16 alternatives well, or any row that fits)
+  if (pieces <= 512 && (a.n_top <= 16 || a.V <= kCandidates))
+    return launch_logprobs_nt<T, 64>(a, s);
   if (a.N <= 512 && pieces > 1024) return launch_logprobs_nt<T, 1024>(a, s);
   return launch_logprobs_nt<T, 256>(a, s);
 }

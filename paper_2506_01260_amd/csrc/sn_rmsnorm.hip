@@ -157,7 +157,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
     uint32_t m = big[0];
 #pragma unroll
     for (int k = 1; k < K; ++k) m = umax(m, big[k]);
-    m = lanes_umax<64>(m);
+    m = wave_umax(m);
     if constexpr (W > 1) {
       if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
       __syncthreads();
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) m = umax(m, abs_bits(h[e]));
     }
-    m = lanes_umax<64>(m);
+    m = wave_umax(m);
     if ((threadIdx.x & 63) == 0) redu[threadIdx.x >> 6] = m;
     __syncthreads();
 #pragma unroll

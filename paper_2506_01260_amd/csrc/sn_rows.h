@@ -102,20 +102,43 @@ __device__ __forceinline__ void store_part(T *row, int64_t c0, int64_t n,
 }
 
 // ---- reductions: every lane / thread gets the result ------------------------
+// Over the wave by data-parallel-primitive moves, which cost a vector instruction
+// each where a shuffle is a trip to the LDS: within rows of 16 lanes, then row 0
+// to 1 and 2 to 3, then the lower half to the upper; lane 63 has the total.  A
+// lane without a source keeps `none`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t v, uint32_t none) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+      static_cast<int>(none), static_cast<int>(v), CTRL, ROWS, 0xF, false));
+}
+template <typename F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, uint32_t none, F &&f) {
+  v = f(v, dpp<0x111, 0xF>(v, none));  // row_shr:1, 2, 4, 8
+  v = f(v, dpp<0x112, 0xF>(v, none));
+  v = f(v, dpp<0x114, 0xF>(v, none));
+  v = f(v, dpp<0x118, 0xF>(v, none));
+  v = f(v, dpp<0x142, 0xA>(v, none));  // row_bcast:15 into rows 1 and 3
+  v = f(v, dpp<0x143, 0xC>(v, none));  // row_bcast:31 into rows 2 and 3
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+  return __uint_as_float(wave_reduce(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
 }
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-  return v;
+  return __uint_as_float(
+      wave_reduce(__float_as_uint(v), __float_as_uint(-INFINITY), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+      }));
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+  return wave_reduce(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
-// Sums / maxima over a workgroup of W waves; red: W floats of LDS that no
-// thread uses between the caller's last barrier and the call, nor after it
-// before the next barrier.  One barrier.  The waves are added in order.
+// Sums over a workgroup of W waves; red: W floats of LDS that no thread uses
+// between the caller's last barrier and the call, nor after it before the next
+// barrier.  One barrier.  The waves are added in order.
 template <int W>
 __device__ __forceinline__ float group_sum(float v, float *red) {
   v = wave_sum(v);
@@ -125,17 +148,6 @@ __device__ __forceinline__ float group_sum(float v, float *red) {
   v = red[0];
 #pragma unroll
   for (int i = 1; i < W; ++i) v += red[i];
-  return v;
-}
-template <int W>
-__device__ __forceinline__ float group_max(float v, float *red) {
-  v = wave_max(v);
-  if constexpr (W == 1) return v;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int i = 1; i < W; ++i) v = fmaxf(v, red[i]);
   return v;
 }
 
