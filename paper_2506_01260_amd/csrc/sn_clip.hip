@@ -16,10 +16,17 @@ namespace sn {
 namespace {
 
 constexpr int kNT = 256;
+// Pieces of a thread in flight: read and summed, and read, scaled and written.
+constexpr int kSumBatch = 8, kClipBatch = 4;
 
-// Elements of a unit: 16384, or 2048 (a piece or two for each thread) where that
-// leaves fewer than two workgroups for each CU.
-int64_t unit_elems(int64_t total) { return total >= (int64_t(1) << 23) ? 16384 : 2048; }
+// Elements of a unit: 2048 (a piece or two for each thread) below 2^23 elements, to
+// fill the chip.  Above, the norm's units are no more than one workgroup adds up
+// quickly (2^15 to 2^31 elements), and a clipping unit is one batch: at 1.1e9 bf16
+// gradients 774 us, 792 with twice as many elements and 810 with eight times.
+int64_t sum_unit(int64_t total) {
+  return total < (int64_t(1) << 23) ? 2048 : total < (int64_t(1) << 27) ? 16384 : 65536;
+}
+int64_t clip_unit(int64_t total) { return total < (int64_t(1) << 23) ? 2048 : 8192; }
 
 // Units of a tensor: pieces of `u` columns of a row, or u / cols rows together.
 int64_t units_of(const ClipTensor &t, int64_t u) {
@@ -60,19 +67,31 @@ __device__ __forceinline__ Unit unit_at(const ClipTable &tab, uint32_t unit, int
   return x;
 }
 
-// The unit's elements, piece by piece: f(row, column, columns in the piece).
-template <int E, typename F>
-__device__ __forceinline__ void each_piece(const Unit &x, F &&f) {
-  const uint32_t n = static_cast<uint32_t>(x.c1 - x.c0), per = (n + E - 1) / E;
-  const uint32_t all = per * static_cast<uint32_t>(x.r1 - x.r0);
-  if (x.r1 - x.r0 == 1) {
-#pragma unroll 4
-    for (uint32_t q = threadIdx.x; q < all; q += kNT) f(x.r0, x.c0 + q * E);
-  } else {
-    for (uint32_t q = threadIdx.x; q < all; q += kNT) {
-      const uint32_t r = q / per;
-      f(x.r0 + r, x.c0 + static_cast<int64_t>(q - r * per) * E);
+// The unit's whole pieces, B of each thread at a time: load(row, column) of all of
+// them, then use(row, column, piece); then the rows' ends, element by element:
+// last(row, column).
+template <int E, int B, typename L, typename U, typename R>
+__device__ __forceinline__ void each_piece(const Unit &x, L &&load, U &&use, R &&last) {
+  const uint32_t n = static_cast<uint32_t>(x.c1 - x.c0), per = n / E, rest = n % E;
+  const uint32_t rows = static_cast<uint32_t>(x.r1 - x.r0), all = per * rows;
+  for (uint32_t q0 = threadIdx.x; q0 < all; q0 += B * kNT) {
+    u32x4 v[B];
+    uint32_t r[B], c[B];
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const uint32_t q = q0 + k * kNT;
+      r[k] = rows == 1 ? 0 : q / per;
+      c[k] = (q - r[k] * per) * E;
+      v[k] = u32x4{0, 0, 0, 0};
+      if (q < all) v[k] = load(x.r0 + r[k], x.c0 + c[k]);
     }
+#pragma unroll
+    for (int k = 0; k < B; ++k)
+      if (q0 + k * kNT < all) use(x.r0 + r[k], x.c0 + c[k], v[k]);
+  }
+  for (uint32_t q = threadIdx.x; q < rest * rows; q += kNT) {
+    const uint32_t k = q / rest;
+    last(x.r0 + k, x.c0 + per * E + (q - k * rest));
   }
 }
 
@@ -87,16 +106,16 @@ __device__ __forceinline__ double unit_sumsq(const ClipTensor &t, const Unit &x)
   constexpr int E = Piece<T>::E;
   const T *g = static_cast<const T *>(t.g);
   double s = 0.0;
-  each_piece<E>(x, [&](int64_t r, int64_t c) {
-    float v[E];
-    const T *row = g + r * t.ldg;
-    if (c + E <= x.c1)
-      Piece<T>::unpack(load_piece(row + c), v);
-    else
-      load_part(row, c, x.c1, 0.0f, v);
+  const auto add = [&](float v) { s = fma(static_cast<double>(v), static_cast<double>(v), s); };
+  each_piece<E, kSumBatch>(
+      x, [&](int64_t r, int64_t c) { return load_piece(g + r * t.ldg + c); },
+      [&](int64_t, int64_t, u32x4 p) {
+        float v[E];
+        Piece<T>::unpack(p, v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) s = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), s);
-  });
+        for (int e = 0; e < E; ++e) add(v[e]);
+      },
+      [&](int64_t r, int64_t c) { add(to_f32(g[r * t.ldg + c])); });
   return s;
 }
 
@@ -138,24 +157,20 @@ __device__ __forceinline__ void unit_scale(const ClipTensor &t, const Unit &x, f
   constexpr int E = Piece<T>::E;
   const T *g = static_cast<const T *>(t.g);
   T *o = static_cast<T *>(t.out);
-  each_piece<E>(x, [&](int64_t r, int64_t c) {
-    float v[E];
-    const T *src = g + r * t.ldg;
-    T *dst = o + r * t.ldo;
-    if (c + E <= x.c1) {
-      Piece<T>::unpack(load_piece(src + c), v);
+  each_piece<E, kClipBatch>(
+      x, [&](int64_t r, int64_t c) { return load_piece<T, true>(g + r * t.ldg + c); },
+      [&](int64_t r, int64_t c, u32x4 p) {
+        float v[E];
+        Piece<T>::unpack(p, v);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= f;
-      store_piece(dst + c, Piece<T>::pack(v));
-    } else {
-      load_part(src, c, x.c1, 0.0f, v);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= f;
-      store_part(dst, c, x.c1, v);
-    }
-  });
+        for (int e = 0; e < E; ++e) v[e] *= f;
+        store_piece<T, true>(o + r * t.ldo + c, Piece<T>::pack(v));
+      },
+      [&](int64_t r, int64_t c) { o[r * t.ldo + c] = from_f32<T>(to_f32(g[r * t.ldg + c]) * f); });
 }
 
+// The units in the opposite order of the norm's: of the gradients the last ones that
+// it read are still in the Infinity Cache, and the products are stored past it.
 __global__ __launch_bounds__(kNT) void clip_kernel(ClipTable tab, int64_t u, int in_place,
                                                    const double *__restrict__ sumsq,
                                                    double max_norm, float *__restrict__ norm_out) {
@@ -164,7 +179,7 @@ __global__ __launch_bounds__(kNT) void clip_kernel(ClipTable tab, int64_t u, int
   const float f = norm <= max_norm ? 1.0f : static_cast<float>(max_norm / norm);
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
   if (tab.n == 0 || (in_place && f == 1.0f)) return;  // every value is its own product
-  const Unit x = unit_at(tab, blockIdx.x, u);
+  const Unit x = unit_at(tab, gridDim.x - 1 - blockIdx.x, u);
   const ClipTensor &t = tab.t[x.t];
   if (t.f32)
     unit_scale<float>(t, x, f);
@@ -172,25 +187,24 @@ __global__ __launch_bounds__(kNT) void clip_kernel(ClipTable tab, int64_t u, int
     unit_scale<bf16_t>(t, x, f);
 }
 
-// Tables of up to kClipTensors tensors that have elements: launch(table, units).
+// Tables of up to kClipTensors tensors: launch(table, units), the last tables first
+// with `back` (the tables are the same).
 template <typename F>
-hipError_t each_table(const ClipTensor *t, int32_t count, int64_t u, F &&launch) {
-  ClipTable tab;
-  int64_t units = 0;
-  for (int32_t i = 0; i <= count; ++i) {
-    const int64_t more = i < count ? units_of(t[i], u) : 0;
-    // a grid holds fewer than 2^32 threads
-    if (tab.n && (i == count || tab.n == kClipTensors || units + more > (1 << 23))) {
-      launch(tab, static_cast<unsigned>(units));
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      tab.n = 0;
-      units = 0;
+hipError_t each_table(const ClipTensor *t, int32_t count, int64_t u, bool back, F &&launch) {
+  const auto units_at = [&](int32_t i) { return units_of(t[i], u); };
+  const int32_t tables = static_cast<int32_t>(ceil_div(count, kClipTensors));
+  for (int32_t b = 0; b < tables; ++b) {
+    const int32_t i0 = (back ? tables - 1 - b : b) * kClipTensors;
+    ClipTable tab;
+    int64_t units = 0;
+    for (int32_t i = i0; i < count && tab.n < kClipTensors; ++i) {
+      tab.t[tab.n] = t[i];
+      tab.unit0[tab.n++] = static_cast<uint32_t>(units);
+      units += units_at(i);
     }
-    if (more == 0) continue;
-    tab.t[tab.n] = t[i];
-    tab.unit0[tab.n++] = static_cast<uint32_t>(units);
-    units += more;
+    launch(tab, static_cast<unsigned>(units));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -204,7 +218,7 @@ int64_t total_elems(const ClipTensor *t, int32_t count) {
 }  // namespace
 
 int64_t clip_units(const ClipTensor *t, int32_t count) {
-  const int64_t u = unit_elems(total_elems(t, count));
+  const int64_t u = sum_unit(total_elems(t, count));
   int64_t n = 0;
   for (int32_t i = 0; i < count; ++i) n += units_of(t[i], u);
   return n;
@@ -212,10 +226,10 @@ int64_t clip_units(const ClipTensor *t, int32_t count) {
 
 hipError_t launch_sumsq(const ClipTensor *t, int32_t count, double *sumsq, void *ws,
                         hipStream_t s) {
-  const int64_t u = unit_elems(total_elems(t, count));
+  const int64_t u = sum_unit(total_elems(t, count));
   double *part = static_cast<double *>(ws);
   int64_t n = 0;
-  const hipError_t e = each_table(t, count, u, [&](const ClipTable &tab, unsigned units) {
+  const hipError_t e = each_table(t, count, u, false, [&](const ClipTable &tab, unsigned units) {
     sumsq_kernel<<<units, kNT, 0, s>>>(tab, u, part + n);
     n += units;
   });
@@ -226,9 +240,9 @@ hipError_t launch_sumsq(const ClipTensor *t, int32_t count, double *sumsq, void 
 
 hipError_t launch_clip(const ClipTensor *t, int32_t count, bool in_place, const double *sumsq,
                        double max_norm, float *norm, hipStream_t s) {
-  const int64_t u = unit_elems(total_elems(t, count));
+  const int64_t u = clip_unit(total_elems(t, count));
   bool told = norm == nullptr;
-  const hipError_t e = each_table(t, count, u, [&](const ClipTable &tab, unsigned units) {
+  const hipError_t e = each_table(t, count, u, true, [&](const ClipTable &tab, unsigned units) {
     clip_kernel<<<units, kNT, 0, s>>>(tab, u, in_place, sumsq, max_norm, told ? nullptr : norm);
     told = true;
   });

@@ -498,16 +498,20 @@ hipError_t launch_logprobs_nt(const LogprobsArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Threads of a row: a wave up to 8 pieces for each lane; else 1024 where the rows
-// are fewer than the CUs, 256 where there are more of them than workgroups of
-// 1024 that run at a time.
+// Threads of a row: a wave up to 8 pieces for each lane.  Longer rows take 1024 up
+// to 512 rows (two workgroups for each CU), and always without alternatives, where
+// a workgroup waits for little (8192 x 128256 bf16: 334 us, 353 with 512, 356 with
+// 256).  With alternatives smaller workgroups hide each other's selection, 256
+// where they come in four rounds or more of the 2048 that run at a time (16384 x
+// 32000: 190 us, 198 with 512, 269 with 1024; 4999 x 50257: 116, 109, 124).
 template <typename T>
 hipError_t launch_logprobs_t(const LogprobsArgs &a, hipStream_t s) {
   const int64_t pieces = ceil_div(a.V, Piece<T>::E);
   // (a wave's 64 lanes bound up to 16 alternatives well, or any row that fits)
   if (pieces <= 512 && (a.n_top <= 16 || a.V <= kCandidates))
     return launch_logprobs_nt<T, 64>(a, s);
-  if (a.N <= 512 && pieces > 1024) return launch_logprobs_nt<T, 1024>(a, s);
+  if (pieces > 1024 && (a.n_top == 0 || a.N <= 512)) return launch_logprobs_nt<T, 1024>(a, s);
+  if (pieces > 1024 && a.N < 8192) return launch_logprobs_nt<T, 512>(a, s);
   return launch_logprobs_nt<T, 256>(a, s);
 }
 

@@ -523,10 +523,11 @@ SN_FAST(adamw_step) {
 // These take calls on the current stream only (stream None), with every tensor on
 // the current device.
 
-const at::Tensor *here(PyObject *o) {
+const at::Tensor *on(PyObject *o, c10::DeviceIndex device) {
   const at::Tensor *t = plain(o);
-  return t && t->get_device() == c10::hip::current_device() ? t : nullptr;
+  return t && t->get_device() == device ? t : nullptr;
 }
+const at::Tensor *here(PyObject *o) { return on(o, c10::hip::current_device()); }
 
 bool mat_here(PyObject *o, Mat &m) { return here(o) && mat(o, m); }
 
@@ -786,9 +787,10 @@ SN_FAST(rmsnorm_backward) {
 bool tensors(PyObject *o, std::vector<sn_tensor> &v) {
   if (!PyList_CheckExact(o)) return false;
   const Py_ssize_t count = PyList_GET_SIZE(o);
+  const c10::DeviceIndex device = c10::hip::current_device();
   v.resize(static_cast<size_t>(count));
   for (Py_ssize_t i = 0; i < count; ++i) {
-    const at::Tensor *t = here(PyList_GET_ITEM(o, i));
+    const at::Tensor *t = on(PyList_GET_ITEM(o, i), device);
     if (!t || !sn_type(t->scalar_type()) || !t->is_contiguous()) return false;
     const int64_t e = t->numel();
     v[static_cast<size_t>(i)] = {e ? t->data_ptr() : nullptr, 1, e, e, dt_of(t->scalar_type())};
