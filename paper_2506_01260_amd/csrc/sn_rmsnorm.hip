@@ -19,28 +19,43 @@ namespace {
 constexpr float kF8Max = 448.0f;
 constexpr uint32_t kTiny = 0x0D800000u;  // 2^-100, the least maximum a scale is made from
 
-// The piece at column c0 of a row of d: 0 past the row's end.  WHOLE: d is a
-// multiple of the piece, so that a piece lies in the row or past it.  Else the
-// row's last piece is the one that ends with the row, shifted: one load, as for
-// the others (element by element it was another round trip to memory, and a
-// backward of width 1601 took a quarter longer).
-template <typename T, bool WHOLE = false>
-__device__ __forceinline__ u32x4 get(const T *row, int64_t c0, int64_t d) {
-  constexpr int E = Piece<T>::E;
-  if (c0 >= d) return u32x4{0, 0, 0, 0};
-  if (WHOLE || c0 + E <= d) return load_piece(row + c0);
-  if (d < E) {
-    float x[E];
-    load_part(row, c0, d, 0.0f, x);
-    return Piece<T>::pack(x);  // exact: the values are T's own
+// The piece at column c0 of a row of d, 0 past the row's end, in two steps: take()
+// loads the piece there, or the one that the row ends with, and fix() moves that
+// one's values to their places.  So every load of a row is issued before any is
+// waited for, also at widths that are no multiple of the piece (where the last
+// piece element by element, or moved as it came, made the backward of 32768 x 1601
+// half as long again).  d >= E.  WHOLE: d is a multiple of the piece.
+template <typename T>
+__device__ __forceinline__ u32x4 take(const T *row, int c0, int d) {
+  return load_piece(row + min(c0, d - Piece<T>::E));
+}
+template <typename T, bool WHOLE>
+__device__ __forceinline__ u32x4 fix(u32x4 v, int c0, int d) {
+  const int by = c0 - (d - Piece<T>::E);  // values that the piece came early by
+  if (by > 0) {
+    uint64_t lo = v.x | static_cast<uint64_t>(v.y) << 32, hi = v.z | static_cast<uint64_t>(v.w) << 32;
+    const int bits = by * 8 * static_cast<int>(sizeof(T));
+    if (WHOLE || bits >= 128) {
+      lo = hi = 0;
+    } else if (bits >= 64) {
+      lo = hi >> (bits - 64);
+      hi = 0;
+    } else {
+      lo = lo >> bits | hi << (64 - bits);
+      hi >>= bits;
+    }
+    v = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32),
+              static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
   }
-  const u32x4 v = load_piece(row + d - E);
-  const int bits = static_cast<int>(c0 - (d - E)) * 8 * static_cast<int>(sizeof(T));  // 16 .. 112
-  uint64_t lo = v.x | static_cast<uint64_t>(v.y) << 32, hi = v.z | static_cast<uint64_t>(v.w) << 32;
-  lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
-  hi = bits < 64 ? hi >> bits : 0;
-  return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32),
-               static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+  return v;
+}
+// The same in one step, for any d and for rows past the registers.
+template <typename T>
+__device__ __forceinline__ void get(const T *row, int64_t c0, int64_t d, float (&x)[Piece<T>::E]) {
+  if (c0 + Piece<T>::E <= d)
+    Piece<T>::unpack(load_piece(row + c0), x);
+  else
+    load_part(row, c0, d, 0.0f, x);
 }
 template <typename T, bool WHOLE = false>
 __device__ __forceinline__ void put(T *row, int64_t c0, int64_t d, const float (&x)[Piece<T>::E]) {
@@ -107,19 +122,19 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
   const T *X = static_cast<const T *>(a.X) + i * a.ldx;
   u32x4 in[K], more[K];
 #pragma unroll
-  for (int k = 0; k < K; ++k) in[k] = get<T, WHOLE>(X, c + k * R * E, d);
+  for (int k = 0; k < K; ++k) in[k] = take(X, c + k * R * E, d);
   if (a.R) {
     const T *Rs = static_cast<const T *>(a.R) + i * a.ldr;
 #pragma unroll
-    for (int k = 0; k < K; ++k) more[k] = get<T, WHOLE>(Rs, c + k * R * E, d);
+    for (int k = 0; k < K; ++k) more[k] = take(Rs, c + k * R * E, d);
   }
   float h[K][E], ss = 0.0f;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    Piece<T>::unpack(in[k], h[k]);
+    Piece<T>::unpack(fix<T, WHOLE>(in[k], c + k * R * E, d), h[k]);
     if (a.R) {
       float r[E];
-      Piece<T>::unpack(more[k], r);
+      Piece<T>::unpack(fix<T, WHOLE>(more[k], c + k * R * E, d), r);
 #pragma unroll
       for (int e = 0; e < E; ++e) h[k][e] += r[e];
     }
@@ -141,7 +156,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
     for (int e = 0; e < E; ++e) h[k][e] *= rho;
     if (w) {
       float g[E];
-      Piece<T>::unpack(get<T, WHOLE>(w, c0, d), g);
+      Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) h[k][e] *= g[e];
     }
@@ -201,9 +216,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
   const T *Rs = a.R ? static_cast<const T *>(a.R) + i * a.ldr : nullptr;
   float h[E], r[E], ss = 0.0f;
   auto sum = [&](int64_t c0) {
-    Piece<T>::unpack(get(X, c0, a.d), h);
+    get(X, c0, a.d, h);
     if (Rs) {
-      Piece<T>::unpack(get(Rs, c0, a.d), r);
+      get(Rs, c0, a.d, r);
 #pragma unroll
       for (int e = 0; e < E; ++e) h[e] += r[e];
     }
@@ -219,7 +234,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) h[e] *= rho;
     if (w) {
-      Piece<T>::unpack(get(w, c0, a.d), r);
+      get(w, c0, a.d, r);
 #pragma unroll
       for (int e = 0; e < E; ++e) h[e] *= r[e];
     }
@@ -277,21 +292,21 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
   const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
   const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
   const T *w = static_cast<const T *>(a.w);
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   float gw[K][E] = {};
-  for (int64_t i = first; i < a.N; i += static_cast<int64_t>(gridDim.x) * ROWS) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + sub; i < a.N;
+       i += static_cast<int64_t>(gridDim.x) * ROWS) {
     const T *H = static_cast<const T *>(a.H) + i * a.ldh;
     const T *dY = static_cast<const T *>(a.dY) + i * a.lddy;
     u32x4 hp[K], yp[K], dp[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      hp[k] = get<T, WHOLE>(H, c + k * R * E, d);
-      yp[k] = get<T, WHOLE>(dY, c + k * R * E, d);
+      hp[k] = take(H, c + k * R * E, d);
+      yp[k] = take(dY, c + k * R * E, d);
     }
     if (a.dH) {
       const T *dH = static_cast<const T *>(a.dH) + i * a.lddh;
 #pragma unroll
-      for (int k = 0; k < K; ++k) dp[k] = get<T, WHOLE>(dH, c + k * R * E, d);
+      for (int k = 0; k < K; ++k) dp[k] = take(dH, c + k * R * E, d);
     } else {
 #pragma unroll
       for (int k = 0; k < K; ++k) dp[k] = u32x4{0, 0, 0, 0};
@@ -301,9 +316,12 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
     for (int e = 0; e < E; ++e) g[e] = 1.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
+      const int c0 = c + k * R * E;
+      hp[k] = fix<T, WHOLE>(hp[k], c0, d);
+      yp[k] = fix<T, WHOLE>(yp[k], c0, d);
       Piece<T>::unpack(hp[k], h);
       Piece<T>::unpack(yp[k], y);
-      if (w) Piece<T>::unpack(get<T, WHOLE>(w, c + k * R * E, d), g);
+      if (w) Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         ss = fmaf(h[e], h[e], ss);
@@ -321,8 +339,8 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
       float o[E];
       Piece<T>::unpack(hp[k], h);
       Piece<T>::unpack(yp[k], y);
-      Piece<T>::unpack(dp[k], o);
-      if (w) Piece<T>::unpack(get<T, WHOLE>(w, c0, d), g);
+      Piece<T>::unpack(fix<T, WHOLE>(dp[k], c0, d), o);
+      if (w) Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         gw[k][e] = fmaf(y[e] * h[e], rho, gw[k][e]);
@@ -334,14 +352,28 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
       if (i + gridDim.x < a.N) __syncthreads();  // the LDS is used again
     }
   }
-  if (a.part && first < a.N) {
-    float *part = a.part + first * a.d;  // the first row's number names the part
+  if (!a.part) return;
+  float *part = a.part + static_cast<int64_t>(blockIdx.x) * a.d;
+  if constexpr (ROWS == 1) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c0 = c + k * R * E;
 #pragma unroll
       for (int e = 0; e < E; ++e)
         if (c0 + e < d) part[c0 + e] = gw[k][e];
+    }
+  } else {  // the waves' rows are added in order
+    __shared__ float sums[ROWS][K * R * E];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) sums[sub][c + k * R * E + e] = gw[k][e];
+    __syncthreads();
+    for (int j = threadIdx.x; j < d; j += NT) {
+      float t = sums[0][j];
+#pragma unroll
+      for (int q = 1; q < ROWS; ++q) t += sums[q][j];
+      part[j] = t;
     }
   }
 }
@@ -359,9 +391,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
     const T *dH = a.dH ? static_cast<const T *>(a.dH) + i * a.lddh : nullptr;
     float h[E], u[E], g[E], ss = 0.0f, uh = 0.0f;
     for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
-      Piece<T>::unpack(get(H, c0, a.d), h);
-      Piece<T>::unpack(get(dY, c0, a.d), u);
-      if (w) Piece<T>::unpack(get(w, c0, a.d), g);
+      get(H, c0, a.d, h);
+      get(dY, c0, a.d, u);
+      if (w) get(w, c0, a.d, g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         ss = fmaf(h[e], h[e], ss);
@@ -375,10 +407,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
     float *part = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
     for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
       float o[E] = {};
-      Piece<T>::unpack(get(H, c0, a.d), h);
-      Piece<T>::unpack(get(dY, c0, a.d), u);
-      if (dH) Piece<T>::unpack(get(dH, c0, a.d), o);
-      if (w) Piece<T>::unpack(get(w, c0, a.d), g);
+      get(H, c0, a.d, h);
+      get(dY, c0, a.d, u);
+      if (dH) get(dH, c0, a.d, o);
+      if (w) get(w, c0, a.d, g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (part && c0 + e < a.d)
@@ -391,25 +423,24 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
   }
 }
 
-// gw[c] += sum over the parts, in float64 and in a fixed order: 16 waves take
-// every 16th part of 64 columns, then the waves in order.
-constexpr int kGainWaves = 16;
-__global__ __launch_bounds__(64 * kGainWaves) void gain_kernel(const float *__restrict__ part,
-                                                               int64_t parts, int64_t d,
-                                                               float *__restrict__ gw) {
-  __shared__ double red[kGainWaves][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+// gw[c] += sum over the parts, in float64 and in a fixed order: 32 groups of threads
+// take every 32nd part of 32 columns, then the groups in order.
+constexpr int kGainCols = 32, kGainGroups = 32;
+__global__ __launch_bounds__(kGainCols *kGainGroups) void gain_kernel(
+    const float *__restrict__ part, int64_t parts, int64_t d, float *__restrict__ gw) {
+  __shared__ double red[kGainGroups][kGainCols];
+  const int lane = threadIdx.x % kGainCols, g = threadIdx.x / kGainCols;
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * kGainCols + lane;
   double s = 0.0;
   if (c < d) {
 #pragma unroll 8
-    for (int64_t b = w; b < parts; b += kGainWaves) s += static_cast<double>(part[b * d + c]);
+    for (int64_t b = g; b < parts; b += kGainGroups) s += static_cast<double>(part[b * d + c]);
   }
-  red[w][lane] = s;
+  red[g][lane] = s;
   __syncthreads();
-  if (w != 0 || c >= d) return;
+  if (g != 0 || c >= d) return;
 #pragma unroll
-  for (int i = 1; i < kGainWaves; ++i) s += red[i][lane];
+  for (int i = 1; i < kGainGroups; ++i) s += red[i][lane];
   gw[c] = static_cast<float>(static_cast<double>(gw[c]) + s);
 }
 
@@ -420,7 +451,9 @@ template <typename T, int OUT, bool WHOLE>
 hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
   const auto grid = [&](int rows) { return groups_grid(ceil_div(a.N, rows)); };
-  if (n <= 64)
+  if (a.d < Piece<T>::E)  // no whole piece to take
+    rmsnorm_long_kernel<T, OUT><<<grid(1), 1024, 0, s>>>(a);
+  else if (n <= 64)
     rmsnorm_kernel<T, 64, 1, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
   else if (n <= 128)
     rmsnorm_kernel<T, 64, 2, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
@@ -449,27 +482,21 @@ hipError_t launch_norm_out(const NormArgs &a, hipStream_t s) {
                  : launch_norm_t<T, kOut8Row, false>(a, s);
 }
 
-// Workgroups of the backward: four of 256 threads for each of the 256 CUs, two of
-// 512 or 1024 (each leaves a part of d values), or a part for each row where they
-// are few.
-struct GradPlan {
-  int rows;       // rows of a workgroup at a time
-  int64_t grid, parts;
-};
-GradPlan grad_plan(int dt, int64_t N, int64_t d) {
+// Workgroups of the backward, each with a part of the gain's gradient: four of 256
+// threads for each of the 256 CUs, two of 512 or 1024, or what the rows fill.
+int64_t grad_groups(int dt, int64_t N, int64_t d) {
   const int64_t n = pieces_of(dt, d), most = n <= 512 ? 1024 : 512;
-  GradPlan p;
-  p.rows = n <= 128 ? 4 : 1;
-  p.grid = ceil_div(N, p.rows) < most ? ceil_div(N, p.rows) : most;
-  p.parts = p.grid * p.rows < N ? p.grid * p.rows : N;
-  return p;
+  const int64_t groups = ceil_div(N, n <= 128 ? 4 : 1);
+  return groups < most ? groups : most;
 }
 
 template <typename T, bool WHOLE>
 hipError_t launch_grad_t(int dt, const NormGradArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
-  const unsigned g = static_cast<unsigned>(grad_plan(dt, a.N, a.d).grid);
-  if (n <= 64)
+  const unsigned g = static_cast<unsigned>(grad_groups(dt, a.N, a.d));
+  if (a.d < Piece<T>::E)
+    rmsnorm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
+  else if (n <= 64)
     rmsnorm_grad_kernel<T, 64, 1, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 128)
     rmsnorm_grad_kernel<T, 64, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
@@ -499,15 +526,15 @@ hipError_t launch_rmsnorm(int dt, const NormArgs &a, hipStream_t s) {
 }
 
 size_t rmsnorm_grad_workspace_bytes(int dt, int64_t N, int64_t d) {
-  return align256(static_cast<size_t>(grad_plan(dt, N, d).parts) * d * sizeof(float));
+  return align256(static_cast<size_t>(grad_groups(dt, N, d)) * d * sizeof(float));
 }
 
 hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipStream_t s) {
   a.part = gw ? static_cast<float *>(ws) : nullptr;
   const hipError_t e = dt == 0 ? launch_grad_d<float>(dt, a, s) : launch_grad_d<bf16_t>(dt, a, s);
   if (e != hipSuccess || !gw) return e;
-  gain_kernel<<<static_cast<unsigned>(ceil_div(a.d, 64)), 64 * kGainWaves, 0, s>>>(
-      a.part, grad_plan(dt, a.N, a.d).parts, a.d, gw);
+  gain_kernel<<<static_cast<unsigned>(ceil_div(a.d, kGainCols)), kGainCols * kGainGroups, 0, s>>>(
+      a.part, grad_groups(dt, a.N, a.d), a.d, gw);
   return hipGetLastError();
 }
 
