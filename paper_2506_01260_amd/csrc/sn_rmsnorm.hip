@@ -482,11 +482,14 @@ hipError_t launch_norm_out(const NormArgs &a, hipStream_t s) {
                  : launch_norm_t<T, kOut8Row, false>(a, s);
 }
 
-// Workgroups of the backward, each with a part of the gain's gradient: four of 256
-// threads for each of the 256 CUs, two of 512 or 1024, or what the rows fill.
+// Workgroups of the backward, each with a part of the gain's gradient: what the
+// kernels' registers let run at a time, or what the rows fill.  Up to 256 pieces a
+// wave has a row of its own and nothing waits at a barrier (32768 x 2048 bf16: 106
+// us, 112 with a workgroup to a row; x 1601: 110, 127).
 int64_t grad_groups(int dt, int64_t N, int64_t d) {
-  const int64_t n = pieces_of(dt, d), most = n <= 512 ? 1024 : 512;
-  const int64_t groups = ceil_div(N, n <= 128 ? 4 : 1);
+  const int64_t n = pieces_of(dt, d);
+  const int64_t most = n <= 128 || (n > 256 && n <= 512) ? 1024 : 512;
+  const int64_t groups = ceil_div(N, n <= 256 ? 4 : 1);
   return groups < most ? groups : most;
 }
 
@@ -501,7 +504,7 @@ hipError_t launch_grad_t(int dt, const NormGradArgs &a, hipStream_t s) {
   else if (n <= 128)
     rmsnorm_grad_kernel<T, 64, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 256)
-    rmsnorm_grad_kernel<T, 256, 1, 256, WHOLE><<<g, 256, 0, s>>>(a);
+    rmsnorm_grad_kernel<T, 64, 4, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 512)
     rmsnorm_grad_kernel<T, 256, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 1024)
