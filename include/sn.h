@@ -459,6 +459,10 @@ int32_t sn_adamw_step(void *W, int64_t ldw, const void *G, int64_t ldg, int32_t 
 /* Largest number of alternatives a call reports for a row. */
 #define SN_MAX_TOP 64
 
+/* Workspace bytes of sn_token_logprobs (0: none needed, or invalid arguments).
+ * Few long rows are worked on in parts, whose results lie there. */
+size_t sn_token_logprobs_workspace_bytes(int64_t N, int64_t V, int32_t dt, int32_t n_top);
+
 /* sn_token_logprobs
  *
  *   Z         N x V logits (dt), row stride ldz >= V
@@ -472,12 +476,15 @@ int32_t sn_adamw_step(void *W, int64_t ldw, const void *G, int64_t ldg, int32_t 
  *   top_logp, top_id   N x n_top (contiguous, float and int32; unused when
  *             n_top == 0): the largest logits' log p and ids, in descending
  *             order, the lower id first among equals
- * Outputs may not overlap Z, tok or each other.  Errors: NULL, SHAPE, DTYPE,
- * ALIGN, ALIAS, UNSUPPORTED (n_top > SN_MAX_TOP), HIP. */
+ *   workspace sn_token_logprobs_workspace_bytes(N, V, dt, n_top) bytes, 256-byte
+ *             aligned; may be NULL where that is 0
+ * Outputs and workspace may not overlap Z, tok or each other.  Errors: NULL,
+ * SHAPE, DTYPE, ALIGN, ALIAS, WORKSPACE, UNSUPPORTED (n_top > SN_MAX_TOP), HIP. */
 int32_t sn_token_logprobs(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
                           double scale, const int32_t *tok, float *logp, float *entropy,
                           float *stats, int32_t n_top, float *top_logp, int32_t *top_id,
-                          int32_t *err_flag, sn_stream stream);
+                          int32_t *err_flag, void *workspace, size_t workspace_bytes,
+                          sn_stream stream);
 
 /* sn_token_logprobs_backward: for given gradients gl of logp and gh of the
  * entropy,  dZ_j = c (gl (d_jt - p_j) - gh p_j (log p_j + H)).

@@ -106,8 +106,9 @@ _SIGNATURES = {
     "sn_adamw_step": (_I32, [_P, _I64, _P, _I64, _I32, _P, _P, _I64, _I64, _I64, _I64,
                              ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                              ctypes.c_double, _I32, _P, _SZ, _P]),
+    "sn_token_logprobs_workspace_bytes": (_SZ, [_I64, _I64, _I32, _I32]),
     "sn_token_logprobs": (_I32, [_P, _I64, _I64, _I64, _I32, _F64, _P, _P, _P, _P, _I32, _P, _P,
-                                 _P, _P]),
+                                 _P, _P, _SZ, _P]),
     "sn_token_logprobs_backward": (_I32, [_P, _I64, _I64, _I64, _I32, _F64, _P, _P, _P, _P, _P, _P,
                                           _I64, _P, _P]),
     "sn_token_loss": (_I32, [_P, _I64, _I64, _I64, _I32, _F64, _P, _P, _P, _P, _I64, _P, _P]),
@@ -788,19 +789,28 @@ def _tokens(tok, name, n):
     return _ids(tok, name, n)
 
 
+def sn_token_logprobs_workspace_bytes(N: int, V: int, dt: int, n_top: int) -> int:
+    return lib().sn_token_logprobs_workspace_bytes(N, V, dt, n_top)
+
+
 def sn_token_logprobs(Z: torch.Tensor, tok=None, n_top: int = 0, scale: float = 1.0,
-                      err_flag=None, stream=None) -> TokenLogprobs:
+                      err_flag=None, workspace=None, stream=None) -> TokenLogprobs:
     """Log probabilities of the tokens tok (-1: none in this row) under the logits
     Z (N x V) times scale, each row's entropy, and its n_top largest logits."""
     native = _native()
     if native is not None:
-        r = native.token_logprobs(Z, tok, n_top, scale, err_flag, stream)
+        r = native.token_logprobs(Z, tok, n_top, scale, err_flag, workspace, stream)
         if r is not None:
             return TokenLogprobs(*r)
     zp, N, V, ldz = _mat(Z, "Z")
     dt, n_top = _dt(Z), int(n_top)
     tok_ptr = _ids(tok, "tok", N)
-    with _on(stream, Z, tok, err_flag):
+    need = sn_token_logprobs_workspace_bytes(N, V, dt, n_top)
+    with _on(stream, Z, tok, err_flag, workspace):
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=Z.device)
+        ws, have = _workspace(workspace, need)
+
         def new(*shape, dtype=torch.float32):
             return torch.empty(shape, dtype=dtype, device=Z.device)
         logp = None if tok is None else new(N)
@@ -811,7 +821,7 @@ def sn_token_logprobs(Z: torch.Tensor, tok=None, n_top: int = 0, scale: float = 
         flag, own = _id_flag(err_flag, Z.device)
         _check(lib().sn_token_logprobs(zp, N, V, ldz, dt, float(scale), tok_ptr, _ptr(logp),
                                        entropy.data_ptr(), stats.data_ptr(), n_top, _ptr(top_logp),
-                                       _ptr(top_id), _ptr(flag), _stream(stream)))
+                                       _ptr(top_id), _ptr(flag), ws, have, _stream(stream)))
         _id_check(own, err_flag, "sn_token_logprobs")
     return TokenLogprobs(logp, entropy, stats, top_logp, top_id)
 

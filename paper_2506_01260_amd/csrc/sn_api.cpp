@@ -919,10 +919,18 @@ int32_t check_clip_alias(const std::vector<sn::ClipTensor> &t) {
 
 extern "C" {
 
+size_t sn_token_logprobs_workspace_bytes(int64_t N, int64_t V, int32_t dt, int32_t n_top) {
+  if (!dtype_ok(dt) || N < 1 || N >= kMaxDim || V < 1 || V >= kMaxDim || n_top < 0 || n_top > V ||
+      n_top > SN_MAX_TOP)
+    return 0;
+  return sn::logprobs_workspace_bytes(dt, N, V, n_top);
+}
+
 int32_t sn_token_logprobs(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
                           double scale, const int32_t *tok, float *logp, float *entropy,
                           float *stats, int32_t n_top, float *top_logp, int32_t *top_id,
-                          int32_t *err_flag, sn_stream stream) {
+                          int32_t *err_flag, void *workspace, size_t workspace_bytes,
+                          sn_stream stream) {
   int32_t st = check_logits(Z, N, V, ldz, dt, scale, tok);
   if (st) return st;
   if (n_top < 0 || n_top > V) return fail(SN_ERR_SHAPE, "need 0 <= n_top <= V");
@@ -945,11 +953,16 @@ int32_t sn_token_logprobs(const void *Z, int64_t N, int64_t V, int64_t ldz, int3
     b.write(span(top_logp, N, n_top, n_top, 4));
     b.write(span(top_id, N, n_top, n_top, 4));
   }
+  const size_t need = sn::logprobs_workspace_bytes(dt, N, V, n_top);
+  if (need) {
+    if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+    b.write(bytes_span(workspace, need));
+  }
   if ((st = b.check("sn_token_logprobs"))) return st;
   const sn::LogprobsArgs a = {Z,       N,     V,     ldz,      static_cast<float>(scale),
                               tok,     tok ? logp : nullptr, entropy, stats,
                               n_top,   top_logp, top_id, err_flag};
-  return hip_status(sn::launch_logprobs(dt, a, static_cast<hipStream_t>(stream)),
+  return hip_status(sn::launch_logprobs(dt, a, workspace, static_cast<hipStream_t>(stream)),
                     "sn_token_logprobs launch");
 }
 

@@ -298,7 +298,8 @@ struct LossArgs {
   int64_t lddz;
   int32_t *err_flag;
 };
-hipError_t launch_logprobs(int dt, const LogprobsArgs &a, hipStream_t s);
+size_t logprobs_workspace_bytes(int dt, int64_t N, int64_t V, int n_top);
+hipError_t launch_logprobs(int dt, const LogprobsArgs &a, void *ws, hipStream_t s);
 hipError_t launch_logprobs_grad(int dt, const LogprobsGradArgs &a, hipStream_t s);
 hipError_t launch_loss(int dt, const LossArgs &a, hipStream_t s);
 

@@ -21,6 +21,16 @@ namespace sn {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxTop = 64;    // SN_MAX_TOP
+constexpr int kMaxParts = 16;  // of a row
+
+// Few long rows in parts: columns of a part, and what the parts leave.
+struct LogprobsParts {
+  int parts;
+  int64_t cols;
+  float *stat;     // (m, s, t) of each part of each row
+  uint64_t *keys;  // n_top of each
+};
 // Below any difference whose exponential is not 0, and far from overflow: a
 // forbidden logit's difference (-inf) is taken as this where it is multiplied by
 // its exponential 0.
@@ -179,6 +189,15 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t k) {
   return k;
 }
 
+// What top_row starts from; a barrier has to follow (join has one, but for a wave).
+template <typename T, int NT>
+__device__ __forceinline__ void init_top(TopLds<NT> &lds, const Running &r, int64_t V) {
+  // 0, below every logit's, for a thread without a piece
+  lds.best[threadIdx.x] = static_cast<int64_t>(threadIdx.x) * Piece<T>::E < V ? ordered(r.best) : 0;
+  if (threadIdx.x == 0) lds.sels = lds.cands = 0;
+  if constexpr (NT == 64) __syncthreads();
+}
+
 // The n largest logits of a row, by the threads that scanned it: put(rank, key)
 // is called once for each rank below n.  A logit below the n-th largest of the
 // threads' maxima has n others above it, so only the pieces of threads whose
@@ -245,6 +264,34 @@ __device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<N
 
 // ---- kernels ---------------------------------------------------------------------
 
+// A row's outputs from its joined statistics: L = -inf where nothing is allowed, NaN
+// where a logit is NaN or +inf.
+template <typename T>
+__device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t i, const T *row,
+                                          const Running &r) {
+  if (threadIdx.x != 0) return;
+  const float L = logf(r.s);
+  if (a.logp) {
+    const int32_t tok = a.tok[i];
+    float lp = 0.0f;
+    if (tok != -1) {
+      const float z = to_f32(row[clamp_id(tok, a.V, a.err_flag, 1)]);
+      lp = r.s > 0.0f ? fmaf(z - r.m, a.scale, -L) : L;
+    }
+    a.logp[i] = lp;
+  }
+  a.entropy[i] = r.s == 0.0f ? 0.0f : L - a.scale * r.t / r.s;
+  a.stats[2 * i] = r.s > 0.0f ? r.m : L;
+  a.stats[2 * i + 1] = L;
+}
+__device__ __forceinline__ void write_top(const LogprobsArgs &a, int64_t i, const Running &r,
+                                          int rank, uint64_t k) {
+  const float L = logf(r.s);
+  const int64_t o = i * a.n_top + rank;
+  a.top_logp[o] = r.s > 0.0f ? fmaf(key_value(k) - r.m, a.scale, -L) : L;
+  a.top_id[o] = r.s == r.s ? static_cast<int32_t>(key_index(k)) : -1;
+}
+
 template <typename T, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobsArgs a) {
   constexpr int W = NT / 64;
@@ -255,40 +302,87 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobsArgs a) {
   if (i >= a.N) return;
   const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
   Running r = scan_row<T, NT, true>(row, a.V, c2);
+  if constexpr (TOP) init_top<T, NT>(lds, r, a.V);
+  r = join<W, true>(r, red, c2);
+  write_row(a, i, row, r);
   if constexpr (TOP) {
-    // 0, below every logit's, for a thread without a piece
-    lds.best[threadIdx.x] = static_cast<int64_t>(threadIdx.x) * Piece<T>::E < a.V ? ordered(r.best) : 0;
-    if (threadIdx.x == 0) lds.sels = lds.cands = 0;
-    if constexpr (W == 1) __syncthreads();
+    if (r.s == r.s)
+      top_row<T, NT>(row, a.V, a.n_top, lds, [&](int rank, uint64_t k) { write_top(a, i, r, rank, k); });
+    else if (threadIdx.x < a.n_top)
+      write_top(a, i, r, threadIdx.x, 0);
+  }
+}
+
+// Few long rows, in parts: a workgroup for each of `parts` pieces of a row leaves its
+// statistics (3 floats) and its n_top largest keys, in order, in the workspace.
+template <typename T, int NT, bool TOP>
+__global__ __launch_bounds__(NT) void logprobs_part_kernel(LogprobsArgs a, LogprobsParts w) {
+  constexpr int W = NT / 64;
+  __shared__ float red[3 * W];
+  __shared__ TopLds<TOP ? NT : 64> lds;
+  const float c2 = a.scale * kLog2e;
+  const int64_t i = blockIdx.x / w.parts, part = blockIdx.x, c0 = (blockIdx.x % w.parts) * w.cols;
+  const T *row = static_cast<const T *>(a.Z) + i * a.ldz + c0;
+  const int64_t V = a.V - c0 < w.cols ? a.V - c0 : w.cols;
+  Running r = scan_row<T, NT, true>(row, V, c2);
+  if constexpr (TOP) {
+    init_top<T, NT>(lds, r, V);
+    for (int j = threadIdx.x; j < a.n_top; j += NT) w.keys[part * a.n_top + j] = 0;
   }
   r = join<W, true>(r, red, c2);
-  const float m = r.m, s = r.s, t = r.t;
-  const float L = logf(s);  // -inf: nothing is allowed; NaN: a logit is NaN or +inf
   if (threadIdx.x == 0) {
-    if (a.logp) {
-      const int32_t tok = a.tok[i];
-      float lp = 0.0f;
-      if (tok != -1) {
-        const float z = to_f32(row[clamp_id(tok, a.V, a.err_flag, 1)]);
-        lp = s > 0.0f ? fmaf(z - m, a.scale, -L) : L;
-      }
-      a.logp[i] = lp;
-    }
-    a.entropy[i] = s == 0.0f ? 0.0f : L - a.scale * t / s;
-    a.stats[2 * i] = s > 0.0f ? m : L;
-    a.stats[2 * i + 1] = L;
+    w.stat[3 * part] = r.m;
+    w.stat[3 * part + 1] = r.s;
+    w.stat[3 * part + 2] = r.t;
   }
   if constexpr (TOP) {
-    const int64_t o = i * a.n_top;
-    if (s == s) {
-      top_row<T, NT>(row, a.V, a.n_top, lds, [&](int rank, uint64_t k) {
-        a.top_logp[o + rank] = s > 0.0f ? fmaf(key_value(k) - m, a.scale, -L) : L;
-        a.top_id[o + rank] = static_cast<int32_t>(key_index(k));
+    if (r.s == r.s)
+      top_row<T, NT>(row, V, a.n_top, lds, [&](int rank, uint64_t k) {
+        w.keys[part * a.n_top + rank] = k - static_cast<uint64_t>(c0);  // the row's own index
       });
-    } else if (threadIdx.x < a.n_top) {
-      a.top_logp[o + threadIdx.x] = s;
-      a.top_id[o + threadIdx.x] = -1;
+  }
+}
+
+// The parts of a row joined: a key's rank is the number of keys above it.
+template <typename T>
+__global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a, LogprobsParts w) {
+  __shared__ uint64_t keys[kMaxParts * kMaxTop];
+  const int64_t i = blockIdx.x;
+  const int lane = threadIdx.x & 63, all = w.parts * a.n_top;
+  const float c2 = a.scale * kLog2e;
+  Running r;
+  if (lane < w.parts) {
+    const float *stat = w.stat + 3 * (i * w.parts + lane);
+    r.m = stat[0];
+    r.s = stat[1];
+    r.t = stat[2];
+  }
+  r = join<1, true>(r, nullptr, c2);
+  write_row(a, i, static_cast<const T *>(a.Z) + i * a.ldz, r);
+  if (r.s != r.s) {
+    if (threadIdx.x < a.n_top) write_top(a, i, r, threadIdx.x, 0);
+    return;
+  }
+  for (int j = threadIdx.x; j < all; j += 256) keys[j] = w.keys[i * all + j];
+  __syncthreads();
+  for (int j = threadIdx.x; j < all; j += 256) {
+    const uint64_t k = keys[j];
+    int rank = 0;
+    if (all <= 256) {  // every thread compares with the same key at a time
+#pragma unroll 8
+      for (int q = 0; q < all; ++q) rank += keys[q] > k;
+    } else {  // halving in each part's descending list: lo of its keys at least are above
+      for (int q = 0; q < w.parts; ++q) {
+        int lo = 0, hi = a.n_top;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (keys[q * a.n_top + mid] > k) lo = mid + 1;
+          else hi = mid;
+        }
+        rank += lo;
+      }
     }
+    if (k != 0 && rank < a.n_top) write_top(a, i, r, rank, k);
   }
 }
 
@@ -505,7 +599,18 @@ hipError_t launch_logprobs_nt(const LogprobsArgs &a, hipStream_t s) {
 // where they come in four rounds or more of the 2048 that run at a time (16384 x
 // 32000: 190 us, 198 with 512, 269 with 1024; 4999 x 50257: 116, 109, 124).
 template <typename T>
-hipError_t launch_logprobs_t(const LogprobsArgs &a, hipStream_t s) {
+hipError_t launch_logprobs_t(const LogprobsArgs &a, const LogprobsParts &w, hipStream_t s) {
+  if (w.parts > 1) {
+    const unsigned g = static_cast<unsigned>(a.N * w.parts);
+    if (a.n_top)
+      logprobs_part_kernel<T, 1024, true><<<g, 1024, 0, s>>>(a, w);
+    else
+      logprobs_part_kernel<T, 1024, false><<<g, 1024, 0, s>>>(a, w);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    logprobs_join_kernel<T><<<static_cast<unsigned>(a.N), 256, 0, s>>>(a, w);
+    return hipGetLastError();
+  }
   const int64_t pieces = ceil_div(a.V, Piece<T>::E);
   // (a wave's 64 lanes bound up to 16 alternatives well, or any row that fits)
   if (pieces <= 512 && (a.n_top <= 16 || a.V <= kCandidates))
@@ -513,6 +618,23 @@ hipError_t launch_logprobs_t(const LogprobsArgs &a, hipStream_t s) {
   if (pieces > 1024 && (a.n_top == 0 || a.N <= 512)) return launch_logprobs_nt<T, 1024>(a, s);
   if (pieces > 1024 && a.N < 8192) return launch_logprobs_nt<T, 512>(a, s);
   return launch_logprobs_nt<T, 256>(a, s);
+}
+
+// The parts of a row: of 1024 pieces or more (one for each thread), as many as give
+// each CU two workgroups of 1024.  One CU alone takes 11 us for the 128256
+// exponentials of a row and 13.6 with five alternatives, which pays for a second
+// launch from about 8192 pieces on, and up to 64 rows.
+LogprobsParts parts_of(int dt, int64_t N, int64_t V) {
+  const int64_t E = dt == 0 ? 4 : 8, pieces = ceil_div(V, E);
+  LogprobsParts w = {};
+  w.parts = 1;
+  w.cols = V;
+  if (N <= 0 || N > 64 || pieces <= 8192) return w;
+  int64_t parts = 512 / N < kMaxParts ? 512 / N : kMaxParts;
+  parts = parts < pieces / 1024 ? parts : pieces / 1024;
+  w.cols = ceil_div(pieces, parts) * E;
+  w.parts = static_cast<int>(ceil_div(V, w.cols));
+  return w;
 }
 
 template <typename T>
@@ -524,8 +646,19 @@ hipError_t launch_grad_t(const LogprobsGradArgs &a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_logprobs(int dt, const LogprobsArgs &a, hipStream_t s) {
-  return dt == 0 ? launch_logprobs_t<float>(a, s) : launch_logprobs_t<bf16_t>(a, s);
+size_t logprobs_workspace_bytes(int dt, int64_t N, int64_t V, int n_top) {
+  const LogprobsParts w = parts_of(dt, N, V);
+  if (w.parts == 1) return 0;
+  const size_t parts = static_cast<size_t>(N) * w.parts;
+  return align256(parts * 3 * sizeof(float)) + align256(parts * n_top * sizeof(uint64_t));
+}
+
+hipError_t launch_logprobs(int dt, const LogprobsArgs &a, void *ws, hipStream_t s) {
+  LogprobsParts w = parts_of(dt, a.N, a.V);
+  w.stat = static_cast<float *>(ws);
+  w.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) +
+                                        align256(a.N * w.parts * 3 * sizeof(float)));
+  return dt == 0 ? launch_logprobs_t<float>(a, w, s) : launch_logprobs_t<bf16_t>(a, w, s);
 }
 
 hipError_t launch_logprobs_grad(int dt, const LogprobsGradArgs &a, hipStream_t s) {

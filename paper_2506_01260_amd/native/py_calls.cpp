@@ -35,7 +35,8 @@ namespace {
   X(sn_project_weights_multi_workspace_bytes) X(sn_grassmann_accumulate)                      \
   X(sn_grassmann_workspace_bytes) X(sn_embed_lowrank_forward) X(sn_embed_lowrank_backward)    \
   X(sn_embed_lowrank_workspace_bytes) X(sn_adamw_step) X(sn_adamw_workspace_bytes)            \
-  X(sn_token_logprobs) X(sn_token_logprobs_backward) X(sn_token_loss) X(sn_rmsnorm)           \
+  X(sn_token_logprobs) X(sn_token_logprobs_workspace_bytes) X(sn_token_logprobs_backward)    \
+  X(sn_token_loss) X(sn_rmsnorm)           \
   X(sn_rmsnorm_quant) X(sn_rmsnorm_backward) X(sn_rmsnorm_backward_workspace_bytes)           \
   X(sn_grad_sumsq) X(sn_grad_sumsq_workspace_bytes) X(sn_grad_clip)
 
@@ -567,6 +568,16 @@ bool output_here(PyObject *o, PyObject *like, at::ScalarType type, int64_t rows,
   return (o == Py_None || here(o)) && output(o, like, type, rows, cols, m, t);
 }
 
+// A workspace of contiguous bytes, or a new one.
+bool workspace_here(PyObject *o, PyObject *like, size_t need, void *&p, size_t &bytes,
+                    at::Tensor &t) {
+  if (o != Py_None) {
+    const at::Tensor *w = here(o);
+    if (!w || w->scalar_type() != at::kByte || !w->is_contiguous()) return false;
+  }
+  return workspace(o, like, need, p, bytes, t);
+}
+
 PyObject *wrap(PyObject *o, at::Tensor &made) {
   return made.defined() ? THPVariable_Wrap(std::move(made)) : given(o);
 }
@@ -596,19 +607,25 @@ bool tokens(PyObject *o, int64_t n, const int32_t *&p) {
 }
 bool flag_here(PyObject *o, int32_t *&p) { return (o == Py_None || here(o)) && flag(o, p); }
 
-// (Z, tok, n_top, scale, err_flag, stream)
+// (Z, tok, n_top, scale, err_flag, workspace, stream)
 SN_FAST(token_logprobs) {
-  return guarded(n, 6, [&](bool &taken) -> PyObject * {
+  return guarded(n, 7, [&](bool &taken) -> PyObject * {
     Mat z;
     const int32_t *tok;
     int32_t *err;
     int64_t top;
     double scale;
     sn_stream s;
-    if (a[5] != Py_None || !mat_here(a[0], z) || !sn_type(z.type) || !tokens(a[1], z.rows, tok) ||
+    if (a[6] != Py_None || !mat_here(a[0], z) || !sn_type(z.type) || !tokens(a[1], z.rows, tok) ||
         !int_of(a[2], top) || top < 0 || top > SN_MAX_TOP || !number(a[3], scale) ||
-        !flag_here(a[4], err) || !stream(a[5], s))
+        !flag_here(a[4], err) || !stream(a[6], s))
       SN_LEAVE;
+    void *ws = nullptr;
+    size_t bytes = 0;
+    at::Tensor wmade;
+    const size_t need = g_lib.sn_token_logprobs_workspace_bytes(z.rows, z.cols, dt_of(z.type),
+                                                                static_cast<int32_t>(top));
+    if (need && !workspace_here(a[5], a[0], need, ws, bytes, wmade)) SN_LEAVE;
     const int64_t N = z.rows;
     at::Tensor lp, h = make(a[0], at::kFloat, {N}), st = make(a[0], at::kFloat, {N, 2}), tl, ti;
     const bool given_tok = a[1] != Py_None;
@@ -622,7 +639,7 @@ SN_FAST(token_logprobs) {
     int32_t *tip = top ? ti.data_ptr<int32_t>() : nullptr;
     if (failed(launch([&] {
           return g_lib.sn_token_logprobs(z.p, N, z.cols, z.ld, dt_of(z.type), scale, tok, lpp, hp,
-                                         sp, static_cast<int32_t>(top), tlp, tip, err, s);
+                                         sp, static_cast<int32_t>(top), tlp, tip, err, ws, bytes, s);
         })))
       return nullptr;
     return tuple_of({wrap(Py_None, lp), wrap(Py_None, h), wrap(Py_None, st), wrap(Py_None, tl),
@@ -768,11 +785,7 @@ SN_FAST(rmsnorm_backward) {
       SN_LEAVE;
     const int32_t dt = dt_of(h.type);
     const size_t need = gw ? g_lib.sn_rmsnorm_backward_workspace_bytes(h.rows, h.cols, dt) : 0;
-    if (a[7] != Py_None) {
-      const at::Tensor *t = here(a[7]);
-      if (!t || t->scalar_type() != at::kByte || !t->is_contiguous()) SN_LEAVE;
-    }
-    if (need && !workspace(a[7], a[0], need, ws, bytes, wmade)) SN_LEAVE;
+    if (need && !workspace_here(a[7], a[0], need, ws, bytes, wmade)) SN_LEAVE;
     if (!output_here(a[6], a[0], h.type, h.rows, h.cols, out, made)) SN_LEAVE;
     const int32_t st = launch([&] {
       return g_lib.sn_rmsnorm_backward(h.p, h.rows, h.cols, h.ld, dt, dy.p, dy.ld, w, eps, dh.p,
@@ -813,11 +826,7 @@ SN_FAST(grad_sumsq) {
     const int32_t count = static_cast<int32_t>(g.size());
     const size_t need = g_lib.sn_grad_sumsq_workspace_bytes(count, g.data());
     if (need == 0) SN_LEAVE;
-    if (a[2] != Py_None) {
-      const at::Tensor *t = here(a[2]);
-      if (!t || t->scalar_type() != at::kByte || !t->is_contiguous()) SN_LEAVE;
-    }
-    if (!workspace(a[2], like, need, ws, bytes, wmade)) SN_LEAVE;
+    if (!workspace_here(a[2], like, need, ws, bytes, wmade)) SN_LEAVE;
     if (!to) {
       made = make(like, at::kDouble, {1});
       to = made.data_ptr();

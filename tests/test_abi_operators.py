@@ -26,7 +26,7 @@ def _call(name, order, base, over):
     return st
 
 
-LOGPROBS = "Z N V ldz dt scale tok logp entropy stats n_top top_logp top_id err stream"
+LOGPROBS = "Z N V ldz dt scale tok logp entropy stats n_top top_logp top_id err ws ws_bytes stream"
 
 
 @pytest.mark.parametrize("over,code", [
@@ -37,11 +37,25 @@ LOGPROBS = "Z N V ldz dt scale tok logp entropy stats n_top top_logp top_id err 
     (dict(n_top=3), 1), (dict(n_top=3, top_logp=F, top_id=F + 8), 5),
     (dict(scale=0.0), 2), (dict(scale=NAN), 2), (dict(scale=INF), 2), (dict(scale=1e-9), 2),
     (dict(entropy=C), 5), (dict(entropy=A + 100), 5), (dict(stats=B + 8), 5),
+    (dict(V=100000, ldz=100000), 1), (dict(V=100000, ldz=100000, ws=F + 8), 4),
+    (dict(V=100000, ldz=100000, ws=F, ws_bytes=255), 9),
+    (dict(V=100000, ldz=100000, ws=A + 256, ws_bytes=1 << 20), 5),
+    (dict(V=100000, ldz=100000, ws=D, ws_bytes=1 << 20), 5),
     (dict(N=0, Z=None, logp=None, entropy=None, stats=None), 0)])
 def test_logprobs(over, code):
     base = dict(Z=A, N=8, V=100, ldz=100, dt=1, scale=1.0, tok=B, logp=C, entropy=D, stats=E, n_top=0,
-                top_logp=None, top_id=None, err=None, stream=None)
+                top_logp=None, top_id=None, err=None, ws=None, ws_bytes=0, stream=None)
     assert _call("sn_token_logprobs", LOGPROBS, base, over) == code
+
+
+def test_logprobs_workspace():
+    """Few long rows take a workspace, the rest none; invalid arguments give 0."""
+    f = sn.sn_token_logprobs_workspace_bytes
+    assert f(1, 128256, 1, 5) > 0 and f(1, 128256, 1, 64) > f(1, 128256, 1, 5) > f(1, 128256, 1, 0)
+    assert f(100000, 128256, 1, 5) == 0 and f(1, 1000, 1, 5) == 0
+    for bad in ((0, 128256, 1, 5), (1, 0, 1, 0), (1, 128256, 2, 5), (1, 128256, 1, 65), (1, 8, 1, 9),
+                (1, 128256, 1, -1), (1 << 31, 128256, 1, 5), (1, 1 << 31, 1, 5)):
+        assert f(*bad) == 0
 
 
 BACKWARD = "Z N V ldz dt scale tok stats entropy g_logp g_entropy dZ lddz err stream"

@@ -144,6 +144,41 @@ def test_ties_forbidden_and_empty_rows(dtype, v):
         _check_forward(Z, tok, n_top, 1.0, f"top {n_top}")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", [(1, 66000), (3, 70001), (2, 131075), (64, 66001)])
+def test_rows_in_parts(dtype, n, v):
+    """Few long rows: ties, a NaN and forbidden logits across the parts."""
+    log(f"[logprobs parts] {dtype} {n} x {v}")
+    Z = _logits(v, n, v, dtype, 1).clone()
+    Z[0] = torch.round(Z[0] * 0.5)  # ties in every part
+    if n > 1:
+        Z[1, 100:] = -INF           # all but the first part's first forbidden
+    if n > 2:
+        Z[2] = -INF
+    if n > 3:
+        Z[3, v - 1] = float("nan")
+        Z[4, : v - 1] = -INF
+        Z[5] = 0.25
+    if n > 3:  # a few rows of many
+        keep = [0, 1, 2, 3, 4, 5, 6, n - 1]
+        r = sn.sn_token_logprobs(Z, n_top=9)
+        ref = orc.token_logprobs(host(Z[keep]), np.full(len(keep), -1), 9)
+        assert np.array_equal(r.top_id[keep].cpu().numpy(), ref[4])
+        _near(host(r.entropy[keep]), ref[1], 1e-4, "entropy")
+        _near(host(r.stats[keep]), ref[2], 1e-4, "stats")
+        return
+    for n_top in (0, 5, 64):
+        ws = torch.empty(sn.sn_token_logprobs_workspace_bytes(n, v, sn._dt(Z), n_top) + 256,
+                         dtype=torch.uint8, device="cuda")
+        _check_forward(Z, _tokens(v, n, v, 0.0), n_top, 0.9, f"top {n_top}")
+        a = sn.sn_token_logprobs(Z, n_top=n_top, workspace=ws)
+        b = sn.sn_token_logprobs(Z, n_top=n_top)
+        assert all(x is y or torch.equal(x, y) for x, y in zip(a, b))
+    with pytest.raises(sn.SnError) as e:
+        sn.sn_token_logprobs(Z, n_top=5, workspace=ws[:256])
+    assert e.value.status == 9
+
+
 def test_rows_without_a_distribution():
     """NaN or +inf: NaN everywhere and ids of -1; the rows beside it are untouched."""
     log("[logprobs NaN]")
