@@ -70,21 +70,22 @@ template <typename T, int NT, bool ENT>
 __device__ __forceinline__ Running scan_row(const T *row, int64_t V, float c2) {
   constexpr int E = Piece<T>::E, U = 4;
   const int full = static_cast<int>(V / E), tid = threadIdx.x;
+  const bool odd = is_odd(row);
   Running r;
   float z[E];
   int b = 0;
   for (; b + U * NT <= full; b += U * NT) {
-    u32x4 v[U];
+    OddPiece v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_own(row, b + u * NT);
+    for (int u = 0; u < U; ++u) v[u] = fetch_own(row, b + u * NT, full, odd);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      Piece<T>::unpack(v[u], z);
+      Piece<T>::unpack(settle_own<T>(v[u], b + u * NT, full, odd), z);
       r.add<E, ENT>(z, c2);
     }
   }
   for (; b + tid < full; b += NT) {
-    Piece<T>::unpack(load_own(row, b), z);
+    Piece<T>::unpack(settle_own<T>(fetch_own(row, b, full, odd), b, full, odd), z);
     r.add<E, ENT>(z, c2);
   }
   if (b + tid == full && V % E != 0) {  // the row's last, short piece
@@ -498,7 +499,8 @@ __global__ __launch_bounds__(NT, WAVES) void loss_kernel(LossArgs a) {
     t = static_cast<int>(clamp_id(tok, a.V, a.err_flag, 1));
     w = a.weight ? a.weight[i] : 1.0f;
   }
-  u32x4 kept[K];
+  const bool odd = is_odd(row);
+  u32x4 kept[K] = {};
   float z[E], last[E], m = 0.0f, f = 0.0f;
 #pragma unroll
   for (int e = 0; e < E; ++e) last[e] = 0.0f;
@@ -506,28 +508,26 @@ __global__ __launch_bounds__(NT, WAVES) void loss_kernel(LossArgs a) {
     const float zt = to_f32(row[t]);
     Running r;
     for (int b = K * NT; b < full; b += 4 * NT) {
-      u32x4 v[4];
+      OddPiece v[4] = {};
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        v[u] = u32x4{0, 0, 0, 0};
-        if (b + u * NT + tid < full) v[u] = load_own(row, b + u * NT);
-      }
+      for (int u = 0; u < 4; ++u)
+        if (b + u * NT + tid < full) v[u] = fetch_own(row, b + u * NT, full, odd);
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (b + u * NT + tid < full) {
-          Piece<T>::unpack(v[u], z);
+          Piece<T>::unpack(settle_own<T>(v[u], b + u * NT, full, odd), z);
           r.add<E, false>(z, c2);
         }
     }
+    OddPiece raw[K] = {};
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      kept[k] = u32x4{0, 0, 0, 0};
-      if (k * NT + tid < full) kept[k] = load_own(row, k * NT);
-    }
+    for (int k = 0; k < K; ++k)
+      if (k * NT + tid < full) raw[k] = fetch_own(row, k * NT, full, odd);
     if (tail) load_part(row, at(full), a.V, -INFINITY, last);
 #pragma unroll
     for (int k = 0; k < K; ++k)
       if (k * NT + tid < full) {
+        kept[k] = settle_own<T>(raw[k], k * NT, full, odd);
         Piece<T>::unpack(kept[k], z);
         r.add<E, false>(z, c2);
       }
@@ -570,15 +570,13 @@ __global__ __launch_bounds__(NT, WAVES) void loss_kernel(LossArgs a) {
       store_part(out, at(full), a.V, last);
     }
     for (int b = (full - 1) / (4 * NT) * (4 * NT); b >= K * NT; b -= 4 * NT) {
-      u32x4 v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        v[u] = u32x4{0, 0, 0, 0};
-        if (b + u * NT + tid < full) v[u] = load_own(row, b + u * NT);
-      }
+      OddPiece v[4] = {};
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (b + u * NT + tid < full) write(v[u], b + u * NT);
+        if (b + u * NT + tid < full) v[u] = fetch_own(row, b + u * NT, full, odd);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (b + u * NT + tid < full) write(settle_own<T>(v[u], b + u * NT, full, odd), b + u * NT);
     }
   }
 }
@@ -592,12 +590,12 @@ hipError_t launch_logprobs_nt(const LogprobsArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Threads of a row: a wave up to 8 pieces for each lane.  Longer rows take 1024 up
-// to 512 rows (two workgroups for each CU), and always without alternatives, where
-// a workgroup waits for little (8192 x 128256 bf16: 334 us, 353 with 512, 356 with
-// 256).  With alternatives smaller workgroups hide each other's selection, 256
-// where they come in four rounds or more of the 2048 that run at a time (16384 x
-// 32000: 190 us, 198 with 512, 269 with 1024; 4999 x 50257: 116, 109, 124).
+// Threads of a row: a wave up to 8 pieces for each lane; 256 up to 1024 pieces; 1024
+// up to 512 rows (two workgroups for each CU).  Else, without alternatives, 1024 from
+// 7 pieces for each on (8192 x 128256 bf16: 334 us, 353 with 512, 356 with 256), 512
+// below (16384 x 32000: 205, 173, 181).  With alternatives smaller workgroups hide
+// each other's selection: 512, and 256 up to 16 pieces for each (five of 8192 x
+// 50264: 171 with 1024, 146, 152; of 16384 x 32000: 271, 196, 190).
 template <typename T>
 hipError_t launch_logprobs_t(const LogprobsArgs &a, const LogprobsParts &w, hipStream_t s) {
   if (w.parts > 1) {
@@ -615,8 +613,9 @@ hipError_t launch_logprobs_t(const LogprobsArgs &a, const LogprobsParts &w, hipS
   // (a wave's 64 lanes bound up to 16 alternatives well, or any row that fits)
   if (pieces <= 512 && (a.n_top <= 16 || a.V <= kCandidates))
     return launch_logprobs_nt<T, 64>(a, s);
-  if (pieces > 1024 && (a.n_top == 0 || a.N <= 512)) return launch_logprobs_nt<T, 1024>(a, s);
-  if (pieces > 1024 && a.N < 8192) return launch_logprobs_nt<T, 512>(a, s);
+  if (pieces <= 1024) return launch_logprobs_nt<T, 256>(a, s);
+  if (a.N <= 512 || (a.n_top == 0 && pieces >= 7 * 1024)) return launch_logprobs_nt<T, 1024>(a, s);
+  if (a.n_top == 0 || pieces > 16 * 256) return launch_logprobs_nt<T, 512>(a, s);
   return launch_logprobs_nt<T, 256>(a, s);
 }
 

@@ -66,6 +66,55 @@ __device__ __forceinline__ u32x4 load_own(const T *row, int base) {
   const auto b = reinterpret_cast<const char *>(row + static_cast<int64_t>(base) * Piece<T>::E);
   return load_piece<T, NT>(reinterpret_cast<const T *>(b + 16u * threadIdx.x));
 }
+
+// Loads of rows that start at an odd element of 2 bytes.  Off a multiple of 4 bytes
+// the memory pipe takes a third longer (reads of such rows were held to 4.8 TB/s,
+// those at any multiple of 4 reach 5.9), so a piece is loaded from one element before
+// its start, and its last element comes from the next lane's, which loaded it: in
+// two steps, so that all loads are under way before the first is waited for.  The
+// values and their order are those of a plain load.
+struct OddPiece {
+  u32x4 v;
+  uint32_t last;  // the piece's last element, where no lane has it
+};
+template <typename T>
+__device__ __forceinline__ bool is_odd(const T *row) {
+  return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(row) & 2) != 0;
+}
+// Piece base + threadIdx.x < full of a row of at least `full` whole pieces.
+template <typename T>
+__device__ __forceinline__ OddPiece fetch_own(const T *row, int base, int full, bool odd) {
+  OddPiece r;
+  r.last = 0;
+  if constexpr (sizeof(T) == 2) {
+    const T *at = row + static_cast<int64_t>(base) * Piece<T>::E;
+    const int p = base + static_cast<int>(threadIdx.x);
+    const bool early = odd && p > 0;  // never before the row
+    r.v = load_piece(at + (static_cast<int>(threadIdx.x) * Piece<T>::E - (early ? 1 : 0)));
+    if (odd && ((threadIdx.x & 63) == 63 || p + 1 >= full))
+      r.last = at[threadIdx.x * Piece<T>::E + (Piece<T>::E - 1)];
+  } else {
+    r.v = load_own(row, base);
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 settle_own(const OddPiece &r, int base, int full, bool odd) {
+  u32x4 v = r.v;
+  if constexpr (sizeof(T) == 2) {
+    if (odd) {
+      // wave_shl:1, lane i from lane i + 1; a lane without a source keeps `last`
+      const uint32_t next = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+          static_cast<int>(r.last), static_cast<int>(v.x), 0x130, 0xF, 0xF, false));
+      const int p = base + static_cast<int>(threadIdx.x);
+      const uint32_t end = (threadIdx.x & 63) == 63 || p + 1 >= full ? r.last : next;
+      if (p > 0)
+        v = u32x4{__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16),
+                  __builtin_amdgcn_alignbit(v.w, v.z, 16), __builtin_amdgcn_alignbit(end, v.w, 16)};
+    }
+  }
+  return v;
+}
 template <typename T, bool NT = false>
 __device__ __forceinline__ void store_own(T *row, int base, u32x4 v) {
   const auto b = reinterpret_cast<char *>(row + static_cast<int64_t>(base) * Piece<T>::E);
