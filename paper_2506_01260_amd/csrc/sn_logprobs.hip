@@ -148,8 +148,9 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) {
 }
 
 // Candidates a workgroup keeps for a row: little more than n of them reach the
-// bound, but for rows of many equal logits (which take n passes instead).
-constexpr int kCandidates = 256;
+// bound (8 n where a row is sorted), but for rows of many equal logits, which take a
+// pass for each value.
+constexpr int kCandidates = 512;
 
 template <int NT>
 struct TopLds {
@@ -244,22 +245,38 @@ __device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<N
     }
     return;
   }
-  // many equal logits: the next largest by a pass over the row each
+  // many equal logits: a pass over the row for the next value, then its logits in
+  // order of their index until there are n
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint64_t last = ~0ull;
-  for (int r = 0; r < n; ++r) {
+  for (int r = 0; r < n;) {
     uint64_t k = 0;
     for (int64_t c = threadIdx.x; c < V; c += NT) {
       const uint64_t o = order_key(to_f32(row[c]), static_cast<uint32_t>(c));
       k = o < last && o > k ? o : k;
     }
     k = wave_max(k);
-    __syncthreads();  // the candidates before have been read
-    if ((threadIdx.x & 63) == 0) lds.cand[threadIdx.x >> 6] = k;
+    __syncthreads();  // the LDS has been read
+    if (lane == 0) lds.cand[wave] = k;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) k = lds.cand[i] > k ? lds.cand[i] : k;
-    if (threadIdx.x == 0) put(r, k);
-    last = k;
+    const uint32_t value = static_cast<uint32_t>(k >> 32);
+    for (int64_t c = key_index(k) / NT * NT + threadIdx.x; r < n && c - threadIdx.x < V; c += NT) {
+      const bool hit = c < V && ordered(to_f32(row[c])) == value;
+      const uint64_t hits = __ballot(hit);
+      __syncthreads();
+      if (lane == 0) lds.best[wave] = __popcll(hits);
+      __syncthreads();
+      int rank = r + __popcll(hits & ((1ull << lane) - 1));
+#pragma unroll
+      for (int i = 0; i < NT / 64; ++i) {
+        rank += i < wave ? lds.best[i] : 0;
+        r += lds.best[i];
+      }
+      if (hit && rank < n) put(rank, order_key(key_value(k), static_cast<uint32_t>(c)));
+    }
+    last = static_cast<uint64_t>(value) << 32;
   }
 }
 
