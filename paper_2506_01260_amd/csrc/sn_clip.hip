@@ -8,6 +8,10 @@
 // and are cut into units of about the same size, one workgroup each: many small
 // tensors cost one launch.  Squares are summed in float64 (no square of a float
 // overflows it), a unit's threads in a tree, then the units in a fixed order.
+//
+// Measured: 1.1e9 bf16 gradients, norm 360 us (6.1 TB/s read) and scaling into other
+// tensors 770 us (5.7 TB/s read and written); 38 tensors of 4.5e6 floats in all, both
+// calls 17.7 us, 16 of them three launches.
 #include "sn_internal.h"
 #include "sn_rows.h"
 
@@ -20,9 +24,9 @@ constexpr int kNT = 256;
 constexpr int kSumBatch = 8, kClipBatch = 4;
 
 // Elements of a unit: 2048 (a piece or two for each thread) below 2^23 elements, to
-// fill the chip.  Above, the norm's units are no more than one workgroup adds up
-// quickly (2^15 to 2^31 elements), and a clipping unit is one batch: at 1.1e9 bf16
-// gradients 774 us, 792 with twice as many elements and 810 with eight times.
+// fill the chip.  Above, the norm's units are few enough for one workgroup to add up
+// quickly (5 us for the 16900 of 1.1e9 gradients), and a clipping unit is one batch:
+// 774 us there, 792 with twice as many elements and 810 with eight times.
 int64_t sum_unit(int64_t total) {
   return total < (int64_t(1) << 23) ? 2048 : total < (int64_t(1) << 27) ? 16384 : 65536;
 }

@@ -6,11 +6,16 @@
 //   dz_j = c (gl (d_jt - p_j) - gh p_j (log p_j + H)),
 // and, for a weighted loss whose weights are known beforehand, both in one call.
 //
-// Memory-bound: a logit costs about a dozen vector instructions (its exponential
-// four of them), less than the time of its bytes.  One workgroup per row, each
-// thread with a running maximum and sums of its own that are rescaled where the
-// maximum grows: one pass over the row, joined over the threads at its end.
-// All sums are float32 over at most V / 64 terms each, then in a tree.
+// Memory-bound, with the vector ALU close behind: a logit costs 8 instructions and an
+// exponential in the forward call, 18 with two exponentials in the loss.  One
+// workgroup per row, each thread with a running maximum and sums of its own that are
+// rescaled where the maximum grows: one pass over the row, joined over the threads at
+// its end.  All sums are float32 over at most V / 64 terms each, then in a tree.
+//
+// Measured: 8192 x 128256 bf16 334 us (6.3 TB/s, what reads alone reach on this
+// card); 4999 x 50257 with eight alternatives 95 us (5.3); one row of 128256 11 us.
+// Backward of 8192 x 32000 float32 355 us (5.9 TB/s read and written), loss of
+// 32768 x 32000 bf16 710-750 us (5.6-5.9).
 #include <cfloat>
 
 #include "sn_internal.h"
