@@ -526,6 +526,8 @@ int32_t sn_token_loss(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t 
 /*   h = x + r,   y = h w / sqrt(mean_j h_j^2 + eps)                          */
 /* over rows of d columns, in float32; h is rounded to dt where it is stored, */
 /* and y is made from the sum before that rounding.                           */
+/* Squares are float32: a row of root mean square past 2^63 counts as         */
+/* infinite (y = 0), one below 2^-74 as zero beside eps.                      */
 /* ------------------------------------------------------------------------ */
 
 /* sn_rmsnorm

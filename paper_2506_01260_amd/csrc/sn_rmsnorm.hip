@@ -4,7 +4,9 @@
 // 8-bit form writes q = y / s in e4m3 (largest value 448) with one float32 scale
 // s = max |y| / 448 for a row or for each 128 columns of it.  Backward, from the
 // stored h, u = dy w and rho = 1 / sqrt(mean h^2 + eps):
-//   dx = rho u - h rho^3 mean(u h) + dh,    gw += sum over rows of dy h rho.
+//   dx = rho u - h rho^3 mean(u h) + dh,    gw += sum over rows of dy h rho,
+// computed as rho (u - n (rho mean(u h))) + dh with n = h rho: rho^3 leaves
+// float32's range where rows are of 2^-43 or 2^50.
 //
 // Memory-bound: each operand passes once, the row staying in registers between
 // its sums and its outputs.  R threads hold a row in K pieces each; with R = 64
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
     ss = group_sum<W>(ss, red[0]);
     uh = group_sum<W>(uh, red[1]);
     const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
-    const float f = rho * rho * rho * (uh * a.inv_d);
+    const float f = uh * a.inv_d * rho;
     T *dX = static_cast<T *>(a.dX) + i * a.lddx;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -348,8 +350,9 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
       if (w) Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        gw[k][e] = fmaf(y[e] * h[e], rho, gw[k][e]);
-        o[e] += fmaf(y[e] * g[e], rho, -h[e] * f);
+        const float n = h[e] * rho;
+        gw[k][e] = fmaf(y[e], n, gw[k][e]);
+        o[e] = fmaf(rho, fmaf(-n, f, y[e] * g[e]), o[e]);
       }
       put<T, WHOLE>(dX, c0, d, o);
     }
@@ -408,7 +411,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
     ss = group_sum<W>(ss, red[0]);
     uh = group_sum<W>(uh, red[1]);
     const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
-    const float f = rho * rho * rho * (uh * a.inv_d);
+    const float f = uh * a.inv_d * rho;
     float *part = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
     for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
       float o[E] = {};
@@ -418,9 +421,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_long_kernel(NormGradArgs a)
       if (w) get(w, c0, a.d, g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
+        const float n = h[e] * rho;
         if (part && c0 + e < a.d)
-          part[c0 + e] = fmaf(u[e] * h[e], rho, i == blockIdx.x ? 0.0f : part[c0 + e]);
-        o[e] += fmaf(w ? u[e] * g[e] : u[e], rho, -h[e] * f);
+          part[c0 + e] = fmaf(u[e], n, i == blockIdx.x ? 0.0f : part[c0 + e]);
+        o[e] = fmaf(rho, fmaf(-n, f, w ? u[e] * g[e] : u[e]), o[e]);
       }
       put(static_cast<T *>(a.dX) + i * a.lddx, c0, a.d, o);
     }

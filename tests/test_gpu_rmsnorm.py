@@ -159,6 +159,24 @@ def _check_backward(dX, gw, start, H, dY, w, dH, dtype, what):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("power,eps", [(-60, 0.0), (50, EPS)])
+@pytest.mark.parametrize("d", [3, 130, 1600, 5000, 40000])
+def test_backward_of_tiny_and_huge_rows(dtype, power, eps, d):
+    """rho^3 = 2^180 or 2^-150 is no float32, the gradient is."""
+    log(f"[rmsnorm backward of tiny and huge rows] {dtype} d={d} 2^{power}")
+    H, dY, w = _mat(1, 5, d, dtype) * 2.0 ** power, _mat(2, 5, d, dtype), _gain(3, d, dtype)
+    gw = torch.zeros(d, device="cuda")
+    dX = sn.sn_rmsnorm_backward(H, dY, w, eps=eps, gw=gw)
+    h, dy, u, s = host(H), host(dY), host(dY) * host(w), _s(d)
+    ref, g = orc.rmsnorm_backward(h, dy, host(w), eps=eps)
+    rho = 1 / np.sqrt((h * h).mean(1, keepdims=True) + eps)
+    tol = rho * np.abs(u) * (s / 2 + 12) + \
+        np.abs(h) * rho ** 3 * np.abs(u * h).mean(1, keepdims=True) * (5 * s / 2 + 20)
+    _near(host(dX), ref, U * tol + _own(ref, dtype), "dX")
+    _near(host(gw), g, U * ((s / 2 + 12 + 64) * np.abs(dy * h * rho).sum(0) + np.abs(g)), "gw")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,d", [(3001, 256), (2049, 1000), (1111, 4096)])
 def test_many_rows(dtype, n, d):
     log(f"[rmsnorm many rows] {dtype} {n} x {d}")
