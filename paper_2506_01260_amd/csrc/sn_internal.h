@@ -333,12 +333,14 @@ struct ClipTensor {
   const void *g;
   void *out;
   int64_t rows, cols, ldg, ldo;  // one row where the rows lie without gaps
-  int32_t f32;
+  uint32_t f32 : 1;
+  uint32_t rows_each : 31;  // of a unit: 1 where a row is a unit or more
+  uint32_t per_row;         // units of a row: 1 where rows are short
 };
-constexpr int kClipTensors = 64;
+constexpr int kClipTensors = 64;  // one for each lane of a wave
 struct ClipTable {  // a kernel argument: below 4 KB
   int n = 0;
-  uint32_t unit0[kClipTensors];
+  uint32_t unit0[kClipTensors];  // a tensor's first unit; past the last one no unit's number
   ClipTensor t[kClipTensors];
 };
 static_assert(sizeof(ClipTable) <= 3968, "kernel arguments stay below 4 KB");
