@@ -153,8 +153,8 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) {
 }
 
 // Candidates a workgroup keeps for a row: little more than n of them reach the
-// bound (8 n where a row is sorted), but for rows of many equal logits, which take a
-// pass for each value.
+// bound (8 n where a row is sorted), but for rows of many equal logits, which look
+// twice or, where many lie above the bound too, take a pass for each value.
 constexpr int kCandidates = 512;
 
 template <int NT>
@@ -223,38 +223,73 @@ __device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<N
   if (mine != 0 && mine >= bound) lds.sel[atomicAdd(&lds.sels, 1u)] = threadIdx.x;
   __syncthreads();
   const uint32_t all = lds.sels * each;
-  for (uint32_t q = threadIdx.x; q < all; q += NT) {
-    const uint32_t k = q / each, p = lds.sel[k] + (q - k * each) * NT;
-    if (p >= pieces) continue;
-    const int64_t c0 = static_cast<int64_t>(p) * E;
-    float z[E];
-    if (c0 + E <= V)
-      Piece<T>::unpack(load_piece(row + c0), z);
-    else
-      load_part(row, c0, V, -INFINITY, z);
+  // the candidates from `least` on, and their number: in all threads
+  const auto look = [&](uint32_t least) {
+    for (uint32_t q = threadIdx.x; q < all; q += NT) {
+      const uint32_t k = q / each, p = lds.sel[k] + (q - k * each) * NT;
+      if (p >= pieces) continue;
+      const int64_t c0 = static_cast<int64_t>(p) * E;
+      float z[E];
+      if (c0 + E <= V)
+        Piece<T>::unpack(load_piece(row + c0), z);
+      else
+        load_part(row, c0, V, -INFINITY, z);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (c0 + e < V && ordered(z[e]) >= bound) {
-        const uint32_t at = atomicAdd(&lds.cands, 1u);
-        if (at < kCandidates) lds.cand[at] = order_key(z[e], static_cast<uint32_t>(c0 + e));
-      }
-  }
-  __syncthreads();
-  const uint32_t count = lds.cands;
-  if (count <= kCandidates) {
+      for (int e = 0; e < E; ++e)
+        if (c0 + e < V && ordered(z[e]) >= least) {
+          const uint32_t at = atomicAdd(&lds.cands, 1u);
+          if (at < kCandidates) lds.cand[at] = order_key(z[e], static_cast<uint32_t>(c0 + e));
+        }
+    }
+    __syncthreads();
+    return lds.cands;
+  };
+  const auto rank_all = [&](uint32_t count) {
     for (uint32_t i = threadIdx.x; i < count; i += NT) {
       const uint64_t k = lds.cand[i];
       int rank = 0;
       for (uint32_t j = 0; j < count; ++j) rank += lds.cand[j] > k;
       if (rank < n) put(rank, k);
     }
-    return;
-  }
-  // many equal logits: a pass over the row for the next value, then its logits in
-  // order of their index until there are n
+  };
+  uint32_t count = look(bound);
+  if (count <= kCandidates) return rank_all(count);
+
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // the logits of one value (ordered() >> low) from index `from` on, in order of their
+  // index, until there are n
+  int r = 0;
+  const auto fill = [&](uint32_t value, int low, int64_t from) {
+    for (int64_t c = from / NT * NT + threadIdx.x; r < n && c - threadIdx.x < V; c += NT) {
+      const float z = c < V ? to_f32(row[c]) : 0.0f;
+      const bool hit = c < V && ordered(z) >> low == value;
+      const uint64_t hits = __ballot(hit);
+      __syncthreads();  // the LDS has been read
+      if (lane == 0) lds.best[wave] = __popcll(hits);
+      __syncthreads();
+      int rank = r + __popcll(hits & ((1ull << lane) - 1));
+#pragma unroll
+      for (int i = 0; i < NT / 64; ++i) {
+        rank += i < wave ? lds.best[i] : 0;
+        r += lds.best[i];
+      }
+      if (hit && rank < n) put(rank, order_key(z, static_cast<uint32_t>(c)));
+    }
+  };
+  // Many logits equal to the bound, which is -inf where few tokens are allowed: those
+  // above it, then those equal to it.
+  __syncthreads();
+  if (threadIdx.x == 0) lds.cands = 0;
+  __syncthreads();
+  count = look(((bound >> LOW) + 1) << LOW);
+  if (count <= kCandidates) {
+    rank_all(count);
+    r = static_cast<int>(count);
+    return fill(bound >> LOW, LOW, 0);
+  }
+  // many above it too: a pass over the row for the next value, then its logits
   uint64_t last = ~0ull;
-  for (int r = 0; r < n;) {
+  while (r < n) {
     uint64_t k = 0;
     for (int64_t c = threadIdx.x; c < V; c += NT) {
       const uint64_t o = order_key(to_f32(row[c]), static_cast<uint32_t>(c));
@@ -266,22 +301,8 @@ __device__ __forceinline__ void top_row(const T *row, int64_t V, int n, TopLds<N
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) k = lds.cand[i] > k ? lds.cand[i] : k;
-    const uint32_t value = static_cast<uint32_t>(k >> 32);
-    for (int64_t c = key_index(k) / NT * NT + threadIdx.x; r < n && c - threadIdx.x < V; c += NT) {
-      const bool hit = c < V && ordered(to_f32(row[c])) == value;
-      const uint64_t hits = __ballot(hit);
-      __syncthreads();
-      if (lane == 0) lds.best[wave] = __popcll(hits);
-      __syncthreads();
-      int rank = r + __popcll(hits & ((1ull << lane) - 1));
-#pragma unroll
-      for (int i = 0; i < NT / 64; ++i) {
-        rank += i < wave ? lds.best[i] : 0;
-        r += lds.best[i];
-      }
-      if (hit && rank < n) put(rank, order_key(key_value(k), static_cast<uint32_t>(c)));
-    }
-    last = static_cast<uint64_t>(value) << 32;
+    fill(static_cast<uint32_t>(k >> 32), 0, key_index(k));
+    last = k >> 32 << 32;
   }
 }
 
@@ -366,13 +387,23 @@ __global__ __launch_bounds__(NT) void logprobs_part_kernel(LogprobsArgs a, Logpr
   }
 }
 
-// The parts of a row joined: a key's rank is the number of keys above it.
+// The parts of a row joined: a key's rank is the number of keys above it (128256 bf16
+// logits with 20 alternatives: 13 us, 20 by halving in the parts' lists).
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a, LogprobsParts w) {
   __shared__ uint64_t keys[kMaxParts * kMaxTop];
+  __shared__ uint32_t kept;
   const int64_t i = blockIdx.x;
   const int lane = threadIdx.x & 63, all = w.parts * a.n_top;
   const float c2 = a.scale * kLog2e;
+  // Each part's list descends, so that the least of the parts' m-th keys, m parts >= n,
+  // has n keys at or above it: the others need no rank.
+  const uint64_t *all_keys = w.keys + i * all;
+  const int m = (a.n_top + w.parts - 1) / w.parts;
+  uint64_t mine = ~0ull, first = 0;
+  if (a.n_top && lane < w.parts) mine = all_keys[lane * a.n_top + m - 1];
+  if (threadIdx.x < all) first = all_keys[threadIdx.x];
+  if (threadIdx.x == 0) kept = 0;
   Running r;
   if (lane < w.parts) {
     const float *stat = w.stat + 3 * (i * w.parts + lane);
@@ -386,26 +417,20 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a, Logp
     if (threadIdx.x < a.n_top) write_top(a, i, r, threadIdx.x, 0);
     return;
   }
-  for (int j = threadIdx.x; j < all; j += 256) keys[j] = w.keys[i * all + j];
+  const uint64_t least = ~wave_max(~mine);
   __syncthreads();
   for (int j = threadIdx.x; j < all; j += 256) {
+    const uint64_t k = j < 256 ? first : all_keys[j];
+    if (k >= least && k != 0) keys[atomicAdd(&kept, 1u)] = k;
+  }
+  __syncthreads();
+  const int count = static_cast<int>(kept);
+  for (int j = threadIdx.x; j < count; j += 256) {
     const uint64_t k = keys[j];
     int rank = 0;
-    if (all <= 256) {  // every thread compares with the same key at a time
 #pragma unroll 8
-      for (int q = 0; q < all; ++q) rank += keys[q] > k;
-    } else {  // halving in each part's descending list: lo of its keys at least are above
-      for (int q = 0; q < w.parts; ++q) {
-        int lo = 0, hi = a.n_top;
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (keys[q * a.n_top + mid] > k) lo = mid + 1;
-          else hi = mid;
-        }
-        rank += lo;
-      }
-    }
-    if (k != 0 && rank < a.n_top) write_top(a, i, r, rank, k);
+    for (int q = 0; q < count; ++q) rank += keys[q] > k;
+    if (rank < a.n_top) write_top(a, i, r, rank, k);
   }
 }
 
@@ -632,8 +657,10 @@ hipError_t launch_logprobs_t(const LogprobsArgs &a, const LogprobsParts &w, hipS
     return hipGetLastError();
   }
   const int64_t pieces = ceil_div(a.V, Piece<T>::E);
-  // (a wave's 64 lanes bound up to 16 alternatives well, or any row that fits)
-  if (pieces <= 512 && (a.n_top <= 16 || a.V <= kCandidates))
+  // (a wave's 64 lanes bound up to 32 alternatives well, or any row that fits: of
+  // 32768 x 1024 bf16 the first 20 take 31 us, 86 with 256 threads to a row; of 64 the
+  // bound is often so low that the candidates overflow)
+  if (pieces <= 512 && (a.n_top <= 32 || a.V <= kCandidates))
     return launch_logprobs_nt<T, 64>(a, s);
   if (pieces <= 1024) return launch_logprobs_nt<T, 256>(a, s);
   if (a.N <= 512 || (a.n_top == 0 && pieces >= 7 * 1024)) return launch_logprobs_nt<T, 1024>(a, s);

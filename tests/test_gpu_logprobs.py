@@ -145,6 +145,29 @@ def test_ties_forbidden_and_empty_rows(dtype, v):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [513, 1024, 2050, 4000, 9001, 32000, 70001])
+def test_few_allowed_and_few_values(dtype, v):
+    """Fewer allowed tokens than alternatives, in one run or far apart; logits of few
+    values, so that many equal the last alternative; many large ones in one place."""
+    log(f"[logprobs few allowed] {dtype} V={v}")
+    Z = _logits(v, 10, v, dtype).clone()
+    for i, allowed in enumerate((range(0, 3), range(v // 2, v // 2 + 20), range(v - 30, v),
+                                 range(7, v, v // 15), range(0, v, v // 300))):
+        keep = Z[i, list(allowed)].clone()
+        Z[i] = -INF
+        Z[i, list(allowed)] = keep
+    Z[5] = (Z[5] > 0).to(Z.dtype)
+    Z[6] = torch.clamp(torch.round(Z[6]), -20, 3)
+    Z[7] = -1.0
+    Z[7, 5::v // 9] = torch.arange(len(range(5, v, v // 9))).to(Z) % 4
+    Z[8, : min(v, 700)] += 100.0
+    Z[9] = -300.0 - Z[9].abs()
+    Z[9, v // 3:] = -300.0
+    for n_top in (1, 17, 32, 33, 64):
+        _check_forward(Z, _tokens(v, 10, v), n_top, 1.0, f"top {n_top}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,v", [(1, 66000), (3, 70001), (2, 131075), (64, 66001)])
 def test_rows_in_parts(dtype, n, v):
     """Few long rows: ties, a NaN and forbidden logits across the parts."""
