@@ -449,18 +449,19 @@ struct RowGrad {
   }
 };
 
-// A unit is kGradPieces pieces of each of 256 threads in one row.
+// A unit is kGradPieces pieces of each of NT threads in one row.
 constexpr int kGradPieces = 4;
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, int64_t per_row,
-                                                            int64_t units) {
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void logprobs_grad_kernel(LogprobsGradArgs a, int64_t per_row,
+                                                           int64_t units) {
   constexpr int E = Piece<T>::E, U = kGradPieces;
+  constexpr bool ODD = sizeof(T) == 2 && NT < 256;
   const int full = static_cast<int>(a.V / E);
   const int64_t unit = group_number();
   if (unit >= units) return;
   const int64_t i = unit / per_row;
-  const int base = static_cast<int>(unit - i * per_row) * (256 * U), first = base + threadIdx.x;
+  const int base = static_cast<int>(unit - i * per_row) * (NT * U), first = base + threadIdx.x;
   const T *row = static_cast<const T *>(a.Z) + i * a.ldz;
   T *out = static_cast<T *>(a.dZ) + i * a.lddz;
   const int32_t tok = a.tok ? a.tok[i] : -1;
@@ -482,31 +483,34 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
     if (g.L != g.L) g.gl = g.L;
   }
   const int tp = t < 0 ? -1 : t / E, te = t - tp * E;  // the given token's piece
-  u32x4 v[U];
+  const bool odd = ODD && is_odd(row);
+  OddPiece v[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    v[u] = u32x4{0, 0, 0, 0};
-    if (!none && first + u * 256 < full)
-      v[u] = load_own<T, true>(row, base + u * 256);
+    v[u] = {u32x4{0, 0, 0, 0}, 0};
+    if (!none && first + u * NT < full) {
+      if constexpr (ODD) v[u] = fetch_own<T, true>(row, base + u * NT, full, odd);
+      else v[u].v = load_own<T, true>(row, base + u * NT);
+    }
   }
   float z[E];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int p = first + u * 256;
+    const int p = first + u * NT;
     if (p >= full) break;
     if (!none) {
-      Piece<T>::unpack(v[u], z);
+      Piece<T>::unpack(ODD ? settle_own<T>(v[u], base + u * NT, full, odd) : v[u].v, z);
       g.apply(z);
       if (p == tp) {
 #pragma unroll
         for (int e = 0; e < E; ++e) z[e] += e == te ? hit : 0.0f;
       }
-      v[u] = Piece<T>::pack(z);
+      v[u].v = Piece<T>::pack(z);
     }
-    store_own<T, true>(out, base + u * 256, v[u]);
+    store_own<T, true>(out, base + u * NT, v[u].v);
   }
   // the row's last, short piece
-  if (a.V % E != 0 && full >= first && full < first + 256 * U && (full - first) % 256 == 0) {
+  if (a.V % E != 0 && full >= first && full < first + NT * U && (full - first) % NT == 0) {
     const int64_t c0 = static_cast<int64_t>(full) * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) z[e] = 0.0f;
@@ -685,11 +689,20 @@ LogprobsParts parts_of(int dt, int64_t N, int64_t V) {
   return w;
 }
 
+template <typename T, int NT>
+hipError_t launch_grad_nt(const LogprobsGradArgs &a, hipStream_t s) {
+  const int64_t per_row = ceil_div(a.V, Piece<T>::E * NT * kGradPieces), units = per_row * a.N;
+  logprobs_grad_kernel<T, NT><<<groups_grid(units), NT, 0, s>>>(a, per_row, units);
+  return hipGetLastError();
+}
+// Short rows are one unit of fewer threads (bf16 25147 x 1024: 20 us, 36 with 256
+// threads, half of them idle; 30000 x 2055: 63, 78).
 template <typename T>
 hipError_t launch_grad_t(const LogprobsGradArgs &a, hipStream_t s) {
-  const int64_t per_row = ceil_div(a.V, Piece<T>::E * 256 * kGradPieces), units = per_row * a.N;
-  logprobs_grad_kernel<T><<<groups_grid(units), 256, 0, s>>>(a, per_row, units);
-  return hipGetLastError();
+  const int64_t pieces = ceil_div(a.V, Piece<T>::E);
+  if (pieces <= 64 * kGradPieces) return launch_grad_nt<T, 64>(a, s);
+  if (pieces <= 128 * kGradPieces) return launch_grad_nt<T, 128>(a, s);
+  return launch_grad_nt<T, 256>(a, s);
 }
 
 }  // namespace

@@ -82,7 +82,7 @@ __device__ __forceinline__ bool is_odd(const T *row) {
   return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(row) & 2) != 0;
 }
 // Piece base + threadIdx.x < full of a row of at least `full` whole pieces.
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ OddPiece fetch_own(const T *row, int base, int full, bool odd) {
   OddPiece r;
   r.last = 0;
@@ -90,11 +90,11 @@ __device__ __forceinline__ OddPiece fetch_own(const T *row, int base, int full, 
     const T *at = row + static_cast<int64_t>(base) * Piece<T>::E;
     const int p = base + static_cast<int>(threadIdx.x);
     const bool early = odd && p > 0;  // never before the row
-    r.v = load_piece(at + (static_cast<int>(threadIdx.x) * Piece<T>::E - (early ? 1 : 0)));
+    r.v = load_piece<T, NT>(at + (static_cast<int>(threadIdx.x) * Piece<T>::E - (early ? 1 : 0)));
     if (odd && ((threadIdx.x & 63) == 63 || p + 1 >= full))
       r.last = at[threadIdx.x * Piece<T>::E + (Piece<T>::E - 1)];
   } else {
-    r.v = load_own(row, base);
+    r.v = load_own<T, NT>(row, base);
   }
   return r;
 }
