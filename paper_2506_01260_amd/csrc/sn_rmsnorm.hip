@@ -456,6 +456,9 @@ __global__ __launch_bounds__(kGainCols *kGainGroups) void gain_kernel(
 // pieces of a row; R * K of them are held by R threads in K pieces each
 int64_t pieces_of(int dt, int64_t d) { return ceil_div(d, dt == 0 ? 4 : 8); }
 
+// Threads and pieces of each: three pieces where two or four would leave a third of
+// the threads idle (8 bits from 20184 x 5632 float32 151 us with 1024 threads, 129
+// with four pieces of 512, 119 with three; backward of 8192 x 12288 bf16 183, 167).
 template <typename T, int OUT, bool WHOLE>
 hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
@@ -470,10 +473,14 @@ hipError_t launch_norm_t(const NormArgs &a, hipStream_t s) {
     rmsnorm_kernel<T, 64, 4, 256, OUT, WHOLE><<<grid(4), 256, 0, s>>>(a);
   else if (n <= 512)
     rmsnorm_kernel<T, 256, 2, 256, OUT, WHOLE><<<grid(1), 256, 0, s>>>(a);
+  else if (n <= 768)
+    rmsnorm_kernel<T, 256, 3, 256, OUT, WHOLE><<<grid(1), 256, 0, s>>>(a);
   else if (n <= 1024)
     rmsnorm_kernel<T, 512, 2, 512, OUT, WHOLE><<<grid(1), 512, 0, s>>>(a);
+  else if (n <= 1536)
+    rmsnorm_kernel<T, 512, 3, 512, OUT, WHOLE><<<grid(1), 512, 0, s>>>(a);
   else if (n <= 2048)
-    rmsnorm_kernel<T, 1024, 2, 1024, OUT, WHOLE><<<grid(1), 1024, 0, s>>>(a);
+    rmsnorm_kernel<T, 512, 4, 512, OUT, WHOLE><<<grid(1), 512, 0, s>>>(a);
   else
     rmsnorm_long_kernel<T, OUT><<<grid(1), 1024, 0, s>>>(a);
   return hipGetLastError();
@@ -494,18 +501,31 @@ hipError_t launch_norm_out(const NormArgs &a, hipStream_t s) {
 // Workgroups of the backward, each with a part of the gain's gradient: what the
 // kernels' registers let run at a time, or what the rows fill.  Up to 256 pieces a
 // wave has a row of its own and nothing waits at a barrier (32768 x 2048 bf16: 106
-// us, 112 with a workgroup to a row; x 1601: 110, 127).
+// us, 112 with a workgroup to a row; x 1601: 110, 127).  Few rows are not worth more
+// parts than two to a CU (1200 x 4096: 18 us with 512, 24 with 1024), many are where
+// registers allow them (16384 x 5120: 145 with 768, 153 with 512).
 int64_t grad_groups(int dt, int64_t N, int64_t d) {
   const int64_t n = pieces_of(dt, d);
-  const int64_t most = n <= 128 || (n > 256 && n <= 512) ? 1024 : 512;
+  int64_t most = 512;
+  if (n <= 128 && N > 8192) most = 1024;
+  if (n > 256 && n <= 512 && N > 4096) most = 1024;
+  if (n > 512 && n <= 768 && N > 4096) most = 768;
   const int64_t groups = ceil_div(N, n <= 256 ? 4 : 1);
   return groups < most ? groups : most;
+}
+// An odd number where every other row starts at an odd bf16 element: those rows take
+// longer, and a workgroup should have as many of them as any other (14096 x 3735: 107
+// us, 122 with an even number).
+int64_t turn_groups(int dt, const NormGradArgs &a) {
+  const int64_t g = grad_groups(dt, a.N, a.d);
+  const bool odd = dt != 0 && ((a.ldh | a.lddy | (a.dH ? a.lddh : 0) | a.lddx) & 1);
+  return odd && pieces_of(dt, a.d) > 256 && a.N >= 8 * g ? g - 1 + g % 2 : g;
 }
 
 template <typename T, bool WHOLE>
 hipError_t launch_grad_t(int dt, const NormGradArgs &a, hipStream_t s) {
   const int64_t n = ceil_div(a.d, Piece<T>::E);
-  const unsigned g = static_cast<unsigned>(grad_groups(dt, a.N, a.d));
+  const unsigned g = static_cast<unsigned>(turn_groups(dt, a));
   if (a.d < Piece<T>::E)
     rmsnorm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
   else if (n <= 64)
@@ -516,8 +536,12 @@ hipError_t launch_grad_t(int dt, const NormGradArgs &a, hipStream_t s) {
     rmsnorm_grad_kernel<T, 64, 4, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 512)
     rmsnorm_grad_kernel<T, 256, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
+  else if (n <= 768)
+    rmsnorm_grad_kernel<T, 256, 3, 256, WHOLE><<<g, 256, 0, s>>>(a);
   else if (n <= 1024)
     rmsnorm_grad_kernel<T, 512, 2, 512, WHOLE><<<g, 512, 0, s>>>(a);
+  else if (n <= 1536)
+    rmsnorm_grad_kernel<T, 512, 3, 512, WHOLE><<<g, 512, 0, s>>>(a);
   else if (n <= 2048)
     rmsnorm_grad_kernel<T, 1024, 2, 1024, WHOLE><<<g, 1024, 0, s>>>(a);
   else
@@ -546,7 +570,7 @@ hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipS
   const hipError_t e = dt == 0 ? launch_grad_d<float>(dt, a, s) : launch_grad_d<bf16_t>(dt, a, s);
   if (e != hipSuccess || !gw) return e;
   gain_kernel<<<static_cast<unsigned>(ceil_div(a.d, kGainCols)), kGainCols * kGainGroups, 0, s>>>(
-      a.part, grad_groups(dt, a.N, a.d), a.d, gw);
+      a.part, turn_groups(dt, a), a.d, gw);
   return hipGetLastError();
 }
 

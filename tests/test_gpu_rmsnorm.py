@@ -193,6 +193,17 @@ def test_many_rows(dtype, n, d):
     assert torch.equal(gw, again)
 
 
+@pytest.mark.parametrize("n,d", [(4096, 2055), (4097, 5003)])
+def test_backward_of_many_odd_rows(n, d):
+    """Rows of bf16 at odd elements, in an odd number of workgroups."""
+    log(f"[rmsnorm backward of odd rows] {n} x {d}")
+    H, dY, dH = (_mat(i, n, d, "bf16") for i in (1, 2, 3))
+    w = _gain(4, d, "bf16")
+    gw = torch.zeros(d, device="cuda")
+    dX = sn.sn_rmsnorm_backward(H, dY, w, dH=dH, eps=EPS, gw=gw)
+    _check_backward(dX, gw, torch.zeros(d), H, dY, w, dH, "bf16", "backward")
+
+
 @pytest.mark.parametrize("d", [130, 1600, 5000, 40000])
 def test_special_rows(d):
     """Zeros, tiny and huge rows, NaN and infinities: rows beside them are untouched."""
