@@ -337,13 +337,28 @@ struct ClipTensor {
   uint32_t rows_each : 31;  // of a unit: 1 where a row is a unit or more
   uint32_t per_row;         // units of a row: 1 where rows are short
 };
-constexpr int kClipTensors = 64;  // one for each lane of a wave
-struct ClipTable {  // a kernel argument: below 4 KB
+// The tensors of a launch: a kernel argument, below 4 KB.  unit0: a tensor's first unit;
+// past the last tensor a number that no unit has.
+struct ClipTable {
+  static constexpr int kTensors = 64;
   int n = 0;
-  uint32_t unit0[kClipTensors];  // a tensor's first unit; past the last one no unit's number
-  ClipTensor t[kClipTensors];
+  uint32_t unit0[kTensors];
+  ClipTensor t[kTensors];
 };
-static_assert(sizeof(ClipTable) <= 3968, "kernel arguments stay below 4 KB");
+// The same where no tensor has gaps.
+struct FlatTable {
+  static constexpr int kTensors = 128;
+  struct Tensor {
+    const void *g;
+    void *out;
+    int64_t size2;  // 2 x elements, + 1 for float32
+  };
+  int n = 0;
+  uint32_t unit0[kTensors];
+  Tensor t[kTensors];
+};
+static_assert(sizeof(ClipTable) <= 3968 && sizeof(FlatTable) <= 3968,
+              "kernel arguments stay below 4 KB");
 int64_t clip_units(const ClipTensor *t, int32_t count);
 hipError_t launch_sumsq(const ClipTensor *t, int32_t count, double *sumsq, void *ws,
                         hipStream_t s);

@@ -95,6 +95,27 @@ def test_strides_and_odd_starts():
             assert torch.equal(b[m], b0[m])
 
 
+@pytest.mark.parametrize("count,gaps", [(64, 1), (65, 1), (128, 0), (129, 0), (200, 200), (257, 3)])
+def test_many_tensors_with_and_without_gaps(count, gaps):
+    """Both forms of the table of tensors, at and past its ends."""
+    log(f"[clip many tensors] {count}, {gaps} of them with gaps")
+    grads = _grads(count, [(3 + i % 5, 20 + 31 * i % 700) for i in range(count)], ["bf16", "f32"])
+    for i in range(gaps):
+        grads[-1 - i] = grads[-1 - i][:, 1:]
+    before = [host(g) for g in grads]
+    total = orc.sumsq(before)
+    got = sn.sn_grad_sumsq(grads)
+    assert abs(float(got) - total) <= 1e-12 * total
+    _, want = orc.clip(before, float(got), 0.5 * math.sqrt(total))
+    outs = [torch.empty_like(g) for g in grads]
+    sn.sn_grad_clip(grads, got, 0.5 * math.sqrt(total), out=outs)
+    sn.sn_grad_clip(grads, got, 0.5 * math.sqrt(total))
+    for g, o, ref in zip(grads, outs, want):
+        assert torch.equal(g, o)
+        tol = (2.0 ** -23 + (2.0 ** -8 if g.dtype == torch.bfloat16 else 0)) * np.abs(ref)
+        assert (np.abs(host(o) - ref) <= tol + 1e-37).all()
+
+
 def test_extreme_values():
     log("[clip extremes]")
     inf, nan = float("inf"), float("nan")
