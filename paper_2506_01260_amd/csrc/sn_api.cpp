@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <cstring>
 #include <exception>
+#include <iterator>
 #include <vector>
 
 #include "sn_internal.h"
@@ -897,14 +898,20 @@ int32_t check_clip_alias(const std::vector<sn::ClipTensor> &t) {
     Span s;
     bool out;
   };
-  std::vector<Item> v;
-  v.reserve(2 * t.size());
+  // Lists that are in the order of their addresses, as gradients allocated one after the
+  // other are, need no sorting.
+  std::vector<Item> gs, os, v;
+  gs.reserve(t.size());
+  os.reserve(t.size());
   for (const sn::ClipTensor &c : t) {
-    const bool same = c.out == c.g && c.ldo == c.ldg;
-    v.push_back({clip_span(c, true), true});
-    if (!same) v.push_back({clip_span(c, false), false});
+    os.push_back({clip_span(c, true), true});
+    if (c.out != c.g || c.ldo != c.ldg) gs.push_back({clip_span(c, false), false});
   }
-  std::sort(v.begin(), v.end(), [](const Item &a, const Item &b) { return a.s.lo < b.s.lo; });
+  const auto below = [](const Item &a, const Item &b) { return a.s.lo < b.s.lo; };
+  for (std::vector<Item> *l : {&gs, &os})
+    if (!std::is_sorted(l->begin(), l->end(), below)) std::sort(l->begin(), l->end(), below);
+  v.reserve(gs.size() + os.size());
+  std::merge(gs.begin(), gs.end(), os.begin(), os.end(), std::back_inserter(v), below);
   uintptr_t any = 0, outs = 0;  // the furthest end of a span, of an output's span
   for (const Item &x : v) {
     if (x.s.lo < (x.out ? any : outs))
