@@ -11,7 +11,8 @@
 //
 // Measured: 1.1e9 bf16 gradients, norm 360 us (6.1 TB/s read) and scaling into other
 // tensors 770 us (5.7 TB/s read and written); 38 tensors of 4.5e6 floats in all, both
-// calls 17.7 us, 16 of them three launches.
+// calls 16.5 us, three launches (6.5, 2.3, 8.4); 155 of 6.9e6 bf16 29 us, 36 with 64
+// tensors to a launch.
 #include <algorithm>
 #include <cstring>
 

@@ -13,7 +13,7 @@
 // its end.  All sums are float32 over at most V / 64 terms each, then in a tree.
 //
 // Measured: 8192 x 128256 bf16 334 us (6.3 TB/s, what reads alone reach on this
-// card); 4999 x 50257 with eight alternatives 95 us (5.3); one row of 128256 11 us.
+// card); 4999 x 50257 with eight alternatives 96 us (5.2); one row of 128256 11 us.
 // Backward of 8192 x 32000 float32 355 us (5.9 TB/s read and written), loss of
 // 32768 x 32000 bf16 710-750 us (5.6-5.9).
 #include <cfloat>
