@@ -552,9 +552,9 @@ int32_t sn_rmsnorm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
  *   Q         N x d bytes, row stride ldq >= d; may not overlap anything
  *   S         float scales, N x (group ? ceil(d / 128) : 1), row stride lds:
  *             s = max(max |y|, 2^-100) / 448 over the scale's columns
- * q is y / s rounded to nearest even.  Columns of a scale that hold a NaN are
- * NaN throughout, and so is their scale.  Other arguments and errors as
- * sn_rmsnorm, and UNSUPPORTED for another group. */
+ * q is the float32 quotient y / s, rounded to nearest even.  Columns of a scale
+ * that hold a NaN are NaN throughout, and so is their scale.  Other arguments
+ * and errors as sn_rmsnorm, and UNSUPPORTED for another group. */
 int32_t sn_rmsnorm_quant(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
                          const void *R, int64_t ldr, const void *w, double eps, void *H,
                          int64_t ldh, int32_t group, void *Q, int64_t ldq, float *S, int64_t lds,

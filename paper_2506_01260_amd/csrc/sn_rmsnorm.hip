@@ -104,11 +104,23 @@ __device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
 __device__ __forceinline__ float scale_of(uint32_t bits) {
   return __uint_as_float(umax(bits, kTiny)) / kF8Max;
 }
-// y / s within e4m3's range (a NaN stays one)
-__device__ __forceinline__ float to_range(float y, float inv) {
-  const float q = y * inv;
-  return q > kF8Max ? kF8Max : q < -kF8Max ? -kF8Max : q;
-}
+// y / s of one scale, rounded to float32 as a division rounds it, within e4m3's range (a
+// NaN stays one).  The product with the rounded reciprocal alone is up to 1.5 units off
+// and gives the other code where y / s lies on a boundary between two, as rows of bf16
+// put it; the product's remainder corrects it (equal to the division for every
+// scale's 2^23 mantissas and the values about every boundary; 4999 x 1600 bf16 13.9 us,
+// 13.4 with the product alone, 32768 x 4096 158 with both).  A zero's sign is kept.
+struct Quotient {
+  float s, inv;
+  __device__ __forceinline__ explicit Quotient(float scale) : s(scale), inv(1.0f / scale) {
+    // an infinite scale: 0 for what is finite, without inf * 0 in the remainder
+    if (s == INFINITY) s = 0.0f;
+  }
+  __device__ __forceinline__ float operator()(float y) const {
+    const float q0 = y * inv, q = fmaf(-fmaf(q0, s, -y), inv, q0);
+    return q > kF8Max ? kF8Max : q < -kF8Max ? -kF8Max : q;
+  }
+};
 
 enum { kOut = 0, kOut8Row = 1, kOut8Group = 2 };
 constexpr int kGroup = 128;  // columns of a scale in the grouped form
@@ -202,9 +214,9 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
     uint8_t *Q = static_cast<uint8_t *>(a.Y) + i * a.ldy;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const float inv = 1.0f / scale_of(big[k]);
+      const Quotient over(scale_of(big[k]));
 #pragma unroll
-      for (int e = 0; e < E; ++e) h[k][e] = to_range(h[k][e], inv);
+      for (int e = 0; e < E; ++e) h[k][e] = over(h[k][e]);
       put8<E, WHOLE>(Q, c + k * R * E, d, h[k]);
     }
   }
@@ -278,9 +290,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
         m = lanes_umax<L>(m);
         if (threadIdx.x % L == 0 && c0 < a.d) a.S[i * a.lds + c0 / kGroup] = scale_of(m);
       }
-      const float inv = 1.0f / scale_of(m);
+      const Quotient over(scale_of(m));
 #pragma unroll
-      for (int e = 0; e < E; ++e) h[e] = to_range(h[e], inv);
+      for (int e = 0; e < E; ++e) h[e] = over(h[e]);
       put8<E>(static_cast<uint8_t *>(a.Y) + i * a.ldy, c0, a.d, h);
     }
   }

@@ -1,0 +1,74 @@
+"""The norm at its limits: 8-bit codes on the boundaries between two codes, against
+the quotient that the header names, code for code."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01260_amd as sn
+from gpu_helpers import host, log
+from oracle import rmsnorm as orc
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _codes(v):
+    return orc.round_e4m3(np.clip(v.astype(np.float64), -448, 448))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [6, 40, 130, 512, 1600, 5000, 16400])
+def test_codes_are_those_of_the_quotient(dtype, d):
+    """Whole numbers up to 28 = 7/8 of 32, so that odd ones above 16 lie on a boundary
+    (448 * 17 / 28 = 272, between 256 and 288), to the last bits of y and s.  Their
+    squares' sum is exact in any order (at most 28^2 * 16400 < 2^24), so that y is the
+    same float32 in every form of the call, and sn_rmsnorm in float32 returns it."""
+    log(f"[rmsnorm codes] {dtype} d={d}")
+    g = torch.Generator().manual_seed(d)
+    n = 96
+    X = torch.randint(-28, 29, (n, d), generator=g).float()
+    X[:, ::5] = 28.0  # each scale's columns reach it
+    X[:, 1::7] = torch.randint(8, 14, (n, len(range(1, d, 7))), generator=g).float() * 2 + 1
+    X[:, 3] = -0.0
+    X = X.cuda()
+    differs = 0
+    for w in (None, (1 + 0.2 * torch.randn(d, generator=g)).bfloat16().cuda()):
+        Y, _ = sn.sn_rmsnorm(X, None if w is None else w.float(), eps=0.0)
+        y = Y.cpu().numpy()
+        for group in (0, 128):
+            Q, S, _ = sn.sn_rmsnorm_quant(X.to(DT[dtype]), None if w is None else w.to(DT[dtype]),
+                                          eps=0.0, group=group)
+            cuts = list(range(0, d, group or d)) + [d]
+            s = np.stack([np.abs(y[:, i:j]).max(1) for i, j in zip(cuts, cuts[1:])], 1) / np.float32(448)
+            assert s.dtype == np.float32 and np.array_equal(S.cpu().numpy(), s)
+            each = orc.spread(s, d, group)
+            want, q = _codes(y / each), host(Q)
+            assert np.array_equal(q, want), f"{int((q != want).sum())} of {q.size} codes"
+            assert np.array_equal(np.signbit(q), np.signbit(want))
+            if w is None:
+                differs += int((_codes(y * (np.float32(1) / each)) != want).sum())
+    # a product with the rounded reciprocal would not do
+    log(f"  ok; a product with 1 / s has {differs} other codes")
+    assert differs > 0 or d < 1000
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_codes_beside_infinities(dtype):
+    """A gain that takes one value past float32's range makes its scale infinite: that
+    value's quotient is NaN, every other one's 0, and other scales are untouched."""
+    log(f"[rmsnorm codes beside infinities] {dtype}")
+    for d in (300, 40000):
+        X = torch.ones(3, d, dtype=DT[dtype], device="cuda")
+        X[1, 5] = -2.0 ** 20  # about sqrt(d) after the norm
+        w = torch.ones(d, dtype=DT[dtype], device="cuda")
+        w[5] = torch.finfo(DT[dtype]).max
+        Q, S, _ = sn.sn_rmsnorm_quant(X, w, group=128)
+        q, s = host(Q), host(S)
+        assert np.isinf(s[1, 0]) and np.isfinite(s[[0, 2]]).all() and np.isfinite(s[1, 1:]).all()
+        assert np.isnan(q[1, 5]) and (np.delete(q[1, :128], 5) == 0).all()
+        assert np.isfinite(q[[0, 2]]).all() and np.isfinite(q[1, 128:]).all()
+        q = host(sn.sn_rmsnorm_quant(X, w)[0])
+        assert np.isnan(q[1, 5]) and (np.delete(q[1], 5) == 0).all() and np.isfinite(q[[0, 2]]).all()
