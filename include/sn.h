@@ -624,7 +624,10 @@ int32_t sn_grad_sumsq(int32_t count, const sn_tensor *grads, double *sumsq, void
  *   norm      device float or NULL, receives sqrt(*sumsq)
  * The factor follows IEEE arithmetic: an infinite norm gives 0 (and NaN for
  * infinite gradients), a NaN norm makes every gradient NaN.  No two outputs may
- * overlap.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, HIP. */
+ * overlap.  Tensors of one row stride are compared by their elements, so that
+ * column blocks of one matrix are separate tensors; of different strides, and
+ * against sumsq and norm, from the first element to the last.  Errors: NULL,
+ * SHAPE, DTYPE, ALIGN, ALIAS, HIP. */
 int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out,
                      const double *sumsq, double max_norm, float *norm, sn_stream stream);
 

@@ -891,33 +891,73 @@ Span clip_span(const sn::ClipTensor &c, bool out) {
   return span(out ? c.out : c.g, c.rows, c.cols, out ? c.ldo : c.ldg, c.f32 ? 4 : 2);
 }
 
-// No output may overlap another tensor's gradient or output: with the spans in
-// order of their starts, each output against the span before it.
-int32_t check_clip_alias(const std::vector<sn::ClipTensor> &t) {
-  struct Item {
-    Span s;
-    bool out;
+// A gradient or output among the others of a clipping call.
+struct ClipItem {
+  Span s;
+  bool out;
+  int32_t tensor;
+};
+
+// Whether two tensors share an element, a the one that starts first.  Rows of one stride
+// (a single row fits any stride that holds it) are compared exactly, so that column
+// blocks of one matrix are told apart; of others the extents are.
+bool share(const std::vector<sn::ClipTensor> &t, const ClipItem &a, const ClipItem &b) {
+  if (!overlap(a.s, b.s)) return false;
+  struct Rows {
+    uintptr_t n, len, step;  // n rows of len bytes, one each step bytes
   };
+  const auto rows = [&](const ClipItem &x) {
+    const sn::ClipTensor &c = t[static_cast<size_t>(x.tensor)];
+    const int64_t es = c.f32 ? 4 : 2;
+    return Rows{static_cast<uintptr_t>(c.rows), static_cast<uintptr_t>(c.cols * es),
+                static_cast<uintptr_t>((x.out ? c.ldo : c.ldg) * es)};
+  };
+  const Rows ra = rows(a), rb = rows(b);
+  const uintptr_t step = ra.n > 1 ? ra.step : rb.step;
+  if ((ra.n == 1 && rb.n == 1) || (ra.n > 1 && rb.n > 1 && ra.step != rb.step) ||
+      ra.len > step || rb.len > step)
+    return true;
+  // b's first row starts in a's row q at byte r, and ends in row q + 1 where it is longer
+  // than what row q has left
+  const uintptr_t q = (b.s.lo - a.s.lo) / step, r = (b.s.lo - a.s.lo) % step;
+  return (q < ra.n && r < ra.len) || (q + 1 < ra.n && r + rb.len > step);
+}
+
+// No output may share an element with another tensor's gradient or output: with the
+// extents in order of their starts, each against the extents before it.
+int32_t check_clip_alias(const std::vector<sn::ClipTensor> &t) {
   // Lists that are in the order of their addresses, as gradients allocated one after the
   // other are, need no sorting.
-  std::vector<Item> gs, os, v;
+  std::vector<ClipItem> gs, os, v;
   gs.reserve(t.size());
   os.reserve(t.size());
   for (const sn::ClipTensor &c : t) {
-    os.push_back({clip_span(c, true), true});
-    if (c.out != c.g || c.ldo != c.ldg) gs.push_back({clip_span(c, false), false});
+    const int32_t i = static_cast<int32_t>(&c - t.data());
+    os.push_back({clip_span(c, true), true, i});
+    if (c.out != c.g || c.ldo != c.ldg) gs.push_back({clip_span(c, false), false, i});
   }
-  const auto below = [](const Item &a, const Item &b) { return a.s.lo < b.s.lo; };
-  for (std::vector<Item> *l : {&gs, &os})
+  const auto below = [](const ClipItem &a, const ClipItem &b) { return a.s.lo < b.s.lo; };
+  for (std::vector<ClipItem> *l : {&gs, &os})
     if (!std::is_sorted(l->begin(), l->end(), below)) std::sort(l->begin(), l->end(), below);
   v.reserve(gs.size() + os.size());
   std::merge(gs.begin(), gs.end(), os.begin(), os.end(), std::back_inserter(v), below);
-  uintptr_t any = 0, outs = 0;  // the furthest end of a span, of an output's span
-  for (const Item &x : v) {
-    if (x.s.lo < (x.out ? any : outs))
-      return fail(SN_ERR_ALIAS, "an output overlaps another gradient or output");
+  uintptr_t any = 0, outs = 0;  // the furthest end of an extent, of an output's extent
+  bool apart = true;
+  for (const ClipItem &x : v) {
+    apart = apart && x.s.lo >= (x.out ? any : outs);
     any = x.s.hi > any ? x.s.hi : any;
     if (x.out) outs = x.s.hi > outs ? x.s.hi : outs;
+  }
+  if (apart) return SN_OK;
+  // extents that overlap: each pair of them
+  std::vector<ClipItem> open;  // those that reach past the present one's start
+  for (const ClipItem &x : v) {
+    const auto ended = [&](const ClipItem &y) { return y.s.hi <= x.s.lo; };
+    open.erase(std::remove_if(open.begin(), open.end(), ended), open.end());
+    for (const ClipItem &y : open)
+      if ((x.out || y.out) && share(t, y, x))
+        return fail(SN_ERR_ALIAS, "an output overlaps another gradient or output");
+    open.push_back(x);
   }
   return SN_OK;
 }

@@ -227,3 +227,75 @@ def test_under_asan_and_ubsan():
     out = r.stdout + r.stderr
     assert r.returncode == 0 and " passed" in r.stdout, out[-4000:]
     assert "ERROR: AddressSanitizer" not in out and "runtime error:" not in out, out[-4000:]
+
+
+def _told_apart(grads, out=None):
+    """What the check between tensors says of a list: the call's norm lies over its
+    sumsq, which is refused too, after the tensors have been told apart."""
+    st = sn.lib().sn_grad_clip(len(grads), _arr(*grads), None if out is None else _arr(*out), E, 1.0,
+                               E + 4, None)
+    assert st == 5
+    return "norm overlaps sumsq" in sn.lib().sn_last_error().decode()
+
+
+def _slice(r, c, rows, cols, ld, dt, base=A):
+    """rows x cols from row r and column c of a matrix of row stride ld."""
+    return (base + (r * ld + c) * (2 if dt else 4), rows, cols, ld, dt)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+def test_clip_tells_column_blocks_apart(dt):
+    """Blocks of one matrix (a fused projection's gradient) share no element."""
+    def block(*a):
+        return _slice(*a, 300, dt)
+    assert _told_apart([block(0, 0, 8, 100), block(0, 100, 8, 100), block(0, 200, 8, 100)])
+    assert _told_apart([block(0, 200, 8, 100), block(0, 0, 8, 100), block(0, 100, 8, 100)])
+    assert _told_apart([block(0, 0, 8, 100), block(3, 150, 20, 150), block(8, 0, 1, 150)])
+    assert _told_apart([block(0, 150, 8, 150), block(1, 0, 7, 150)])      # the later one is further left
+    assert _told_apart([block(0, 0, 1, 100), block(0, 100, 8, 100)])      # one row of it
+    assert _told_apart([block(0, 50, 8, 200), block(0, 250, 8, 100)])     # into the next row's first columns
+    assert _told_apart([block(0, 100, 1, 250), block(0, 50, 8, 1)])
+    # into blocks of the same matrix, and of another
+    assert _told_apart([block(0, 0, 8, 100), block(0, 100, 8, 50)], [block(0, 150, 8, 100), block(0, 250, 8, 50)])
+    assert _told_apart([block(0, 0, 8, 100)] * 2, [_slice(0, c, 8, 100, 777, dt, B) for c in (5, 105)])
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+def test_clip_finds_blocks_that_meet(dt):
+    def block(*a):
+        return _slice(*a, 300, dt)
+    for bad in ([block(0, 0, 8, 100), block(0, 99, 8, 100)], [block(0, 0, 8, 101), block(7, 100, 8, 100)],
+                [block(0, 50, 8, 200), block(0, 250, 8, 101)],             # past the row's end
+                [block(0, 0, 8, 100), block(0, 100, 8, 100), block(5, 199, 1, 1)],
+                [block(0, 100, 1, 251), block(0, 50, 8, 1)],
+                [block(0, 0, 8, 100), _slice(0, 150, 8, 100, 299, dt)],   # other strides: their extents
+                [block(0, 0, 8, 100), (_slice(0, 150, 1, 1, 1, dt)[0], 1, 301, 301, dt)]):
+        assert not _told_apart(bad) and not _told_apart(bad[::-1])
+    assert not _told_apart([block(0, 0, 8, 100)], [block(0, 99, 8, 100)])
+    # one pair of many blocks
+    many = [block(0, 3 * i, 500, 3) for i in range(100)]
+    assert _told_apart(many)
+    assert not _told_apart(many + [block(499, 150, 1, 1)]) and _told_apart(many + [block(500, 150, 1, 1)])
+
+
+def test_clip_blocks_against_sets_of_elements():
+    """Random pairs of blocks, the check against the sets of their elements."""
+    import random
+    rng = random.Random(1)
+    seen = [0, 0]
+    for _ in range(2000):
+        ld = rng.randint(1, 9)
+        pair, sets = [], []
+        for _ in range(2):
+            at, rows, cols = rng.randint(0, 40), rng.randint(2, 5), rng.randint(1, ld)
+            pair.append(_slice(0, at, rows, cols, ld, 1))
+            sets.append({at + i * ld + j for i in range(rows) for j in range(cols)})
+            if cols == ld:
+                pair.pop()  # no gaps: a single row of all
+                pair.append(_slice(0, at, 1, rows * cols, rows * cols, 1))
+        meet = bool(sets[0] & sets[1])
+        extents = max(map(min, sets)) <= min(map(max, sets))
+        exact = all(p[1] > 1 for p in pair)
+        assert _told_apart(pair) == (not (meet if exact else extents)), (ld, pair)
+        seen[meet] += exact
+    assert min(seen) > 100
