@@ -30,7 +30,9 @@ constexpr int kSumBatch = 8, kClipBatch = 4;
 // Elements of a unit: 2048 (a piece or two for each thread) below 2^23 elements, to
 // fill the chip.  Above, the norm's units are few enough for one workgroup to add up
 // quickly (5 us for the 16900 of 1.1e9 gradients), and a clipping unit is one batch:
-// 774 us there, 792 with twice as many elements and 810 with eight times.
+// 774 us there, 792 with twice as many elements and 810 with eight times.  A tensor is
+// of fewer than 2^40 elements and its units of more than half as many as these, so that
+// a launch has fewer than 2^29: more than one grid dimension's 2^32 threads.
 int64_t sum_unit(int64_t total) {
   return total < (int64_t(1) << 23) ? 2048 : total < (int64_t(1) << 27) ? 16384 : 65536;
 }
@@ -141,11 +143,13 @@ __device__ __forceinline__ double unit_sumsq(const ClipTensor &t, const Unit &x)
 }
 
 template <typename TAB>
-__global__ __launch_bounds__(kNT) void sumsq_kernel(TAB tab, int64_t u,
+__global__ __launch_bounds__(kNT) void sumsq_kernel(TAB tab, uint32_t units, int64_t u,
                                                     double *__restrict__ part) {
   __shared__ double red[kNT / 64];
+  const uint32_t unit = static_cast<uint32_t>(group_number());
+  if (unit >= units) return;
   ClipTensor t;
-  const Unit x = unit_at(tab, blockIdx.x, u, t);
+  const Unit x = unit_at(tab, unit, u, t);
   double s = t.f32 ? unit_sumsq<float>(t, x) : unit_sumsq<bf16_t>(t, x);
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -153,7 +157,7 @@ __global__ __launch_bounds__(kNT) void sumsq_kernel(TAB tab, int64_t u,
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 1; i < kNT / 64; ++i) s += red[i];
-    part[blockIdx.x] = s;
+    part[unit] = s;
   }
 }
 
@@ -194,16 +198,18 @@ __device__ __forceinline__ void unit_scale(const ClipTensor &t, const Unit &x, f
 // The units in the opposite order of the norm's: of the gradients the last ones that
 // it read are still in the Infinity Cache, and the products are stored past it.
 template <typename TAB>
-__global__ __launch_bounds__(kNT) void clip_kernel(TAB tab, int64_t u, int in_place,
+__global__ __launch_bounds__(kNT) void clip_kernel(TAB tab, uint32_t units, int64_t u, int in_place,
                                                    const double *__restrict__ sumsq,
                                                    double max_norm, float *__restrict__ norm_out) {
+  const uint32_t group = static_cast<uint32_t>(group_number());
+  if (group >= units) return;
   const double norm = sqrt(*sumsq);
   // a NaN norm fails the comparison and makes the factor a NaN
   const float f = norm <= max_norm ? 1.0f : static_cast<float>(max_norm / norm);
-  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
+  if (norm_out && group == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
   if (tab.n == 0 || (in_place && f == 1.0f)) return;  // every value is its own product
   ClipTensor t;
-  const Unit x = unit_at(tab, gridDim.x - 1 - blockIdx.x, u, t);
+  const Unit x = unit_at(tab, units - 1 - group, u, t);
   if (t.f32)
     unit_scale<float>(t, x, f);
   else
@@ -235,7 +241,7 @@ hipError_t each_table(const ClipTensor *t, int32_t count, int64_t u, bool back, 
       tab.unit0[tab.n++] = static_cast<uint32_t>(units);
       units += units_of(t[i], u);
     }
-    launch(tab, static_cast<unsigned>(units));
+    launch(tab, static_cast<uint32_t>(units));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -268,8 +274,8 @@ hipError_t launch_sumsq(const ClipTensor *t, int32_t count, double *sumsq, void 
   const int64_t u = sum_unit(total_elems(t, count));
   double *part = static_cast<double *>(ws);
   int64_t n = 0;
-  const hipError_t e = each_table(t, count, u, false, [&](const auto &tab, unsigned units) {
-    sumsq_kernel<<<units, kNT, 0, s>>>(tab, u, part + n);
+  const hipError_t e = each_table(t, count, u, false, [&](const auto &tab, uint32_t units) {
+    sumsq_kernel<<<groups_grid(units), kNT, 0, s>>>(tab, units, u, part + n);
     n += units;
   });
   if (e != hipSuccess) return e;
@@ -281,12 +287,13 @@ hipError_t launch_clip(const ClipTensor *t, int32_t count, bool in_place, const 
                        double max_norm, float *norm, hipStream_t s) {
   const int64_t u = clip_unit(total_elems(t, count));
   bool told = norm == nullptr;
-  const hipError_t e = each_table(t, count, u, true, [&](const auto &tab, unsigned units) {
-    clip_kernel<<<units, kNT, 0, s>>>(tab, u, in_place, sumsq, max_norm, told ? nullptr : norm);
+  const hipError_t e = each_table(t, count, u, true, [&](const auto &tab, uint32_t units) {
+    clip_kernel<<<groups_grid(units), kNT, 0, s>>>(tab, units, u, in_place, sumsq, max_norm,
+                                                   told ? nullptr : norm);
     told = true;
   });
   if (e != hipSuccess || told) return e;
-  clip_kernel<<<1, kNT, 0, s>>>(FlatTable(), u, in_place, sumsq, max_norm, norm);  // nothing to scale
+  clip_kernel<<<1, kNT, 0, s>>>(FlatTable(), 1, u, in_place, sumsq, max_norm, norm);  // nothing to scale
   return hipGetLastError();
 }
 

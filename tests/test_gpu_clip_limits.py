@@ -49,3 +49,29 @@ def test_column_blocks_in_place(dtype):
     with pytest.raises(sn.SnError) as e:
         sn.sn_grad_clip([whole[:, :333], whole[:, 332:400]], s, most)
     assert e.value.status == 5
+
+
+def test_more_units_than_a_grid_dimension_has():
+    """Units of 256 threads past 2^24, so past 2^32 threads of one launch.  The norm: one
+    matrix of 2^18 + 1 rows with gaps, a row a unit, listed 64 times.  Clipping: 2^24 + 99
+    rows of 4097, again a row a unit; of its memory the first and last rows are looked at."""
+    log("[clip units past 2^24]")
+    if torch.cuda.mem_get_info()[0] < 160e9:
+        pytest.skip("needs 140 GB of device memory")
+    rows, cols = (1 << 18) + 1, 32769
+    g = torch.zeros(rows, cols + 1, dtype=torch.bfloat16, device="cuda")
+    g[0, 0], g[-1, cols - 1], g[:, cols] = 3.0, 4.0, float("nan")
+    s = sn.sn_grad_sumsq([g[:, :cols]] * 64)
+    assert float(s) == 64 * 25.0
+    del g
+    torch.cuda.empty_cache()
+    rows, cols = (1 << 24) + 99, 4097
+    g = torch.empty(rows, cols + 1, dtype=torch.bfloat16, device="cuda")
+    for part in (g[:5], g[-5:], g[(1 << 24) - 3:(1 << 24) + 3]):
+        part.fill_(6.0)
+    norm = sn.sn_grad_clip([g[:, :cols]], torch.full((1,), 16.0, dtype=torch.float64, device="cuda"), 2.0)
+    assert float(norm) == 4.0
+    for part in (g[:5], g[-5:], g[(1 << 24) - 3:(1 << 24) + 3]):
+        assert bool((part[:, :cols] == 3.0).all()) and bool((part[:, cols] == 6.0).all())
+    del g, part
+    torch.cuda.empty_cache()
