@@ -451,7 +451,8 @@ __global__ __launch_bounds__(kGainCols *kGainGroups) void gain_kernel(
     const float *__restrict__ part, int64_t parts, int64_t d, float *__restrict__ gw) {
   __shared__ double red[kGainGroups][kGainCols];
   const int lane = threadIdx.x % kGainCols, g = threadIdx.x / kGainCols;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * kGainCols + lane;
+  const int64_t c0 = group_number() * kGainCols, c = c0 + lane;
+  if (c0 >= d) return;
   double s = 0.0;
   if (c < d) {
 #pragma unroll 8
@@ -581,7 +582,7 @@ hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipS
   a.part = gw ? static_cast<float *>(ws) : nullptr;
   const hipError_t e = dt == 0 ? launch_grad_d<float>(dt, a, s) : launch_grad_d<bf16_t>(dt, a, s);
   if (e != hipSuccess || !gw) return e;
-  gain_kernel<<<static_cast<unsigned>(ceil_div(a.d, kGainCols)), kGainCols * kGainGroups, 0, s>>>(
+  gain_kernel<<<groups_grid(ceil_div(a.d, kGainCols)), kGainCols * kGainGroups, 0, s>>>(
       a.part, turn_groups(dt, a), a.d, gw);
   return hipGetLastError();
 }

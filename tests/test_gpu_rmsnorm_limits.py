@@ -72,3 +72,22 @@ def test_codes_beside_infinities(dtype):
         assert np.isfinite(q[[0, 2]]).all() and np.isfinite(q[1, 128:]).all()
         q = host(sn.sn_rmsnorm_quant(X, w)[0])
         assert np.isnan(q[1, 5]) and (np.delete(q[1], 5) == 0).all() and np.isfinite(q[[0, 2]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gain_gradient_past_2_32_threads(dtype):
+    """2^27 + 77 columns: the gain gradient's workgroups of 1024 threads for 32 columns
+    take more than one grid dimension has.  Rows of ones with eps = 0, whose squares' sum
+    is exact, so that rho is 1 to its last bits and gw the rows' sum of dy."""
+    log(f"[rmsnorm gain gradient, 2^27 columns] {dtype}")
+    n, d = 2, (1 << 27) + 77
+    H = torch.ones(n, d, dtype=DT[dtype], device="cuda")
+    dY = torch.zeros_like(H)
+    gw = torch.ones(d, device="cuda")
+    at = torch.tensor([0, 31, 1 << 20, (1 << 25) + 1, (1 << 27) - 1, 1 << 27, d - 1], device="cuda")
+    dY[0, at], dY[1, at] = 2.0, -4.0
+    dY[:, 5] = 6.0
+    sn.sn_rmsnorm_backward(H, dY, eps=0.0, gw=gw)
+    want = torch.ones(d, device="cuda")
+    want[at], want[5] = -1.0, 13.0
+    assert float((gw - want).abs().max()) <= 1e-5
