@@ -526,8 +526,12 @@ int32_t sn_token_loss(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t 
 /*   h = x + r,   y = h w / sqrt(mean_j h_j^2 + eps)                          */
 /* over rows of d columns, in float32; h is rounded to dt where it is stored, */
 /* and y is made from the sum before that rounding.                           */
-/* Squares are float32: a row of root mean square past 2^63 counts as         */
-/* infinite (y = 0), one below 2^-74 as zero beside eps.                      */
+/* A row's squares are summed in float32 as they are: from a sum of 2^128 on, */
+/* a root mean square of 2^64 / sqrt(d) (2^58 at d = 4096), the row counts as */
+/* infinite: y = 0, dX = dH, and nothing for w.  Squares lose bits below 2^-126*/
+/* and are 0 below 2^-150, which any eps >= 2^-100 covers; with eps = 0, y loses*/
+/* bits in rows below 2^-63, and is infinite (of zeros: NaN) where all squares*/
+/* are 0.                                                                     */
 /* ------------------------------------------------------------------------ */
 
 /* sn_rmsnorm

@@ -91,3 +91,48 @@ def test_gain_gradient_past_2_32_threads(dtype):
     want = torch.ones(d, device="cuda")
     want[at], want[5] = -1.0, 13.0
     assert float((gw - want).abs().max()) <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [5, 300, 4096, 8190, 40000])
+def test_largest_and_smallest_rows(dtype, d):
+    """Rows of +-2^p on both sides of a sum of squares of 2^128, and the smallest ones.
+    Inside, y is the sign to the rounding of rho (float32 sums of equal powers of two,
+    at most d / 64 + 48 roundings, half of their error) and of a bf16 output."""
+    log(f"[rmsnorm largest and smallest rows] {dtype} d={d}")
+    u = 2.0 ** -24
+    p = max(q for q in range(70) if d * 4.0 ** q < 2.0 ** 128)
+    g = torch.Generator().manual_seed(d)
+    sign = torch.randint(0, 2, (2, d), generator=g).float() * 2 - 1
+    tol = u * (d / 128 + 40) + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    H = torch.stack([sign[0] * 2.0 ** p, sign[1] * 2.0 ** (p + 1)]).to(DT[dtype]).cuda()
+    for w in (None, torch.full((d,), 0.5, dtype=DT[dtype], device="cuda")):
+        k = 1.0 if w is None else 0.5
+        Y, _ = sn.sn_rmsnorm(H, w)
+        assert np.abs(host(Y)[0] - k * sign[0].numpy()).max() <= tol * k and float(Y[1].abs().max()) == 0.0
+        Q, S, _ = sn.sn_rmsnorm_quant(H, w)
+        assert np.abs(host(Q)[0] * host(S)[0] - k * sign[0].numpy()).max() <= k * u * (d / 128 + 48)
+        assert float(Q[1].float().abs().max()) == 0.0
+    # dx = rho (u - n mean(u n)), |n| = 1: at most the roundings of rho, of the mean (float32
+    # over d terms) and of five operations, of |u| + mean |u| < 2
+    dY = torch.rand(2, d, generator=g).to(DT[dtype]).cuda()
+    dH = torch.randn(2, d, generator=g).to(DT[dtype]).cuda()
+    gw = torch.ones(d, device="cuda")
+    dX = sn.sn_rmsnorm_backward(H, dY, gw=gw)
+    ref, gref = orc.rmsnorm_backward(host(H), host(dY))
+    err = np.abs(host(dX)[0] - ref[0]) / 2.0 ** -p
+    own = 2.0 ** -8 * np.abs(ref[0]) * 2.0 ** p if dtype == "bf16" else 0.0
+    assert (err <= 2 * u * (d / 64 + 60) + own).all()
+    assert float(dX[1].abs().max()) == 0.0
+    # only the first row counts: |dy n| < 1
+    want = 1.0 + host(dY)[0] * sign[0].numpy()
+    assert np.abs(host(gw) - want).max() <= u * (d / 128 + 48)
+    assert torch.equal(sn.sn_rmsnorm_backward(H, dY, dH=dH)[1], dH[1])
+    # the small end: 2^-62 has its bits without eps, 2^-80 with one
+    for power, eps in ((-62, 0.0), (-80, 1e-6), (-80, 2.0 ** -100)):
+        X = (sign * 2.0 ** power).to(DT[dtype]).cuda()
+        ref = sign.numpy() * 2.0 ** power / np.sqrt(4.0 ** power + float(np.float32(eps)))
+        Y, _ = sn.sn_rmsnorm(X, eps=eps)
+        assert (np.abs(host(Y) - ref) <= tol * np.abs(ref)).all(), power
+    Y, _ = sn.sn_rmsnorm(X, eps=0.0)
+    assert np.isinf(host(Y)).all() and bool(torch.isnan(sn.sn_rmsnorm(0 * X, eps=0.0)[0]).all())
