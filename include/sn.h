@@ -448,11 +448,15 @@ int32_t sn_adamw_step(void *W, int64_t ldw, const void *G, int64_t ldg, int32_t 
 /* temperature.  With m = max z, x = c (z - m), S = sum e^x and L = log S:    */
 /*   log p_j = x_j - L,   H = -sum_j p_j log p_j                              */
 /* logp[i] is log p of the row's given token tok[i]; tok[i] = -1 marks a row  */
-/* without one (padding): logp 0, and no gradient flows through it.           */
+/* without one (padding): its logp is 0, and neither its gradient of logp nor */
+/* its weight counts. Its entropy is that of its logits, and a gradient of    */
+/* the entropy flows through it as through any row: pass 0 there for a row    */
+/* that is to be left out.                                                    */
 /* A logit of -inf is a forbidden token: p = 0, log p = -inf, 0 log 0 = 0.    */
 /* A row whose logits are all -inf has p = 0 throughout: logp -inf, H 0,      */
 /* stats (-inf, -inf).  A row that holds NaN or +inf has no distribution:     */
-/* logp, entropy, stats, top_logp and gradients are NaN, top_id -1.           */
+/* logp (but padding's 0), entropy, stats, top_logp and gradients are NaN,    */
+/* top_id -1.  A difference z - m past float32's range counts as -inf.        */
 /* Sums are float32; scale lies in [2^-20, 2^20], V < 2^31.                   */
 /* ------------------------------------------------------------------------ */
 
@@ -492,13 +496,13 @@ int32_t sn_token_logprobs(const void *Z, int64_t N, int64_t V, int64_t ldz, int3
  *   Z, N, V, ldz, dt, scale, tok   as in the forward call
  *   stats, entropy   as the forward call wrote them (entropy may be NULL when
  *             g_entropy is)
- *   g_logp    float[N] or NULL (0); needs tok
- *   g_entropy float[N] or NULL (0)
+ *   g_logp    float[N] or NULL (0); needs tok, and counts where tok is not -1
+ *   g_entropy float[N] or NULL (0); counts in every row, padding among them
  *   dZ        N x V gradient (dt), row stride lddz >= V.  May be Z itself (same
  *             pointer and stride), else may not overlap an input
- * A row whose gradients are both 0 (or whose token is -1, with g_entropy 0)
- * gets zeros and its logits are not read.  Errors: NULL, SHAPE, DTYPE, ALIGN,
- * ALIAS, HIP. */
+ * A row whose gradients are both 0 (or whose token is -1, with g_entropy 0 or
+ * NULL) gets zeros and its logits are not read.  Errors: NULL, SHAPE, DTYPE,
+ * ALIGN, ALIAS, HIP. */
 int32_t sn_token_logprobs_backward(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t dt,
                                    double scale, const int32_t *tok, const float *stats,
                                    const float *entropy, const float *g_logp,
@@ -528,10 +532,10 @@ int32_t sn_token_loss(const void *Z, int64_t N, int64_t V, int64_t ldz, int32_t 
 /* and y is made from the sum before that rounding.                           */
 /* A row's squares are summed in float32 as they are: from a sum of 2^128 on, */
 /* a root mean square of 2^64 / sqrt(d) (2^58 at d = 4096), the row counts as */
-/* infinite: y = 0, dX = dH, and nothing for w.  Squares lose bits below 2^-126*/
-/* and are 0 below 2^-150, which any eps >= 2^-100 covers; with eps = 0, y loses*/
-/* bits in rows below 2^-63, and is infinite (of zeros: NaN) where all squares*/
-/* are 0.                                                                     */
+/* infinite: y = 0, dX = dH, and nothing for w. Squares lose bits below       */
+/* 2^-126 and are 0 below 2^-150, which any eps >= 2^-100 covers; with eps =  */
+/* 0, y loses bits in rows below 2^-63, and is infinite (of zeros: NaN) where */
+/* all squares are 0.                                                         */
 /* ------------------------------------------------------------------------ */
 
 /* sn_rmsnorm

@@ -841,7 +841,8 @@ def sn_token_logprobs_backward(Z: torch.Tensor, stats: torch.Tensor, entropy=Non
                                g_logp=None, g_entropy=None, scale: float = 1.0, out=None,
                                err_flag=None, stream=None) -> torch.Tensor:
     """dZ from the gradients of logp and entropy, with the forward call's stats and
-    entropy; out may be Z."""
+    entropy; out may be Z.  g_entropy counts in rows without a token (-1) too: pass 0
+    there to leave padding out."""
     native = _native()
     if native is not None:
         dZ = native.token_logprobs_backward(Z, stats, entropy, tok, g_logp, g_entropy, scale, out,
