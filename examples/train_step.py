@@ -127,10 +127,11 @@ class Model:
 
 
 def batch(g, n_seq=BATCH, seq=SEQ, vocab=VOCAB):
-    """Random sequences; the next token is 5 t + 7, and the last one has none."""
+    """Random sequences, and for each token t the one to answer with, 5 t + 7; a
+    sequence's first position has none, as padding has none."""
     tok = torch.randint(0, vocab, (n_seq, seq), generator=g, device="cuda", dtype=torch.int32)
     target = (5 * tok + 7) % vocab
-    target[:, 0] = -1  # stands in for positions without a target
+    target[:, 0] = -1
     return tok.reshape(-1), target.reshape(-1)
 
 

@@ -1016,8 +1016,9 @@ def _workspace(t, need):
 
 
 def _tensors(ts, name):
-    """sn_tensor array of a list of device tensors: vectors, matrices with any row
-    stride, and tensors of any shape without gaps."""
+    """sn_tensor array of a list of device tensors: contiguous ones of any shape,
+    vectors with any stride and row-major matrices with any row stride.  Others, a
+    transposed view among them, are refused."""
     arr = (_Tensor * max(1, len(ts)))()
     for i, t in enumerate(ts):
         if not t.is_cuda:
@@ -1032,7 +1033,8 @@ def _tensors(ts, name):
 
 def sn_grad_sumsq(grads, out=None, workspace=None, stream=None) -> torch.Tensor:
     """Sum of the squares of every value of every tensor of the list, one float64
-    device value (out: float64, one value)."""
+    device value (out: float64, one value).  Tensors are contiguous ones of any shape,
+    vectors with any stride, or row-major matrices with any row stride."""
     native = _native()
     if native is not None:
         r = native.grad_sumsq(grads, out, workspace, stream)
@@ -1056,7 +1058,8 @@ def sn_grad_clip(grads, sumsq: torch.Tensor, max_norm: float, out=None, norm=Non
                  stream=None) -> torch.Tensor:
     """Scale the gradients by min(1, max_norm / sqrt(sumsq)), in place or into the
     tensors of the list out (same shapes and dtypes); returns the norm (float32,
-    one value)."""
+    one value).  Tensors as in sn_grad_sumsq; column blocks of one matrix may be given
+    as tensors of their own."""
     native = _native()
     if native is not None:
         r = native.grad_clip(grads, sumsq, max_norm, out, norm, stream)

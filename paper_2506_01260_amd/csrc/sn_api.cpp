@@ -843,8 +843,8 @@ sn::NormArgs norm_args(const void *X, int64_t N, int64_t d, int64_t ldx, const v
   return a;
 }
 
-// The tensors of a clipping call as the kernels take them (rows without gaps as
-// one row), checked; spans of those with elements go to `reads` where given.
+// The tensors of a clipping call as the kernels take them, checked: rows without gaps
+// as one row, and tensors without elements left out.
 int32_t clip_tensors(int32_t count, const sn_tensor *grads, const sn_tensor *out, bool shapes_only,
                      std::vector<sn::ClipTensor> &t) {
   if (count < 0) return fail(SN_ERR_SHAPE, "count must be >= 0");
