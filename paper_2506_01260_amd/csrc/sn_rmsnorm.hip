@@ -13,7 +13,7 @@
 // a wave has a row of its own and no barrier.
 //
 // Measured: 32768 x 4096 bf16 with residual 181 us (5.9 TB/s read and written, the
-// rate of an addition of two arrays on this card), 8 bits out 162 us; one row 2.7 us;
+// rate of an addition of two arrays on this card), 8 bits out 158-162 us; one row 2.7 us;
 // backward of 16383 x 8192 with the stream's gradient 207 us (5.2 TB/s), 5 of them the
 // gain's sum over workgroups.
 #include "sn_internal.h"
@@ -302,7 +302,8 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(NormArgs a) {
 // part of the gain's gradient in registers; the parts are summed by gain_kernel.
 // Everything of a row is loaded before its sums are joined, and stays as loaded
 // (16 bytes a piece) until it is used: at d = 8192 bf16 registers for two
-// workgroups of 8 waves on a CU instead of one.
+// workgroups of 8 waves on a CU instead of one.  Ragged bf16 rows of 12289 to 16383
+// columns need more registers than 1024 threads have: 36 bytes of scratch.
 template <typename T, int R, int K, int NT, bool WHOLE>
 __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(NormGradArgs a) {
   constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
