@@ -27,7 +27,7 @@ namespace {
 
 // e^(c d) is 2^(c2 d) with c2 = c log2 e rounded to float32, one multiplication of the
 // difference d: |c d| 2^-24 of the exponential more than with exp(c d), so that float32
-// outputs lie up to twice as far from 64 bits (5e-8 to 9e-8 of the outputs' norm for 4e-8
+// outputs lie up to twice as far from 64 bits (5e-8 to 9e-8 of the outputs' norm for 3e-8
 // to 6e-8), below one unit of theirs.
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxTop = 64;    // SN_MAX_TOP
