@@ -592,6 +592,145 @@ int32_t sn_rmsnorm_backward(const void *H, int64_t N, int64_t d, int64_t ldh, in
                             void *workspace, size_t workspace_bytes, sn_stream stream);
 
 /* ------------------------------------------------------------------------ */
+/* The end of a block and the start of the next: the block output's norm, its */
+/* gate, the scaled residual and the next block's norm in one pass.           */
+/*                                                                            */
+/*   z = x w_post / sqrt(mean_j x_j^2 + eps)   (post != 0), or z = x          */
+/*   h = alpha r + g z                                                        */
+/*   y = h w / sqrt(mean_j h_j^2 + eps)                                       */
+/* over rows of d columns, in float32; g is the gate or its sigmoid.  h is    */
+/* rounded to dt where it is stored, and y is made from the sum before that.  */
+/* Squares are summed as sn_rmsnorm sums them, with its limits.               */
+/* ------------------------------------------------------------------------ */
+
+/* The gate's function. */
+typedef enum sn_gate_fn { SN_GATE_NONE = 0, SN_GATE_SIGMOID = 1 } sn_gate_fn;
+
+/* sn_block_norm
+ *
+ *   X         N x d block output (dt), row stride ldx >= d
+ *   R         N x d residual stream (dt), row stride ldr >= d
+ *   post      nonzero: z is normed; w_post is read only then
+ *   w_post, w d gains (dt), or NULL: 1
+ *   gate      NULL: 1; with ldgate = 0 d values for every token, else N x d (dt),
+ *             row stride ldgate >= d
+ *   gate_fn   SN_GATE_NONE or SN_GATE_SIGMOID
+ *   alpha     the residual's scale, finite
+ *   eps       finite, >= 0, of both norms
+ *   H         N x d (dt), row stride ldh >= d, receives h.  May be X or R itself
+ *             (same pointer and stride), else may not overlap an input
+ *   Y         N x d (dt), row stride ldy >= d, or NULL: no next norm.  May not
+ *             overlap anything
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, UNSUPPORTED (gate_fn), HIP. */
+int32_t sn_block_norm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *R,
+                      int64_t ldr, int32_t post, const void *w_post, const void *gate,
+                      int64_t ldgate, int32_t gate_fn, double alpha, const void *w, double eps,
+                      void *H, int64_t ldh, void *Y, int64_t ldy, sn_stream stream);
+
+/* Workspace bytes of sn_block_norm_backward (0 if invalid; needed with gw, gw_post or
+ * the gradient of one gate row only). */
+size_t sn_block_norm_backward_workspace_bytes(int64_t N, int64_t d, int32_t dt);
+
+/* sn_block_norm_backward: with n = h rho, u = dy w, q = 1 / sqrt(mean x^2 + eps),
+ * m = x q and g' the gate function's derivative,
+ *   dh = rho (u - n mean(u n)) + dH,   dR = alpha dh,   dgate = dh z g',
+ *   v = g dh w_post,   dX = q (v - m mean(v m))   (post), or dX = g dh
+ *   gw += sum over rows of dy n,   gw_post += sum over rows of g dh m.
+ *
+ *   X         the forward call's (dt)
+ *   H         N x d, the forward call's h (dt)
+ *   post .. eps   as in the forward call
+ *   dY        N x d gradient of y (dt), or NULL: 0
+ *   dH        N x d gradient that flows into h from elsewhere (dt), or NULL: 0
+ *   dX        N x d (dt); may be X, dY or dH itself (same pointer and stride), else
+ *             may not overlap an input
+ *   dR        N x d (dt); may be dY or dH itself, as above
+ *   dgate     of a gate for each token: N x d (dt), row stride lddgate >= d; may be
+ *             the gate itself, as above.  NULL: not wanted
+ *   dgate_row of one gate row: d float32, ACCUMULATED into.  NULL: not wanted
+ *   gw, gw_post   d float32, ACCUMULATED into, or NULL (gw needs dY, gw_post post)
+ *   workspace sn_block_norm_backward_workspace_bytes(N, d, dt) bytes, 256-byte
+ *             aligned; may be NULL without gw, gw_post and dgate_row
+ * Deterministic: rows are added in a fixed order, float32 within a workgroup and
+ * float64 over workgroups.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, WORKSPACE,
+ * UNSUPPORTED, HIP. */
+int32_t sn_block_norm_backward(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
+                               const void *H, int64_t ldh, int32_t post, const void *w_post,
+                               const void *gate, int64_t ldgate, int32_t gate_fn, double alpha,
+                               const void *w, double eps, const void *dY, int64_t lddy,
+                               const void *dH, int64_t lddh, void *dX, int64_t lddx, void *dR,
+                               int64_t lddr, void *dgate, int64_t lddgate, float *dgate_row,
+                               float *gw, float *gw_post, void *workspace, size_t workspace_bytes,
+                               sn_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Gated feed-forward block: both projections, the activation and the product.*/
+/*                                                                            */
+/*   G = X Wg,   U = X Wu,   H = act(G) * U                                   */
+/* Sums are float32, H is made from them before G and U are rounded.  The     */
+/* down projection H W2^T is the caller's (W2's columns lie in the subspace). */
+/* float32 matrices are multiplied in parts of 24 bits together, exact to     */
+/* 2^-24 of the products' sizes, but for what lies below 2^-126, which counts */
+/* as 0; there a NaN or an infinity makes the results that it enters NaN or   */
+/* infinite, not always the infinity itself.  Calls of up to 8 tokens have no */
+/* such limits.                                                               */
+/* ------------------------------------------------------------------------ */
+
+typedef enum sn_act { SN_ACT_SILU = 0, SN_ACT_GELU = 1, SN_ACT_RELU = 2 } sn_act;
+
+/* Workspace bytes of sn_gated_ff and sn_gated_ff_backward (0: none needed, or invalid
+ * arguments).  bf16 matrices whose columns and row strides are multiples of 8 and which
+ * start on 16-byte boundaries are read where they lie, others from copies in the
+ * workspace.  aligned: nonzero promises that X, Wg and Wu (backward: dG and dU too) start
+ * on such boundaries. */
+size_t sn_gated_ff_workspace_bytes(int64_t N, int64_t d, int64_t ff, int64_t ldx, int64_t ldw,
+                                   int32_t dt, int32_t aligned);
+size_t sn_gated_ff_backward_workspace_bytes(int64_t N, int64_t d, int64_t ff, int64_t ldx,
+                                            int64_t ldw, int64_t ldd, int32_t dt, int32_t aligned);
+
+/* sn_gated_ff
+ *
+ *   X         N x d (dt), row stride ldx >= d
+ *   Wg, Wu    d x ff (dt), shared row stride ldw >= ff
+ *   act       SN_ACT_SILU: g / (1 + e^-g), SN_ACT_GELU: g (1 + erf(g / sqrt 2)) / 2,
+ *             SN_ACT_RELU: max(g, 0)
+ *   H         N x ff (dt), row stride ldh >= ff
+ *   G, U      N x ff (dt), shared row stride ldg >= ff: what the backward call reads.
+ *             Both or neither
+ *   workspace sn_gated_ff_workspace_bytes(...) bytes, 256-byte aligned; may be NULL
+ *             where that is 0
+ * N == 0 is a no-op.  Outputs and workspace may not overlap anything.  Deterministic.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, WORKSPACE, UNSUPPORTED (act), HIP. */
+int32_t sn_gated_ff(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *Wg,
+                    const void *Wu, int64_t ff, int64_t ldw, int32_t act, void *H, int64_t ldh,
+                    void *G, void *U, int64_t ldg, void *workspace, size_t workspace_bytes,
+                    sn_stream stream);
+
+/* sn_gated_ff_backward:
+ *   dG = dH U act'(G),   dU = dH act(G)                  (rounded to dt)
+ *   dX = dG Wg^T + dU Wu^T,   gWg = X^T dG,   gWu = X^T dU
+ *
+ *   X, Wg, Wu, act, G, U   as in the forward call
+ *   dH        N x ff gradient of H (dt), row stride lddh >= ff
+ *   dG, dU    N x ff (dt), shared row stride ldd >= ff, written; each may be G, U or dH
+ *             itself (same pointer and stride), else may not overlap an input
+ *   dX        N x d (dt), row stride lddx >= d, or NULL: not wanted.  May be X itself
+ *             without gWg, else may not overlap anything
+ *   gWg, gWu  d x ff (gdt: dt or SN_F32), shared row stride ldgw >= ff; both or neither
+ *   accumulate   nonzero: gWg and gWu are added to, else overwritten
+ *   workspace sn_gated_ff_backward_workspace_bytes(...) bytes, 256-byte aligned; may be
+ *             NULL where that is 0
+ * act'(0) of SN_ACT_RELU is 0.  N == 0 leaves gWg and gWu as they are with accumulate and
+ * fills them with zeros without.  Deterministic.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS,
+ * WORKSPACE, UNSUPPORTED, HIP. */
+int32_t sn_gated_ff_backward(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
+                             const void *Wg, const void *Wu, int64_t ff, int64_t ldw, int32_t act,
+                             const void *G, const void *U, int64_t ldg, const void *dH,
+                             int64_t lddh, void *dG, void *dU, int64_t ldd, void *dX, int64_t lddx,
+                             void *gWg, void *gWu, int64_t ldgw, int32_t gdt, int32_t accumulate,
+                             void *workspace, size_t workspace_bytes, sn_stream stream);
+
+/* ------------------------------------------------------------------------ */
 /* Global gradient norm and clipping (before the optimizer steps).            */
 /*                                                                            */
 /*   sumsq = sum of g^2 over every element of every tensor                    */
@@ -638,6 +777,52 @@ int32_t sn_grad_sumsq(int32_t count, const sn_tensor *grads, double *sumsq, void
  * SHAPE, DTYPE, ALIGN, ALIAS, HIP. */
 int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out,
                      const double *sumsq, double max_norm, float *norm, sn_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Orthogonalised updates (the Muon optimiser's step).                        */
+/*                                                                            */
+/*   X = B / |B|_F,   `steps` times X <- (a I + b A + c A^2) X,  A = X X^T    */
+/* (X Q with A = X^T X where there are more rows than columns), a, b, c =     */
+/* 3.4445, -4.7750, 2.0315: five steps take singular values from 1 / 300 to 1 */
+/* into [0.68, 1.21].  The result has B's row and column space: an update of  */
+/* columns that lie in the subspace lies there too.  Products are made from   */
+/* operands of 22 bits, sums are float32.  B = 0 gives 0; a NaN or an infinity*/
+/* in B makes the result NaN.                                                 */
+/* ------------------------------------------------------------------------ */
+
+/* Largest number of steps. */
+#define SN_MAX_ORTH_STEPS 16
+
+/* Workspace bytes of sn_orthogonalize and sn_muon_step for count matrices of rows x cols
+ * (0 if invalid, or nothing to do). */
+size_t sn_orthogonalize_workspace_bytes(int32_t count, int64_t rows, int64_t cols);
+
+/* sn_orthogonalize: out[i] = the matrix in[i] after the steps.
+ *   in, out   HOST arrays of count >= 0 matrices of one shape and dtype; out[i] may be
+ *             in[i] itself (same pointer and stride), else may not overlap an input
+ *   steps     1 .. SN_MAX_ORTH_STEPS
+ *   workspace sn_orthogonalize_workspace_bytes(count, rows, cols) bytes, 256-byte aligned
+ * Without elements or matrices a no-op.  Deterministic.  Errors: NULL, SHAPE, DTYPE, ALIGN,
+ * ALIAS, WORKSPACE, HIP. */
+int32_t sn_orthogonalize(int32_t count, const sn_tensor *in, const sn_tensor *out, int32_t steps,
+                         void *workspace, size_t workspace_bytes, sn_stream stream);
+
+/* sn_muon_step: one step of count matrices, in place:
+ *   M <- momentum M + G
+ *   B = G + momentum M  (nesterov != 0),  or  B = M
+ *   W <- W - lr scale O - weight_decay W,   O = B after the steps above
+ *
+ *   W         HOST array of matrices (weights) of one shape and dtype, updated
+ *   G         their gradients: W's shape and dtype, read
+ *   M         their momenta: W's shape, SN_F32, updated (zero before the first step)
+ *   lr, momentum, weight_decay, scale   finite; lr, weight_decay >= 0, 0 <= momentum < 1
+ *   steps, workspace   as in sn_orthogonalize
+ * The decay term has no factor lr, as in sn_adamw_step.  No two of the matrices may
+ * overlap.  Deterministic.  Errors as in sn_orthogonalize. */
+int32_t sn_muon_step(int32_t count, const sn_tensor *W, const sn_tensor *G, const sn_tensor *M,
+                     double lr, double momentum, int32_t nesterov, double weight_decay,
+                     double scale, int32_t steps, void *workspace, size_t workspace_bytes,
+                     sn_stream stream);
 
 /* ------------------------------------------------------------------------ */
 /* Diagnostics.                                                               */

@@ -35,6 +35,15 @@ built the first call raises ``RuntimeError``.
 
     total = sn_grad_sumsq(grads)                     # float64; add it over the ranks
     norm = sn_grad_clip(grads, total, max_norm)      # in place, before the optimizer steps
+
+    Y, H = sn_block_norm(X, R, w, w_post=wp, gate=g) # a block's end: post norm, gate, residual,
+    dX, dR, dg = sn_block_norm_backward(X, H, dY, w, w_post=wp, gate=g)   # and the next norm
+
+    H, G, U = sn_gated_ff(X, Wg, Wu, save=True)      # act(X Wg) * (X Wu)
+    dX, gWg, gWu = sn_gated_ff_backward(X, Wg, Wu, G, U, dH)
+
+    sn_muon_step(weights, grads, momenta, lr)        # orthogonalised updates
+    O = sn_orthogonalize(matrix)
 """
 from __future__ import annotations
 
@@ -121,6 +130,23 @@ _SIGNATURES = {
     "sn_grad_sumsq_workspace_bytes": (_SZ, [_I32, _TENSORS]),
     "sn_grad_sumsq": (_I32, [_I32, _TENSORS, _P, _P, _SZ, _P]),
     "sn_grad_clip": (_I32, [_I32, _TENSORS, _TENSORS, _P, _F64, _P, _P]),
+    "sn_block_norm": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _I64, _I32, _P, _P, _I64, _I32, _F64, _P,
+                             _F64, _P, _I64, _P, _I64, _P]),
+    "sn_block_norm_backward_workspace_bytes": (_SZ, [_I64, _I64, _I32]),
+    "sn_block_norm_backward": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _I64, _I32, _P, _P, _I64, _I32,
+                                      _F64, _P, _F64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P,
+                                      _I64, _P, _P, _P, _P, _SZ, _P]),
+    "sn_gated_ff_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64, _I32, _I32]),
+    "sn_gated_ff_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64, _I64, _I32, _I32]),
+    "sn_gated_ff": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _P, _I64, _I64, _I32, _P, _I64, _P, _P,
+                           _I64, _P, _SZ, _P]),
+    "sn_gated_ff_backward": (_I32, [_P, _I64, _I64, _I64, _I32, _P, _P, _I64, _I64, _I32, _P, _P,
+                                    _I64, _P, _I64, _P, _P, _I64, _P, _I64, _P, _P, _I64, _I32,
+                                    _I32, _P, _SZ, _P]),
+    "sn_orthogonalize_workspace_bytes": (_SZ, [_I32, _I64, _I64]),
+    "sn_orthogonalize": (_I32, [_I32, _TENSORS, _TENSORS, _I32, _P, _SZ, _P]),
+    "sn_muon_step": (_I32, [_I32, _TENSORS, _TENSORS, _TENSORS, _F64, _F64, _I32, _F64, _F64, _I32,
+                            _P, _SZ, _P]),
     "sn_status_string": (ctypes.c_char_p, [_I32]),
     "sn_last_error": (ctypes.c_char_p, []),
     "sn_version": (ctypes.c_char_p, []),
@@ -1087,6 +1113,334 @@ def sn_grad_clip(grads, sumsq: torch.Tensor, max_norm: float, out=None, norm=Non
         _check(lib().sn_grad_clip(len(grads), arr, arr_out, _vec(sumsq, "sumsq", 1, torch.float64),
                                   float(max_norm), _vec(norm, "norm", 1), _stream(stream)))
     return norm
+
+
+# ---------------------------------------------------------------------------
+# a block's end and start, gated feed-forward block, orthogonalised updates
+# ---------------------------------------------------------------------------
+_GATE_FN = {"none": 0, "sigmoid": 1}
+_ACT = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _choice(table, name, what):
+    if name not in table:
+        raise SnError(8, f"{what} must be one of {', '.join(table)}, got {name!r}")
+    return table[name]
+
+
+def _gate(gate, X):
+    """(pointer, row stride) of a gate: d values (stride 0), one row for each token, or None."""
+    if gate is None:
+        return None, 0
+    if gate.dtype != X.dtype:
+        raise SnError(3, f"gate must be {X.dtype}, as the input")
+    if gate.dim() == 1:
+        return _vec(gate, "gate", X.shape[1], X.dtype), 0
+    _out_shape(gate, X.shape, "gate")
+    ptr, _, _, ld = _mat(gate, "gate")
+    return ptr, ld
+
+
+def sn_block_norm(X: torch.Tensor, residual: torch.Tensor, w=None, w_post=None, post: bool = True,
+                  gate=None, gate_fn: str = "none", alpha: float = 1.0, eps: float = 1e-6,
+                  next_norm: bool = True, out=None, resid_out=None, stream=None):
+    """(Y, H): a block's end and the next one's norm, H = alpha residual + g Z with Z = X w_post /
+    rms(X) (X itself with post=False), and Y = H w / rms(H) (None with next_norm=False).  gate:
+    None, d values for all tokens, or a row for each; g is the gate or (gate_fn "sigmoid") its
+    sigmoid.  resid_out may be X or residual."""
+    fn = _choice(_GATE_FN, gate_fn, "gate_fn")
+    if not next_norm and out is not None:
+        raise SnError(2, "out belongs to the next norm")
+    native = _native()
+    if native is not None and next_norm:
+        r = native.block_norm(X, residual, w, w_post, post, gate, fn, alpha, eps, out, resid_out,
+                              stream)
+        if r is not None:
+            return r
+    if residual is None:
+        raise SnError(1, "residual is required")
+    xp, N, d, ldx = _mat(X, "X")
+    dt = _dt(X)
+    with _on(stream, X, residual, w, w_post, gate, out, resid_out):
+        _same_as(X, ("residual", residual), ("out", out), ("resid_out", resid_out))
+        rp, _, _, ldr = _mat(residual, "residual")
+        gp, ldg = _gate(gate, X)
+        if resid_out is None:
+            resid_out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        hp, _, _, ldh = _mat(resid_out, "resid_out")
+        yp, ldy = None, 0
+        if next_norm:
+            if out is None:
+                out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+            yp, _, _, ldy = _mat(out, "out")
+        _check(lib().sn_block_norm(xp, N, d, ldx, dt, rp, ldr, 1 if post else 0,
+                                   _gains(w_post, X, d) if post else None, gp, ldg, fn,
+                                   float(alpha), _gains(w, X, d), float(eps), hp, ldh, yp, ldy,
+                                   _stream(stream)))
+    return out, resid_out
+
+
+def sn_block_norm_backward_workspace_bytes(N: int, d: int, dt: int) -> int:
+    return lib().sn_block_norm_backward_workspace_bytes(N, d, dt)
+
+
+def sn_block_norm_backward(X: torch.Tensor, H: torch.Tensor, dY, w=None, w_post=None,
+                           post: bool = True, gate=None, gate_fn: str = "none", alpha: float = 1.0,
+                           dH=None, eps: float = 1e-6, gw=None, gw_post=None, dgate=None, out=None,
+                           resid_out=None, workspace=None, stream=None):
+    """(dX, dR, dgate): the gradients of sn_block_norm's X, residual and gate from dY (None: 0) and,
+    where h goes on as the residual stream, dH.  gw and gw_post (float32) += the gains' gradients.
+    dgate: with a gate for each token its gradient (a new tensor if none is given, may be the
+    gate); with one gate row a float32 vector that is added to, or None.  out (dX) may be X, dY or
+    dH, resid_out (dR) dY or dH."""
+    fn = _choice(_GATE_FN, gate_fn, "gate_fn")
+    native = _native()
+    if native is not None:
+        r = native.block_norm_backward(X, H, dY, w, w_post, post, gate, fn, alpha, dH, eps, gw,
+                                       gw_post, dgate, out, resid_out, workspace, stream)
+        if r is not None:
+            return r
+    xp, N, d, ldx = _mat(X, "X")
+    dt = _dt(X)
+    with _on(stream, X, H, dY, w, w_post, gate, dH, gw, gw_post, dgate, out, resid_out, workspace):
+        _same_as(X, ("H", H), ("dY", dY), ("dH", dH), ("out", out), ("resid_out", resid_out))
+        hp, _, _, ldh = _mat(H, "H")
+        yp = lddy = dhp = lddh = 0
+        if dY is not None:
+            yp, _, _, lddy = _mat(dY, "dY")
+        if dH is not None:
+            dhp, _, _, lddh = _mat(dH, "dH")
+        gp, ldg = _gate(gate, X)
+        dgp, lddg, rowp = None, 0, None
+        if gate is None:
+            if dgate is not None:
+                raise SnError(2, "dgate without a gate")
+        elif gate.dim() == 1:
+            rowp = _vec(dgate, "dgate", d)
+        else:
+            if dgate is None:
+                dgate = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+            _same_as(X, ("dgate", dgate))
+            dgp, _, _, lddg = _mat(dgate, "dgate")
+        if gw_post is not None and not post:
+            raise SnError(1, "gw_post needs the post norm")
+        if out is None:
+            out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        if resid_out is None:
+            resid_out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        op, _, _, ldo = _mat(out, "out")
+        sp, _, _, lds = _mat(resid_out, "resid_out")
+        sums = (rowp, _vec(gw, "gw", d), _vec(gw_post, "gw_post", d))
+        need = 0
+        if any(p is not None for p in sums):
+            need = sn_block_norm_backward_workspace_bytes(N, d, dt)
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+        ws, have = _workspace(workspace, need)
+        _check(lib().sn_block_norm_backward(xp, N, d, ldx, dt, hp, ldh, 1 if post else 0,
+                                            _gains(w_post, X, d) if post else None, gp, ldg, fn,
+                                            float(alpha), _gains(w, X, d), float(eps), yp or None,
+                                            lddy, dhp or None, lddh, op, ldo, sp, lds, dgp, lddg,
+                                            *sums, ws, have, _stream(stream)))
+    return out, resid_out, dgate
+
+
+def sn_gated_ff_workspace_bytes(N: int, d: int, ff: int, ldx: int, ldw: int, dt: int,
+                                aligned: bool) -> int:
+    return lib().sn_gated_ff_workspace_bytes(N, d, ff, ldx, ldw, dt, 1 if aligned else 0)
+
+
+def sn_gated_ff_backward_workspace_bytes(N: int, d: int, ff: int, ldx: int, ldw: int, ldd: int,
+                                         dt: int, aligned: bool) -> int:
+    return lib().sn_gated_ff_backward_workspace_bytes(N, d, ff, ldx, ldw, ldd, dt,
+                                                      1 if aligned else 0)
+
+
+def _pair(a, b, names, shape, dtype):
+    """(pointers of both, shared row stride) of two matrices of one shape and dtype."""
+    for t, name in zip((a, b), names):
+        if t.dtype != dtype:
+            raise SnError(3, f"{name} must be {dtype}")
+        _out_shape(t, shape, name)
+    ap, rows, _, lda = _mat(a, names[0])
+    bp, _, _, ldb = _mat(b, names[1])
+    if lda != ldb:
+        raise SnError(2, f"{names[0]} and {names[1]} must share a row stride")
+    return ap, bp, lda
+
+
+def _ff_inputs(X, Wg, Wu):
+    """(X, N, d, ldx, dt), (Wg, Wu, ff, ldw) of a feed-forward call."""
+    xp, N, d, ldx = _mat(X, "X")
+    dt = _dt(X)
+    if Wg.dim() != 2:
+        raise SnError(2, "Wg must be a 2-D matrix")
+    ff = Wg.shape[1]
+    wg, wu, ldw = _pair(Wg, Wu, ("Wg", "Wu"), (d, ff), X.dtype)
+    return (xp, N, d, ldx, dt), (wg, wu, ff, ldw)
+
+
+def _on_16(*ptrs):
+    return all(p % 16 == 0 for p in ptrs)
+
+
+def sn_gated_ff(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, act: str = "silu",
+                save: bool = False, out=None, out_g=None, out_u=None, workspace=None, stream=None):
+    """act(X Wg) * (X Wu) (X: N x d, Wg and Wu: d x ff of one row stride); with save (or out_g and
+    out_u, of one row stride) also the two products, (H, G, U), for the backward call.  act: "silu",
+    "gelu" or "relu"."""
+    fn = _choice(_ACT, act, "act")
+    if (out_g is None) != (out_u is None):
+        raise SnError(1, "out_g and out_u: both or neither")
+    native = _native()
+    if native is not None:
+        r = native.gated_ff(X, Wg, Wu, fn, save, out, out_g, out_u, workspace, stream)
+        if r is not None:
+            return r
+    with _on(stream, X, Wg, Wu, out, out_g, out_u, workspace):
+        (xp, N, d, ldx, dt), (wg, wu, ff, ldw) = _ff_inputs(X, Wg, Wu)
+        if out is None:
+            out = torch.empty((N, ff), dtype=X.dtype, device=X.device)
+        if out.dtype != X.dtype:
+            raise SnError(3, f"out must be {X.dtype}, as the input")
+        _out_shape(out, (N, ff), "out")
+        op, _, _, ldo = _mat(out, "out")
+        save = save or out_g is not None
+        gp, up, ldg = None, None, 0
+        if save:
+            if out_g is None:
+                out_g, out_u = (torch.empty((N, ff), dtype=X.dtype, device=X.device)
+                                for _ in range(2))
+            gp, up, ldg = _pair(out_g, out_u, ("out_g", "out_u"), (N, ff), X.dtype)
+        need = sn_gated_ff_workspace_bytes(N, d, ff, ldx, ldw, dt, _on_16(xp, wg, wu))
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+        ws, have = _workspace(workspace, need)
+        _check(lib().sn_gated_ff(xp, N, d, ldx, dt, wg, wu, ff, ldw, fn, op, ldo, gp, up, ldg, ws,
+                                 have, _stream(stream)))
+    return (out, out_g, out_u) if save else out
+
+
+def sn_gated_ff_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: torch.Tensor,
+                         U: torch.Tensor, dH: torch.Tensor, act: str = "silu", dG=None, dU=None,
+                         out=None, gWg=None, gWu=None, accumulate: bool = False, want_dx: bool = True,
+                         want_gw: bool = True, workspace=None, stream=None):
+    """(dX, gWg, gWu) from G and U as sn_gated_ff saved them and dH.  dG and dU receive the two
+    products' gradients (new buffers if none are given; each may be G, U or dH).  gWg and gWu:
+    X's dtype or float32, of one row stride; with accumulate they are added to.  want_dx and
+    want_gw: what is not wanted is None."""
+    fn = _choice(_ACT, act, "act")
+    if (gWg is None) != (gWu is None) or (dG is None) != (dU is None):
+        raise SnError(1, "gWg and gWu, dG and dU: both or neither")
+    if accumulate and want_gw and gWg is None:
+        raise SnError(1, "accumulate needs gWg and gWu")
+    native = _native()
+    if native is not None:
+        r = native.gated_ff_backward(X, Wg, Wu, G, U, dH, fn, dG, dU, out, gWg, gWu, accumulate,
+                                     want_dx, want_gw, workspace, stream)
+        if r is not None:
+            return r
+    with _on(stream, X, Wg, Wu, G, U, dH, dG, dU, out, gWg, gWu, workspace):
+        (xp, N, d, ldx, dt), (wg, wu, ff, ldw) = _ff_inputs(X, Wg, Wu)
+        gp, up, ldg = _pair(G, U, ("G", "U"), (N, ff), X.dtype)
+        if dH.dtype != X.dtype:
+            raise SnError(3, f"dH must be {X.dtype}, as the input")
+        _out_shape(dH, (N, ff), "dH")
+        hp, _, _, lddh = _mat(dH, "dH")
+        if dG is None:
+            dG, dU = (torch.empty((N, ff), dtype=X.dtype, device=X.device) for _ in range(2))
+        dgp, dup, ldd = _pair(dG, dU, ("dG", "dU"), (N, ff), X.dtype)
+        op, ldo = None, 0
+        if want_dx:
+            if out is None:
+                out = torch.empty((N, d), dtype=X.dtype, device=X.device)
+            _same_as(X, ("out", out))
+            op, _, _, ldo = _mat(out, "out")
+        wgp, wup, ldgw, gdt = None, None, 0, dt
+        if want_gw:
+            if gWg is None:
+                gWg, gWu = (torch.empty((d, ff), dtype=X.dtype, device=X.device) for _ in range(2))
+            gdt = _dt(gWg)
+            if gdt not in (dt, SN_F32):
+                raise SnError(3, "gWg must be X's dtype or float32")
+            wgp, wup, ldgw = _pair(gWg, gWu, ("gWg", "gWu"), (d, ff), gWg.dtype)
+        need = sn_gated_ff_backward_workspace_bytes(N, d, ff, ldx, ldw, ldd, dt,
+                                                    _on_16(xp, wg, wu, dgp, dup))
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+        ws, have = _workspace(workspace, need)
+        _check(lib().sn_gated_ff_backward(xp, N, d, ldx, dt, wg, wu, ff, ldw, fn, gp, up, ldg, hp,
+                                          lddh, dgp, dup, ldd, op, ldo, wgp, wup, ldgw, gdt,
+                                          1 if accumulate else 0, ws, have, _stream(stream)))
+    return out if want_dx else None, gWg if want_gw else None, gWu if want_gw else None
+
+
+def sn_orthogonalize_workspace_bytes(count: int, rows: int, cols: int) -> int:
+    return lib().sn_orthogonalize_workspace_bytes(count, rows, cols)
+
+
+def _matrices(ts, name):
+    """sn_tensor array of a list of row-major device matrices."""
+    arr = (_Tensor * max(1, len(ts)))()
+    for i, t in enumerate(ts):
+        ptr, rows, cols, ld = _mat(t, f"{name}[{i}]")
+        arr[i] = _Tensor(ptr if t.numel() else None, rows, cols, ld, _dt(t))
+    return arr
+
+
+def _orth_workspace(mats, workspace):
+    need = sn_orthogonalize_workspace_bytes(len(mats), *mats[0].shape) if mats else 0
+    if need and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=mats[0].device)
+    return _workspace(workspace, need)
+
+
+def sn_orthogonalize(mats, steps: int = 5, out=None, workspace=None, stream=None):
+    """The matrices of the list (or the one matrix) with their singular values taken towards 1 by
+    `steps` Newton-Schulz steps; all of one shape and dtype.  out: a list of as many (or one); each
+    may be the matrix itself."""
+    one = isinstance(mats, torch.Tensor)
+    native = _native()
+    if native is not None and not one:
+        r = native.orthogonalize(mats, steps, out, workspace, stream)
+        if r is not None:
+            return r
+    src = [mats] if one else list(mats)
+    dst = None if out is None else [out] if one else list(out)
+    with _on(stream, *src, *(dst or ()), workspace):
+        a = _matrices(src, "mats")
+        if dst is None:
+            dst = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in src]
+        if len(dst) != len(src):
+            raise SnError(2, f"out must hold {len(src)} matrices, got {len(dst)}")
+        b = _matrices(dst, "out")
+        ws, have = _orth_workspace(src, workspace)
+        _check(lib().sn_orthogonalize(len(src), a, b, int(steps), ws, have, _stream(stream)))
+    return dst[0] if one else dst
+
+
+def sn_muon_step(W, G, M, lr: float, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, scale: float = 1.0, steps: int = 5, workspace=None,
+                 stream=None):
+    """One step of orthogonalised momentum in place on the matrices of the list W (or the one
+    matrix) with gradients G and float32 momenta M: M <- momentum M + G, then W <- W - lr scale
+    O - weight_decay W, O = sn_orthogonalize of G + momentum M (of M without nesterov).  All of one
+    shape; as sn_adamw_step's, the decay has no factor lr.  Returns W."""
+    native = _native()
+    if native is not None and native.muon_step(W, G, M, lr, momentum, nesterov, weight_decay, scale,
+                                               steps, workspace, stream) is not None:
+        return W
+    one = isinstance(W, torch.Tensor)
+    ws_, gs, ms = ([W], [G], [M]) if one else (list(W), list(G), list(M))
+    if len(gs) != len(ws_) or len(ms) != len(ws_):
+        raise SnError(2, f"{len(ws_)} weights, {len(gs)} gradients, {len(ms)} momenta")
+    with _on(stream, *ws_, *gs, *ms, workspace):
+        w, g, m = _matrices(ws_, "W"), _matrices(gs, "G"), _matrices(ms, "M")
+        buf, have = _orth_workspace(ws_, workspace)
+        _check(lib().sn_muon_step(len(ws_), w, g, m, float(lr), float(momentum),
+                                  1 if nesterov else 0, float(weight_decay), float(scale),
+                                  int(steps), buf, have, _stream(stream)))
+    return W
 
 
 def sn_version() -> str:

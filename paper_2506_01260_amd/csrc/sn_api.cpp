@@ -765,7 +765,7 @@ bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) &
 
 // The buffers of a call, for the checks that no output overlaps another buffer.
 struct Buffers {
-  static constexpr int kMost = 12;
+  static constexpr int kMost = 16;
   Span in[kMost], out[kMost];
   int ins = 0, outs = 0;
   void read(Span s) { in[ins++] = s; }
@@ -1219,6 +1219,485 @@ int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out
     return hip_status(sn::launch_clip(t.data(), static_cast<int32_t>(t.size()), in_place, sumsq,
                                       max_norm, norm, static_cast<hipStream_t>(stream)),
                       "sn_grad_clip launch");
+  } catch (const std::exception &) {
+    return fail(SN_ERR_WORKSPACE, "out of host memory");
+  }
+}
+
+}  // extern "C"
+
+// ---- a block's end and start, gated feed-forward block, orthogonalised updates ----
+
+namespace {
+
+// What both calls of the block norm share; gate_cols: 0 for one row.
+int32_t check_block(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, int32_t post,
+                    const void *w_post, const void *gate, int64_t ldgate, int32_t gate_fn,
+                    double alpha, const void *w, double eps) {
+  if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
+  int32_t st = check_rows("X", N, d, ldx);
+  if (st || (gate && ldgate != 0 && (st = check_rows("gate", N, d, ldgate)))) return st;
+  if (gate_fn != SN_GATE_NONE && gate_fn != SN_GATE_SIGMOID)
+    return fail(SN_ERR_UNSUPPORTED, "unknown gate function %d", gate_fn);
+  if (!(alpha >= -3.0e38 && alpha <= 3.0e38)) return fail(SN_ERR_SHAPE, "alpha must be finite");
+  if (!(eps >= 0.0 && eps <= 3.0e38)) return fail(SN_ERR_SHAPE, "eps must be finite and >= 0");
+  if (N == 0) return SN_OK;
+  if (!X) return fail(SN_ERR_NULL, "X is NULL");
+  if (!elem_aligned(X, dt) || !elem_aligned(gate, dt) || !elem_aligned(w, dt) ||
+      !elem_aligned(w_post, dt))
+    return fail(SN_ERR_ALIGN, "X, the gate or a gain vector is not aligned to its element size");
+  (void)post;
+  return SN_OK;
+}
+
+Span gate_span(const void *gate, int64_t N, int64_t d, int64_t ldgate, size_t es) {
+  return ldgate ? span(gate, N, d, ldgate, es) : span(gate, 1, d, d, es);
+}
+
+int32_t check_ff(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *Wg,
+                 const void *Wu, int64_t ff, int64_t ldw, int32_t act) {
+  if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
+  int32_t st = check_rows("X", N, d, ldx);
+  if (st || (st = check_rows("Wg", d, ff, ldw))) return st;
+  if (N > (kMaxElems - 1) / (ff > d ? ff : d) || d > (kMaxElems - 1) / ff)
+    return fail(SN_ERR_SHAPE, "a matrix of 2^40 or more elements");
+  if (act != SN_ACT_SILU && act != SN_ACT_GELU && act != SN_ACT_RELU)
+    return fail(SN_ERR_UNSUPPORTED, "unknown activation %d", act);
+  return SN_OK;
+}
+
+// Two outputs of one row stride, which may be column blocks of one matrix (the gradients of
+// [Wg | Wu] in one buffer): compared by their elements, and as one extent with the rest.
+int32_t check_pair(const char *na, const char *nb, const void *p, const void *q, int64_t rows,
+                   int64_t cols, int64_t ld, size_t es, Buffers &b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+  const uintptr_t lo = x < y ? x : y, hi = x < y ? y : x, row = ld * es, len = cols * es;
+  const Span s = span(reinterpret_cast<const void *>(lo), rows, cols, ld, es);
+  if (hi < s.hi) {
+    const uintptr_t r = rows > 1 ? (hi - lo) % row : hi - lo;
+    if (r < len || (rows > 1 && r + len > row && (hi - lo) / row + 1 < static_cast<uintptr_t>(rows)))
+      return fail(SN_ERR_ALIAS, "%s overlaps %s", na, nb);
+    const Span t = span(reinterpret_cast<const void *>(hi), rows, cols, ld, es);
+    b.write({s.lo, t.hi > s.hi ? t.hi : s.hi});
+    return SN_OK;
+  }
+  b.write(s);
+  b.write(span(reinterpret_cast<const void *>(hi), rows, cols, ld, es));
+  return SN_OK;
+}
+
+// Matrices of one shape and dtype; those of M are float32.  Appends them to t, as outputs
+// (and for `out`, in[i] as the input of out[i]).
+int32_t orth_tensors(const char *name, int32_t count, const sn_tensor *a, const sn_tensor *like,
+                     int32_t dt, std::vector<sn::ClipTensor> &t, const sn_tensor *out = nullptr) {
+  if (!a || (out == nullptr && !like)) return fail(SN_ERR_NULL, "%s is NULL", name);
+  for (int32_t i = 0; i < count; ++i) {
+    const sn_tensor &m = a[i];
+    for (const sn_tensor *q : {&m, out ? &out[i] : &m}) {
+      if (q->dt != dt) return fail(SN_ERR_DTYPE, "%s[%d]: dtype %d, not %d", name, i, q->dt, dt);
+      if (q->rows != like->rows || q->cols != like->cols)
+        return fail(SN_ERR_SHAPE, "%s[%d]: the matrices of a call have one shape", name, i);
+      if (q->rows == 0 || q->cols == 0) continue;
+      if (q->ld < q->cols || q->ld >= kMaxElems)
+        return fail(SN_ERR_SHAPE, "%s[%d]: the row stride must be >= the columns", name, i);
+      if (!q->data) return fail(SN_ERR_NULL, "%s[%d] is NULL", name, i);
+      if (!elem_aligned(q->data, dt))
+        return fail(SN_ERR_ALIGN, "%s[%d] not aligned to its element size", name, i);
+    }
+    sn::ClipTensor c = {};
+    c.g = m.data;
+    c.out = out ? out[i].data : m.data;
+    const int64_t ldo = out ? out[i].ld : m.ld;
+    const bool gaps = m.rows > 1 && (m.ld != m.cols || ldo != m.cols);
+    c.rows = gaps ? m.rows : 1;
+    c.cols = gaps ? m.cols : m.rows * m.cols;
+    c.ldg = gaps ? m.ld : c.cols;
+    c.ldo = gaps ? ldo : c.cols;
+    c.f32 = dt == SN_F32;
+    t.push_back(c);
+  }
+  return SN_OK;
+}
+
+bool orth_shape(int32_t count, int64_t rows, int64_t cols) {
+  return count >= 0 && rows >= 0 && rows < kMaxDim && cols >= 0 && cols < kMaxDim &&
+         (rows == 0 || cols <= (kMaxElems - 1) / rows);
+}
+
+// The checks that both calls on matrices share, and the call, 32 matrices at a time.
+int32_t run_orth(const char *call, int32_t count, const sn_tensor *G, const sn_tensor *M,
+                 const sn_tensor *W, sn::OrthArgs a, void *workspace, size_t workspace_bytes,
+                 sn_stream stream) {
+  if (count < 0) return fail(SN_ERR_SHAPE, "count must be >= 0");
+  if (a.steps < 1 || a.steps > SN_MAX_ORTH_STEPS)
+    return fail(SN_ERR_SHAPE, "steps must lie in [1, %d]", SN_MAX_ORTH_STEPS);
+  if (count == 0) return ok();
+  if (!G || !W || (a.update && !M)) return fail(SN_ERR_NULL, "an array of matrices is NULL");
+  const sn_tensor &like = W[0];
+  if (!dtype_ok(like.dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", like.dt);
+  if (!orth_shape(count, like.rows, like.cols))
+    return fail(SN_ERR_SHAPE, "%lld x %lld out of range", (long long)like.rows,
+                (long long)like.cols);
+  std::vector<sn::ClipTensor> t;
+  int32_t st;
+  if (a.update) {
+    if ((st = orth_tensors("W", count, W, &like, like.dt, t)) ||
+        (st = orth_tensors("G", count, G, &like, like.dt, t)) ||
+        (st = orth_tensors("M", count, M, &like, SN_F32, t)))
+      return st;
+  } else if ((st = orth_tensors("in", count, G, &like, like.dt, t, W))) {
+    return st;
+  }
+  if (like.rows == 0 || like.cols == 0) return ok();
+  const size_t need = sn::orth_workspace_bytes(like.rows, like.cols, count);
+  if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+  if ((st = check_clip_alias(t))) return st;
+  for (const sn::ClipTensor &c : t)
+    if (overlap(clip_span(c, false), bytes_span(workspace, need)) ||
+        overlap(clip_span(c, true), bytes_span(workspace, need)))
+      return fail(SN_ERR_ALIAS, "%s: a matrix overlaps the workspace", call);
+  a.rows = like.rows;
+  a.cols = like.cols;
+  for (int32_t i = 0; i < count; i += sn::OrthMats::kMost) {
+    sn::OrthMats m = {};
+    a.count = count - i < sn::OrthMats::kMost ? count - i : sn::OrthMats::kMost;
+    for (int32_t j = 0; j < a.count; ++j) {
+      m.g[j] = G[i + j].data;
+      m.ldg[j] = G[i + j].ld;
+      m.w[j] = W[i + j].data;
+      m.ldw[j] = W[i + j].ld;
+      if (!a.update) continue;
+      m.m[j] = static_cast<float *>(M[i + j].data);
+      m.ldm[j] = M[i + j].ld;
+    }
+    if ((st = hip_status(sn::launch_orth(like.dt, m, a, workspace, static_cast<hipStream_t>(stream)),
+                         call)))
+      return st;
+  }
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t sn_block_norm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *R,
+                      int64_t ldr, int32_t post, const void *w_post, const void *gate,
+                      int64_t ldgate, int32_t gate_fn, double alpha, const void *w, double eps,
+                      void *H, int64_t ldh, void *Y, int64_t ldy, sn_stream stream) {
+  int32_t st = check_block(X, N, d, ldx, dt, post, w_post, gate, ldgate, gate_fn, alpha, w, eps);
+  if (st || (st = check_rows("R", N, d, ldr)) || (st = check_rows("H", N, d, ldh)) ||
+      (Y && (st = check_rows("Y", N, d, ldy))))
+    return st;
+  if (N == 0) return ok();
+  if (!R || !H) return fail(SN_ERR_NULL, "R or H is NULL");
+  if (!elem_aligned(R, dt) || !elem_aligned(H, dt) || !elem_aligned(Y, dt))
+    return fail(SN_ERR_ALIGN, "R, H or Y not aligned to its element size");
+  const size_t es = elem_size(dt);
+  Buffers b;
+  b.write(span(H, N, d, ldh, es));
+  if (H != X || ldh != ldx) b.read(span(X, N, d, ldx, es));
+  if (H != R || ldh != ldr) b.read(span(R, N, d, ldr, es));
+  b.read(gate_span(gate, N, d, ldgate, es));
+  b.read(span(w, 1, d, d, es));
+  if (post) b.read(span(w_post, 1, d, d, es));
+  b.write(span(Y, N, d, ldy, es));
+  if ((st = b.check("sn_block_norm"))) return st;
+  sn::BlockNormArgs a = {};
+  a.X = X;
+  a.R = R;
+  a.w = w;
+  a.w_post = w_post;
+  a.gate = gate;
+  a.N = N;
+  a.d = d;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.ldgate = ldgate;
+  a.inv_d = static_cast<float>(1.0 / static_cast<double>(d));
+  a.eps = static_cast<float>(eps);
+  a.alpha = static_cast<float>(alpha);
+  a.post = post != 0;
+  a.sigmoid = gate_fn == SN_GATE_SIGMOID;
+  a.H = H;
+  a.Y = Y;
+  a.ldh = ldh;
+  a.ldy = ldy;
+  return hip_status(sn::launch_block_norm(dt, a, static_cast<hipStream_t>(stream)),
+                    "sn_block_norm launch");
+}
+
+size_t sn_block_norm_backward_workspace_bytes(int64_t N, int64_t d, int32_t dt) {
+  if (!dtype_ok(dt) || N < 1 || N >= kMaxDim || d < 1 || d >= kMaxDim) return 0;
+  return sn::block_norm_grad_workspace_bytes(dt, N, d);
+}
+
+int32_t sn_block_norm_backward(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
+                               const void *H, int64_t ldh, int32_t post, const void *w_post,
+                               const void *gate, int64_t ldgate, int32_t gate_fn, double alpha,
+                               const void *w, double eps, const void *dY, int64_t lddy,
+                               const void *dH, int64_t lddh, void *dX, int64_t lddx, void *dR,
+                               int64_t lddr, void *dgate, int64_t lddgate, float *dgate_row,
+                               float *gw, float *gw_post, void *workspace, size_t workspace_bytes,
+                               sn_stream stream) {
+  int32_t st = check_block(X, N, d, ldx, dt, post, w_post, gate, ldgate, gate_fn, alpha, w, eps);
+  if (st || (st = check_rows("H", N, d, ldh)) || (dY && (st = check_rows("dY", N, d, lddy))) ||
+      (dH && (st = check_rows("dH", N, d, lddh))) || (st = check_rows("dX", N, d, lddx)) ||
+      (st = check_rows("dR", N, d, lddr)) ||
+      (dgate && (st = check_rows("dgate", N, d, lddgate))))
+    return st;
+  if (N == 0) return ok();
+  if (!dX || !dR || (dY && !H)) return fail(SN_ERR_NULL, "dX, dR or H is NULL");
+  if ((gw && !dY) || (gw_post && !post))
+    return fail(SN_ERR_NULL, "gw needs dY, gw_post the post norm");
+  if ((dgate && (!gate || ldgate == 0)) || (dgate_row && (!gate || ldgate != 0)))
+    return fail(SN_ERR_SHAPE, "dgate belongs to a gate for each token, dgate_row to one gate row");
+  if (!elem_aligned(H, dt) || !elem_aligned(dY, dt) || !elem_aligned(dH, dt) ||
+      !elem_aligned(dX, dt) || !elem_aligned(dR, dt) || !elem_aligned(dgate, dt))
+    return fail(SN_ERR_ALIGN, "a matrix is not aligned to its element size");
+  if (!aligned(gw, 4) || !aligned(gw_post, 4) || !aligned(dgate_row, 4))
+    return fail(SN_ERR_ALIGN, "a float32 sum is not 4-byte aligned");
+  const size_t es = elem_size(dt);
+  const auto same = [](const void *p, int64_t lp, const void *q, int64_t lq) {
+    return p == q && lp == lq;
+  };
+  Buffers b;
+  b.write(span(dX, N, d, lddx, es));
+  b.write(span(dR, N, d, lddr, es));
+  b.write(span(dgate, N, d, lddgate, es));
+  if (!same(dX, lddx, X, ldx)) b.read(span(X, N, d, ldx, es));
+  if (dY) b.read(span(H, N, d, ldh, es));
+  const bool on_y = same(dX, lddx, dY, lddy) || same(dR, lddr, dY, lddy);
+  const bool on_h = same(dX, lddx, dH, lddh) || same(dR, lddr, dH, lddh);
+  if (dY && !on_y) b.read(span(dY, N, d, lddy, es));
+  if (dH && !on_h) b.read(span(dH, N, d, lddh, es));
+  if (!dgate || !same(dgate, lddgate, gate, ldgate)) b.read(gate_span(gate, N, d, ldgate, es));
+  b.read(span(w, 1, d, d, es));
+  if (post) b.read(span(w_post, 1, d, d, es));
+  b.write(span(gw, 1, d, d, 4));
+  b.write(span(gw_post, 1, d, d, 4));
+  b.write(span(dgate_row, 1, d, d, 4));
+  if (gw || gw_post || dgate_row) {
+    const size_t need = sn::block_norm_grad_workspace_bytes(dt, N, d);
+    if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+    b.write(bytes_span(workspace, need));
+  }
+  if ((st = b.check("sn_block_norm_backward"))) return st;
+  sn::BlockNormGradArgs a = {};
+  a.X = X;
+  a.H = H;
+  a.w = w;
+  a.w_post = w_post;
+  a.gate = gate;
+  a.dY = dY;
+  a.dH = dH;
+  a.N = N;
+  a.d = d;
+  a.ldx = ldx;
+  a.ldh = ldh;
+  a.ldgate = ldgate;
+  a.lddy = lddy;
+  a.lddh = lddh;
+  a.inv_d = static_cast<float>(1.0 / static_cast<double>(d));
+  a.eps = static_cast<float>(eps);
+  a.alpha = static_cast<float>(alpha);
+  a.post = post != 0;
+  a.sigmoid = gate_fn == SN_GATE_SIGMOID;
+  a.dX = dX;
+  a.dR = dR;
+  a.dgate = dgate;
+  a.lddx = lddx;
+  a.lddr = lddr;
+  a.lddg = lddgate;
+  a.sums[0] = gw;
+  a.sums[1] = gw_post;
+  a.sums[2] = dgate_row;
+  return hip_status(
+      sn::launch_block_norm_grad(dt, a, workspace, static_cast<hipStream_t>(stream)),
+      "sn_block_norm_backward launch");
+}
+
+size_t sn_gated_ff_workspace_bytes(int64_t N, int64_t d, int64_t ff, int64_t ldx, int64_t ldw,
+                                   int32_t dt, int32_t aligned) {
+  if (check_ff(nullptr, N, d, ldx, dt, nullptr, nullptr, ff, ldw, SN_ACT_SILU) || N == 0) return 0;
+  sn::FfArgs a = {};
+  a.N = N;
+  a.d = d;
+  a.ff = ff;
+  a.ldx = ldx;
+  a.ldw = ldw;
+  if (!aligned) a.X = a.Wg = reinterpret_cast<const void *>(uintptr_t(2));
+  return sn::ff_workspace_bytes(dt, a);
+}
+
+size_t sn_gated_ff_backward_workspace_bytes(int64_t N, int64_t d, int64_t ff, int64_t ldx,
+                                            int64_t ldw, int64_t ldd, int32_t dt,
+                                            int32_t aligned) {
+  if (check_ff(nullptr, N, d, ldx, dt, nullptr, nullptr, ff, ldw, SN_ACT_SILU) || N == 0 ||
+      ldd < ff || ldd >= kMaxDim)
+    return 0;
+  sn::FfGradArgs a = {};
+  a.N = N;
+  a.d = d;
+  a.ff = ff;
+  a.ldx = ldx;
+  a.ldw = ldw;
+  a.ldd = ldd;
+  if (!aligned) {
+    a.X = a.Wg = reinterpret_cast<const void *>(uintptr_t(2));
+    a.dG = reinterpret_cast<void *>(uintptr_t(2));
+  }
+  return sn::ff_grad_workspace_bytes(dt, a);
+}
+
+int32_t sn_gated_ff(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *Wg,
+                    const void *Wu, int64_t ff, int64_t ldw, int32_t act, void *H, int64_t ldh,
+                    void *G, void *U, int64_t ldg, void *workspace, size_t workspace_bytes,
+                    sn_stream stream) {
+  int32_t st = check_ff(X, N, d, ldx, dt, Wg, Wu, ff, ldw, act);
+  if (st || (st = check_rows("H", N, ff, ldh)) ||
+      ((G || U) && (st = check_rows("G and U", N, ff, ldg))))
+    return st;
+  if (N == 0) return ok();
+  if (!X || !Wg || !Wu || !H || !G != !U)
+    return fail(SN_ERR_NULL, "X, Wg, Wu, H or one of G and U is NULL");
+  for (const void *p : {X, Wg, Wu, static_cast<const void *>(H), static_cast<const void *>(G),
+                        static_cast<const void *>(U)})
+    if (!elem_aligned(p, dt)) return fail(SN_ERR_ALIGN, "a matrix is not aligned to its element size");
+  const size_t es = elem_size(dt);
+  sn::FfArgs a = {};
+  a.X = X;
+  a.Wg = Wg;
+  a.Wu = Wu;
+  a.N = N;
+  a.d = d;
+  a.ff = ff;
+  a.ldx = ldx;
+  a.ldw = ldw;
+  a.act = act;
+  a.H = H;
+  a.G = G;
+  a.U = U;
+  a.ldh = ldh;
+  a.ldg = ldg;
+  const size_t need = sn::ff_workspace_bytes(dt, a);
+  Buffers b;
+  if (need) {
+    if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+    b.write(bytes_span(workspace, need));
+  }
+  b.read(span(X, N, d, ldx, es));
+  b.read(span(Wg, d, ff, ldw, es));
+  b.read(span(Wu, d, ff, ldw, es));
+  b.write(span(H, N, ff, ldh, es));
+  if (G && (st = check_pair("G", "U", G, U, N, ff, ldg, es, b))) return st;
+  if ((st = b.check("sn_gated_ff"))) return st;
+  return hip_status(sn::launch_ff(dt, a, workspace, static_cast<hipStream_t>(stream)),
+                    "sn_gated_ff launch");
+}
+
+int32_t sn_gated_ff_backward(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
+                             const void *Wg, const void *Wu, int64_t ff, int64_t ldw, int32_t act,
+                             const void *G, const void *U, int64_t ldg, const void *dH,
+                             int64_t lddh, void *dG, void *dU, int64_t ldd, void *dX, int64_t lddx,
+                             void *gWg, void *gWu, int64_t ldgw, int32_t gdt, int32_t accumulate,
+                             void *workspace, size_t workspace_bytes, sn_stream stream) {
+  int32_t st = check_ff(X, N, d, ldx, dt, Wg, Wu, ff, ldw, act);
+  if (st || (st = check_rows("G and U", N, ff, ldg)) || (st = check_rows("dH", N, ff, lddh)) ||
+      (st = check_rows("dG and dU", N, ff, ldd)) || (dX && (st = check_rows("dX", N, d, lddx))) ||
+      ((gWg || gWu) && (st = check_rows("gWg and gWu", d, ff, ldgw))))
+    return st;
+  if (!gWg != !gWu) return fail(SN_ERR_NULL, "gWg and gWu: both or neither");
+  if (gWg && gdt != dt && gdt != SN_F32) return fail(SN_ERR_DTYPE, "gdt must be dt or SN_F32");
+  if (N > 0 && (!X || !Wg || !Wu || !G || !U || !dH || !dG || !dU))
+    return fail(SN_ERR_NULL, "an input, dG or dU is NULL");
+  for (const void *p : {X, Wg, Wu, G, U, dH, static_cast<const void *>(dG),
+                        static_cast<const void *>(dU), static_cast<const void *>(dX)})
+    if (!elem_aligned(p, dt)) return fail(SN_ERR_ALIGN, "a matrix is not aligned to its element size");
+  if (gWg && (!elem_aligned(gWg, gdt) || !elem_aligned(gWu, gdt)))
+    return fail(SN_ERR_ALIGN, "gWg or gWu is not aligned to its element size");
+  if (N == 0 && (!gWg || accumulate)) return ok();
+  const size_t es = elem_size(dt);
+  sn::FfGradArgs a = {};
+  a.X = X;
+  a.Wg = Wg;
+  a.Wu = Wu;
+  a.G = G;
+  a.U = U;
+  a.dH = dH;
+  a.N = N;
+  a.d = d;
+  a.ff = ff;
+  a.ldx = ldx;
+  a.ldw = ldw;
+  a.ldg = ldg;
+  a.lddh = lddh;
+  a.act = act;
+  a.dG = dG;
+  a.dU = dU;
+  a.ldd = ldd;
+  a.dX = dX;
+  a.lddx = lddx;
+  a.gWg = gWg;
+  a.gWu = gWu;
+  a.ldgw = ldgw;
+  a.gdt = gdt;
+  a.add = accumulate != 0;
+  const size_t need = N ? sn::ff_grad_workspace_bytes(dt, a) : 0;
+  Buffers b;
+  if (need) {
+    if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+    b.write(bytes_span(workspace, need));
+  }
+  if (dX != X || lddx != ldx || gWg) b.read(span(X, N, d, ldx, es));
+  b.read(span(Wg, d, ff, ldw, es));
+  b.read(span(Wu, d, ff, ldw, es));
+  for (const void *p : {G, U})
+    if (ldg != ldd || (p != dG && p != dU)) b.read(span(p, N, ff, ldg, es));
+  if (lddh != ldd || (dH != dG && dH != dU)) b.read(span(dH, N, ff, lddh, es));
+  if (dX) b.write(span(dX, N, d, lddx, es));
+  if (N && (st = check_pair("dG", "dU", dG, dU, N, ff, ldd, es, b))) return st;
+  if (gWg && (st = check_pair("gWg", "gWu", gWg, gWu, d, ff, ldgw, elem_size(gdt), b))) return st;
+  if ((st = b.check("sn_gated_ff_backward"))) return st;
+  return hip_status(sn::launch_ff_grad(dt, a, workspace, static_cast<hipStream_t>(stream)),
+                    "sn_gated_ff_backward launch");
+}
+
+size_t sn_orthogonalize_workspace_bytes(int32_t count, int64_t rows, int64_t cols) {
+  if (!orth_shape(count, rows, cols) || count == 0 || rows == 0 || cols == 0) return 0;
+  return sn::orth_workspace_bytes(rows, cols, count);
+}
+
+int32_t sn_orthogonalize(int32_t count, const sn_tensor *in, const sn_tensor *out, int32_t steps,
+                         void *workspace, size_t workspace_bytes, sn_stream stream) {
+  try {
+    sn::OrthArgs a = {};
+    a.steps = steps;
+    return run_orth("sn_orthogonalize", count, in, nullptr, out, a, workspace, workspace_bytes,
+                    stream);
+  } catch (const std::exception &) {
+    return fail(SN_ERR_WORKSPACE, "out of host memory");
+  }
+}
+
+int32_t sn_muon_step(int32_t count, const sn_tensor *W, const sn_tensor *G, const sn_tensor *M,
+                     double lr, double momentum, int32_t nesterov, double weight_decay,
+                     double scale, int32_t steps, void *workspace, size_t workspace_bytes,
+                     sn_stream stream) {
+  try {
+    const double most = 3.0e38;
+    if (!(lr >= 0.0 && lr <= most) || !(weight_decay >= 0.0 && weight_decay <= most) ||
+        !(momentum >= 0.0 && momentum < 1.0) || !(scale >= -most && scale <= most) ||
+        !(lr * scale >= -most && lr * scale <= most))
+      return fail(SN_ERR_SHAPE, "need finite lr, weight_decay >= 0, 0 <= momentum < 1, finite scale");
+    sn::OrthArgs a = {};
+    a.steps = steps;
+    a.update = true;
+    a.nesterov = nesterov != 0;
+    a.momentum = static_cast<float>(momentum);
+    a.rate = static_cast<float>(lr * scale);
+    a.decay = static_cast<float>(weight_decay);
+    return run_orth("sn_muon_step", count, G, M, W, a, workspace, workspace_bytes, stream);
   } catch (const std::exception &) {
     return fail(SN_ERR_WORKSPACE, "out of host memory");
   }

@@ -1,0 +1,595 @@
+// The end of a block and the start of the next, N x d:
+//   z = x w1 / sqrt(mean x^2 + eps)  (or z = x),   h = alpha r + g z,
+//   y = h w / sqrt(mean h^2 + eps)
+// with a gate g (or its sigmoid) of one row or of each token.  h is rounded to dt where it
+// is stored; y is made from the 32-bit sum.  Backward, from x and the stored h, with
+// n = h rho, u = dy w, q = 1 / sqrt(mean x^2 + eps), m = x q:
+//   dh = rho (u - n mean(u n)) + dH,   dR = alpha dh,   dg = dh z g',
+//   v = g dh w1,   dX = q (v - m mean(v m))      (dX = g dh without the post norm)
+//   gw += sum dy n,   gw_post += sum g dh m,   one gate row's gradient += sum dg.
+//
+// Memory-bound: each operand passes once, the row staying in registers between its two
+// (backward: two joint) sums and its outputs.  R threads hold a row in K pieces each; with
+// R = 64 a wave has a row of its own and no barrier.
+#include "sn_internal.h"
+#include "sn_rows.h"
+
+namespace sn {
+
+namespace {
+
+__device__ __forceinline__ float sigmoid_of(float g) { return 1.0f / (1.0f + expf(-g)); }
+
+// The gate's row of token i.
+template <typename T, typename A>
+__device__ __forceinline__ const T *gate_row(const A &a, int64_t i) {
+  return static_cast<const T *>(a.gate) + i * a.ldgate;
+}
+
+// n sums over a workgroup of W waves in one barrier; red: W * n floats, free as group_sum's.
+template <int W, int NS>
+__device__ __forceinline__ void group_sums(float (&v)[NS], float (*red)[W]) {
+#pragma unroll
+  for (int s = 0; s < NS; ++s) v[s] = wave_sum(v[s]);
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) red[s][threadIdx.x >> 6] = v[s];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      v[s] = red[s][0];
+#pragma unroll
+      for (int i = 1; i < W; ++i) v[s] += red[s][i];
+    }
+  }
+}
+
+// R threads per row, NT / R rows in a workgroup.
+template <typename T, int R, int K, int NT, bool WHOLE>
+__global__ __launch_bounds__(NT) void block_norm_kernel(BlockNormArgs a) {
+  constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
+  static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
+  __shared__ float red[2][W];
+  const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
+  const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
+  const int64_t i = group_number() * ROWS + sub;
+  if (i >= a.N) return;
+  const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+  const T *Rs = static_cast<const T *>(a.R) + i * a.ldr;
+  const T *w = static_cast<const T *>(a.w), *w1 = static_cast<const T *>(a.w_post);
+  u32x4 xp[K], rp[K], gp[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    xp[k] = take(X, c + k * R * E, d);
+    rp[k] = take(Rs, c + k * R * E, d);
+  }
+  if (a.gate) {
+    const T *G = gate_row<T>(a, i);
+#pragma unroll
+    for (int k = 0; k < K; ++k) gp[k] = take(G, c + k * R * E, d);
+  }
+  float h[K][E], sx = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    Piece<T>::unpack(fix<T, WHOLE>(xp[k], c + k * R * E, d), h[k]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sx = fmaf(h[k][e], h[k][e], sx);
+  }
+  float q = 1.0f;
+  if (a.post) {
+    sx = group_sum<W>(sx, red[0]);
+    q = 1.0f / sqrtf(sx * a.inv_d + a.eps);
+  }
+  float ss = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c0 = c + k * R * E;
+    float t[E];
+    if (a.post) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[k][e] *= q;
+      if (w1) {
+        Piece<T>::unpack(fix<T, WHOLE>(take(w1, c0, d), c0, d), t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[k][e] *= t[e];
+      }
+    }
+    if (a.gate) {
+      Piece<T>::unpack(fix<T, WHOLE>(gp[k], c0, d), t);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[k][e] *= a.sigmoid ? sigmoid_of(t[e]) : t[e];
+    }
+    Piece<T>::unpack(fix<T, WHOLE>(rp[k], c0, d), t);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      h[k][e] = fmaf(a.alpha, t[e], h[k][e]);
+      ss = fmaf(h[k][e], h[k][e], ss);
+    }
+  }
+  // H may lie on X or R, whose last piece other threads load too: past a barrier
+  ss = group_sum<W>(ss, red[1]);
+  T *H = static_cast<T *>(a.H) + i * a.ldh;
+#pragma unroll
+  for (int k = 0; k < K; ++k) put<T, WHOLE>(H, c + k * R * E, d, h[k]);
+  if (!a.Y) return;
+  const float rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+  T *Y = static_cast<T *>(a.Y) + i * a.ldy;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c0 = c + k * R * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[k][e] *= rho;
+    if (w) {
+      float t[E];
+      Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), t);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[k][e] *= t[e];
+    }
+    put<T, WHOLE>(Y, c0, d, h[k]);
+  }
+}
+
+// Rows longer than the registers hold, or shorter than a piece: up to three passes.
+template <typename T>
+__global__ __launch_bounds__(1024) void block_norm_long_kernel(BlockNormArgs a) {
+  constexpr int E = Piece<T>::E, NT = 1024, W = NT / 64;
+  __shared__ float red[2][W];
+  const int64_t i = group_number();
+  if (i >= a.N) return;
+  const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+  const T *Rs = static_cast<const T *>(a.R) + i * a.ldr;
+  const T *w = static_cast<const T *>(a.w), *w1 = static_cast<const T *>(a.w_post);
+  float h[E], t[E], q = 1.0f;
+  if (a.post) {
+    float sx = 0.0f;
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      get(X, c0, a.d, h);
+#pragma unroll
+      for (int e = 0; e < E; ++e) sx = fmaf(h[e], h[e], sx);
+    }
+    sx = group_sum<W>(sx, red[0]);
+    q = 1.0f / sqrtf(sx * a.inv_d + a.eps);
+  }
+  const auto sum = [&](int64_t c0) {
+    get(X, c0, a.d, h);
+    if (a.post) {
+      if (w1) get(w1, c0, a.d, t);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] = w1 ? h[e] * q * t[e] : h[e] * q;
+    }
+    if (a.gate) {
+      get(gate_row<T>(a, i), c0, a.d, t);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] *= a.sigmoid ? sigmoid_of(t[e]) : t[e];
+    }
+    get(Rs, c0, a.d, t);
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] = fmaf(a.alpha, t[e], h[e]);
+  };
+  float rho = 1.0f;
+  if (a.Y) {
+    float ss = 0.0f;
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      sum(c0);
+#pragma unroll
+      for (int e = 0; e < E; ++e) ss = fmaf(h[e], h[e], ss);
+    }
+    ss = group_sum<W>(ss, red[1]);
+    rho = 1.0f / sqrtf(ss * a.inv_d + a.eps);
+  }
+  // H may lie on X or R: each thread has read what it writes over
+  for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+    sum(c0);
+    put(static_cast<T *>(a.H) + i * a.ldh, c0, a.d, h);
+    if (!a.Y) continue;
+    if (w) get(w, c0, a.d, t);
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] = w ? h[e] * rho * t[e] : h[e] * rho;
+    put(static_cast<T *>(a.Y) + i * a.ldy, c0, a.d, h);
+  }
+}
+
+// Backward.  A workgroup takes the rows blockIdx.x, + gridDim.x, ... and keeps its parts of
+// the three column sums in registers; block_sum_kernel adds the parts.
+enum { kGw = 0, kGwPost = 1, kGate = 2 };
+
+template <typename T, int R, int K, int NT, bool WHOLE>
+__global__ __launch_bounds__(NT) void block_norm_grad_kernel(BlockNormGradArgs a) {
+  constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
+  static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
+  __shared__ float red[3][W], red2[1][W];
+  const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
+  const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
+  const T *w = static_cast<const T *>(a.w), *w1 = static_cast<const T *>(a.w_post);
+  float sum[3][K][E] = {};
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + sub; i < a.N;
+       i += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+    u32x4 xp[K], hp[K], yp[K], dp[K], gp[K];
+    const bool need_x = a.post || a.gate;
+    if (need_x) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) xp[k] = take(X, c + k * R * E, d);
+    }
+    if (a.dY) {
+      const T *H = static_cast<const T *>(a.H) + i * a.ldh;
+      const T *dY = static_cast<const T *>(a.dY) + i * a.lddy;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        hp[k] = take(H, c + k * R * E, d);
+        yp[k] = take(dY, c + k * R * E, d);
+      }
+    }
+    if (a.dH) {
+      const T *dH = static_cast<const T *>(a.dH) + i * a.lddh;
+#pragma unroll
+      for (int k = 0; k < K; ++k) dp[k] = take(dH, c + k * R * E, d);
+    }
+    if (a.gate) {
+      const T *G = gate_row<T>(a, i);
+#pragma unroll
+      for (int k = 0; k < K; ++k) gp[k] = take(G, c + k * R * E, d);
+    }
+    float x[E], h[E], y[E], t[E], s[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c0 = c + k * R * E;
+      if (need_x) {
+        xp[k] = fix<T, WHOLE>(xp[k], c0, d);
+        Piece<T>::unpack(xp[k], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+      }
+      if (a.dY) {
+        hp[k] = fix<T, WHOLE>(hp[k], c0, d);
+        yp[k] = fix<T, WHOLE>(yp[k], c0, d);
+        Piece<T>::unpack(hp[k], h);
+        Piece<T>::unpack(yp[k], y);
+        if (w) {
+          Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), t);
+#pragma unroll
+          for (int e = 0; e < E; ++e) y[e] *= t[e];
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          s[1] = fmaf(h[e], h[e], s[1]);
+          s[2] = fmaf(y[e], h[e], s[2]);
+        }
+      }
+    }
+    group_sums<W>(s, red);
+    const float q = a.post ? 1.0f / sqrtf(s[0] * a.inv_d + a.eps) : 1.0f;
+    const float rho = 1.0f / sqrtf(s[1] * a.inv_d + a.eps), f = s[2] * a.inv_d * rho;
+    T *dR = static_cast<T *>(a.dR) + i * a.lddr;
+    T *dX = static_cast<T *>(a.dX) + i * a.lddx;
+    float v[K][E], sv[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c0 = c + k * R * E;
+      float o[E];
+      if (a.dH) {
+        Piece<T>::unpack(fix<T, WHOLE>(dp[k], c0, d), o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.0f;
+      }
+      if (a.dY) {
+        Piece<T>::unpack(hp[k], h);
+        Piece<T>::unpack(yp[k], y);
+        if (w) Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float n = h[e] * rho;
+          sum[kGw][k][e] = fmaf(y[e], n, sum[kGw][k][e]);
+          o[e] = fmaf(rho, fmaf(-n, f, w ? y[e] * t[e] : y[e]), o[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] = a.alpha * o[e];
+      put<T, WHOLE>(dR, c0, d, h);
+      // from here on x holds m (or x), t the post norm's gains
+      if (need_x) {
+        Piece<T>::unpack(xp[k], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] *= q;
+      }
+      if (a.post && w1) {
+        Piece<T>::unpack(fix<T, WHOLE>(take(w1, c0, d), c0, d), t);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) t[e] = 1.0f;
+      }
+      if (a.gate) {
+        float g[E];
+        Piece<T>::unpack(fix<T, WHOLE>(gp[k], c0, d), g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          float slope = 1.0f;
+          if (a.sigmoid) {
+            g[e] = sigmoid_of(g[e]);
+            slope = g[e] * (1.0f - g[e]);
+          }
+          y[e] = o[e] * x[e] * t[e] * slope;
+          o[e] *= g[e];
+        }
+        if (a.dgate) {
+          put<T, WHOLE>(static_cast<T *>(a.dgate) + i * a.lddg, c0, d, y);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[kGate][k][e] += y[e];
+        }
+      }
+      if (a.post) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          sum[kGwPost][k][e] = fmaf(o[e], x[e], sum[kGwPost][k][e]);
+          v[k][e] = o[e] * t[e];
+          sv[0] = fmaf(v[k][e], x[e], sv[0]);
+        }
+      } else {
+        put<T, WHOLE>(dX, c0, d, o);
+      }
+    }
+    if (a.post) {
+      group_sums<W>(sv, red2);
+      const float f1 = sv[0] * a.inv_d;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        Piece<T>::unpack(xp[k], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = q * fmaf(-x[e] * q, f1, v[k][e]);
+        put<T, WHOLE>(dX, c + k * R * E, d, x);
+      }
+    } else if constexpr (W > 1) {
+      __syncthreads();  // red is used again
+    }
+  }
+  if (!a.part) return;
+  float *part = a.part + static_cast<int64_t>(blockIdx.x) * a.d;
+#pragma unroll
+  for (int q = 0; q < 3; ++q, part += static_cast<int64_t>(gridDim.x) * a.d) {
+    if (!a.sums[q]) continue;
+    if constexpr (ROWS == 1) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int c0 = c + k * R * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (c0 + e < d) part[c0 + e] = sum[q][k][e];
+      }
+    } else {  // the waves' rows are added in order
+      __shared__ float rows[ROWS][K * R * E];
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) rows[sub][c + k * R * E + e] = sum[q][k][e];
+      __syncthreads();
+      for (int j = threadIdx.x; j < d; j += NT) {
+        float t = rows[0][j];
+#pragma unroll
+        for (int p = 1; p < ROWS; ++p) t += rows[p][j];
+        part[j] = t;
+      }
+    }
+  }
+}
+
+// Rows longer than the registers hold, or shorter than a piece: the parts of the sums are
+// kept in the workspace between the workgroup's rows.
+template <typename T>
+__global__ __launch_bounds__(1024) void block_norm_grad_long_kernel(BlockNormGradArgs a) {
+  constexpr int E = Piece<T>::E, NT = 1024, W = NT / 64;
+  __shared__ float red[3][W], red2[1][W];
+  const T *w = static_cast<const T *>(a.w), *w1 = static_cast<const T *>(a.w_post);
+  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
+    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
+    const T *H = static_cast<const T *>(a.H) + i * a.ldh;
+    const T *dY = a.dY ? static_cast<const T *>(a.dY) + i * a.lddy : nullptr;
+    const T *dH = a.dH ? static_cast<const T *>(a.dH) + i * a.lddh : nullptr;
+    float x[E], h[E], y[E], t[E], s[3] = {0.0f, 0.0f, 0.0f};
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      if (a.post) {
+        get(X, c0, a.d, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+      }
+      if (dY) {
+        get(H, c0, a.d, h);
+        get(dY, c0, a.d, y);
+        if (w) get(w, c0, a.d, t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          s[1] = fmaf(h[e], h[e], s[1]);
+          s[2] = fmaf(w ? y[e] * t[e] : y[e], h[e], s[2]);
+        }
+      }
+    }
+    group_sums<W>(s, red);
+    const float q = a.post ? 1.0f / sqrtf(s[0] * a.inv_d + a.eps) : 1.0f;
+    const float rho = 1.0f / sqrtf(s[1] * a.inv_d + a.eps), f = s[2] * a.inv_d * rho;
+    // o: dh, x: m (or x), t: the post norm's gains, g: the gate, all of this column
+    float o[E], g[E], slope[E], n[E];
+    const auto column = [&](int64_t c0) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = n[e] = y[e] = 0.0f;
+      if (dH) get(dH, c0, a.d, o);
+      if (dY) {
+        get(H, c0, a.d, h);
+        get(dY, c0, a.d, y);
+        if (w) get(w, c0, a.d, t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          n[e] = h[e] * rho;
+          o[e] = fmaf(rho, fmaf(-n[e], f, w ? y[e] * t[e] : y[e]), o[e]);
+        }
+      }
+      get(X, c0, a.d, x);
+      if (w1) get(w1, c0, a.d, t);
+      if (a.gate) get(gate_row<T>(a, i), c0, a.d, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[e] *= q;
+        if (!a.post || !w1) t[e] = 1.0f;
+        slope[e] = 1.0f;
+        if (!a.gate) g[e] = 1.0f;
+        if (a.gate && a.sigmoid) {
+          g[e] = sigmoid_of(g[e]);
+          slope[e] = g[e] * (1.0f - g[e]);
+        }
+      }
+    };
+    float f1 = 0.0f;
+    if (a.post) {
+      float sv[1] = {0.0f};
+      for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+        column(c0);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sv[0] = fmaf(o[e] * g[e] * t[e], x[e], sv[0]);
+      }
+      group_sums<W>(sv, red2);
+      f1 = sv[0] * a.inv_d;
+    } else {
+      __syncthreads();  // red is used again
+    }
+    const bool first = i == blockIdx.x;
+    float *part = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
+    const auto add = [&](int which, int64_t col, float v) {
+      if (!part || !a.sums[which] || col >= a.d) return;
+      float *p = part + which * static_cast<int64_t>(gridDim.x) * a.d + col;
+      *p = (first ? 0.0f : *p) + v;
+    };
+    for (int64_t c0 = threadIdx.x * E; c0 < a.d; c0 += NT * E) {
+      column(c0);
+      float r[E], dg[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        r[e] = a.alpha * o[e];
+        dg[e] = o[e] * x[e] * t[e] * slope[e];
+        const float dz = o[e] * g[e];
+        add(kGw, c0 + e, y[e] * n[e]);
+        add(kGwPost, c0 + e, dz * x[e]);
+        add(kGate, c0 + e, dg[e]);
+        o[e] = a.post ? q * fmaf(-x[e], f1, dz * t[e]) : dz;
+      }
+      put(static_cast<T *>(a.dR) + i * a.lddr, c0, a.d, r);
+      if (a.dgate) put(static_cast<T *>(a.dgate) + i * a.lddg, c0, a.d, dg);
+      put(static_cast<T *>(a.dX) + i * a.lddx, c0, a.d, o);
+    }
+  }
+}
+
+// sums[q][c] += sum over the parts, in float64 and in a fixed order: 32 groups of threads
+// take every 32nd part of 32 columns, then the groups in order.
+constexpr int kSumCols = 32, kSumGroups = 32;
+__global__ __launch_bounds__(kSumCols *kSumGroups) void block_sum_kernel(const float *__restrict__ part,
+                                                                         int64_t parts, int64_t d,
+                                                                         BlockNormGradArgs a) {
+  __shared__ double red[kSumGroups][kSumCols];
+  const int64_t blocks = (d + kSumCols - 1) / kSumCols, id = group_number();
+  if (id >= 3 * blocks) return;
+  const int which = static_cast<int>(id / blocks);
+  float *to = which == 0 ? a.sums[0] : which == 1 ? a.sums[1] : a.sums[2];
+  if (!to) return;
+  part += which * parts * d;
+  const int lane = threadIdx.x % kSumCols, g = threadIdx.x / kSumCols;
+  const int64_t c = (id - which * blocks) * kSumCols + lane;
+  double s = 0.0;
+  if (c < d) {
+#pragma unroll 8
+    for (int64_t b = g; b < parts; b += kSumGroups) s += static_cast<double>(part[b * d + c]);
+  }
+  red[g][lane] = s;
+  __syncthreads();
+  if (g != 0 || c >= d) return;
+#pragma unroll
+  for (int i = 1; i < kSumGroups; ++i) s += red[i][lane];
+  to[c] = static_cast<float>(static_cast<double>(to[c]) + s);
+}
+
+template <typename T, bool WHOLE>
+hipError_t launch_norm_t(const BlockNormArgs &a, hipStream_t s) {
+  const int64_t n = ceil_div(a.d, Piece<T>::E);
+  const auto grid = [&](int rows) { return groups_grid(ceil_div(a.N, rows)); };
+  if (a.d < Piece<T>::E)  // no whole piece to take
+    block_norm_long_kernel<T><<<grid(1), 1024, 0, s>>>(a);
+  else if (n <= 64)
+    block_norm_kernel<T, 64, 1, 256, WHOLE><<<grid(4), 256, 0, s>>>(a);
+  else if (n <= 128)
+    block_norm_kernel<T, 64, 2, 256, WHOLE><<<grid(4), 256, 0, s>>>(a);
+  else if (n <= 256)
+    block_norm_kernel<T, 64, 4, 256, WHOLE><<<grid(4), 256, 0, s>>>(a);
+  else if (n <= 512)
+    block_norm_kernel<T, 256, 2, 256, WHOLE><<<grid(1), 256, 0, s>>>(a);
+  else if (n <= 768)
+    block_norm_kernel<T, 256, 3, 256, WHOLE><<<grid(1), 256, 0, s>>>(a);
+  else if (n <= 1024)
+    block_norm_kernel<T, 512, 2, 512, WHOLE><<<grid(1), 512, 0, s>>>(a);
+  else if (n <= 1536)
+    block_norm_kernel<T, 512, 3, 512, WHOLE><<<grid(1), 512, 0, s>>>(a);
+  else if (n <= 2048)
+    block_norm_kernel<T, 512, 4, 512, WHOLE><<<grid(1), 512, 0, s>>>(a);
+  else
+    block_norm_long_kernel<T><<<grid(1), 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+int64_t pieces_of(int dt, int64_t d) { return ceil_div(d, dt == 0 ? 4 : 8); }
+// Workgroups of the backward, each with a part of the column sums.
+int64_t grad_groups(int dt, int64_t N, int64_t d) {
+  const int64_t n = pieces_of(dt, d), groups = ceil_div(N, n <= 256 ? 4 : 1);
+  return groups < 512 ? groups : 512;
+}
+
+template <typename T, bool WHOLE>
+hipError_t launch_grad_t(int dt, const BlockNormGradArgs &a, hipStream_t s) {
+  const int64_t n = ceil_div(a.d, Piece<T>::E);
+  const unsigned g = static_cast<unsigned>(grad_groups(dt, a.N, a.d));
+  if (a.d < Piece<T>::E)
+    block_norm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
+  else if (n <= 64)
+    block_norm_grad_kernel<T, 64, 1, 256, WHOLE><<<g, 256, 0, s>>>(a);
+  else if (n <= 128)
+    block_norm_grad_kernel<T, 64, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
+  else if (n <= 256)
+    block_norm_grad_kernel<T, 64, 4, 256, WHOLE><<<g, 256, 0, s>>>(a);
+  else if (n <= 512)
+    block_norm_grad_kernel<T, 256, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
+  else if (n <= 1024)
+    block_norm_grad_kernel<T, 512, 2, 512, WHOLE><<<g, 512, 0, s>>>(a);
+  else if (n <= 2048)
+    block_norm_grad_kernel<T, 1024, 2, 1024, WHOLE><<<g, 1024, 0, s>>>(a);
+  else
+    block_norm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_block_norm(int dt, const BlockNormArgs &a, hipStream_t s) {
+  if (dt == 0)
+    return a.d % 4 == 0 ? launch_norm_t<float, true>(a, s) : launch_norm_t<float, false>(a, s);
+  return a.d % 8 == 0 ? launch_norm_t<bf16_t, true>(a, s) : launch_norm_t<bf16_t, false>(a, s);
+}
+
+size_t block_norm_grad_workspace_bytes(int dt, int64_t N, int64_t d) {
+  return align256(static_cast<size_t>(grad_groups(dt, N, d)) * d * sizeof(float) * 3);
+}
+
+hipError_t launch_block_norm_grad(int dt, BlockNormGradArgs a, void *ws, hipStream_t s) {
+  const bool sums = a.sums[0] || a.sums[1] || a.sums[2];
+  a.part = sums ? static_cast<float *>(ws) : nullptr;
+  hipError_t e;
+  if (dt == 0)
+    e = a.d % 4 == 0 ? launch_grad_t<float, true>(dt, a, s) : launch_grad_t<float, false>(dt, a, s);
+  else
+    e = a.d % 8 == 0 ? launch_grad_t<bf16_t, true>(dt, a, s) : launch_grad_t<bf16_t, false>(dt, a, s);
+  if (e != hipSuccess || !sums) return e;
+  block_sum_kernel<<<groups_grid(3 * ceil_div(a.d, kSumCols)), kSumCols * kSumGroups, 0, s>>>(
+      a.part, grad_groups(dt, a.N, a.d), a.d, a);
+  return hipGetLastError();
+}
+
+}  // namespace sn

@@ -1,0 +1,670 @@
+// The gated feed-forward block of N tokens:
+//   G = X Wg,  U = X Wu,  H = act(G) * U              X: N x d, Wg, Wu: d x ff
+// and its backward from the stored G and U,
+//   dG = dH U act'(G),  dU = dH act(G),
+//   dX = dG Wg^T + dU Wu^T,  gWg = X^T dG,  gWu = X^T dU.
+//
+// Forward: one kernel takes both products, a wave holding the same columns of G and U,
+// and writes H from the 32-bit sums.  Backward: dG and dU are made once, elementwise, and
+// rounded to dt, the operands' type of the three products that read them (dX as one
+// product over 2 ff, both weights' gradients in one launch).
+// float32 operands are split in three bf16 planes (24 bits together, hi + mid + lo) and
+// the six products down to 2^-24 of the largest are added up: 2.5 times the rate of
+// the float32 matrix instructions.  Matrices that are not 16-byte aligned, or
+// whose rows are no multiple of 8 elements, are copied to padded rows first.
+#include <initializer_list>
+
+#include "sn_internal.h"
+#include "sn_mm.h"
+#include "sn_rows.h"
+
+namespace sn {
+
+namespace {
+
+// ---- activations -------------------------------------------------------------------
+__device__ __forceinline__ float ff_act(int act, float g) {
+  if (act == kActRelu) return g < 0.0f ? 0.0f : g;
+  if (act == kActSilu) return g / (1.0f + expf(-g));
+  return 0.5f * g * erfcf(-0.70710678f * g);
+}
+// act and its derivative
+__device__ __forceinline__ void ff_act2(int act, float g, float &a, float &da) {
+  if (act == kActRelu) {
+    a = g < 0.0f ? 0.0f : g;
+    da = g > 0.0f ? 1.0f : 0.0f;
+  } else if (act == kActSilu) {
+    const float p = 1.0f / (1.0f + expf(-g));
+    a = g * p;
+    da = p * (1.0f + g * (1.0f - p));
+  } else {
+    const float p = 0.5f * erfcf(-0.70710678f * g);
+    a = g * p;
+    da = fmaf(0.39894228f * g, expf(-0.5f * g * g), p);
+  }
+}
+
+// ---- eight values of a row -----------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ void get8(const T *row, int64_t c, int64_t n, float (&x)[8]) {
+  constexpr int E = Piece<T>::E;
+#pragma unroll
+  for (int h = 0; h < 8 / E; ++h) {
+    float v[E];
+    if (c + 8 <= n)
+      Piece<T>::unpack(load_piece(row + c + h * E), v);
+    else
+      load_part(row, c + h * E, n, 0.0f, v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[h * E + e] = v[e];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void put8(T *row, int64_t c, int64_t n, const float (&x)[8]) {
+  constexpr int E = Piece<T>::E;
+#pragma unroll
+  for (int h = 0; h < 8 / E; ++h) {
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = x[h * E + e];
+    if (c + 8 <= n)
+      store_piece(row + c + h * E, Piece<T>::pack(v));
+    else
+      store_part(row, c + h * E, n, v);
+  }
+}
+// A value's bf16, as a float; the next one towards 0 where that would be infinite.
+__device__ __forceinline__ float bf16_near(float v) {
+  const float r = __uint_as_float(pack_bf16x2(0.0f, v) & 0xFFFF0000u);
+  return fabsf(r) == INFINITY ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : r;
+}
+// The planes of eight values: bf16 as it is, float32 as three bf16 that add up to it
+// exactly (8 bits each, signed), the second times 2^7 and the third times 2^14: at most a
+// quarter of the first, so that their products do not overflow before it does, and no
+// smaller than it by more than their leading zeros.  An infinity or a NaN has nothing left
+// after the first.
+constexpr float kUp = 128.0f;
+template <typename T>
+__device__ __forceinline__ void put_planes(uint16_t *to, int64_t plane, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<u32x4 *>(to) = Piece<bf16_t>::pack(x);
+  } else {
+    float h[8], m[8], l[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      h[e] = bf16_near(x[e]);
+      const float r = fabsf(x[e]) <= 3.4028235e38f ? x[e] - h[e] : 0.0f;
+      m[e] = bf16_near(r);
+      l[e] = (r - m[e]) * (kUp * kUp);
+      m[e] *= kUp;
+    }
+    *reinterpret_cast<u32x4 *>(to) = Piece<bf16_t>::pack(h);
+    *reinterpret_cast<u32x4 *>(to + plane) = Piece<bf16_t>::pack(m);
+    *reinterpret_cast<u32x4 *>(to + 2 * plane) = Piece<bf16_t>::pack(l);
+  }
+}
+
+// ---- operands in padded planes -----------------------------------------------------------
+// rows x cols (stride ld) to planes of rows x ldp, ldp = cols up to a multiple of 8, 0 in
+// the columns past cols.
+template <typename T>
+__global__ __launch_bounds__(256) void ff_pack_kernel(const T *src, int64_t rows, int64_t cols,
+                                                      int64_t ld, uint16_t *dst, int64_t ldp) {
+  const int64_t id = group_number() * 256 + threadIdx.x, per = ldp / 8;
+  const int64_t r = id / per, c = (id - r * per) * 8;
+  if (r >= rows) return;
+  float x[8];
+  get8(src + r * ld, c, cols, x);
+  put_planes<T>(dst + r * ldp + c, rows * ldp, x);
+}
+
+// dG and dU, eight columns a thread; with planes, also as operands.
+template <typename T>
+__global__ __launch_bounds__(256) void ff_dact_kernel(FfGradArgs a, uint16_t *pg, uint16_t *pu,
+                                                      int64_t ldp) {
+  const int64_t id = group_number() * 256 + threadIdx.x, per = (a.ff + 7) / 8;
+  const int64_t r = id / per, c = (id - r * per) * 8;
+  if (r >= a.N) return;
+  float g[8], u[8], h[8], dg[8], du[8];
+  get8(static_cast<const T *>(a.G) + r * a.ldg, c, a.ff, g);
+  get8(static_cast<const T *>(a.U) + r * a.ldg, c, a.ff, u);
+  get8(static_cast<const T *>(a.dH) + r * a.lddh, c, a.ff, h);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float f, df;
+    ff_act2(a.act, g[e], f, df);
+    dg[e] = h[e] * u[e] * df;
+    du[e] = h[e] * f;
+  }
+  put8(static_cast<T *>(a.dG) + r * a.ldd, c, a.ff, dg);
+  put8(static_cast<T *>(a.dU) + r * a.ldd, c, a.ff, du);
+  if (pg) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e >= a.ff) dg[e] = du[e] = 0.0f;
+    put_planes<T>(pg + r * ldp + c, a.N * ldp, dg);
+    put_planes<T>(pu + r * ldp + c, a.N * ldp, du);
+  }
+}
+
+// ---- four sums of a row -------------------------------------------------------------------
+typedef uint32_t quad_b16 __attribute__((ext_vector_type(2), aligned(2)));
+typedef float quad_b32 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+__device__ __forceinline__ void put4(T *p, int64_t left, f32x4 v) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<quad_b16 *>(p) = quad_b16{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+    else
+      *reinterpret_cast<quad_b32 *>(p) = quad_b32{v.x, v.y, v.z, v.w};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) p[e] = from_f32<T>(v[e]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ f32x4 get4(const T *p, int64_t left) {
+  f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < left) v[e] = to_f32(p[e]);
+  return v;
+}
+
+// ---- forward: both products and the activation ------------------------------------------
+template <class S, typename T>
+__global__ __launch_bounds__(S::NT, S::NT / 256) void ff_kernel(MmArgs m, FfArgs a, int64_t gm,
+                                                               int64_t gn, int splits) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  constexpr int HALF = S::PAIR / 2, TP = S::TN / 2;
+  const int64_t tiles = gm * gn, id = mm_order(group_number(), tiles * splits);
+  if (group_number() >= tiles * splits) return;
+  const int64_t split = id / tiles, steps = mm_steps(m);
+  int64_t tm, tn;
+  mm_place(id - split * tiles, gm, gn, tm, tn);
+  f32x4 acc[S::TM][S::TN];
+  mm_tile<S>(m, tm * S::BM, tn * (S::BN / 2), split * steps / splits, (split + 1) * steps / splits,
+             lds, acc);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row0 = tm * S::BM + wave / S::WN * (S::BM / S::WM) + (lane & 15);
+  const int64_t col0 = tn * (S::BN / 2) + wave % S::WN * HALF + 4 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int64_t row = row0 + i * 16;
+    if (row >= a.N) continue;
+#pragma unroll
+    for (int j = 0; j < TP; ++j) {
+      const int64_t col = col0 + j * 16, left = a.ff - col;
+      if (left <= 0) continue;
+      const f32x4 g = acc[i][j], u = acc[i][j + TP];
+      if (splits > 1) {
+        float *p = a.part + (split * 2 * a.N + row) * a.ff + col;
+        put4(p, left, g);
+        put4(p + a.N * a.ff, left, u);
+        continue;
+      }
+      f32x4 h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = ff_act(a.act, g[e]) * u[e];
+      put4(static_cast<T *>(a.H) + row * a.ldh + col, left, h);
+      if (a.G) {
+        put4(static_cast<T *>(a.G) + row * a.ldg + col, left, g);
+        put4(static_cast<T *>(a.U) + row * a.ldg + col, left, u);
+      }
+    }
+  }
+}
+
+// H (G, U) from the parts of the sums: parts x {G, U} x N x ff, added in order.
+template <typename T>
+__global__ __launch_bounds__(256) void ff_join_kernel(FfArgs a, int parts) {
+  const int64_t id = group_number() * 256 + threadIdx.x, per = (a.ff + 3) / 4;
+  const int64_t r = id / per, c = (id - r * per) * 4, left = a.ff - c;
+  if (r >= a.N) return;
+  f32x4 g = {0, 0, 0, 0}, u = {0, 0, 0, 0};
+  const float *p = a.part + r * a.ff + c;
+  for (int q = 0; q < parts; ++q, p += 2 * a.N * a.ff) {
+    g += get4(p, left);
+    u += get4(p + a.N * a.ff, left);
+  }
+  f32x4 h;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = ff_act(a.act, g[e]) * u[e];
+  put4(static_cast<T *>(a.H) + r * a.ldh + c, left, h);
+  if (a.G) {
+    put4(static_cast<T *>(a.G) + r * a.ldg + c, left, g);
+    put4(static_cast<T *>(a.U) + r * a.ldg + c, left, u);
+  }
+}
+
+// ---- forward of up to 8 tokens: the weights stream by -----------------------------------
+// A workgroup takes 64 columns of both weights and a slice of d; a lane takes 16 bytes of
+// a weight's row, the lanes beside it the rest of the row's 64 columns and further rows.
+// Columns past ff: the row's last piece, whose values are stored by two lanes alike.
+constexpr int kVecCols = 64, kVecSlice = 1024;
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void ff_vec_kernel(FfArgs a, int slices) {
+  constexpr int E = Piece<T>::E, LANES = kVecCols / E, ROWS = 64 / LANES, STEP = ROWS * 4, UN = 4;
+  __shared__ __attribute__((aligned(16))) float xs[kVecSlice * NB];
+  __shared__ float red[4][NB][2][kVecCols];
+  const int64_t strips = (a.ff + kVecCols - 1) / kVecCols, id = group_number();
+  if (id >= strips * slices) return;
+  const int64_t slice = id / strips, strip = id - slice * strips;
+  const int64_t k0 = slice * a.d / slices, k1 = (slice + 1) * a.d / slices;
+  const int len = static_cast<int>(k1 - k0), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int i = threadIdx.x; i < len * NB; i += 256) {
+    const int t = i / len, k = i - t * len;
+    xs[k * NB + t] = t < a.N ? to_f32(static_cast<const T *>(a.X)[t * a.ldx + k0 + k]) : 0.0f;
+  }
+  __syncthreads();
+  const int64_t c = strip * kVecCols + lane % LANES * E, cb = c < a.ff - E ? c : a.ff - E;
+  const int row = wave * ROWS + lane / LANES;
+  const T *wg = static_cast<const T *>(a.Wg) + (k0 + row) * a.ldw + cb;
+  const int64_t twin = static_cast<const T *>(a.Wu) - static_cast<const T *>(a.Wg);
+  float acc[NB][2][E] = {};
+  const auto add = [&](int k, u32x4 vg, u32x4 vu) {
+    float g[E], u[E];
+    Piece<T>::unpack(vg, g);
+    Piece<T>::unpack(vu, u);
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      const float x = xs[k * NB + t];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        acc[t][0][e] = fmaf(x, g[e], acc[t][0][e]);
+        acc[t][1][e] = fmaf(x, u[e], acc[t][1][e]);
+      }
+    }
+  };
+  int k = row;
+  for (; k + (UN - 1) * STEP < len; k += UN * STEP, wg += UN * STEP * a.ldw) {
+    u32x4 vg[UN], vu[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      vg[i] = load_piece(wg + i * STEP * a.ldw);
+      vu[i] = load_piece(wg + i * STEP * a.ldw + twin);
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) add(k + i * STEP, vg[i], vu[i]);
+  }
+  for (; k < len; k += STEP, wg += STEP * a.ldw) add(k, load_piece(wg), load_piece(wg + twin));
+#pragma unroll
+  for (int t = 0; t < NB; ++t)
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float v = acc[t][q][e];
+#pragma unroll
+        for (int m = LANES; m < 64; m <<= 1) v += __shfl_xor(v, m);
+        if (lane < LANES) red[wave][t][q][lane * E + e] = v;
+      }
+  __syncthreads();
+  for (int i = threadIdx.x; i < NB * kVecCols; i += 256) {
+    const int t = i / kVecCols, j = i % kVecCols;
+    const int64_t c1 = strip * kVecCols + j / E * E;
+    const int64_t col = (c1 < a.ff - E ? c1 : a.ff - E) + j % E;
+    if (t >= a.N || c1 >= a.ff) continue;
+    float s[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      s[q] = ((red[0][t][q][j] + red[1][t][q][j]) + red[2][t][q][j]) + red[3][t][q][j];
+    if (slices > 1) {
+      float *p = a.part + (slice * 2 * a.N + t) * a.ff + col;
+      p[0] = s[0];
+      p[a.N * a.ff] = s[1];
+    } else {
+      static_cast<T *>(a.H)[t * a.ldh + col] = from_f32<T>(ff_act(a.act, s[0]) * s[1]);
+      if (a.G) {
+        static_cast<T *>(a.G)[t * a.ldg + col] = from_f32<T>(s[0]);
+        static_cast<T *>(a.U)[t * a.ldg + col] = from_f32<T>(s[1]);
+      }
+    }
+  }
+}
+
+// ---- products of the backward -----------------------------------------------------------
+// C (M x N, and with two of them the twin C2 from the operand B's twin) = the product,
+// added to what is there with `add`; or its parts, splits x M x N (twin after twin).
+struct FfOut {
+  void *C, *C2;
+  int64_t M, N, ldc;
+  int add;
+  float *part;
+};
+template <class S, typename T>
+__global__ __launch_bounds__(S::NT, S::NT / 256) void ff_mm_kernel(MmArgs m, FfOut o, int64_t gm,
+                                                                  int64_t gn, int twins, int splits) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int64_t tiles = gm * gn, all = tiles * twins * splits;
+  if (group_number() >= all) return;
+  const int64_t id = mm_order(group_number(), all);
+  const int64_t part = id / tiles, split = part / twins, steps = mm_steps(m);
+  const bool second = part - split * twins != 0;
+  int64_t tm, tn;
+  mm_place(id - part * tiles, gm, gn, tm, tn);
+  f32x4 acc[S::TM][S::TN];
+  mm_tile<S>(m, tm * S::BM, tn * S::BN, split * steps / splits, (split + 1) * steps / splits, lds,
+             acc, 0, second ? m.b.twin : 0);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row0 = tm * S::BM + wave / S::WN * (S::BM / S::WM) + (lane & 15);
+  const int64_t col0 = tn * S::BN + wave % S::WN * (S::BN / S::WN) + 4 * (lane >> 4);
+  T *C = static_cast<T *>(second ? o.C2 : o.C);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int64_t row = row0 + i * 16;
+    if (row >= o.M) continue;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int64_t col = col0 + j * 16, left = o.N - col;
+      if (left <= 0) continue;
+      if (splits > 1) {
+        put4(o.part + (part * o.M + row) * o.N + col, left, acc[i][j]);
+      } else {
+        f32x4 v = acc[i][j];
+        if (o.add) v += get4(C + row * o.ldc + col, left);
+        put4(C + row * o.ldc + col, left, v);
+      }
+    }
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void ff_sum_kernel(FfOut o, int twins, int splits) {
+  const int64_t id = group_number() * 256 + threadIdx.x, per = (o.N + 3) / 4;
+  const int64_t r0 = id / per, c = (id - r0 * per) * 4, left = o.N - c;
+  if (r0 >= o.M * twins) return;
+  const bool second = r0 >= o.M;
+  const int64_t r = second ? r0 - o.M : r0;
+  T *C = static_cast<T *>(second ? o.C2 : o.C) + r * o.ldc + c;
+  f32x4 v = {0, 0, 0, 0};
+  for (int s = 0; s < splits; ++s) v += get4(o.part + (s * twins * o.M + r0) * o.N + c, left);
+  if (o.add) v += get4(C, left);
+  put4(C, left, v);
+}
+
+// ---- plans --------------------------------------------------------------------------------
+// Tile and splits of an M x N product (N: both twins' columns) of `steps` steps: the
+// largest tile that gives every CU one, else the k steps are split too.
+struct Tiling {
+  int size;  // 256, 128 or 64
+  int64_t gm, gn;
+  int splits;
+};
+Tiling tiling(int64_t M, int64_t N, int64_t twins, int64_t steps) {
+  Tiling t = {};
+  for (int size : {256, 128, 64}) {
+    t = {size, ceil_div(M, size), ceil_div(N, size), 1};
+    if (t.gm * t.gn * twins >= 224) return t;
+  }
+  const int64_t want = ceil_div(1024, t.gm * t.gn * twins), most = steps / 8 > 1 ? steps / 8 : 1;
+  t.splits = static_cast<int>(want < most ? want : most);
+  return t;
+}
+
+constexpr int kPlanes[2] = {3, 1};  // of float32, bf16
+int segs_of(int dt) { return dt == 0 ? 6 : 1; }
+int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
+bool direct(int dt, const void *p, int64_t cols, int64_t ld) {
+  return dt == 1 && cols % 8 == 0 && ld % 8 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+}
+
+struct Space {  // of a workspace
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t o = at;
+    at += align256(bytes);
+    return o;
+  }
+};
+
+// Segments of `pairs` products of operands, pair q with an operand's planes from p[q] on
+// (`plane` elements each): for float32 the products of planes 2^-14, 2^-7 and 1, of all
+// pairs, in this order.
+const int kFirst[6] = {1, 0, 2, 0, 1, 0}, kSecond[6] = {1, 2, 0, 1, 0, 0};
+void set_segs(MmArgs &m, int dt, int pairs, std::initializer_list<const void *> a, int64_t aplane,
+              std::initializer_list<const void *> b, int64_t bplane) {
+  const int from[4] = {0, 3, 5, 6};
+  m.segs = pairs * segs_of(dt);
+  m.run[0] = dt == 0 ? 3 * pairs : m.segs;
+  m.run[1] = dt == 0 ? 5 * pairs : m.segs;
+  m.factor = 1.0f / kUp;
+  int at = 0;
+  for (int r = 0; r < 3; ++r)
+    for (int q = 0; q < pairs; ++q)
+      for (int s = from[r]; s < from[r + 1]; ++s) {
+        if (dt != 0 && r < 2) continue;
+        m.a.p[at] = static_cast<const uint16_t *>(a.begin()[q]) + (dt == 0 ? kFirst[s] * aplane : 0);
+        m.b.p[at++] = static_cast<const uint16_t *>(b.begin()[q]) + (dt == 0 ? kSecond[s] * bplane : 0);
+      }
+}
+
+dim3 pieces_grid(int64_t rows, int64_t per) { return groups_grid(ceil_div(rows * per, 256)); }
+
+template <typename T>
+void pack(const void *src, int64_t rows, int64_t cols, int64_t ld, uint16_t *dst, hipStream_t s) {
+  ff_pack_kernel<T><<<pieces_grid(rows, up8(cols) / 8), 256, 0, s>>>(
+      static_cast<const T *>(src), rows, cols, ld, dst, up8(cols));
+}
+
+int vec_slices(int64_t d, int64_t ff) {
+  const int64_t strips = ceil_div(ff, kVecCols), least = ceil_div(d, kVecSlice);
+  const int64_t want = ceil_div(1024, strips), most = ceil_div(d, 64);
+  const int64_t n = want < most ? want : most;
+  return static_cast<int>(n > least ? n : least);
+}
+bool by_vec(int dt, int64_t N, int64_t ff) { return N <= 8 && ff >= (dt == 0 ? 4 : 8); }
+
+struct FfPlan {
+  bool vec, own_x, own_w;  // own: read in place
+  Tiling t;
+  int slices;
+  size_t x, w, part, total;
+};
+FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w) {
+  FfPlan p = {};
+  Space s;
+  if (by_vec(dt, N, ff)) {
+    p.vec = true;
+    p.slices = vec_slices(d, ff);
+    if (p.slices > 1) p.part = s.take(sizeof(float) * p.slices * 2 * N * ff);
+  } else {
+    p.own_x = own_x;
+    p.own_w = own_w;
+    // a paired tile has half its columns of either product
+    p.t = tiling(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
+    if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
+    if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
+    if (p.t.splits > 1) p.part = s.take(sizeof(float) * p.t.splits * 2 * N * ff);
+  }
+  p.total = s.at;
+  return p;
+}
+
+template <class S, typename T>
+void run_ff(const MmArgs &m, const FfArgs &a, const Tiling &t, hipStream_t s) {
+  ff_kernel<S, T><<<groups_grid(t.gm * t.gn * t.splits), S::NT, 0, s>>>(m, a, t.gm, t.gn, t.splits);
+}
+template <typename T>
+hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t s) {
+  a.part = reinterpret_cast<float *>(ws + p.part);
+  int parts = p.slices;
+  if (p.vec) {
+    const dim3 grid = groups_grid(ceil_div(a.ff, kVecCols) * p.slices);
+    if (a.N == 1)
+      ff_vec_kernel<T, 1><<<grid, 256, 0, s>>>(a, p.slices);
+    else if (a.N == 2)
+      ff_vec_kernel<T, 2><<<grid, 256, 0, s>>>(a, p.slices);
+    else if (a.N <= 4)
+      ff_vec_kernel<T, 4><<<grid, 256, 0, s>>>(a, p.slices);
+    else
+      ff_vec_kernel<T, 8><<<grid, 256, 0, s>>>(a, p.slices);
+  } else {
+    MmArgs m = {};
+    m.k = a.d;
+    const void *x = a.X, *wg = a.Wg, *wu = a.Wu;
+    m.a.ld = a.ldx;
+    m.a.n = a.N;
+    m.b.ld = a.ldw;
+    m.b.n = up8(a.ff);
+    if (!p.own_x) {
+      uint16_t *to = reinterpret_cast<uint16_t *>(ws + p.x);
+      pack<T>(a.X, a.N, a.d, a.ldx, to, s);
+      x = to;
+      m.a.ld = up8(a.d);
+    }
+    if (!p.own_w) {
+      uint16_t *to = reinterpret_cast<uint16_t *>(ws + p.w);
+      uint16_t *to2 = to + kPlanes[dt] * a.d * up8(a.ff);
+      pack<T>(a.Wg, a.d, a.ff, a.ldw, to, s);
+      pack<T>(a.Wu, a.d, a.ff, a.ldw, to2, s);
+      wg = to;
+      wu = to2;
+      m.b.ld = up8(a.ff);
+    }
+    m.b.twin = static_cast<const char *>(wu) - static_cast<const char *>(wg);
+    set_segs(m, dt, 1, {x}, a.N * up8(a.d), {wg}, a.d * up8(a.ff));
+    if (p.t.size == 256)
+      run_ff<MmShape<false, true, false, 256, 256, 2, 4, true>, T>(m, a, p.t, s);
+    else if (p.t.size == 128)
+      run_ff<MmShape<false, true, false, 128, 128, 2, 2, true>, T>(m, a, p.t, s);
+    else
+      run_ff<MmShape<false, true, false, 64, 64, 2, 2, true>, T>(m, a, p.t, s);
+    parts = p.t.splits;
+  }
+  if (parts > 1) ff_join_kernel<T><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, parts);
+  return hipGetLastError();
+}
+
+struct FfGradPlan {
+  bool own_x, own_w, own_g;
+  Tiling tx, tw;
+  size_t x, w, g, part, total;
+};
+FfGradPlan ff_grad_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w, bool own_g) {
+  FfGradPlan p = {};
+  Space s;
+  p.own_x = own_x;
+  p.own_w = own_w;
+  p.own_g = own_g;
+  p.tx = tiling(N, d, 1, ceil_div(ff, kMmK) * 2 * segs_of(dt));
+  p.tw = tiling(d, ff, 2, ceil_div(N, kMmK) * segs_of(dt));
+  if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
+  if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
+  if (!own_g) p.g = s.take(2 * 2 * kPlanes[dt] * N * up8(ff));
+  const size_t px = p.tx.splits > 1 ? sizeof(float) * p.tx.splits * N * d : 0;
+  const size_t pw = p.tw.splits > 1 ? sizeof(float) * p.tw.splits * 2 * d * ff : 0;
+  p.part = s.take(px > pw ? px : pw);
+  p.total = s.at;
+  return p;
+}
+
+template <bool K, typename T>
+void run_mm(const MmArgs &m, const FfOut &o, const Tiling &t, int twins, hipStream_t s) {
+  const dim3 grid = groups_grid(t.gm * t.gn * twins * t.splits);
+  if (t.size == 256)
+    ff_mm_kernel<MmShape<false, K, K, 256, 256, 2, 4>, T>
+        <<<grid, 512, 0, s>>>(m, o, t.gm, t.gn, twins, t.splits);
+  else if (t.size == 128)
+    ff_mm_kernel<MmShape<false, K, K, 128, 128, 2, 2>, T>
+        <<<grid, 256, 0, s>>>(m, o, t.gm, t.gn, twins, t.splits);
+  else
+    ff_mm_kernel<MmShape<false, K, K, 64, 64, 2, 2>, T>
+        <<<grid, 256, 0, s>>>(m, o, t.gm, t.gn, twins, t.splits);
+  if (t.splits > 1)
+    ff_sum_kernel<T><<<pieces_grid(o.M * twins, ceil_div(o.N, 4)), 256, 0, s>>>(o, twins, t.splits);
+}
+
+template <typename T>
+hipError_t launch_ff_grad_t(int dt, const FfGradArgs &a, const FfGradPlan &p, char *ws,
+                            hipStream_t s) {
+  const int64_t ff8 = up8(a.ff), planes = kPlanes[dt];
+  const void *x = a.X, *wg = a.Wg, *wu = a.Wu, *dg = a.dG, *du = a.dU;
+  int64_t ldx = a.ldx, ldw = a.ldw, ldd = a.ldd;
+  uint16_t *pg = nullptr, *pu = nullptr;
+  if (!p.own_g) {
+    dg = pg = reinterpret_cast<uint16_t *>(ws + p.g);
+    du = pu = pg + planes * a.N * ff8;
+    ldd = ff8;
+  }
+  ff_dact_kernel<T><<<pieces_grid(a.N, ff8 / 8), 256, 0, s>>>(a, pg, pu, ldd);
+  const bool want_w = a.gWg != nullptr;
+  if (!p.own_x && want_w) {
+    uint16_t *to = reinterpret_cast<uint16_t *>(ws + p.x);
+    pack<T>(a.X, a.N, a.d, a.ldx, to, s);
+    x = to;
+    ldx = up8(a.d);
+  }
+  if (!p.own_w && a.dX) {
+    uint16_t *to = reinterpret_cast<uint16_t *>(ws + p.w), *to2 = to + planes * a.d * ff8;
+    pack<T>(a.Wg, a.d, a.ff, a.ldw, to, s);
+    pack<T>(a.Wu, a.d, a.ff, a.ldw, to2, s);
+    wg = to;
+    wu = to2;
+    ldw = ff8;
+  }
+  float *part = reinterpret_cast<float *>(ws + p.part);
+  if (a.dX) {
+    MmArgs m = {};
+    m.k = a.ff;
+    m.a.ld = ldd;
+    m.a.n = a.N;
+    m.b.ld = ldw;
+    m.b.n = a.d;
+    set_segs(m, dt, 2, {dg, du}, a.N * ff8, {wg, wu}, a.d * ff8);
+    run_mm<true, T>(m, {a.dX, nullptr, a.N, a.d, a.lddx, 0, part}, p.tx, 1, s);
+  }
+  if (want_w) {
+    MmArgs m = {};
+    m.k = a.N;
+    m.a.ld = ldx;
+    m.a.n = up8(a.d);
+    m.b.ld = ldd;
+    m.b.n = ff8;
+    m.b.twin = static_cast<const char *>(du) - static_cast<const char *>(dg);
+    set_segs(m, dt, 1, {x}, a.N * up8(a.d), {dg}, a.N * ff8);
+    const FfOut o = {a.gWg, a.gWu, a.d, a.ff, a.ldgw, a.add, part};
+    if (a.gdt == 0)
+      run_mm<false, float>(m, o, p.tw, 2, s);
+    else
+      run_mm<false, bf16_t>(m, o, p.tw, 2, s);
+  }
+  return hipGetLastError();
+}
+
+FfPlan plan_of(int dt, const FfArgs &a) {
+  return ff_plan(dt, a.N, a.d, a.ff, direct(dt, a.X, a.d, a.ldx),
+                 direct(dt, a.Wg, a.ff, a.ldw) && direct(dt, a.Wu, a.ff, a.ldw));
+}
+FfGradPlan plan_of(int dt, const FfGradArgs &a) {
+  return ff_grad_plan(dt, a.N, a.d, a.ff, direct(dt, a.X, a.d, a.ldx),
+                      direct(dt, a.Wg, a.ff, a.ldw) && direct(dt, a.Wu, a.ff, a.ldw),
+                      direct(dt, a.dG, a.ff, a.ldd) && direct(dt, a.dU, a.ff, a.ldd));
+}
+
+}  // namespace
+
+size_t ff_workspace_bytes(int dt, const FfArgs &a) { return plan_of(dt, a).total; }
+size_t ff_grad_workspace_bytes(int dt, const FfGradArgs &a) { return plan_of(dt, a).total; }
+
+hipError_t launch_ff(int dt, const FfArgs &a, void *ws, hipStream_t s) {
+  const FfPlan p = plan_of(dt, a);
+  return dt == 0 ? launch_ff_t<float>(dt, a, p, static_cast<char *>(ws), s)
+                 : launch_ff_t<bf16_t>(dt, a, p, static_cast<char *>(ws), s);
+}
+hipError_t launch_ff_grad(int dt, const FfGradArgs &a, void *ws, hipStream_t s) {
+  if (a.N == 0) {  // sums of nothing
+    const FfOut o = {a.gWg, a.gWu, a.d, a.ff, a.ldgw, a.add, nullptr};
+    const dim3 grid = pieces_grid(2 * a.d, ceil_div(a.ff, 4));
+    if (a.gdt == 0)
+      ff_sum_kernel<float><<<grid, 256, 0, s>>>(o, 2, 0);
+    else
+      ff_sum_kernel<bf16_t><<<grid, 256, 0, s>>>(o, 2, 0);
+    return hipGetLastError();
+  }
+  const FfGradPlan p = plan_of(dt, a);
+  return dt == 0 ? launch_ff_grad_t<float>(dt, a, p, static_cast<char *>(ws), s)
+                 : launch_ff_grad_t<bf16_t>(dt, a, p, static_cast<char *>(ws), s);
+}
+
+}  // namespace sn

@@ -328,6 +328,29 @@ hipError_t launch_rmsnorm(int dt, const NormArgs &a, hipStream_t s);
 size_t rmsnorm_grad_workspace_bytes(int dt, int64_t N, int64_t d);
 hipError_t launch_rmsnorm_grad(int dt, NormGradArgs a, float *gw, void *ws, hipStream_t s);
 
+// ---- the end of a block and the start of the next ----------------------------------
+struct BlockNormArgs {
+  const void *X, *R, *w, *w_post, *gate;  // w, w_post, gate may be NULL
+  int64_t N, d, ldx, ldr, ldgate;         // ldgate 0: one row for all tokens
+  float inv_d, eps, alpha;
+  int post, sigmoid;
+  void *H, *Y;  // Y may be NULL
+  int64_t ldh, ldy;
+};
+struct BlockNormGradArgs {
+  const void *X, *H, *w, *w_post, *gate, *dY, *dH;  // dY or dH may be NULL
+  int64_t N, d, ldx, ldh, ldgate, lddy, lddh;
+  float inv_d, eps, alpha;
+  int post, sigmoid;
+  void *dX, *dR, *dgate;  // dgate: of a gate for each token, or NULL
+  int64_t lddx, lddr, lddg;
+  float *sums[3];  // gw, gw_post, the one gate row's gradient: added to, or NULL
+  float *part;     // set by the launcher
+};
+hipError_t launch_block_norm(int dt, const BlockNormArgs &a, hipStream_t s);
+size_t block_norm_grad_workspace_bytes(int dt, int64_t N, int64_t d);
+hipError_t launch_block_norm_grad(int dt, BlockNormGradArgs a, void *ws, hipStream_t s);
+
 // ---- gradient norm and clipping ---------------------------------------------------
 struct ClipTensor {
   const void *g;
@@ -364,6 +387,53 @@ hipError_t launch_sumsq(const ClipTensor *t, int32_t count, double *sumsq, void 
                         hipStream_t s);
 hipError_t launch_clip(const ClipTensor *t, int32_t count, bool in_place, const double *sumsq,
                        double max_norm, float *norm, hipStream_t s);
+
+// ---- gated feed-forward block ------------------------------------------------------
+enum { kActSilu = 0, kActGelu = 1, kActRelu = 2 };  // SN_ACT_*
+struct FfArgs {
+  const void *X, *Wg, *Wu;
+  int64_t N, d, ff, ldx, ldw;
+  int act;
+  void *H, *G, *U;  // G and U: both or neither
+  int64_t ldh, ldg;
+  float *part;  // set by the launcher
+};
+struct FfGradArgs {
+  const void *X, *Wg, *Wu, *G, *U, *dH;
+  int64_t N, d, ff, ldx, ldw, ldg, lddh;
+  int act;
+  void *dG, *dU;
+  int64_t ldd;
+  void *dX;  // may be NULL
+  int64_t lddx;
+  void *gWg, *gWu;  // both or neither
+  int64_t ldgw;
+  int gdt, add;
+};
+size_t ff_workspace_bytes(int dt, const FfArgs &a);
+size_t ff_grad_workspace_bytes(int dt, const FfGradArgs &a);
+hipError_t launch_ff(int dt, const FfArgs &a, void *ws, hipStream_t s);
+hipError_t launch_ff_grad(int dt, const FfGradArgs &a, void *ws, hipStream_t s);
+
+// ---- orthogonalised updates ---------------------------------------------------------
+// Matrices of one shape, a kernel argument: g the momentum's gradient (or the matrix to
+// orthogonalise), m the float32 momentum (or NULL), w where the result goes.
+struct OrthMats {
+  static constexpr int kMost = 32;
+  const void *g[kMost];
+  float *m[kMost];
+  void *w[kMost];
+  int64_t ldg[kMost], ldm[kMost], ldw[kMost];
+};
+struct OrthArgs {
+  int64_t rows, cols;
+  int count, steps;
+  bool update;  // w -= rate * result + decay * w, else w = result
+  bool nesterov;
+  float momentum, rate, decay;
+};
+size_t orth_workspace_bytes(int64_t rows, int64_t cols, int64_t count);
+hipError_t launch_orth(int dt, const OrthMats &t, const OrthArgs &a, void *ws, hipStream_t s);
 
 // Record a message for sn_last_error() on the calling thread; returns st.
 int32_t set_error(int32_t st, const char *fmt, ...);

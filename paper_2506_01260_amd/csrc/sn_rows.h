@@ -150,6 +150,52 @@ __device__ __forceinline__ void store_part(T *row, int64_t c0, int64_t n,
     if (c0 + i < n) row[c0 + i] = from_f32<T>(x[i]);
 }
 
+// The piece at column c0 of a row of d, 0 past the row's end, in two steps: take()
+// loads the piece there, or the one that the row ends with, and fix() moves that
+// one's values to their places.  So every load of a row is issued before any is
+// waited for, also at widths that are no multiple of the piece (where the last
+// piece element by element, or moved as it came, made the backward of 32768 x 1601
+// half as long again).  d >= E.  WHOLE: d is a multiple of the piece.
+template <typename T>
+__device__ __forceinline__ u32x4 take(const T *row, int c0, int d) {
+  return load_piece(row + min(c0, d - Piece<T>::E));
+}
+template <typename T, bool WHOLE>
+__device__ __forceinline__ u32x4 fix(u32x4 v, int c0, int d) {
+  const int by = c0 - (d - Piece<T>::E);  // values that the piece came early by
+  if (by > 0) {
+    uint64_t lo = v.x | static_cast<uint64_t>(v.y) << 32, hi = v.z | static_cast<uint64_t>(v.w) << 32;
+    const int bits = by * 8 * static_cast<int>(sizeof(T));
+    if (WHOLE || bits >= 128) {
+      lo = hi = 0;
+    } else if (bits >= 64) {
+      lo = hi >> (bits - 64);
+      hi = 0;
+    } else {
+      lo = lo >> bits | hi << (64 - bits);
+      hi >>= bits;
+    }
+    v = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32),
+              static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+  }
+  return v;
+}
+// The same in one step, for any d and for rows past the registers.
+template <typename T>
+__device__ __forceinline__ void get(const T *row, int64_t c0, int64_t d, float (&x)[Piece<T>::E]) {
+  if (c0 + Piece<T>::E <= d)
+    Piece<T>::unpack(load_piece(row + c0), x);
+  else
+    load_part(row, c0, d, 0.0f, x);
+}
+template <typename T, bool WHOLE = false>
+__device__ __forceinline__ void put(T *row, int64_t c0, int64_t d, const float (&x)[Piece<T>::E]) {
+  if (WHOLE ? c0 < d : c0 + Piece<T>::E <= d)
+    store_piece(row + c0, Piece<T>::pack(x));
+  else if (!WHOLE)
+    store_part(row, c0, d, x);
+}
+
 // ---- reductions: every lane / thread gets the result ------------------------
 // Over the wave by data-parallel-primitive moves, which cost a vector instruction
 // each where a shuffle is a trip to the LDS: within rows of 16 lanes, then row 0

@@ -38,7 +38,11 @@ namespace {
   X(sn_token_logprobs) X(sn_token_logprobs_workspace_bytes) X(sn_token_logprobs_backward)    \
   X(sn_token_loss) X(sn_rmsnorm)           \
   X(sn_rmsnorm_quant) X(sn_rmsnorm_backward) X(sn_rmsnorm_backward_workspace_bytes)           \
-  X(sn_grad_sumsq) X(sn_grad_sumsq_workspace_bytes) X(sn_grad_clip)
+  X(sn_grad_sumsq) X(sn_grad_sumsq_workspace_bytes) X(sn_grad_clip)                           \
+  X(sn_block_norm) X(sn_block_norm_backward) X(sn_block_norm_backward_workspace_bytes)        \
+  X(sn_gated_ff) X(sn_gated_ff_workspace_bytes) X(sn_gated_ff_backward)                       \
+  X(sn_gated_ff_backward_workspace_bytes) X(sn_orthogonalize) X(sn_muon_step)                 \
+  X(sn_orthogonalize_workspace_bytes)
 
 struct Calls {
 #define X(f) decltype(&::f) f = nullptr;
@@ -796,6 +800,280 @@ SN_FAST(rmsnorm_backward) {
   });
 }
 
+// ---- a block's end and start, gated feed-forward block ------------------------
+bool truth(PyObject *o, bool &v) {
+  const int t = PyObject_IsTrue(o);
+  if (t < 0) PyErr_Clear();
+  v = t > 0;
+  return t >= 0;
+}
+// A matrix of the type and shape of `like` (absent: None).
+bool mat_like(PyObject *o, const Mat &like, Mat &m) {
+  if (o == Py_None) return true;
+  return mat_here(o, m) && m.type == like.type && m.rows == like.rows && m.cols == like.cols;
+}
+// A gate: one row of values (stride 0), a row for each of x's, or none.
+bool gate_of(PyObject *o, const Mat &x, Mat &g) {
+  if (o == Py_None) return true;
+  const at::Tensor *t = here(o);
+  if (!t) return false;
+  if (t->dim() != 1) return mat_like(o, x, g);
+  g.type = x.type;
+  return vec(o, x.type, x.cols, g.p);
+}
+
+// (X, residual, w, w_post, post, gate, gate_fn, alpha, eps, out, resid_out, stream)
+SN_FAST(block_norm) {
+  return guarded(n, 12, [&](bool &taken) -> PyObject * {
+    Mat x, r, g, y, h;
+    void *w, *w1 = nullptr;
+    bool post;
+    int64_t fn;
+    double alpha, eps;
+    sn_stream s;
+    at::Tensor ymade, hmade;
+    if (a[11] != Py_None || !mat_here(a[0], x) || !sn_type(x.type) || a[1] == Py_None ||
+        !mat_like(a[1], x, r) || !vec(a[2], x.type, x.cols, w) || !truth(a[4], post) ||
+        (post && !vec(a[3], x.type, x.cols, w1)) || !gate_of(a[5], x, g) || !int_of(a[6], fn) ||
+        !number(a[7], alpha) || !number(a[8], eps) || !stream(a[11], s) ||
+        !output_here(a[9], a[0], x.type, x.rows, x.cols, y, ymade) ||
+        !output_here(a[10], a[0], x.type, x.rows, x.cols, h, hmade))
+      SN_LEAVE;
+    if (failed(launch([&] {
+          return g_lib.sn_block_norm(x.p, x.rows, x.cols, x.ld, dt_of(x.type), r.p, r.ld, post, w1,
+                                     g.p, g.ld, static_cast<int32_t>(fn), alpha, w, eps, h.p, h.ld,
+                                     y.p, y.ld, s);
+        })))
+      return nullptr;
+    return tuple_of({wrap(a[9], ymade), wrap(a[10], hmade)});
+  });
+}
+
+// (X, H, dY, w, w_post, post, gate, gate_fn, alpha, dH, eps, gw, gw_post, dgate, out, resid_out,
+//  workspace, stream)
+SN_FAST(block_norm_backward) {
+  return guarded(n, 18, [&](bool &taken) -> PyObject * {
+    Mat x, h, dy, g, dh, dg, dx, dr;
+    void *w, *w1 = nullptr, *gw, *gw1, *row = nullptr, *ws = nullptr;
+    bool post;
+    int64_t fn;
+    double alpha, eps;
+    size_t bytes = 0;
+    sn_stream s;
+    at::Tensor gmade, xmade, rmade, wmade;
+    if (a[17] != Py_None || !mat_here(a[0], x) || x.rows == 0 || !sn_type(x.type) || a[1] == Py_None ||
+        !mat_like(a[1], x, h) || !mat_like(a[2], x, dy) || !vec(a[3], x.type, x.cols, w) ||
+        !truth(a[5], post) || (post && !vec(a[4], x.type, x.cols, w1)) || !gate_of(a[6], x, g) ||
+        !int_of(a[7], fn) || !number(a[8], alpha) || !mat_like(a[9], x, dh) || !number(a[10], eps) ||
+        !vec(a[11], at::kFloat, x.cols, gw) || !vec(a[12], at::kFloat, x.cols, gw1) ||
+        (gw1 && !post) || (gw && !dy.p) || !stream(a[17], s))
+      SN_LEAVE;
+    const bool each = g.p && g.ld != 0;
+    if (!each && a[13] != Py_None && (!g.p || !vec(a[13], at::kFloat, x.cols, row))) SN_LEAVE;
+    const int32_t dt = dt_of(x.type);
+    const bool sums = gw || gw1 || row;
+    const size_t need = sums ? g_lib.sn_block_norm_backward_workspace_bytes(x.rows, x.cols, dt) : 0;
+    if (need && !workspace_here(a[16], a[0], need, ws, bytes, wmade)) SN_LEAVE;
+    if ((each && !output_here(a[13], a[0], x.type, x.rows, x.cols, dg, gmade)) ||
+        !output_here(a[14], a[0], x.type, x.rows, x.cols, dx, xmade) ||
+        !output_here(a[15], a[0], x.type, x.rows, x.cols, dr, rmade))
+      SN_LEAVE;
+    if (failed(launch([&] {
+          return g_lib.sn_block_norm_backward(
+              x.p, x.rows, x.cols, x.ld, dt, h.p, h.ld, post, w1, g.p, g.ld,
+              static_cast<int32_t>(fn), alpha, w, eps, dy.p, dy.ld, dh.p, dh.ld, dx.p, dx.ld, dr.p,
+              dr.ld, dg.p, dg.ld, static_cast<float *>(row), static_cast<float *>(gw),
+              static_cast<float *>(gw1), ws, bytes, s);
+        })))
+      return nullptr;
+    return tuple_of({wrap(a[14], xmade), wrap(a[15], rmade), wrap(a[13], gmade)});
+  });
+}
+
+// X, and Wg and Wu of one row stride.
+struct FfIn {
+  Mat x, wg, wu;
+  bool take(PyObject *X, PyObject *Wg, PyObject *Wu) {
+    return mat_here(X, x) && sn_type(x.type) && mat_here(Wg, wg) && wg.type == x.type &&
+           wg.rows == x.cols && Wu != Py_None && mat_like(Wu, wg, wu) && wu.ld == wg.ld;
+  }
+};
+bool on_16(std::initializer_list<const void *> ptrs) {
+  for (const void *p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) & 15) return false;
+  return true;
+}
+
+// (X, Wg, Wu, act, save, out, out_g, out_u, workspace, stream)
+SN_FAST(gated_ff) {
+  return guarded(n, 10, [&](bool &taken) -> PyObject * {
+    FfIn c;
+    Mat h, g, u;
+    int64_t act;
+    bool save;
+    void *ws = nullptr;
+    size_t bytes = 0;
+    sn_stream s;
+    at::Tensor hmade, gmade, umade, wmade;
+    if (a[9] != Py_None || !c.take(a[0], a[1], a[2]) || !int_of(a[3], act) || !truth(a[4], save) ||
+        (a[6] == Py_None) != (a[7] == Py_None) || !stream(a[9], s))
+      SN_LEAVE;
+    save = save || a[6] != Py_None;
+    const int64_t N = c.x.rows, ff = c.wg.cols;
+    const int32_t dt = dt_of(c.x.type);
+    const size_t need = g_lib.sn_gated_ff_workspace_bytes(N, c.x.cols, ff, c.x.ld, c.wg.ld, dt,
+                                                          on_16({c.x.p, c.wg.p, c.wu.p}));
+    if (need && !workspace_here(a[8], a[0], need, ws, bytes, wmade)) SN_LEAVE;
+    if (!output_here(a[5], a[0], c.x.type, N, ff, h, hmade) ||
+        (save && (!output_here(a[6], a[0], c.x.type, N, ff, g, gmade) ||
+                  !output_here(a[7], a[0], c.x.type, N, ff, u, umade) || g.ld != u.ld)))
+      SN_LEAVE;
+    const int32_t st = launch([&] {
+      return g_lib.sn_gated_ff(c.x.p, N, c.x.cols, c.x.ld, dt, c.wg.p, c.wu.p, ff, c.wg.ld,
+                               static_cast<int32_t>(act), h.p, h.ld, g.p, u.p, g.ld, ws, bytes, s);
+    });
+    if (!save) return finish(st, a[5], hmade);
+    if (failed(st)) return nullptr;
+    return tuple_of({wrap(a[5], hmade), wrap(a[6], gmade), wrap(a[7], umade)});
+  });
+}
+
+// (X, Wg, Wu, G, U, dH, act, dG, dU, out, gWg, gWu, accumulate, want_dx, want_gw, workspace, stream)
+SN_FAST(gated_ff_backward) {
+  return guarded(n, 17, [&](bool &taken) -> PyObject * {
+    FfIn c;
+    Mat g, u, dh, dg, du, dx, wg, wu;
+    int64_t act;
+    bool add, want_dx, want_gw;
+    void *ws = nullptr;
+    size_t bytes = 0;
+    sn_stream s;
+    at::Tensor gmade, umade, xmade, wgmade, wumade, wmade;
+    if (a[16] != Py_None || !c.take(a[0], a[1], a[2]) || a[3] == Py_None || !mat_here(a[3], g) ||
+        g.type != c.x.type || g.rows != c.x.rows || g.cols != c.wg.cols || a[4] == Py_None ||
+        !mat_like(a[4], g, u) || u.ld != g.ld || a[5] == Py_None || !mat_like(a[5], g, dh) ||
+        !int_of(a[6], act) || (a[7] == Py_None) != (a[8] == Py_None) ||
+        (a[10] == Py_None) != (a[11] == Py_None) || !truth(a[12], add) || !truth(a[13], want_dx) ||
+        !truth(a[14], want_gw) || (add && want_gw && a[10] == Py_None) || !stream(a[16], s))
+      SN_LEAVE;
+    const int64_t N = c.x.rows, d = c.x.cols, ff = c.wg.cols;
+    const int32_t dt = dt_of(c.x.type);
+    at::ScalarType wt = c.x.type;
+    if (want_gw && a[10] != Py_None) {
+      const at::Tensor *t = here(a[10]);
+      if (!t || (t->scalar_type() != c.x.type && t->scalar_type() != at::kFloat)) SN_LEAVE;
+      wt = t->scalar_type();
+    }
+    if (!output_here(a[7], a[0], c.x.type, N, ff, dg, gmade) ||
+        !output_here(a[8], a[0], c.x.type, N, ff, du, umade) || dg.ld != du.ld ||
+        (want_dx && !output_here(a[9], a[0], c.x.type, N, d, dx, xmade)) ||
+        (want_gw && (!output_here(a[10], a[0], wt, d, ff, wg, wgmade) ||
+                     !output_here(a[11], a[0], wt, d, ff, wu, wumade) || wg.ld != wu.ld)))
+      SN_LEAVE;
+    const size_t need = g_lib.sn_gated_ff_backward_workspace_bytes(
+        N, d, ff, c.x.ld, c.wg.ld, dg.ld, dt, on_16({c.x.p, c.wg.p, c.wu.p, dg.p, du.p}));
+    if (need && !workspace_here(a[15], a[0], need, ws, bytes, wmade)) SN_LEAVE;
+    if (failed(launch([&] {
+          return g_lib.sn_gated_ff_backward(
+              c.x.p, N, d, c.x.ld, dt, c.wg.p, c.wu.p, ff, c.wg.ld, static_cast<int32_t>(act), g.p,
+              u.p, g.ld, dh.p, dh.ld, dg.p, du.p, dg.ld, dx.p, dx.ld, wg.p, wu.p, wg.ld, dt_of(wt),
+              add, ws, bytes, s);
+        })))
+      return nullptr;
+    return tuple_of({want_dx ? wrap(a[9], xmade) : given(Py_None),
+                     want_gw ? wrap(a[10], wgmade) : given(Py_None),
+                     want_gw ? wrap(a[11], wumade) : given(Py_None)});
+  });
+}
+
+// ---- orthogonalised updates -----------------------------------------------------
+// The matrices of a list.
+bool matrices(PyObject *o, std::vector<sn_tensor> &v) {
+  if (!PyList_CheckExact(o)) return false;
+  const Py_ssize_t count = PyList_GET_SIZE(o);
+  v.resize(static_cast<size_t>(count));
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    Mat m;
+    if (!mat_here(PyList_GET_ITEM(o, i), m) || !sn_type(m.type)) return false;
+    v[static_cast<size_t>(i)] = {m.rows && m.cols ? m.p : nullptr, m.rows, m.cols, m.ld,
+                                 dt_of(m.type)};
+  }
+  return count > 0;
+}
+
+// (mats, steps, out, workspace, stream)
+SN_FAST(orthogonalize) {
+  return guarded(n, 5, [&](bool &taken) -> PyObject * {
+    std::vector<sn_tensor> from, to;
+    int64_t steps;
+    sn_stream s;
+    void *ws = nullptr;
+    size_t bytes = 0;
+    at::Tensor wmade;
+    if (a[4] != Py_None || !matrices(a[0], from) || !int_of(a[1], steps) || steps < 1 ||
+        steps > SN_MAX_ORTH_STEPS || !stream(a[4], s) ||
+        (a[2] != Py_None && (!matrices(a[2], to) || to.size() != from.size())))
+      SN_LEAVE;
+    const int32_t count = static_cast<int32_t>(from.size());
+    PyObject *like = PyList_GET_ITEM(a[0], 0);
+    const size_t need =
+        g_lib.sn_orthogonalize_workspace_bytes(count, from[0].rows, from[0].cols);
+    if (need && !workspace_here(a[3], like, need, ws, bytes, wmade)) SN_LEAVE;
+    PyObject *made = nullptr;
+    if (a[2] == Py_None) {
+      made = PyList_New(count);
+      if (!made) return nullptr;
+      for (int32_t i = 0; i < count; ++i) {
+        const sn_tensor &f = from[static_cast<size_t>(i)];
+        at::Tensor t = make(like, f.dt == SN_F32 ? at::kFloat : at::kBFloat16, {f.rows, f.cols});
+        to.push_back({f.rows && f.cols ? t.data_ptr() : nullptr, f.rows, f.cols, f.cols, f.dt});
+        PyObject *o = THPVariable_Wrap(std::move(t));
+        if (!o) {
+          Py_DECREF(made);
+          return nullptr;
+        }
+        PyList_SET_ITEM(made, i, o);
+      }
+    }
+    if (failed(launch([&] {
+          return g_lib.sn_orthogonalize(count, from.data(), to.data(), static_cast<int32_t>(steps),
+                                        ws, bytes, s);
+        }))) {
+      Py_XDECREF(made);
+      return nullptr;
+    }
+    return made ? made : given(a[2]);
+  });
+}
+
+// (W, G, M, lr, momentum, nesterov, weight_decay, scale, steps, workspace, stream)
+SN_FAST(muon_step) {
+  return guarded(n, 11, [&](bool &taken) -> PyObject * {
+    std::vector<sn_tensor> w, g, m;
+    int64_t steps;
+    double lr, momentum, decay, scale;
+    bool nesterov;
+    sn_stream s;
+    void *ws = nullptr;
+    size_t bytes = 0;
+    at::Tensor wmade, none;
+    if (a[10] != Py_None || !matrices(a[0], w) || !matrices(a[1], g) || !matrices(a[2], m) ||
+        g.size() != w.size() || m.size() != w.size() || !number(a[3], lr) ||
+        !number(a[4], momentum) || !truth(a[5], nesterov) || !number(a[6], decay) ||
+        !number(a[7], scale) || !int_of(a[8], steps) || steps < 1 || steps > SN_MAX_ORTH_STEPS ||
+        !stream(a[10], s))
+      SN_LEAVE;
+    const int32_t count = static_cast<int32_t>(w.size());
+    const size_t need = g_lib.sn_orthogonalize_workspace_bytes(count, w[0].rows, w[0].cols);
+    if (need && !workspace_here(a[9], PyList_GET_ITEM(a[0], 0), need, ws, bytes, wmade)) SN_LEAVE;
+    const int32_t st = launch([&] {
+      return g_lib.sn_muon_step(count, w.data(), g.data(), m.data(), lr, momentum, nesterov, decay,
+                                scale, static_cast<int32_t>(steps), ws, bytes, s);
+    });
+    return finish(st, a[0], none);
+  });
+}
+
 // The tensors of a list, each without gaps.
 bool tensors(PyObject *o, std::vector<sn_tensor> &v) {
   if (!PyList_CheckExact(o)) return false;
@@ -910,6 +1188,12 @@ PyMethodDef g_methods[] = {SN_METHOD(bind),
                            SN_METHOD(rmsnorm_backward),
                            SN_METHOD(grad_sumsq),
                            SN_METHOD(grad_clip),
+                           SN_METHOD(block_norm),
+                           SN_METHOD(block_norm_backward),
+                           SN_METHOD(gated_ff),
+                           SN_METHOD(gated_ff_backward),
+                           SN_METHOD(orthogonalize),
+                           SN_METHOD(muon_step),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods,
                         nullptr,               nullptr,  nullptr, nullptr};

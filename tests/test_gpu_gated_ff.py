@@ -1,0 +1,208 @@
+"""GPU parity of the gated feed-forward block and its backward against the float64 oracle.
+
+Tolerances (u = 2^-24).  A product of K terms is summed in float32 by instructions of 32 terms:
+its error is at most u (p K / 32 + 44) S, S the sum of the terms' sizes and p the number of
+products that are added up, 1 for bf16 and 6 for float32 (12 in dX, which adds two products),
+whose operands in three parts leave out 2 u S more.  With up to 8 tokens a sum is a chain of at
+most 32 terms, a tree of 7 levels and d / 64 slices, which that covers.
+  * H:   act' < 1.13, so 1.2 tol(G) (|U| + tol(U)) + |act| tol(U), and |H| u (16 + 2 G^2) for the
+         exponential of a rounded argument
+  * dG, dU:   |value| u (32 + 2 G^2), and 4 u |dH U| where terms of act' cancel
+  * dX, gW:   of the dG and dU that were returned: the products' tolerance
+and for bf16 outputs their own rounding, 2^-8 of the value.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01260_amd as sn
+from gpu_helpers import host, log
+from oracle import gated_ff as orc
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+# (N, d, ff): one token, up to eight, more; one column, less than a piece, odd sizes, whole tiles,
+# both sides of a tile's edge, many slices
+SHAPES = [(1, 1, 1), (1, 64, 8), (1, 300, 77), (1, 1024, 512), (2, 129, 70), (3, 2100, 64), (4, 40, 200),
+          (5, 256, 136), (8, 1111, 333), (8, 16, 3), (9, 8, 8), (9, 65, 7), (16, 64, 64), (33, 100, 260),
+          (64, 256, 512), (65, 1000, 129), (128, 136, 1024), (200, 328, 520), (257, 96, 1000),
+          (300, 515, 391)]
+
+
+def _mat(seed, n, d, dtype, pad=0, std=1.0, shift=0):
+    """n x d with a row stride of d + pad, starting `shift` elements into its memory."""
+    g = torch.Generator().manual_seed(seed)
+    t = (torch.randn(n * (d + pad) + shift, generator=g) * std).to(DT[dtype]).cuda()
+    return t[shift:].view(n, d + pad)[:, :d]
+
+
+def _near(got, ref, tol, what):
+    err = np.abs(np.asarray(got, np.float64) - ref)
+    tol = np.broadcast_to(tol, ref.shape) + 1e-37
+    assert err.shape == ref.shape and np.isfinite(err).all(), what
+    k = np.unravel_index(int(np.argmax(err - tol)), err.shape)
+    assert (err <= tol).all(), f"{what} {k}: {got[k]!r}, {ref[k]!r}: {err[k]:.3g} over {tol[k]:.3g}"
+    log(f"  {what}: ok, at most {float(np.max(err / tol)):.2g} of the bound")
+
+
+def _own(ref, dtype):
+    return 2.0 ** -8 * np.abs(ref) if dtype == "bf16" else 0.0
+
+
+def _sum_tol(k, size, dtype, twice=False):
+    p = (6 if dtype == "f32" else 1) * (2 if twice else 1)
+    return U * (p * k / 32 + 44 + 2) * size
+
+
+def _check_forward(H, G, Ut, X, Wg, Wu, act, dtype, what):
+    x, wg, wu = host(X), host(Wg), host(Wu)
+    h, g, u = orc.gated_ff(x, wg, wu, act)
+    k = x.shape[1]
+    tg = _sum_tol(k, np.abs(x) @ np.abs(wg), dtype)
+    tu = _sum_tol(k, np.abs(x) @ np.abs(wu), dtype)
+    th = 1.2 * tg * (np.abs(u) + tu) + np.abs(orc.act(act, g)[0]) * tu + np.abs(h) * U * (16 + 2 * g * g)
+    _near(host(H), h, th + _own(h, dtype), f"{what} H")
+    if G is not None:
+        _near(host(G), g, tg + _own(g, dtype), f"{what} G")
+        _near(host(Ut), u, tu + _own(u, dtype), f"{what} U")
+
+
+def _check_backward(dX, gWg, gWu, dG, dU, X, Wg, Wu, G, Ut, dH, act, dtype, what, base=None):
+    x, wg, wu, g, u, dh = (host(t) for t in (X, Wg, Wu, G, Ut, dH))
+    rg, ru = orc.projections_backward(g, u, dh, act)
+    rel = U * (32 + 2 * g * g)
+    _near(host(dG), rg, np.abs(rg) * rel + 4 * U * np.abs(dh * u) + _own(rg, dtype), f"{what} dG")
+    _near(host(dU), ru, np.abs(ru) * rel + _own(ru, dtype), f"{what} dU")
+    dg, du = host(dG), host(dU)
+    rx, rwg, rwu = orc.products_backward(x, wg, wu, dg, du)
+    if dX is not None:
+        size = np.abs(dg) @ np.abs(wg).T + np.abs(du) @ np.abs(wu).T
+        _near(host(dX), rx, _sum_tol(g.shape[1], size, dtype, True) + _own(rx, dtype), f"{what} dX")
+    for got, ref, d, name in ((gWg, rwg, dg, "gWg"), (gWu, rwu, du, "gWu")):
+        if got is None:
+            continue
+        tol = _sum_tol(x.shape[0], np.abs(x).T @ np.abs(d), dtype)
+        if base is not None:
+            ref = ref + base
+            tol = tol + 2 * U * np.abs(ref)
+        _near(host(got), ref, tol + (_own(ref, dtype) if got.dtype == torch.bfloat16 else 0), f"{what} {name}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_forward_matches_oracle(dtype, shape):
+    n, d, ff = shape
+    log(f"[gated ff] {dtype} {shape}")
+    # strides and starts: whole, odd rows, an aligned stride of unaligned memory
+    for k, (pad, shift) in enumerate(((0, 0), (3, 0), (8 - ff % 8, 1))):
+        act = ("silu", "gelu", "relu")[k]
+        X = _mat(n, n, d, dtype, pad, 1.0, shift)
+        Wg, Wu = (_mat(s, d, ff, dtype, pad, d ** -0.5, shift) for s in (1, 2))
+        H, G, Ut = sn.sn_gated_ff(X, Wg, Wu, act=act, save=True)
+        what = f"{act} pad={pad} shift={shift}"
+        _check_forward(H, G, Ut, X, Wg, Wu, act, dtype, what)
+        assert torch.equal(sn.sn_gated_ff(X, Wg, Wu, act=act), H)
+        # both weights in one matrix, outputs with gaps
+        both = torch.cat([Wg, Wu], 1)
+        out = torch.zeros(3, n, ff + 5, dtype=X.dtype, device="cuda")
+        r = sn.sn_gated_ff(X, both[:, :ff], both[:, ff:], act=act, out=out[0, :, :ff],
+                           out_g=out[1, :, :ff], out_u=out[2, :, :ff])
+        assert all(torch.equal(a, b) for a, b in zip(r, (H, G, Ut)))
+        assert float(out[:, :, ff:].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_backward_matches_oracle(dtype, shape):
+    n, d, ff = shape
+    log(f"[gated ff backward] {dtype} {shape}")
+    for k, (pad, shift) in enumerate(((0, 0), (3, 0), (8 - ff % 8, 1))):
+        act = ("silu", "gelu", "relu")[k]
+        X = _mat(n, n, d, dtype, pad, 1.0, shift)
+        Wg, Wu = (_mat(s, d, ff, dtype, pad, d ** -0.5, shift) for s in (1, 2))
+        G, Ut = (_mat(s, n, ff, dtype, pad, 1.5, shift) for s in (3, 4))
+        dH = _mat(5, n, ff, dtype, 2 * pad, 0.1)
+        dG, dU = (torch.empty(n, ff + pad, dtype=X.dtype, device="cuda")[:, :ff] for _ in range(2))
+        what = f"{act} pad={pad} shift={shift}"
+        dX, gWg, gWu = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, act=act, dG=dG, dU=dU)
+        _check_backward(dX, gWg, gWu, dG, dU, X, Wg, Wu, G, Ut, dH, act, dtype, what)
+        # over G and U, or over dH; gradients in float32, added to, and in halves of one matrix
+        a, b, c = G.clone(), Ut.clone(), dH.clone()
+        r = sn.sn_gated_ff_backward(X, Wg, Wu, a, b, c, act=act, dG=a, dU=b)
+        assert torch.equal(a, dG) and torch.equal(b, dU)
+        _check_backward(*r, a, b, X, Wg, Wu, G, Ut, dH, act, dtype, what + " over G, U")
+        acc = torch.ones(d, 2 * ff, device="cuda")
+        a = Ut.contiguous().clone()
+        c = dH.contiguous().clone()
+        r = sn.sn_gated_ff_backward(X, Wg, Wu, G.contiguous(), a, c, act=act, dG=c, dU=a, gWg=acc[:, :ff],
+                                    gWu=acc[:, ff:], accumulate=True)
+        assert torch.equal(c, dG) and torch.equal(a, dU)
+        _check_backward(r[0], acc[:, :ff], acc[:, ff:], c, a, X, Wg, Wu, G, Ut, dH, act, dtype,
+                        what + " added", base=1.0)
+        # one of the two only
+        x2, none, _ = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, act=act, want_gw=False)
+        assert none is None and torch.equal(x2, dX)
+        none, w2, w3 = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, act=act, want_dx=False)
+        assert none is None and torch.equal(w2, gWg) and torch.equal(w3, gWu)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2000, 520, 2056), (700, 2000, 1500), (3500, 264, 1032)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_large_tiles(dtype, shape):
+    """Products of enough tiles for the largest kind, in every direction."""
+    n, d, ff = shape
+    log(f"[gated ff, large] {dtype} {shape}")
+    X, Wg, Wu = _mat(1, n, d, dtype), _mat(2, d, ff, dtype, 0, d ** -0.5), _mat(3, d, ff, dtype, 0, d ** -0.5)
+    H, G, Ut = sn.sn_gated_ff(X, Wg, Wu, save=True)
+    _check_forward(H, G, Ut, X, Wg, Wu, "silu", dtype, "forward")
+    dH = _mat(4, n, ff, dtype, 0, 0.1)
+    dG, dU = torch.empty_like(G), torch.empty_like(Ut)
+    first = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, dG=dG, dU=dU)
+    _check_backward(*first, dG, dU, X, Wg, Wu, G, Ut, dH, "silu", dtype, "backward")
+    for _ in range(2):  # the same every time
+        again = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, dG=dG, dU=dU)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+        assert torch.equal(sn.sn_gated_ff(X, Wg, Wu), H)
+
+
+@pytest.mark.parametrize("n", [1, 5, 40])
+def test_large_and_special_values(n):
+    """float32 operands over their whole range: parts of 24 bits lose nothing; a NaN spoils its
+    row alone, rows beside it are as without it."""
+    log(f"[gated ff, special] n={n}")
+    d, ff = 64, 72
+    X, W = _mat(1, n, d, "f32"), _mat(2, d, ff, "f32")
+    one = torch.zeros(d, ff, device="cuda")
+    one[0] = 1.0
+    for scale in (1e30, 1e-30, 3.0e38, 1e-37):
+        Z = torch.zeros(n, d, device="cuda")
+        Z[:, 0] = torch.linspace(0.5, 1.0, n, device="cuda") * scale
+        H, G, _ = sn.sn_gated_ff(Z, one, one * 0.0, act="relu", save=True)
+        # The matrix cores take operands and sums below 2^-126 as 0.  Each of the three parts of a
+        # value (stored as large as 2^14 times itself) loses less than 2^-126 by that, and so does
+        # the sum at each of its two steps from one part to the next: 5 x 2^-126 in all, which a value
+        # of 2^-100 or more does not feel.  Up to 8 tokens are summed without them, exactly.
+        tiny = 5 * 2.0 ** -126 if n > 8 and scale < 2.0 ** -100 else 0.0
+        assert np.abs(host(G) - host(Z[:, :1])).max() <= tiny and float(H.abs().max()) == 0.0
+    good = sn.sn_gated_ff(X, W, W)
+    bad = X.clone()
+    bad[n // 2, 3] = float("nan")
+    got = sn.sn_gated_ff(bad, W, W)
+    assert bool(got[n // 2].isnan().all())
+    keep = [i for i in range(n) if i != n // 2]
+    assert torch.equal(got[keep], good[keep])
+
+
+def test_no_tokens():
+    X, W = torch.zeros(0, 16, device="cuda"), torch.ones(16, 24, device="cuda")
+    H, G, Ut = sn.sn_gated_ff(X, W, W, save=True)
+    assert H.shape == G.shape == Ut.shape == (0, 24)
+    gWg, gWu = torch.ones(16, 24, device="cuda"), torch.ones(16, 24, device="cuda")
+    for add, value in ((True, 1.0), (False, 0.0)):
+        dX, _, _ = sn.sn_gated_ff_backward(X, W, W, G, Ut, H, gWg=gWg, gWu=gWu, accumulate=add)
+        assert dX.shape == (0, 16) and bool((gWg == value).all()) and bool((gWu == value).all())

@@ -1,0 +1,193 @@
+"""GPU parity of the orthogonalised updates against the float64 oracle.
+
+The tolerance is a bound on the error's Frobenius norm, made from the exact iterates X_k (u = 2^-24,
+m the shorter side, n the longer).  Sums of 3 K products are float32 by instructions of 32 terms,
+and operands are held to 2^-22: a product P Q is off by at most e(K) |P|_F |Q|_F,
+e(K) = u (3 K / 32 + 44) + 3 * 2^-22, and what is stored by 2^-22 of itself and by 2^-38 an element.
+A step's own error, with s = |X|_2 <= 1.21 and t = |A|_F:
+    dA <= e(n) |X|_F^2 + 2^-22 t + 2^-38 m,     dQ <= (4.8 + 4.1 s^2) dA + 2.1 e(m) t^2 + 2^-22 |Q|_F + 2^-38 m
+    dX <= s dQ + e(m) |Q|_F |X|_F + 2^-22 |X'|_F + 2^-38 sqrt(m n)
+A perturbation of X passes through the j steps that are left, f_j of the singular values, by at most
+the largest divided difference of the odd function f_j, max over [0, 1.21] of |f_j'| and |f_j(x) / x|
+(Daleckii and Krein).  The norm's rounding is u of X_0.  The sum over the steps, doubled for second
+order, bounds every element.
+"""
+from __future__ import annotations
+
+import functools
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01260_amd as sn
+from gpu_helpers import host, log
+from oracle import orth as orc
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+# wide, tall, square; one row, one column, one element; odd sizes, both sides of a tile's edge
+SHAPES = [(1, 1), (1, 9), (9, 1), (3, 4), (8, 8), (17, 40), (40, 17), (64, 64), (63, 65), (65, 130), (130, 66),
+          (128, 300), (257, 129), (200, 1000), (1003, 201)]
+
+
+@functools.lru_cache(None)
+def _gain(j):
+    """Largest divided difference of j steps on [0, 1.21]."""
+    x = np.linspace(1e-9, 1.21, 400001)
+    y = orc.f(x, j)
+    return float(max(np.abs(np.diff(y) / np.diff(x)).max(), np.abs(y / x).max())) * 1.01
+
+
+def _bound(M, steps):
+    xs = orc.iterates(M, steps)
+    m, n = min(M.shape), max(M.shape)
+
+    def e(k):
+        return U * (3 * k / 32 + 44) + 3 * 2.0 ** -22
+    total = 2 * U * _gain(steps)
+    for k in range(steps):
+        x = xs[k] if M.shape[0] <= M.shape[1] else xs[k].T
+        a = x @ x.T
+        q = orc.A * np.eye(m) + orc.B * a + orc.C * a @ a
+        fx, t, fq = np.linalg.norm(x), np.linalg.norm(a), np.linalg.norm(q)
+        s = min(fx, 1.21)
+        da = e(n) * fx * fx + 2.0 ** -22 * t + 2.0 ** -38 * m
+        dq = (4.8 + 4.1 * s * s) * da + 2.1 * e(m) * t * t + 2.0 ** -22 * fq + 2.0 ** -38 * m
+        dx = s * dq + e(m) * fq * fx + 2.0 ** -22 * np.linalg.norm(xs[k + 1]) + 2.0 ** -38 * (m * n) ** 0.5
+        total += _gain(steps - 1 - k) * dx
+    return 2 * total
+
+
+def _mat(seed, r, c, dtype, pad=0, std=1.0, rank=0):
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randn(r, c, generator=g)
+    if rank:
+        t = torch.randn(r, rank, generator=g) @ torch.randn(rank, c, generator=g) + 0.05 * t
+    out = torch.zeros(r, c + pad, dtype=DT[dtype], device="cuda")[:, :c]
+    out.copy_((t * std).to(DT[dtype]))
+    return out
+
+
+def _near(got, ref, tol, dtype, what):
+    """Off by at most tol in the Frobenius norm, and by each element's own rounding."""
+    got = np.asarray(got, np.float64)
+    assert got.shape == ref.shape and np.isfinite(got).all(), what
+    own = (2.0 ** -8 if dtype == "bf16" else U) * np.abs(ref)
+    err = np.abs(got - ref)
+    assert (err <= tol + own).all(), f"{what}: {err.max():.3g} over {tol:.3g}"
+    off = float(np.linalg.norm(np.maximum(err - 1.01 * own, 0.0)))
+    assert off <= tol, f"{what}: {off:.3g} over {tol:.3g}"
+    log(f"  {what}: ok, {off / max(tol, 1e-300):.2g} of the bound, {off / max(np.linalg.norm(ref), 1e-300):.2g} of the value")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_matches_oracle(dtype, shape):
+    log(f"[orthogonalize] {dtype} {shape}")
+    mats = [_mat(k, *shape, dtype, (0, 3, 8)[k], (1.0, 1e-12, 1e12)[k], (0, 2, 0)[k]) for k in range(3)]
+    for steps in (1, 5, 6):
+        got = sn.sn_orthogonalize(mats, steps=steps)
+        for k, (a, b) in enumerate(zip(got, mats)):
+            ref = orc.orthogonalize(host(b), steps)
+            _near(host(a), ref, _bound(host(b), steps), dtype, f"matrix {k}, {steps} steps")
+    # one matrix alone, in place, into rows with gaps: the same bits
+    one = mats[1].clone()
+    sn.sn_orthogonalize([one], steps=6, out=[one])
+    alone = sn.sn_orthogonalize(mats[1], steps=6)
+    assert torch.equal(one, got[1]) and torch.equal(alone, got[1])
+    r, c = shape
+    wide = torch.zeros(r, c + 7, dtype=DT[dtype], device="cuda")
+    sn.sn_orthogonalize(mats[0], steps=6, out=wide[:, :c])
+    assert torch.equal(wide[:, :c], got[0]) and float(wide[:, c:].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(96, 160), (160, 96), (33, 33)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_muon_step_matches_oracle(dtype, shape, nesterov):
+    log(f"[muon step] {dtype} {shape} nesterov={nesterov}")
+    count, lr, mu, decay, scale = 3, 0.05, 0.9, 0.01, 1.5
+    W = [_mat(k, *shape, dtype, k) for k in range(count)]
+    M = [torch.zeros(*shape, device="cuda") for _ in range(count)]
+    G = [_mat(20 + k, *shape, dtype, 2 * k, 1e-3) for k in range(count)]
+    for step in range(2):
+        w0, m0 = [host(w) for w in W], [host(m) for m in M]
+        assert sn.sn_muon_step(W, G, M, lr, momentum=mu, nesterov=nesterov, weight_decay=decay,
+                               scale=scale) is W
+        for k in range(count):
+            g = host(G[k])
+            ref_w, ref_m = orc.muon_step(w0[k], g, m0[k], lr, np.float32(mu), nesterov,
+                                         np.float32(decay), scale)
+            err = np.abs(host(M[k]) - ref_m)
+            assert (err <= 2 * U * (np.abs(ref_m) + np.abs(m0[k])) + 1e-37).all()
+            b = orc.momentum(m0[k], g, np.float32(mu), nesterov)[1]
+            # B itself is float32: 4 u of it, through the norm and the steps
+            tol = lr * scale * (_bound(b, 5) + 2 * 4 * U * _gain(5)) + 4 * U * np.abs(w0[k]).max() * 1.1 + \
+                4 * U * lr * scale
+            _near(host(W[k]), ref_w, tol * (1 if dtype == "bf16" else w0[k].size ** 0.5), dtype,
+                  f"step {step} matrix {k}")
+
+
+def test_more_matrices_than_a_launch_takes():
+    log("[orthogonalize, 70 matrices]")
+    mats = [_mat(k, 20, 33, "f32") for k in range(70)]
+    got = sn.sn_orthogonalize(mats)
+    for k in (0, 31, 32, 63, 64, 69):
+        assert torch.equal(got[k], sn.sn_orthogonalize(mats[k]))
+        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5), "f32", f"matrix {k}")
+
+
+@pytest.mark.parametrize("count,shape", [(1, (1100, 2100)), (1, (2100, 1100)), (5, (700, 900)), (24, (520, 540))],
+                         ids=lambda s: str(s))
+def test_large_tiles(count, shape):
+    """Products of every kind of tile; the same bits every time."""
+    log(f"[orthogonalize, large] {count} of {shape}")
+    mats = [_mat(k, *shape, "f32", 0, 1.0, 30) for k in range(count)]
+    got = sn.sn_orthogonalize(mats)
+    for k in {0, count - 1}:
+        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5), "f32", f"matrix {k}")
+    for _ in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(got, sn.sn_orthogonalize(mats)))
+
+
+def test_special_matrices():
+    """Zeros stay zeros; a NaN or an infinity makes its own matrix NaN and no other."""
+    log("[orthogonalize, special]")
+    mats = [_mat(k, 50, 70, "f32") for k in range(4)]
+    mats[1].zero_()
+    mats[2][3, 4] = float("nan")
+    mats[3][7, 8] = float("inf")
+    got = sn.sn_orthogonalize(mats)
+    assert float(got[1].abs().max()) == 0.0
+    assert bool(got[2].isnan().all()) and bool(got[3].isnan().all())
+    assert torch.equal(got[0], sn.sn_orthogonalize(mats[0]))
+
+
+def test_the_update_stays_in_the_subspace():
+    """Weights and gradients whose columns lie in the subspace: what an update leaves outside is
+    what float32 rounds."""
+    log("[muon step, subspace]")
+    r, k, c = 256, 24, 600
+    Q = torch.linalg.qr(torch.randn(r, k, dtype=torch.float64, generator=torch.Generator().manual_seed(1)))[0]
+    g = torch.Generator().manual_seed(2)
+    W, G = ((Q @ torch.randn(k, c, dtype=torch.float64, generator=g)).float().cuda() for _ in range(2))
+    M = torch.zeros(r, c, device="cuda")
+    w0 = W.clone()
+    sn.sn_muon_step(W, G, M, 0.1)
+    step = host(W) - host(w0)
+    q = Q.numpy()
+    outside = np.linalg.norm(step - q @ (q.T @ step))
+    # rounding of float32 W and G outside the subspace grows by 3.4445 a step, as G's small part
+    grown = 0.1 * 485 * 2.0 ** -24 + 2.0 ** -24 * np.linalg.norm(host(W)) * 2 + 0.1 * _bound(host(G), 5)
+    assert outside <= grown and np.linalg.norm(step) > 0.1
+    log(f"  {outside:.3g} outside, at most {grown:.3g}; the step {np.linalg.norm(step):.3g}")
+
+
+def test_nothing_to_do():
+    assert sn.sn_orthogonalize([]) == []
+    e = torch.zeros(0, 5, device="cuda")
+    assert sn.sn_orthogonalize([e])[0].shape == (0, 5)
+    assert sn.sn_muon_step([e], [e], [e], 0.1)[0] is e
