@@ -9,12 +9,17 @@
 // or with its rows contiguous (rows of the other index, one for each k, as W in X W).
 //
 // A workgroup holds BM x BN sums in registers and takes 64 k values a step: both
-// tiles come straight to the LDS (16 bytes a lane, no registers), two steps of them,
-// the next one on its way while this one is multiplied.  A tile's 16-byte pieces are
+// tiles come straight to the LDS (16 bytes a lane, no registers), into two places in turn.
+// A step is two halves of 32 k values.  While a half is multiplied, the next one's
+// operands are read, each register as its last product has been started; between the
+// halves the step that follows has landed, the present one's place is read out, and the
+// step after the next is sent for into it.  One barrier a step.  A tile's 16-byte pieces are
 // permuted so that the reads of an operand touch every LDS bank:
 //   KC    64 k values are 8 pieces of a row; piece p of row r lies at p ^ (r / 2 % 8)
-//   else  a k's row is R / 16 chunks of 16 values; chunk c of row k lies at c ^ (k % 8),
+//   else  a k's row is R / 16 chunks of 16 values; chunk c of row k lies at c ^ mm_key(k),
 //         and ds_read_b64_tr_b16 turns 4 k x 16 values into 4 k values of a lane
+// (ds_read_b128 serves lanes 0-3, 12-15 and 20-27 of a wave's half at a time, b64 32 lanes.
+// KC rows of 32 k values, 64 bytes, took a third longer: half lines from the L2.)
 // MFMA 16x16x32: lane l = 16 g + n supplies k = 8 g .. 8 g + 7 of row n of either
 // operand.  B is passed first, so that a lane's 4 results are 4 consecutive columns
 // j = 4 g + e of the row i = n.
@@ -57,8 +62,26 @@ struct MmArgs {
 // Source of the pieces past k: 16 bytes of zeros that every lane may load.
 __device__ const u32x4 mm_zeros = {0, 0, 0, 0};
 
-__device__ __forceinline__ void lds_load_16(const void *src, void *dst) {
-  __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)(dst), 16, 0, 0);
+// The 16 bytes at src (per lane) to LDS address dst + 16 * lane, dst the same in the wave.  In
+// assembly, as the compiler would wait for every such load before the first transposed
+// read after it (22 percent of the time of an 8192 x 8192 x 8192 product); it has no output
+// register, and the tile loop waits for it.
+__device__ __forceinline__ void lds_load_16(const void *src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(dst), "v"(src)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)(p)));
+}
+
+// Where the chunks of k's row lie in a tile of R values a row: rows k, k + 1, .. k + 3 and
+// k + 8, .. k + 11 are read together.
+template <int R>
+__device__ __forceinline__ int mm_key(int k) {
+  return R >= 128 ? (k & 3) | (k >> 1 & 4) : R == 64 ? (k >> 1 & 1) | (k >> 2 & 2) : 0;
 }
 
 // This thread's share of an operand's tile: L loads of 16 bytes a step.
@@ -68,7 +91,7 @@ __device__ __forceinline__ void lds_load_16(const void *src, void *dst) {
 template <bool KC, int R, int WAVES, int PAIR = 0>
 struct MmLoader {
   static constexpr int L = R / 8 / WAVES;
-  static_assert(L >= 1 && R % (8 * WAVES) == 0, "a step is whole loads of every wave");
+  static_assert(L >= 1 && R % (8 * WAVES) == 0 && WAVES >= 4, "a step is whole loads of every wave");
   const char *p[L];
   int64_t step;  // bytes
   int klane;     // the lane's first k of a step for load 0; KROW more for each further load
@@ -86,9 +109,9 @@ struct MmLoader {
         p[j] = reinterpret_cast<const char *>(o.p[0] + row * o.ld + kp * 8);
         klane = kp * 8;
       } else {
-        constexpr int S = R / 8, MASK = R >= 128 ? 7 : R / 16 - 1;
+        constexpr int S = R / 8;
         const int kr = idx / S, slot = idx % S;
-        int v = (((slot >> 1) ^ (kr & MASK)) << 4) | ((slot & 1) << 3);
+        int v = (((slot >> 1) ^ mm_key<R>(kr)) << 4) | ((slot & 1) << 3);
         int64_t twin = 0;
         if constexpr (PAIR > 0) {
           twin = v % PAIR >= PAIR / 2 ? o.twin : 0;
@@ -100,18 +123,14 @@ struct MmLoader {
       }
     }
   }
-  // Loads the step at k0 of a segment of k values into lds (this operand's tile) and
+  // Loads a step of which `left` k values are there into lds (this operand's tile) and
   // moves on.
-  __device__ __forceinline__ void load(char *lds, int64_t left, int wave) {
-    if (left >= kMmK) {
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(uint32_t lds, int64_t left, int wave) {
 #pragma unroll
-      for (int j = 0; j < L; ++j) lds_load_16(p[j], lds + (j * WAVES + wave) * 1024);
-    } else {
-#pragma unroll
-      for (int j = 0; j < L; ++j)
-        lds_load_16(klane + j * KROW < left ? static_cast<const void *>(p[j]) : &mm_zeros,
-                    lds + (j * WAVES + wave) * 1024);
-    }
+    for (int j = 0; j < L; ++j)
+      lds_load_16(WHOLE || klane + j * KROW < left ? static_cast<const void *>(p[j]) : &mm_zeros,
+                  lds + (j * WAVES + wave) * 1024);
 #pragma unroll
     for (int j = 0; j < L; ++j) p[j] += step;
   }
@@ -124,32 +143,30 @@ struct MmLoader {
 // The operand's fragment of 16 rows from a tile in the LDS.
 template <bool KC, int R>
 struct MmReader {
-  int off[2];  // KC: of the two halves of a step; else: of k % 8 < 4 and >= 4
+  int off[2];  // KC: of a step's halves; else: of k % 8 < 4 and >= 4
   __device__ __forceinline__ void init(int first, int lane) {
     const int g = lane >> 4, n = lane & 15;
     if constexpr (KC) {
-      const int s = (n >> 1) & 7;
-      off[0] = (first + n) * 128 + ((g ^ s) << 4);
+      off[0] = (first + n) * 128 + ((g ^ ((n >> 1) & 7)) << 4);
       off[1] = off[0] ^ 64;
     } else {
-      constexpr int MASK = R >= 128 ? 7 : R / 16 - 1;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int kr = 8 * g + 4 * h + (n >> 2);
-        off[h] = kr * R * 2 + ((((first >> 4) ^ (kr & MASK))) << 5) + (n & 3) * 8;
+        off[h] = kr * R * 2 + (((first >> 4) ^ mm_key<R>(kr)) << 5) + (n & 3) * 8;
       }
     }
   }
-  // fragment `tile` (16 rows each), half ks of the step
-  __device__ __forceinline__ u32x4 read(const char *lds, int tile, int ks) const {
+  // fragment `tile` (16 rows each) of half h of the step in lds
+  __device__ __forceinline__ u32x4 read(const char *lds, int tile, int h) const {
     if constexpr (KC) {
-      return *reinterpret_cast<const u32x4 *>(lds + off[ks] + tile * 2048);
+      return *reinterpret_cast<const u32x4 *>(lds + off[h] + tile * 2048);
     } else {
       u32x2 v[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const char *q = lds + ((off[h] ^ (tile << 5)) + ks * 32 * R * 2);
-        v[h] = __builtin_bit_cast(
+      for (int q4 = 0; q4 < 2; ++q4) {
+        const char *q = lds + (off[q4] ^ (tile << 5)) + h * 32 * R * 2;
+        v[q4] = __builtin_bit_cast(
             u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                        (__attribute__((address_space(3))) s16x4 *)(const_cast<char *>(q))));
       }
@@ -178,9 +195,10 @@ struct MmShape {
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // fragments of a wave
   static constexpr int PAIR = PAIRED_ ? BN / WN : 0;
   static constexpr int kTileBytes = (BM + BN) * kMmK * 2, kLds = 2 * kTileBytes;
+  static constexpr int kLoads = (BM + BN) / 8 / WAVES;  // of a lane and step
 };
 
-// Steps of 64 k values over all segments.
+// Steps over all segments.
 __host__ __device__ __forceinline__ int64_t mm_steps(const MmArgs &m) {
   return (m.k + kMmK - 1) / kMmK * m.segs;
 }
@@ -211,9 +229,16 @@ __device__ __forceinline__ void mm_tile(const MmArgs &m, int64_t r0, int64_t c0,
   int64_t left = m.k - done * kMmK;
   la.move((m.a.p[seg] - m.a.p[0]) * 2 + done * la.step + a_off);
   lb.move((m.b.p[seg] - m.b.p[0]) * 2 + done * lb.step + b_off);
-  const auto load = [&](char *buf) {
-    la.load(buf, left, wave);
-    lb.load(buf + S::BM * kMmK * 2, left, wave);
+  constexpr int kB = S::BM * kMmK * 2;  // B's tile of a step lies behind A's
+  const uint32_t place = __builtin_amdgcn_readfirstlane(lds_address(lds));
+  const auto load = [&](uint32_t to) {
+    if (left >= kMmK) {
+      la.template load<true>(to, left, wave);
+      lb.template load<true>(to + kB, left, wave);
+    } else {
+      la.template load<false>(to, left, wave);
+      lb.template load<false>(to + kB, left, wave);
+    }
     left -= kMmK;
     if (left <= 0 && seg + 1 < m.segs) {
       la.move((m.a.p[seg + 1] - m.a.p[seg]) * 2 - steps * la.step);
@@ -222,12 +247,44 @@ __device__ __forceinline__ void mm_tile(const MmArgs &m, int64_t r0, int64_t c0,
       left = m.k;
     }
   };
-  load(lds);
-  int cur = 0;
+  u32x4 fa[S::TM], fb[2][S::TN];
+  load(place);
+  if (t0 + 1 < t1) {
+    load(place + S::kTileBytes);
+    wait_vmcnt<S::kLoads>();
+  } else {
+    wait_vmcnt<0>();
+  }
+  lds_barrier();
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j) fb[0][j] = rb.read(lds + kB, j, 0);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) fa[i] = ra.read(lds, i, 0);
+  // the products of half h; meanwhile the operands of half `to` from buf
+  const auto half = [&](const char *buf, int h, int to) {
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) fb[to][j] = rb.read(buf + kB, j, to);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) acc[i][j] = mm_mfma<S::F16>(fb[h][j], fa[i], acc[i][j]);
+      fa[i] = ra.read(buf, i, to);
+    }
+    // A's reads each behind the products that it is free after, B's behind the first
+    constexpr int RA = S::AK ? 1 : 2, RB = S::BK ? 1 : 2;
+    __builtin_amdgcn_sched_group_barrier(0x008, S::TN, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, RA + S::TN * RB, 0);
+#pragma unroll
+    for (int i = 1; i < S::TM; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, S::TN, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
+    }
+  };
   int64_t t = t0;
+  uint32_t cur = 0;  // where the present step lies
 #pragma unroll 1
   for (int r = 0; r < 3; ++r) {
-    const int64_t end = r < 2 ? m.run[r] * steps : t1;
+    const int64_t end = r < 2 && m.run[r] * steps < t1 ? m.run[r] * steps : t1;
     if (r && m.run[r - 1] < m.segs) {
 #pragma unroll
       for (int i = 0; i < S::TM; ++i)
@@ -235,23 +292,13 @@ __device__ __forceinline__ void mm_tile(const MmArgs &m, int64_t r0, int64_t c0,
         for (int j = 0; j < S::TN; ++j) acc[i][j] *= m.factor;
     }
 #pragma unroll 1
-    for (; t < end && t < t1; ++t, cur ^= 1) {
-      const char *buf = lds + cur * S::kTileBytes;
-      wait_vmcnt<0>();
+    for (; t < end; ++t) {
+      half(lds + cur, 0, 1);
+      wait_vmcnt<0>();  // the next step's loads
       lds_barrier();
-      if (t + 1 < t1) load(lds + (cur ^ 1) * S::kTileBytes);
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        u32x4 fa[S::TM], fb[S::TN];
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j) fb[j] = rb.read(buf + S::BM * kMmK * 2, j, ks);
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i) fa[i] = ra.read(buf, i, ks);
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-          for (int j = 0; j < S::TN; ++j) acc[i][j] = mm_mfma<S::F16>(fb[j], fa[i], acc[i][j]);
-      }
+      if (t + 2 < t1) load(place + cur);
+      cur ^= S::kTileBytes;
+      half(lds + cur, 1, 0);  // behind the last step, operands that nothing uses
     }
   }
 }
