@@ -7,12 +7,20 @@
 //
 // Small singular values grow by 3.44 a step, and so do errors in their directions: bf16
 // operands would leave an error of some percent.  So X, A and Q = a I + b A + c A^2 are held
-// as two fp16 planes, hi + lo (22 bits), and hi hi + hi lo + lo hi are added up in
+// as two fp16 planes, hi + lo (22 bits), and hi lo + lo hi + hi hi are added up in
 // float32: a third of the matrix cores' 16-bit rate for results like float32's.  fp16's
 // range is no limit: |X| <= 1.21 by the polynomial's maximum on [0, 1.21] and |A|, |Q| by
 // 1.45 and 3.45, each is stored times a power of two that keeps it below 65504, and lo
 // times 2^11, as large as hi at most, so that what fp16's least normal number, 2^-14, cuts
 // off lies below 2^-28 in hi and 2^-39 in all.
+// Where the result is rounded to bf16, products are left out whose part of it is small beside
+// that rounding (1.7e-3 of the result's norm): A is made of hi hi, A^2 too but in the last
+// two steps, and Q X of Q's hi with both planes of X but in the last step: 16 products of
+// m x m x n, a symmetric one for half, where 30 make five whole steps.  The error is
+// 0.7e-3 to 1.6e-3 of the result's norm (Gaussian matrices, few strong directions, singular
+// values over four decades, rank 20 of 384).  What must not go is X's lo: with hi alone
+// it is 7e-3 over four decades and 4e-2 in rank 20, where the rounded-off part of X grows
+// into directions that X does not have.
 // A and Q are symmetric: the tiles on and below the diagonal are computed and mirrored.
 // Matrices of one shape share every launch.
 #include "sn_internal.h"
@@ -86,8 +94,8 @@ __device__ __forceinline__ float f16_value(uint16_t v) {
 __device__ __forceinline__ uint16_t f16_bits(float v) {
   return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
 }
-// fp16 planes of four values
-__device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v) {
+// fp16 planes of four values (low: both of them)
+__device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v, bool low = true) {
   uint16_t h[4], l[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -96,6 +104,7 @@ __device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v) {
   }
   *reinterpret_cast<u32x2 *>(to) =
       u32x2{h[0] | static_cast<uint32_t>(h[1]) << 16, h[2] | static_cast<uint32_t>(h[3]) << 16};
+  if (!low) return;
   *reinterpret_cast<u32x2 *>(to + plane) =
       u32x2{l[0] | static_cast<uint32_t>(l[1]) << 16, l[2] | static_cast<uint32_t>(l[3]) << 16};
 }
@@ -130,7 +139,8 @@ __global__ __launch_bounds__(256) void orth_split_kernel(OrthMats t, OrthArgs a,
 template <class S, bool POLY>
 __global__ __launch_bounds__(S::NT, S::NT / 256) void orth_sym_kernel(MmArgs m, int64_t n, int64_t ldp,
                                                                      int64_t side, int64_t from,
-                                                                     const uint16_t *A, uint16_t *to) {
+                                                                     const uint16_t *A, uint16_t *to,
+                                                                     bool low) {
   static_assert(S::BM == S::BN, "a tile on the diagonal is square");
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
   const int64_t tiles = side * (side + 1) / 2;
@@ -172,14 +182,14 @@ __global__ __launch_bounds__(S::NT, S::NT / 256) void orth_sym_kernel(MmArgs m, 
         }
         if (!inside) v[e] = 0.0f;
       }
-      if (row < n) orth_put(out + row * ldp + col, plane, v);
+      if (row < n) orth_put(out + row * ldp + col, plane, v, low);
       if (ti == tj) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (col + e >= n) continue;
         uint16_t *p = out + (col + e) * ldp + row;
         p[0] = f16_bits(v[e]);
-        p[plane] = f16_bits((v[e] - f16_value(p[0])) * kUp);
+        if (low) p[plane] = f16_bits((v[e] - f16_value(f16_bits(v[e]))) * kUp);
       }
     }
   }
@@ -262,16 +272,22 @@ OrthPlan orth_plan(int64_t rows, int64_t cols, int64_t count) {
   return p;
 }
 
-void planes(MmArgs &m, const uint16_t *a, int64_t aplane, const uint16_t *b, int64_t bplane) {
-  m.segs = 3;  // hi lo, lo hi, then hi hi
-  m.run[0] = 2;
-  m.run[1] = 3;
+// The products that are added up: hi lo, lo hi and hi hi; hi hi alone; with both planes of
+// one operand.
+enum Products { kAll, kHigh, kBothOfA, kBothOfB };
+void planes(MmArgs &m, const uint16_t *a, int64_t aplane, const uint16_t *b, int64_t bplane,
+            Products which) {
+  m.segs = 0;
   m.factor = 1.0f / kUp;
-  const int first[3] = {0, 1, 0}, second[3] = {1, 0, 0};
-  for (int s = 0; s < 3; ++s) {
-    m.a.p[s] = a + first[s] * aplane;
-    m.b.p[s] = b + second[s] * bplane;
-  }
+  const auto add = [&](int pa, int pb) {
+    m.a.p[m.segs] = a + pa * aplane;
+    m.b.p[m.segs++] = b + pb * bplane;
+  };
+  if (which == kAll || which == kBothOfB) add(0, 1);
+  if (which == kAll || which == kBothOfA) add(1, 0);
+  m.run[0] = m.segs ? m.segs : 1;
+  add(0, 0);
+  m.run[1] = m.segs;
 }
 
 // Largest tile that gives most CUs one.
@@ -285,16 +301,16 @@ int orth_tile(int64_t gm, int64_t gn, int64_t count, bool sym) {
 
 template <bool K, bool POLY>
 void run_sym(const MmArgs &m, int64_t n, int64_t ldp, int64_t count, int64_t from, const uint16_t *A,
-             uint16_t *to, hipStream_t s) {
+             uint16_t *to, bool low, hipStream_t s) {
   const int size = orth_tile(n, n, count, true);
   const int64_t side = ceil_div(n, size);
   const unsigned grid = static_cast<unsigned>(side * (side + 1) / 2 * count);
   if (size == 256)
-    orth_sym_kernel<MmShape<true, K, K, 256, 256, 2, 4>, POLY><<<grid, 512, 0, s>>>(m, n, ldp, side, from, A, to);
+    orth_sym_kernel<MmShape<true, K, K, 256, 256, 2, 4>, POLY><<<grid, 512, 0, s>>>(m, n, ldp, side, from, A, to, low);
   else if (size == 128)
-    orth_sym_kernel<MmShape<true, K, K, 128, 128, 2, 2>, POLY><<<grid, 256, 0, s>>>(m, n, ldp, side, from, A, to);
+    orth_sym_kernel<MmShape<true, K, K, 128, 128, 2, 2>, POLY><<<grid, 256, 0, s>>>(m, n, ldp, side, from, A, to, low);
   else
-    orth_sym_kernel<MmShape<true, K, K, 64, 64, 2, 2>, POLY><<<grid, 256, 0, s>>>(m, n, ldp, side, from, A, to);
+    orth_sym_kernel<MmShape<true, K, K, 64, 64, 2, 2>, POLY><<<grid, 256, 0, s>>>(m, n, ldp, side, from, A, to, low);
 }
 
 template <bool BK, bool LAST, typename T>
@@ -332,21 +348,21 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
     m.k = tall ? a.rows : a.cols;
     m.a.ld = m.b.ld = p.ldx;
     m.a.n = m.b.n = tall ? p.ldx : a.rows;
-    planes(m, x, xplane, x, xplane);
+    const bool whole = sizeof(T) == 4, last = i + 1 == a.steps;
+    planes(m, x, xplane, x, xplane, whole ? kAll : kHigh);
     if (tall)
-      run_sym<false, false>(m, p.n, p.lda, a.count, 4 * xplane, nullptr, A, s);
+      run_sym<false, false>(m, p.n, p.lda, a.count, 4 * xplane, nullptr, A, true, s);
     else
-      run_sym<true, false>(m, p.n, p.lda, a.count, 4 * xplane, nullptr, A, s);
+      run_sym<true, false>(m, p.n, p.lda, a.count, 4 * xplane, nullptr, A, true, s);
     m.k = p.n;
     m.a.ld = m.b.ld = p.lda;
     m.a.n = m.b.n = p.n;
-    planes(m, A, aplane, A, aplane);
-    run_sym<true, true>(m, p.n, p.lda, a.count, 4 * aplane, A, Q, s);
-    const bool last = i + 1 == a.steps;
+    planes(m, A, aplane, A, aplane, whole || i + 2 >= a.steps ? kAll : kHigh);
+    run_sym<true, true>(m, p.n, p.lda, a.count, 4 * aplane, A, Q, whole, s);
     if (tall) {
       m.a.ld = p.ldx;
       m.a.n = a.rows;
-      planes(m, x, xplane, Q, aplane);
+      planes(m, x, xplane, Q, aplane, whole ? kAll : last ? kHigh : kBothOfA);
       if (last)
         run_apply<true, true, T>(m, t, a, 4 * xplane, 4 * aplane, next, p.ldx, s);
       else
@@ -354,7 +370,7 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
     } else {
       m.b.ld = p.ldx;
       m.b.n = p.ldx;
-      planes(m, Q, aplane, x, xplane);
+      planes(m, Q, aplane, x, xplane, whole ? kAll : last ? kHigh : kBothOfB);
       if (last)
         run_apply<false, true, T>(m, t, a, 4 * aplane, 4 * xplane, next, p.ldx, s);
       else

@@ -1,12 +1,15 @@
 """GPU parity of the orthogonalised updates against the float64 oracle.
 
 The tolerance is a bound on the error's Frobenius norm, made from the exact iterates X_k (u = 2^-24,
-m the shorter side, n the longer).  Sums of 3 K products are float32 by instructions of 32 terms,
-and operands are held to 2^-22: a product P Q is off by at most e(K) |P|_F |Q|_F,
-e(K) = u (3 K / 32 + 44) + 3 * 2^-22, and what is stored by 2^-22 of itself and by 2^-38 an element.
+m the shorter side, n the longer).  Sums of p K products are float32 by instructions of 32 terms,
+and operands are held to 2^-22, or to 2^-11 where only their high plane counts: a product P Q is off by
+at most e |P|_F |Q|_F, e = u (p K / 32 + 44) + r, r the sum of both operands' roundings (and 2^-22 for
+lo lo), and what is stored by 2^-22 of itself and by 2^-38 an element.  For float32 all products have
+p = 3 and r = 3 * 2^-22; for bf16 A = X X^T has p = 1 and r = 2^-10, A^2 the same but in the last two
+steps, and Q X has p = 2 and r = 2^-11 + 2^-22, in the last step 1 and 2^-10.
 A step's own error, with s = |X|_2 <= 1.21 and t = |A|_F:
-    dA <= e(n) |X|_F^2 + 2^-22 t + 2^-38 m,     dQ <= (4.8 + 4.1 s^2) dA + 2.1 e(m) t^2 + 2^-22 |Q|_F + 2^-38 m
-    dX <= s dQ + e(m) |Q|_F |X|_F + 2^-22 |X'|_F + 2^-38 sqrt(m n)
+    dA <= e |X|_F^2 + 2^-22 t + 2^-38 m,     dQ <= (4.8 + 4.1 s^2) dA + 2.1 e t^2 + 2^-22 |Q|_F + 2^-38 m
+    dX <= s dQ + e |Q|_F |X|_F + 2^-22 |X'|_F + 2^-38 sqrt(m n)
 A perturbation of X passes through the j steps that are left, f_j of the singular values, by at most
 the largest divided difference of the odd function f_j, max over [0, 1.21] of |f_j'| and |f_j(x) / x|
 (Daleckii and Krein).  The norm's rounding is u of X_0.  The sum over the steps, doubled for second
@@ -41,22 +44,28 @@ def _gain(j):
     return float(max(np.abs(np.diff(y) / np.diff(x)).max(), np.abs(y / x).max())) * 1.01
 
 
-def _bound(M, steps):
+def _bound(M, steps, dtype):
     xs = orc.iterates(M, steps)
     m, n = min(M.shape), max(M.shape)
 
-    def e(k):
-        return U * (3 * k / 32 + 44) + 3 * 2.0 ** -22
+    def e(k, p, r):
+        return U * (p * k / 32 + 44) + r
+    whole = 3, 3 * 2.0 ** -22
     total = 2 * U * _gain(steps)
     for k in range(steps):
+        gram = square = apply = whole
+        if dtype == "bf16":
+            gram = 1, 2.0 ** -10
+            square = whole if k + 2 >= steps else gram
+            apply = gram if k + 1 == steps else (2, 2.0 ** -11 + 2.0 ** -22)
         x = xs[k] if M.shape[0] <= M.shape[1] else xs[k].T
         a = x @ x.T
         q = orc.A * np.eye(m) + orc.B * a + orc.C * a @ a
         fx, t, fq = np.linalg.norm(x), np.linalg.norm(a), np.linalg.norm(q)
         s = min(fx, 1.21)
-        da = e(n) * fx * fx + 2.0 ** -22 * t + 2.0 ** -38 * m
-        dq = (4.8 + 4.1 * s * s) * da + 2.1 * e(m) * t * t + 2.0 ** -22 * fq + 2.0 ** -38 * m
-        dx = s * dq + e(m) * fq * fx + 2.0 ** -22 * np.linalg.norm(xs[k + 1]) + 2.0 ** -38 * (m * n) ** 0.5
+        da = e(n, *gram) * fx * fx + 2.0 ** -22 * t + 2.0 ** -38 * m
+        dq = (4.8 + 4.1 * s * s) * da + 2.1 * e(m, *square) * t * t + 2.0 ** -22 * fq + 2.0 ** -38 * m
+        dx = s * dq + e(m, *apply) * fq * fx + 2.0 ** -22 * np.linalg.norm(xs[k + 1]) + 2.0 ** -38 * (m * n) ** 0.5
         total += _gain(steps - 1 - k) * dx
     return 2 * total
 
@@ -92,7 +101,7 @@ def test_orthogonalize_matches_oracle(dtype, shape):
         got = sn.sn_orthogonalize(mats, steps=steps)
         for k, (a, b) in enumerate(zip(got, mats)):
             ref = orc.orthogonalize(host(b), steps)
-            _near(host(a), ref, _bound(host(b), steps), dtype, f"matrix {k}, {steps} steps")
+            _near(host(a), ref, _bound(host(b), steps, dtype), dtype, f"matrix {k}, {steps} steps")
     # one matrix alone, in place, into rows with gaps: the same bits
     one = mats[1].clone()
     sn.sn_orthogonalize([one], steps=6, out=[one])
@@ -125,10 +134,23 @@ def test_muon_step_matches_oracle(dtype, shape, nesterov):
             assert (err <= 2 * U * (np.abs(ref_m) + np.abs(m0[k])) + 1e-37).all()
             b = orc.momentum(m0[k], g, np.float32(mu), nesterov)[1]
             # B itself is float32: 4 u of it, through the norm and the steps
-            tol = lr * scale * (_bound(b, 5) + 2 * 4 * U * _gain(5)) + 4 * U * np.abs(w0[k]).max() * 1.1 + \
+            tol = lr * scale * (_bound(b, 5, dtype) + 2 * 4 * U * _gain(5)) + 4 * U * np.abs(w0[k]).max() * 1.1 + \
                 4 * U * lr * scale
             _near(host(W[k]), ref_w, tol * (1 if dtype == "bf16" else w0[k].size ** 0.5), dtype,
                   f"step {step} matrix {k}")
+
+
+@pytest.mark.parametrize("shape,rank,std", [((384, 640), 0, 1.0), ((384, 640), 48, 1e-3), ((512, 300), 20, 1e-5),
+                                            ((256, 256), 0, 1e3)], ids=str)
+def test_bf16_results_are_as_good_as_their_rounding(shape, rank, std):
+    """Random roundings add up as their squares do: the products that bf16 results leave out cost at
+    most 1.6e-3 of the norm over such matrices, the rounding to bf16 2^-9 / sqrt(3) * 1.5 = 1.7e-3."""
+    log(f"[orthogonalize, bf16] {shape} rank {rank}")
+    a = _mat(5, *shape, "bf16", 0, std, rank)
+    ref = orc.orthogonalize(host(a))
+    off = np.linalg.norm(host(sn.sn_orthogonalize(a)) - ref) / np.linalg.norm(ref)
+    log(f"  {off:.2e} of the norm")
+    assert off <= 1.1 * (1.6e-3 ** 2 + 1.7e-3 ** 2) ** 0.5
 
 
 def test_more_matrices_than_a_launch_takes():
@@ -137,7 +159,7 @@ def test_more_matrices_than_a_launch_takes():
     got = sn.sn_orthogonalize(mats)
     for k in (0, 31, 32, 63, 64, 69):
         assert torch.equal(got[k], sn.sn_orthogonalize(mats[k]))
-        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5), "f32", f"matrix {k}")
+        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, "f32"), "f32", f"matrix {k}")
 
 
 @pytest.mark.parametrize("count,shape", [(1, (1100, 2100)), (1, (2100, 1100)), (5, (700, 900)), (24, (520, 540))],
@@ -148,7 +170,7 @@ def test_large_tiles(count, shape):
     mats = [_mat(k, *shape, "f32", 0, 1.0, 30) for k in range(count)]
     got = sn.sn_orthogonalize(mats)
     for k in {0, count - 1}:
-        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5), "f32", f"matrix {k}")
+        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, "f32"), "f32", f"matrix {k}")
     for _ in range(2):
         assert all(torch.equal(a, b) for a, b in zip(got, sn.sn_orthogonalize(mats)))
 
@@ -181,7 +203,7 @@ def test_the_update_stays_in_the_subspace():
     q = Q.numpy()
     outside = np.linalg.norm(step - q @ (q.T @ step))
     # rounding of float32 W and G outside the subspace grows by 3.4445 a step, as G's small part
-    grown = 0.1 * 485 * 2.0 ** -24 + 2.0 ** -24 * np.linalg.norm(host(W)) * 2 + 0.1 * _bound(host(G), 5)
+    grown = 0.1 * 485 * 2.0 ** -24 + 2.0 ** -24 * np.linalg.norm(host(W)) * 2 + 0.1 * _bound(host(G), 5, "f32")
     assert outside <= grown and np.linalg.norm(step) > 0.1
     log(f"  {outside:.3g} outside, at most {grown:.3g}; the step {np.linalg.norm(step):.3g}")
 
