@@ -804,8 +804,9 @@ size_t sn_orthogonalize_workspace_bytes(int32_t count, int64_t rows, int64_t col
  *             in[i] itself (same pointer and stride), else may not overlap an input
  *   steps     1 .. SN_MAX_ORTH_STEPS
  *   workspace sn_orthogonalize_workspace_bytes(count, rows, cols) bytes, 256-byte aligned
- * Without elements or matrices a no-op.  Deterministic.  Errors: NULL, SHAPE, DTYPE, ALIGN,
- * ALIAS, WORKSPACE, HIP. */
+ * Without elements or matrices a no-op.  Deterministic; the order of a matrix's sums, and with
+ * it the last bits, depends on the number of matrices in the call.  Errors: NULL, SHAPE, DTYPE,
+ * ALIGN, ALIAS, WORKSPACE, HIP. */
 int32_t sn_orthogonalize(int32_t count, const sn_tensor *in, const sn_tensor *out, int32_t steps,
                          void *workspace, size_t workspace_bytes, sn_stream stream);
 

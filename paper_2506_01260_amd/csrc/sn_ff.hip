@@ -147,63 +147,20 @@ __global__ __launch_bounds__(256) void ff_dact_kernel(FfGradArgs a, uint16_t *pg
   }
 }
 
-// ---- four sums of a row -------------------------------------------------------------------
-typedef uint32_t quad_b16 __attribute__((ext_vector_type(2), aligned(2)));
-typedef float quad_b32 __attribute__((ext_vector_type(4), aligned(4)));
-template <typename T>
-__device__ __forceinline__ void put4(T *p, int64_t left, f32x4 v) {
-  if (left >= 4) {
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<quad_b16 *>(p) = quad_b16{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
-    else
-      *reinterpret_cast<quad_b32 *>(p) = quad_b32{v.x, v.y, v.z, v.w};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (e < left) p[e] = from_f32<T>(v[e]);
-  }
-}
-template <typename T>
-__device__ __forceinline__ f32x4 get4(const T *p, int64_t left) {
-  f32x4 v = {0, 0, 0, 0};
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < left) v[e] = to_f32(p[e]);
-  return v;
-}
-
 // ---- forward: both products and the activation ------------------------------------------
-template <class S, typename T>
-__global__ __launch_bounds__(S::NT, S::NT / 256) void ff_kernel(MmArgs m, FfArgs a, int64_t gm,
-                                                               int64_t gn, int splits) {
-  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  constexpr int HALF = S::PAIR / 2, TP = S::TN / 2;
-  const int64_t tiles = gm * gn, id = mm_order(group_number(), tiles * splits);
-  if (group_number() >= tiles * splits) return;
-  const int64_t split = id / tiles, steps = mm_steps(m);
-  int64_t tm, tn;
-  mm_place(id - split * tiles, gm, gn, tm, tn);
-  f32x4 acc[S::TM][S::TN];
-  mm_tile<S>(m, tm * S::BM, tn * (S::BN / 2), split * steps / splits, (split + 1) * steps / splits,
-             lds, acc);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row0 = tm * S::BM + wave / S::WN * (S::BM / S::WM) + (lane & 15);
-  const int64_t col0 = tn * (S::BN / 2) + wave % S::WN * HALF + 4 * (lane >> 4);
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int64_t row = row0 + i * 16;
-    if (row >= a.N) continue;
+template <typename T>
+struct FfEpilogue {
+  FfArgs a;
+  template <class S>
+  __device__ __forceinline__ void row(const MmPlace &, int64_t row, int64_t col0,
+                                      f32x4 (&acc)[S::TN]) const {
+    constexpr int TP = S::TN / 2;
+    if (row >= a.N) return;
 #pragma unroll
     for (int j = 0; j < TP; ++j) {
       const int64_t col = col0 + j * 16, left = a.ff - col;
       if (left <= 0) continue;
-      const f32x4 g = acc[i][j], u = acc[i][j + TP];
-      if (splits > 1) {
-        float *p = a.part + (split * 2 * a.N + row) * a.ff + col;
-        put4(p, left, g);
-        put4(p + a.N * a.ff, left, u);
-        continue;
-      }
+      const f32x4 g = acc[j], u = acc[j + TP];
       f32x4 h;
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[e] = ff_act(a.act, g[e]) * u[e];
@@ -214,7 +171,7 @@ __global__ __launch_bounds__(S::NT, S::NT / 256) void ff_kernel(MmArgs m, FfArgs
       }
     }
   }
-}
+};
 
 // H (G, U) from the parts of the sums: parts x {G, U} x N x ff, added in order.
 template <typename T>
@@ -325,83 +282,36 @@ __global__ __launch_bounds__(256) void ff_vec_kernel(FfArgs a, int slices) {
 }
 
 // ---- products of the backward -----------------------------------------------------------
-// C (M x N, and with two of them the twin C2 from the operand B's twin) = the product,
-// added to what is there with `add`; or its parts, splits x M x N (twin after twin).
+// C (M x N; C2 for the second matrix) = the product, added to what is there with `add`.
+template <typename T>
 struct FfOut {
-  void *C, *C2;
+  T *C, *C2;
   int64_t M, N, ldc;
   int add;
-  float *part;
-};
-template <class S, typename T>
-__global__ __launch_bounds__(S::NT, S::NT / 256) void ff_mm_kernel(MmArgs m, FfOut o, int64_t gm,
-                                                                  int64_t gn, int twins, int splits) {
-  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  const int64_t tiles = gm * gn, all = tiles * twins * splits;
-  if (group_number() >= all) return;
-  const int64_t id = mm_order(group_number(), all);
-  const int64_t part = id / tiles, split = part / twins, steps = mm_steps(m);
-  const bool second = part - split * twins != 0;
-  int64_t tm, tn;
-  mm_place(id - part * tiles, gm, gn, tm, tn);
-  f32x4 acc[S::TM][S::TN];
-  mm_tile<S>(m, tm * S::BM, tn * S::BN, split * steps / splits, (split + 1) * steps / splits, lds,
-             acc, 0, second ? m.b.twin : 0);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row0 = tm * S::BM + wave / S::WN * (S::BM / S::WM) + (lane & 15);
-  const int64_t col0 = tn * S::BN + wave % S::WN * (S::BN / S::WN) + 4 * (lane >> 4);
-  T *C = static_cast<T *>(second ? o.C2 : o.C);
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int64_t row = row0 + i * 16;
-    if (row >= o.M) continue;
+  template <class S>
+  __device__ __forceinline__ void row(const MmPlace &p, int64_t row, int64_t col0,
+                                      f32x4 (&acc)[S::TN]) const {
+    if (row >= M) return;
+    T *to = (p.z ? C2 : C) + row * ldc + col0;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
-      const int64_t col = col0 + j * 16, left = o.N - col;
+      const int64_t left = N - col0 - j * 16;
       if (left <= 0) continue;
-      if (splits > 1) {
-        put4(o.part + (part * o.M + row) * o.N + col, left, acc[i][j]);
-      } else {
-        f32x4 v = acc[i][j];
-        if (o.add) v += get4(C + row * o.ldc + col, left);
-        put4(C + row * o.ldc + col, left, v);
-      }
+      f32x4 v = acc[j];
+      if (add) v += get4(to + j * 16, left);
+      put4(to + j * 16, left, v);
     }
   }
-}
+};
 template <typename T>
-__global__ __launch_bounds__(256) void ff_sum_kernel(FfOut o, int twins, int splits) {
+__global__ __launch_bounds__(256) void ff_zero_kernel(FfOut<T> o) {
   const int64_t id = group_number() * 256 + threadIdx.x, per = (o.N + 3) / 4;
-  const int64_t r0 = id / per, c = (id - r0 * per) * 4, left = o.N - c;
-  if (r0 >= o.M * twins) return;
-  const bool second = r0 >= o.M;
-  const int64_t r = second ? r0 - o.M : r0;
-  T *C = static_cast<T *>(second ? o.C2 : o.C) + r * o.ldc + c;
-  f32x4 v = {0, 0, 0, 0};
-  for (int s = 0; s < splits; ++s) v += get4(o.part + (s * twins * o.M + r0) * o.N + c, left);
-  if (o.add) v += get4(C, left);
-  put4(C, left, v);
+  const int64_t r = id / per, c = (id - r * per) * 4;
+  if (r >= 2 * o.M) return;
+  put4((r < o.M ? o.C + r * o.ldc : o.C2 + (r - o.M) * o.ldc) + c, o.N - c, f32x4{0, 0, 0, 0});
 }
 
 // ---- plans --------------------------------------------------------------------------------
-// Tile and splits of an M x N product (N: both twins' columns) of `steps` steps: the
-// largest tile that gives every CU one, else the k steps are split too.
-struct Tiling {
-  int size;  // 256, 128 or 64
-  int64_t gm, gn;
-  int splits;
-};
-Tiling tiling(int64_t M, int64_t N, int64_t twins, int64_t steps) {
-  Tiling t = {};
-  for (int size : {256, 128, 64}) {
-    t = {size, ceil_div(M, size), ceil_div(N, size), 1};
-    if (t.gm * t.gn * twins >= 224) return t;
-  }
-  const int64_t want = ceil_div(1024, t.gm * t.gn * twins), most = steps / 8 > 1 ? steps / 8 : 1;
-  t.splits = static_cast<int>(want < most ? want : most);
-  return t;
-}
-
 constexpr int kPlanes[2] = {3, 1};  // of float32, bf16
 int segs_of(int dt) { return dt == 0 ? 6 : 1; }
 int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
@@ -457,7 +367,7 @@ bool by_vec(int dt, int64_t N, int64_t ff) { return N <= 8 && ff >= (dt == 0 ? 4
 
 struct FfPlan {
   bool vec, own_x, own_w;  // own: read in place
-  Tiling t;
+  MmPlan t;
   int slices;
   size_t x, w, part, total;
 };
@@ -472,23 +382,18 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
     p.own_x = own_x;
     p.own_w = own_w;
     // a paired tile has half its columns of either product
-    p.t = tiling(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
+    p.t = mm_plan(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
     if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
     if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
-    if (p.t.splits > 1) p.part = s.take(sizeof(float) * p.t.splits * 2 * N * ff);
+    p.part = s.take(p.t.part_bytes);
   }
   p.total = s.at;
   return p;
 }
 
-template <class S, typename T>
-void run_ff(const MmArgs &m, const FfArgs &a, const Tiling &t, hipStream_t s) {
-  ff_kernel<S, T><<<groups_grid(t.gm * t.gn * t.splits), S::NT, 0, s>>>(m, a, t.gm, t.gn, t.splits);
-}
 template <typename T>
 hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t s) {
   a.part = reinterpret_cast<float *>(ws + p.part);
-  int parts = p.slices;
   if (p.vec) {
     const dim3 grid = groups_grid(ceil_div(a.ff, kVecCols) * p.slices);
     if (a.N == 1)
@@ -499,6 +404,8 @@ hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t 
       ff_vec_kernel<T, 4><<<grid, 256, 0, s>>>(a, p.slices);
     else
       ff_vec_kernel<T, 8><<<grid, 256, 0, s>>>(a, p.slices);
+    if (p.slices > 1)
+      ff_join_kernel<T><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, p.slices);
   } else {
     MmArgs m = {};
     m.k = a.d;
@@ -524,21 +431,22 @@ hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t 
     }
     m.b.twin = static_cast<const char *>(wu) - static_cast<const char *>(wg);
     set_segs(m, dt, 1, {x}, a.N * up8(a.d), {wg}, a.d * up8(a.ff));
+    MmGrid g = p.t.grid;
+    g.part = a.part;
+    const FfEpilogue<T> e = {a};
     if (p.t.size == 256)
-      run_ff<MmShape<false, true, false, 256, 256, 2, 4, true>, T>(m, a, p.t, s);
+      mm_launch<MmShape<false, true, false, 256, 256, 2, 4, 2, true>>(m, g, e, s);
     else if (p.t.size == 128)
-      run_ff<MmShape<false, true, false, 128, 128, 2, 2, true>, T>(m, a, p.t, s);
+      mm_launch<MmShape<false, true, false, 128, 128, 2, 2, 2, true>>(m, g, e, s);
     else
-      run_ff<MmShape<false, true, false, 64, 64, 2, 2, true>, T>(m, a, p.t, s);
-    parts = p.t.splits;
+      mm_launch<MmShape<false, true, false, 64, 64, 2, 2, 4, true>>(m, g, e, s);
   }
-  if (parts > 1) ff_join_kernel<T><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, parts);
   return hipGetLastError();
 }
 
 struct FfGradPlan {
   bool own_x, own_w, own_g;
-  Tiling tx, tw;
+  MmPlan tx, tw;
   size_t x, w, g, part, total;
 };
 FfGradPlan ff_grad_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w, bool own_g) {
@@ -547,32 +455,31 @@ FfGradPlan ff_grad_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bo
   p.own_x = own_x;
   p.own_w = own_w;
   p.own_g = own_g;
-  p.tx = tiling(N, d, 1, ceil_div(ff, kMmK) * 2 * segs_of(dt));
-  p.tw = tiling(d, ff, 2, ceil_div(N, kMmK) * segs_of(dt));
+  p.tx = mm_plan(N, d, 1, ceil_div(ff, kMmK) * 2 * segs_of(dt));
+  p.tw = mm_plan(d, ff, 2, ceil_div(N, kMmK) * segs_of(dt));
   if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
   if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
   if (!own_g) p.g = s.take(2 * 2 * kPlanes[dt] * N * up8(ff));
-  const size_t px = p.tx.splits > 1 ? sizeof(float) * p.tx.splits * N * d : 0;
-  const size_t pw = p.tw.splits > 1 ? sizeof(float) * p.tw.splits * 2 * d * ff : 0;
-  p.part = s.take(px > pw ? px : pw);
+  p.part = s.take(p.tx.part_bytes > p.tw.part_bytes ? p.tx.part_bytes : p.tw.part_bytes);
   p.total = s.at;
   return p;
 }
 
 template <bool K, typename T>
-void run_mm(const MmArgs &m, const FfOut &o, const Tiling &t, int twins, hipStream_t s) {
-  const dim3 grid = groups_grid(t.gm * t.gn * twins * t.splits);
+void run_mm(const MmArgs &m, const FfOut<T> &o, const MmPlan &t, float *part, hipStream_t s) {
+  MmGrid g = t.grid;
+  g.part = part;
   if (t.size == 256)
-    ff_mm_kernel<MmShape<false, K, K, 256, 256, 2, 4>, T>
-        <<<grid, 512, 0, s>>>(m, o, t.gm, t.gn, twins, t.splits);
+    mm_launch<MmShape<false, K, K, 256, 256, 2, 4>>(m, g, o, s);
   else if (t.size == 128)
-    ff_mm_kernel<MmShape<false, K, K, 128, 128, 2, 2>, T>
-        <<<grid, 256, 0, s>>>(m, o, t.gm, t.gn, twins, t.splits);
+    mm_launch<MmShape<false, K, K, 128, 128, 2, 2>>(m, g, o, s);
   else
-    ff_mm_kernel<MmShape<false, K, K, 64, 64, 2, 2>, T>
-        <<<grid, 256, 0, s>>>(m, o, t.gm, t.gn, twins, t.splits);
-  if (t.splits > 1)
-    ff_sum_kernel<T><<<pieces_grid(o.M * twins, ceil_div(o.N, 4)), 256, 0, s>>>(o, twins, t.splits);
+    mm_launch<MmShape<false, K, K, 64, 64, 2, 2, 4>>(m, g, o, s);
+}
+
+template <typename T>
+FfOut<T> out_of(const FfGradArgs &a) {
+  return {static_cast<T *>(a.gWg), static_cast<T *>(a.gWu), a.d, a.ff, a.ldgw, a.add};
 }
 
 template <typename T>
@@ -612,7 +519,7 @@ hipError_t launch_ff_grad_t(int dt, const FfGradArgs &a, const FfGradPlan &p, ch
     m.b.ld = ldw;
     m.b.n = a.d;
     set_segs(m, dt, 2, {dg, du}, a.N * ff8, {wg, wu}, a.d * ff8);
-    run_mm<true, T>(m, {a.dX, nullptr, a.N, a.d, a.lddx, 0, part}, p.tx, 1, s);
+    run_mm<true, T>(m, {static_cast<T *>(a.dX), nullptr, a.N, a.d, a.lddx, 0}, p.tx, part, s);
   }
   if (want_w) {
     MmArgs m = {};
@@ -621,13 +528,12 @@ hipError_t launch_ff_grad_t(int dt, const FfGradArgs &a, const FfGradPlan &p, ch
     m.a.n = up8(a.d);
     m.b.ld = ldd;
     m.b.n = ff8;
-    m.b.twin = static_cast<const char *>(du) - static_cast<const char *>(dg);
+    m.b.batch = static_cast<const char *>(du) - static_cast<const char *>(dg);
     set_segs(m, dt, 1, {x}, a.N * up8(a.d), {dg}, a.N * ff8);
-    const FfOut o = {a.gWg, a.gWu, a.d, a.ff, a.ldgw, a.add, part};
     if (a.gdt == 0)
-      run_mm<false, float>(m, o, p.tw, 2, s);
+      run_mm<false, float>(m, out_of<float>(a), p.tw, part, s);
     else
-      run_mm<false, bf16_t>(m, o, p.tw, 2, s);
+      run_mm<false, bf16_t>(m, out_of<bf16_t>(a), p.tw, part, s);
   }
   return hipGetLastError();
 }
@@ -654,12 +560,11 @@ hipError_t launch_ff(int dt, const FfArgs &a, void *ws, hipStream_t s) {
 }
 hipError_t launch_ff_grad(int dt, const FfGradArgs &a, void *ws, hipStream_t s) {
   if (a.N == 0) {  // sums of nothing
-    const FfOut o = {a.gWg, a.gWu, a.d, a.ff, a.ldgw, a.add, nullptr};
     const dim3 grid = pieces_grid(2 * a.d, ceil_div(a.ff, 4));
     if (a.gdt == 0)
-      ff_sum_kernel<float><<<grid, 256, 0, s>>>(o, 2, 0);
+      ff_zero_kernel<<<grid, 256, 0, s>>>(out_of<float>(a));
     else
-      ff_sum_kernel<bf16_t><<<grid, 256, 0, s>>>(o, 2, 0);
+      ff_zero_kernel<<<grid, 256, 0, s>>>(out_of<bf16_t>(a));
     return hipGetLastError();
   }
   const FfGradPlan p = plan_of(dt, a);

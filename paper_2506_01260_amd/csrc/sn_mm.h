@@ -9,11 +9,11 @@
 // or with its rows contiguous (rows of the other index, one for each k, as W in X W).
 //
 // A workgroup holds BM x BN sums in registers and takes 64 k values a step: both
-// tiles come straight to the LDS (16 bytes a lane, no registers), into two places in turn.
+// tiles come straight to the LDS (16 bytes a lane, no registers), into DEPTH places in turn.
 // A step is two halves of 32 k values.  While a half is multiplied, the next one's
 // operands are read, each register as its last product has been started; between the
-// halves the step that follows has landed, the present one's place is read out, and the
-// step after the next is sent for into it.  One barrier a step.  A tile's 16-byte pieces are
+// halves the step that follows has landed, the present one's place is read out, and a
+// later step (with two places, the one after the next) is sent for into it.  One barrier a step.  A tile's 16-byte pieces are
 // permuted so that the reads of an operand touch every LDS bank:
 //   KC    64 k values are 8 pieces of a row; piece p of row r lies at p ^ (r / 2 % 8)
 //   else  a k's row is R / 16 chunks of 16 values; chunk c of row k lies at c ^ mm_key(k),
@@ -45,6 +45,7 @@ struct MmOperand {
   int64_t ld;                  // elements between rows (KC), or between k (else)
   int64_t n;                   // rows (KC) or values for each k (else; a multiple of 8)
   int64_t twin;                // bytes from a segment to its twin's (paired columns)
+  int64_t batch;               // bytes from a matrix's segment to the next matrix's
 };
 
 // Segments of split operands go from the smallest products to the largest in up to three
@@ -187,14 +188,16 @@ __device__ __forceinline__ f32x4 mm_mfma(u32x4 a, u32x4 b, f32x4 c) {
 
 // Sizes of a kernel: BM x BN sums, WM x WN waves, the operands' layouts.
 // PAIRED: every wave has columns of the operand B and the same ones of its twin.
-template <bool F16_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, bool PAIRED_ = false>
+// DEPTH: steps in the LDS.
+template <bool F16_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int DEPTH_ = 2,
+          bool PAIRED_ = false>
 struct MmShape {
   static constexpr bool F16 = F16_, AK = AK_, BK = BK_;
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_;
   static constexpr int WAVES = WM * WN, NT = WAVES * 64;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // fragments of a wave
   static constexpr int PAIR = PAIRED_ ? BN / WN : 0;
-  static constexpr int kTileBytes = (BM + BN) * kMmK * 2, kLds = 2 * kTileBytes;
+  static constexpr int kTileBytes = (BM + BN) * kMmK * 2, kLds = DEPTH * kTileBytes;
   static constexpr int kLoads = (BM + BN) / 8 / WAVES;  // of a lane and step
 };
 
@@ -248,13 +251,17 @@ __device__ __forceinline__ void mm_tile(const MmArgs &m, int64_t r0, int64_t c0,
     }
   };
   u32x4 fa[S::TM], fb[2][S::TN];
+  // With more than two places, steps past the last are loaded as zeros, so that as many loads
+  // are on their way as ever.
+  constexpr bool kAlways = S::DEPTH > 2;
   load(place);
-  if (t0 + 1 < t1) {
-    load(place + S::kTileBytes);
-    wait_vmcnt<S::kLoads>();
-  } else {
+#pragma unroll
+  for (int d = 1; d < S::DEPTH; ++d)
+    if (kAlways || t0 + d < t1) load(place + d * S::kTileBytes);
+  if (kAlways || t0 + 1 < t1)
+    wait_vmcnt<(S::DEPTH - 1) * S::kLoads>();
+  else
     wait_vmcnt<0>();
-  }
   lds_barrier();
 #pragma unroll
   for (int j = 0; j < S::TN; ++j) fb[0][j] = rb.read(lds + kB, j, 0);
@@ -294,13 +301,14 @@ __device__ __forceinline__ void mm_tile(const MmArgs &m, int64_t r0, int64_t c0,
 #pragma unroll 1
     for (; t < end; ++t) {
       half(lds + cur, 0, 1);
-      wait_vmcnt<0>();  // the next step's loads
+      wait_vmcnt<(S::DEPTH - 2) * S::kLoads>();  // the next step's loads
       lds_barrier();
-      if (t + 2 < t1) load(place + cur);
-      cur ^= S::kTileBytes;
+      if (kAlways || t + S::DEPTH < t1) load(place + cur);
+      cur = cur + S::kTileBytes == S::kLds ? 0 : cur + S::kTileBytes;
       half(lds + cur, 1, 0);  // behind the last step, operands that nothing uses
     }
   }
+  if (kAlways) wait_vmcnt<0>();  // the LDS is another workgroup's when this one ends
 }
 
 // Workgroup `id` of n, one for each tile: the tile's number.  Workgroups go to the eight
@@ -316,6 +324,190 @@ __device__ __forceinline__ void mm_place(int64_t t, int64_t gm, int64_t gn, int6
   const int64_t rows = gm - g * kMmGroup < kMmGroup ? gm - g * kMmGroup : kMmGroup;
   tm = g * kMmGroup + in % rows;
   tn = in / rows;
+}
+
+// Four values of a row from p on, of which `left` lie in it; at any alignment.
+typedef uint32_t quad_b16 __attribute__((ext_vector_type(2), aligned(2)));
+typedef float quad_b32 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+__device__ __forceinline__ void put4(T *p, int64_t left, f32x4 v) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<quad_b16 *>(p) = quad_b16{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+    else
+      *reinterpret_cast<quad_b32 *>(p) = quad_b32{v.x, v.y, v.z, v.w};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) p[e] = from_f32<T>(v[e]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ f32x4 get4(const T *p, int64_t left) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 2) {
+      const quad_b16 w = *reinterpret_cast<const quad_b16 *>(p);
+      return f32x4{bf_lo(w.x), bf_hi(w.x), bf_lo(w.y), bf_hi(w.y)};
+    } else {
+      const quad_b32 w = *reinterpret_cast<const quad_b32 *>(p);
+      return f32x4{w.x, w.y, w.z, w.w};
+    }
+  }
+  f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < left) v[e] = to_f32(p[e]);
+  return v;
+}
+
+// The workgroups of a product: `mats` matrices of gm x gn tiles, or the tiles on and below
+// the diagonal of gm x gm.  The first `whole` tiles have a workgroup each; the `rest`, too few
+// to keep every CU busy, are cut into `splits` runs of steps, whose sums go to `part` as the
+// threads hold them and are added, in order, by mm_finish_kernel.
+struct MmGrid {
+  int64_t gm, gn, mats;
+  bool sym;
+  int64_t whole, rest;
+  int splits;
+  float *part;
+};
+struct MmPlace {
+  int64_t z, tm, tn;
+};
+__device__ __forceinline__ MmPlace mm_where(const MmGrid &g, int64_t tile) {
+  MmPlace p;
+  if (g.sym) {
+    const int64_t each = g.gm * (g.gm + 1) / 2;
+    p.z = tile / each;
+    const int64_t k = tile - p.z * each;
+    p.tm = static_cast<int64_t>((sqrtf(8.0f * static_cast<float>(k) + 1.0f) - 1.0f) * 0.5f);
+    while (p.tm * (p.tm + 1) / 2 > k) --p.tm;
+    while ((p.tm + 1) * (p.tm + 2) / 2 <= k) ++p.tm;
+    p.tn = k - p.tm * (p.tm + 1) / 2;
+  } else {
+    const int64_t each = g.gm * g.gn;
+    p.z = tile / each;
+    mm_place(tile - p.z * each, g.gm, g.gn, p.tm, p.tn);
+  }
+  return p;
+}
+// A row of fragments to the epilogue: e.row<S>(place, row, column of this lane's first sum of
+// the first fragment, sums); fragment j lies 16 j columns on (paired: the twin's sums in the
+// second half of the fragments).
+template <class S, class Epi>
+__device__ __forceinline__ void mm_row(const Epi &e, const MmPlace &p, int i, f32x4 (&acc)[S::TN]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int C = S::PAIR ? 2 : 1;
+  const int64_t row = p.tm * S::BM + wave / S::WN * (S::BM / S::WM) + i * 16 + (lane & 15);
+  const int64_t col = p.tn * (S::BN / C) + wave % S::WN * (S::BN / S::WN / C) + 4 * (lane >> 4);
+  e.template row<S>(p, row, col, acc);
+}
+
+template <class S, class Epi>
+__global__ __launch_bounds__(S::NT, S::NT / 256) void mm_kernel(MmArgs m, MmGrid g, Epi e) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int64_t id = static_cast<int64_t>(blockIdx.y) * (1 << 20) + blockIdx.x;
+  if (id >= g.whole + g.rest * g.splits) return;
+  const int64_t steps = mm_steps(m);
+  int64_t tile, t0 = 0, t1 = steps, split = 0;
+  if (id < g.whole) {
+    tile = mm_order(id, g.whole);
+  } else {
+    split = (id - g.whole) / g.rest;
+    tile = id - split * g.rest;
+    t0 = split * steps / g.splits;
+    t1 = (split + 1) * steps / g.splits;
+  }
+  const MmPlace p = mm_where(g, tile);
+  f32x4 acc[S::TM][S::TN];
+  mm_tile<S>(m, p.tm * S::BM, p.tn * (S::PAIR ? S::BN / 2 : S::BN), t0, t1, lds, acc,
+             p.z * m.a.batch, p.z * m.b.batch);
+  if (id < g.whole || g.splits == 1) {
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) mm_row<S>(e, p, i, acc[i]);
+  } else {
+    f32x4 *to = reinterpret_cast<f32x4 *>(g.part) +
+                ((tile - g.whole) * g.splits + split) * (S::TM * S::TN * S::NT) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) to[(i * S::TN + j) * S::NT] = acc[i][j];
+  }
+}
+// A workgroup for each row of fragments of the cut tiles.
+template <class S, class Epi>
+__global__ __launch_bounds__(S::NT) void mm_finish_kernel(MmGrid g, Epi e) {
+  const int64_t id = static_cast<int64_t>(blockIdx.y) * (1 << 20) + blockIdx.x;
+  if (id >= g.rest * S::TM) return;
+  const int64_t tile = id / S::TM;
+  const int i = static_cast<int>(id - tile * S::TM);
+  const f32x4 *from = reinterpret_cast<const f32x4 *>(g.part) +
+                      (tile * g.splits * S::TM + i) * (S::TN * S::NT) + threadIdx.x;
+  f32x4 acc[S::TN];
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j) acc[j] = f32x4{0, 0, 0, 0};
+  for (int s = 0; s < g.splits; ++s, from += S::TM * S::TN * S::NT)
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) acc[j] += from[j * S::NT];
+  const MmPlace p = mm_where(g, g.whole + tile);
+  mm_row<S>(e, p, i, acc);
+}
+
+inline dim3 mm_groups(int64_t n) {
+  return dim3(static_cast<unsigned>(n < (1 << 20) ? n : 1 << 20),
+              static_cast<unsigned>(ceil_div(n, 1 << 20)));
+}
+template <class S, class Epi>
+void mm_launch(const MmArgs &m, const MmGrid &g, const Epi &e, hipStream_t s) {
+  mm_kernel<S, Epi><<<mm_groups(g.whole + g.rest * g.splits), S::NT, 0, s>>>(m, g, e);
+  if (g.splits > 1) mm_finish_kernel<S, Epi><<<mm_groups(g.rest * S::TM), S::NT, 0, s>>>(g, e);
+}
+
+// How a product of M x N sums over `steps` steps is cut (N: both twins' columns where they are
+// paired): the tile and the splits of the shortest time by this model, in us.  A step of a tile
+// takes what the kernels measured on full CUs; a CU holds one workgroup of 256 x 256, two of
+// 128 x 128 or 64 x 64; the parts are written and read at 4 TB/s, and adding them takes a launch.
+struct MmPlan {
+  int size;
+  MmGrid grid;
+  size_t part_bytes;
+};
+inline MmPlan mm_plan(int64_t M, int64_t N, int64_t mats, int64_t steps, bool sym = false) {
+  struct Kind {
+    int size, per_cu;
+    double step;
+  };
+  const Kind kinds[3] = {{256, 1, 1.93}, {128, 2, 1.06}, {64, 2, 0.45}};
+  MmPlan best = {};
+  double least = 0.0;
+  for (const Kind &k : kinds) {
+    MmGrid g = {};
+    g.gm = ceil_div(M, k.size);
+    g.gn = ceil_div(N, k.size);
+    g.mats = mats;
+    g.sym = sym;
+    const int64_t tiles = (sym ? g.gm * (g.gm + 1) / 2 : g.gm * g.gn) * mats, slots = 256 * k.per_cu;
+    for (int s = 1; s <= 16; ++s) {
+      g.splits = s;
+      if (s > 1 && steps / s < 4) break;
+      const int64_t rounds = tiles / slots;
+      g.whole = s == 1 ? tiles : rounds * slots;
+      g.rest = tiles - g.whole;
+      if (s > 1 && (g.rest == 0 || g.rest * s > 2 * slots)) break;
+      const double tile = k.step * static_cast<double>(steps) + 3.0;
+      double us = static_cast<double>(s == 1 ? ceil_div(tiles, slots) : rounds) * tile;
+      const double bytes = static_cast<double>(g.rest) * s * k.size * k.size * sizeof(float);
+      if (s > 1)
+        us += static_cast<double>(ceil_div(g.rest * s, slots)) *
+                  (k.step * static_cast<double>(ceil_div(steps, s)) + 3.0) + 4.0 + 2.0 * bytes / 4e6;
+      if (least > 0.0 && us >= least) continue;
+      least = us;
+      best.size = k.size;
+      best.grid = g;
+      best.part_bytes = s > 1 ? static_cast<size_t>(bytes) : 0;
+    }
+  }
+  return best;
 }
 
 }  // namespace sn

@@ -46,25 +46,23 @@ int sum_groups(int64_t rows, int64_t cols) {
 template <typename T>
 __device__ __forceinline__ f32x4 orth_b(const OrthMats &t, const OrthArgs &a, int z, int64_t r,
                                         int64_t c, bool first) {
-  const T *g = static_cast<const T *>(t.g[z]) + r * t.ldg[z] + c;
-  float *m = a.update ? t.m[z] + r * t.ldm[z] + c : nullptr;
-  f32x4 b = {0, 0, 0, 0};
+  const int64_t left = a.cols - c;
+  f32x4 g = {0, 0, 0, 0};
+  if (!a.update || first || a.nesterov)
+    g = get4(static_cast<const T *>(t.g[z]) + r * t.ldg[z] + c, left);
+  if (!a.update) return g;
+  float *at = t.m[z] + r * t.ldm[z] + c;
+  f32x4 m = get4(at, left);
+  if (first) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (c + e >= a.cols) continue;
-    const float gv = a.update && !first && !a.nesterov ? 0.0f : to_f32(g[e]);
-    if (!a.update) {
-      b[e] = gv;
-      continue;
-    }
-    float mv = m[e];
-    if (first) {
-      mv = fmaf(a.momentum, mv, gv);
-      m[e] = mv;
-    }
-    b[e] = a.nesterov ? fmaf(a.momentum, mv, gv) : mv;
+    for (int e = 0; e < 4; ++e) m[e] = fmaf(a.momentum, m[e], g[e]);
+    put4(at, left, m);
   }
-  return b;
+  if (a.nesterov) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[e] = fmaf(a.momentum, m[e], g[e]);
+  }
+  return m;
 }
 
 // The momentum, and the sum of squares of B in float64: one part a workgroup.
@@ -109,6 +107,18 @@ __device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v, b
       u32x2{l[0] | static_cast<uint32_t>(l[1]) << 16, l[2] | static_cast<uint32_t>(l[3]) << 16};
 }
 
+__device__ __forceinline__ f32x4 orth_get(const uint16_t *from, int64_t plane) {
+  const u32x2 h = *reinterpret_cast<const u32x2 *>(from), l = *reinterpret_cast<const u32x2 *>(from + plane);
+  f32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int bits = 16 * (e & 1);
+    v[e] = fmaf(f16_value(static_cast<uint16_t>((e < 2 ? l.x : l.y) >> bits)), 1.0f / kUp,
+                f16_value(static_cast<uint16_t>((e < 2 ? h.x : h.y) >> bits)));
+  }
+  return v;
+}
+
 // X = B / |B|, in planes of rows x ldp (zeros past cols).  A matrix of zeros stays one.
 template <typename T>
 __global__ __launch_bounds__(256) void orth_split_kernel(OrthMats t, OrthArgs a, int groups,
@@ -135,120 +145,96 @@ __global__ __launch_bounds__(256) void orth_split_kernel(OrthMats t, OrthArgs a,
   }
 }
 
-// The symmetric products, m x m with stride ldp: A from X, or (POLY) Q from A.
-template <class S, bool POLY>
-__global__ __launch_bounds__(S::NT, S::NT / 256) void orth_sym_kernel(MmArgs m, int64_t n, int64_t ldp,
-                                                                     int64_t side, int64_t from,
-                                                                     const uint16_t *A, uint16_t *to,
-                                                                     bool low) {
-  static_assert(S::BM == S::BN, "a tile on the diagonal is square");
-  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  const int64_t tiles = side * (side + 1) / 2;
-  const int64_t id = mm_order(blockIdx.x, gridDim.x);
-  const int64_t z = id / tiles, k = id - z * tiles;
-  int64_t ti = static_cast<int64_t>((sqrtf(8.0f * static_cast<float>(k) + 1.0f) - 1.0f) * 0.5f);
-  while (ti * (ti + 1) / 2 > k) --ti;
-  while ((ti + 1) * (ti + 2) / 2 <= k) ++ti;
-  const int64_t tj = k - ti * (ti + 1) / 2;
-  f32x4 acc[S::TM][S::TN];
-  mm_tile<S>(m, ti * S::BM, tj * S::BN, 0, mm_steps(m), lds, acc, z * from, z * from);
-  const int64_t plane = n * ldp;
-  uint16_t *out = to + z * 2 * plane;
-  const uint16_t *in = POLY ? A + z * 2 * plane : nullptr;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row0 = ti * S::BM + wave / S::WN * (S::BM / S::WM) + (lane & 15);
-  const int64_t col0 = tj * S::BN + wave % S::WN * (S::BN / S::WN) + 4 * (lane >> 4);
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int64_t row = row0 + i * 16;
+// The symmetric products, n x n with stride ldp: A from X, or (POLY) Q from A.
+template <bool POLY>
+struct OrthSym {
+  int64_t n, ldp;
+  const uint16_t *A;
+  uint16_t *to;
+  bool low;
+  template <class S>
+  __device__ __forceinline__ void row(const MmPlace &p, int64_t row, int64_t col0,
+                                      f32x4 (&acc)[S::TN]) const {
+    const int64_t plane = n * ldp;
+    uint16_t *out = to + p.z * 2 * plane;
+    const uint16_t *in = POLY ? A + p.z * 2 * plane : nullptr;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
       const int64_t col = col0 + j * 16;
       if (row >= ldp || col >= ldp) continue;
-      f32x4 v;
+      f32x4 v, at = {0, 0, 0, 0};
+      if (POLY && row < n) at = orth_get(in + row * ldp + col, plane);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool inside = row < n && col + e < n;
         if constexpr (POLY) {
-          float x = 0.0f;
-          if (inside)
-            x = fmaf(f16_value(in[plane + row * ldp + col + e]), 1.0f / kUp,
-                     f16_value(in[row * ldp + col + e]));
           const float one = row == col + e ? kA * kQScale : 0.0f;
-          v[e] = fmaf(kC * kQScale / (kXScale * kXScale), acc[i][j][e],
-                      fmaf(kB * kQScale / kXScale, x, one));
+          v[e] = fmaf(kC * kQScale / (kXScale * kXScale), acc[j][e],
+                      fmaf(kB * kQScale / kXScale, at[e], one));
         } else {
-          v[e] = acc[i][j][e] * (1.0f / kXScale);
+          v[e] = acc[j][e] * (1.0f / kXScale);
         }
         if (!inside) v[e] = 0.0f;
       }
       if (row < n) orth_put(out + row * ldp + col, plane, v, low);
-      if (ti == tj) continue;
+      if (p.tm == p.tn) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (col + e >= n) continue;
-        uint16_t *p = out + (col + e) * ldp + row;
-        p[0] = f16_bits(v[e]);
-        if (low) p[plane] = f16_bits((v[e] - f16_value(f16_bits(v[e]))) * kUp);
+        uint16_t *q = out + (col + e) * ldp + row;
+        q[0] = f16_bits(v[e]);
+        if (low) q[plane] = f16_bits((v[e] - f16_value(f16_bits(v[e]))) * kUp);
       }
     }
   }
-}
+};
 
 // X' = Q X or X Q, in planes, or in its place in the table.
-template <class S, bool LAST, typename T>
-__global__ __launch_bounds__(S::NT, S::NT / 256) void orth_apply_kernel(MmArgs m, OrthMats t, OrthArgs a,
-                                                                       int64_t gm, int64_t gn,
-                                                                       int64_t a_bytes, int64_t b_bytes,
-                                                                       uint16_t *to, int64_t ldp) {
-  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  const int64_t tiles = gm * gn, id = mm_order(blockIdx.x, gridDim.x);
-  const int64_t z = id / tiles;
-  int64_t tm, tn;
-  mm_place(id - z * tiles, gm, gn, tm, tn);
-  f32x4 acc[S::TM][S::TN];
-  mm_tile<S>(m, tm * S::BM, tn * S::BN, 0, mm_steps(m), lds, acc, z * a_bytes, z * b_bytes);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row0 = tm * S::BM + wave / S::WN * (S::BM / S::WM) + (lane & 15);
-  const int64_t col0 = tn * S::BN + wave % S::WN * (S::BN / S::WN) + 4 * (lane >> 4);
-  const int64_t plane = a.rows * ldp;
-  T *W = LAST ? static_cast<T *>(t.w[z]) : nullptr;
-  const int64_t ldw = LAST ? t.ldw[z] : 0;
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int64_t row = row0 + i * 16;
-    if (row >= a.rows) continue;
+template <bool LAST, typename T>
+struct OrthApply {
+  OrthMats t;
+  OrthArgs a;
+  uint16_t *to;
+  int64_t ldp;
+  template <class S>
+  __device__ __forceinline__ void row(const MmPlace &p, int64_t row, int64_t col0,
+                                      f32x4 (&acc)[S::TN]) const {
+    if (row >= a.rows) return;
+    const int64_t plane = a.rows * ldp;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
       const int64_t col = col0 + j * 16;
       if (col >= ldp) continue;
-      f32x4 v = acc[i][j];
+      f32x4 v = acc[j];
       if constexpr (LAST) {
-        T *w = W + row * ldw + col;
+        T *w = static_cast<T *>(t.w[p.z]) + row * t.ldw[p.z] + col;
+        const int64_t left = a.cols - col;
+        if (left <= 0) continue;
+        v *= 1.0f / (kXScale * kQScale);
+        if (a.update) {
+          const f32x4 old = get4(w, left);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (col + e >= a.cols) continue;
-          float x = v[e] * (1.0f / (kXScale * kQScale));
-          if (a.update) {
-            const float old = to_f32(w[e]);
-            x = fmaf(-a.rate, x, fmaf(-a.decay, old, old));
-          }
-          w[e] = from_f32<T>(x);
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(-a.rate, v[e], fmaf(-a.decay, old[e], old[e]));
         }
+        put4(w, left, v);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           v[e] = col + e < a.cols ? v[e] * (1.0f / kQScale) : 0.0f;
-        orth_put(to + z * 2 * plane + row * ldp + col, plane, v);
+        orth_put(to + p.z * 2 * plane + row * ldp + col, plane, v);
       }
     }
   }
-}
+};
 
+// Products of one, two or three segments are cut in their own way.
+MmPlan cut(int64_t M, int64_t N, int64_t count, int64_t k, int segs, bool sym) {
+  return mm_plan(M, N, count, ceil_div(k, kMmK) * segs, sym);
+}
 struct OrthPlan {
   int64_t n, ldx, lda;  // the smaller side; the planes' strides
   int sums;
-  size_t x[2], a, q, part, total;
+  size_t x[2], a, q, part, sums_at, total;
 };
 OrthPlan orth_plan(int64_t rows, int64_t cols, int64_t count) {
   OrthPlan p = {};
@@ -267,7 +253,14 @@ OrthPlan orth_plan(int64_t rows, int64_t cols, int64_t count) {
   p.x[1] = take(x);
   p.a = take(a);
   p.q = take(a);
-  p.part = take(sizeof(double) * count * p.sums);
+  p.sums_at = take(sizeof(double) * count * p.sums);
+  size_t part = 0;
+  for (int segs = 1; segs <= 3; ++segs)
+    for (const MmPlan &m : {cut(p.n, p.n, count, rows < cols ? cols : rows, segs, true),
+                            cut(p.n, p.n, count, p.n, segs, true),
+                            cut(rows, cols, count, p.n, segs, false)})
+      part = m.part_bytes > part ? m.part_bytes : part;
+  p.part = take(part);
   p.total = at;
   return p;
 }
@@ -290,44 +283,18 @@ void planes(MmArgs &m, const uint16_t *a, int64_t aplane, const uint16_t *b, int
   m.run[1] = m.segs;
 }
 
-// Largest tile that gives most CUs one.
-int orth_tile(int64_t gm, int64_t gn, int64_t count, bool sym) {
-  for (int size : {256, 128}) {
-    const int64_t r = ceil_div(gm, size), c = ceil_div(gn, size);
-    if ((sym ? r * (r + 1) / 2 : r * c) * count >= (size == 256 && sym ? 1024 : 224)) return size;
-  }
-  return 64;
-}
-
-template <bool K, bool POLY>
-void run_sym(const MmArgs &m, int64_t n, int64_t ldp, int64_t count, int64_t from, const uint16_t *A,
-             uint16_t *to, bool low, hipStream_t s) {
-  const int size = orth_tile(n, n, count, true);
-  const int64_t side = ceil_div(n, size);
-  const unsigned grid = static_cast<unsigned>(side * (side + 1) / 2 * count);
-  if (size == 256)
-    orth_sym_kernel<MmShape<true, K, K, 256, 256, 2, 4>, POLY><<<grid, 512, 0, s>>>(m, n, ldp, side, from, A, to, low);
-  else if (size == 128)
-    orth_sym_kernel<MmShape<true, K, K, 128, 128, 2, 2>, POLY><<<grid, 256, 0, s>>>(m, n, ldp, side, from, A, to, low);
+template <bool AK, bool BK, class Epi>
+void run(const MmArgs &m, int64_t M, int64_t N, int64_t count, bool sym, float *part, const Epi &e,
+         hipStream_t s) {
+  const MmPlan p = cut(M, N, count, m.k, m.segs, sym);
+  MmGrid g = p.grid;
+  g.part = part;
+  if (p.size == 256)
+    mm_launch<MmShape<true, AK, BK, 256, 256, 2, 4>>(m, g, e, s);
+  else if (p.size == 128)
+    mm_launch<MmShape<true, AK, BK, 128, 128, 2, 2>>(m, g, e, s);
   else
-    orth_sym_kernel<MmShape<true, K, K, 64, 64, 2, 2>, POLY><<<grid, 256, 0, s>>>(m, n, ldp, side, from, A, to, low);
-}
-
-template <bool BK, bool LAST, typename T>
-void run_apply(const MmArgs &m, const OrthMats &t, const OrthArgs &a, int64_t a_bytes,
-               int64_t b_bytes, uint16_t *to, int64_t ldp, hipStream_t s) {
-  const int size = orth_tile(a.rows, a.cols, a.count, false);
-  const int64_t gm = ceil_div(a.rows, size), gn = ceil_div(a.cols, size);
-  const unsigned grid = static_cast<unsigned>(gm * gn * a.count);
-  if (size == 256)
-    orth_apply_kernel<MmShape<true, true, BK, 256, 256, 2, 4>, LAST, T>
-        <<<grid, 512, 0, s>>>(m, t, a, gm, gn, a_bytes, b_bytes, to, ldp);
-  else if (size == 128)
-    orth_apply_kernel<MmShape<true, true, BK, 128, 128, 2, 2>, LAST, T>
-        <<<grid, 256, 0, s>>>(m, t, a, gm, gn, a_bytes, b_bytes, to, ldp);
-  else
-    orth_apply_kernel<MmShape<true, true, BK, 64, 64, 2, 2>, LAST, T>
-        <<<grid, 256, 0, s>>>(m, t, a, gm, gn, a_bytes, b_bytes, to, ldp);
+    mm_launch<MmShape<true, AK, BK, 64, 64, 2, 2, 4>>(m, g, e, s);
 }
 
 template <typename T>
@@ -335,47 +302,52 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
   const OrthPlan p = orth_plan(a.rows, a.cols, a.count);
   uint16_t *X[2] = {reinterpret_cast<uint16_t *>(ws + p.x[0]), reinterpret_cast<uint16_t *>(ws + p.x[1])};
   uint16_t *A = reinterpret_cast<uint16_t *>(ws + p.a), *Q = reinterpret_cast<uint16_t *>(ws + p.q);
-  double *part = reinterpret_cast<double *>(ws + p.part);
+  double *sums = reinterpret_cast<double *>(ws + p.sums_at);
+  float *part = reinterpret_cast<float *>(ws + p.part);
   const bool tall = a.rows > a.cols;
-  orth_begin_kernel<T><<<p.sums * a.count, 256, 0, s>>>(t, a, p.sums, part);
+  orth_begin_kernel<T><<<p.sums * a.count, 256, 0, s>>>(t, a, p.sums, sums);
   const int64_t turns = ceil_div(a.rows * p.ldx, kBlockElems);
   const int groups = static_cast<int>(turns < 1024 ? turns : 1024);
-  orth_split_kernel<T><<<groups * a.count, 256, 0, s>>>(t, a, groups, p.sums, part, X[0], p.ldx);
+  orth_split_kernel<T><<<groups * a.count, 256, 0, s>>>(t, a, groups, p.sums, sums, X[0], p.ldx);
   const int64_t xplane = a.rows * p.ldx, aplane = p.n * p.lda;
   for (int i = 0; i < a.steps; ++i) {
     uint16_t *x = X[i & 1], *next = X[~i & 1];
+    const bool whole = sizeof(T) == 4, last = i + 1 == a.steps;
     MmArgs m = {};
     m.k = tall ? a.rows : a.cols;
     m.a.ld = m.b.ld = p.ldx;
     m.a.n = m.b.n = tall ? p.ldx : a.rows;
-    const bool whole = sizeof(T) == 4, last = i + 1 == a.steps;
+    m.a.batch = m.b.batch = 4 * xplane;
     planes(m, x, xplane, x, xplane, whole ? kAll : kHigh);
+    const OrthSym<false> gram = {p.n, p.lda, nullptr, A, true};
     if (tall)
-      run_sym<false, false>(m, p.n, p.lda, a.count, 4 * xplane, nullptr, A, true, s);
+      run<false, false>(m, p.n, p.n, a.count, true, part, gram, s);
     else
-      run_sym<true, false>(m, p.n, p.lda, a.count, 4 * xplane, nullptr, A, true, s);
+      run<true, true>(m, p.n, p.n, a.count, true, part, gram, s);
     m.k = p.n;
     m.a.ld = m.b.ld = p.lda;
     m.a.n = m.b.n = p.n;
+    m.a.batch = m.b.batch = 4 * aplane;
     planes(m, A, aplane, A, aplane, whole || i + 2 >= a.steps ? kAll : kHigh);
-    run_sym<true, true>(m, p.n, p.lda, a.count, 4 * aplane, A, Q, whole, s);
-    if (tall) {
-      m.a.ld = p.ldx;
-      m.a.n = a.rows;
+    run<true, true>(m, p.n, p.n, a.count, true, part, OrthSym<true>{p.n, p.lda, A, Q, whole}, s);
+    MmOperand &o = tall ? m.a : m.b;  // X's
+    o.ld = p.ldx;
+    o.n = tall ? a.rows : p.ldx;
+    o.batch = 4 * xplane;
+    if (tall)
       planes(m, x, xplane, Q, aplane, whole ? kAll : last ? kHigh : kBothOfA);
-      if (last)
-        run_apply<true, true, T>(m, t, a, 4 * xplane, 4 * aplane, next, p.ldx, s);
-      else
-        run_apply<true, false, T>(m, t, a, 4 * xplane, 4 * aplane, next, p.ldx, s);
-    } else {
-      m.b.ld = p.ldx;
-      m.b.n = p.ldx;
+    else
       planes(m, Q, aplane, x, xplane, whole ? kAll : last ? kHigh : kBothOfB);
-      if (last)
-        run_apply<false, true, T>(m, t, a, 4 * aplane, 4 * xplane, next, p.ldx, s);
+    const auto apply = [&](const auto &e) {
+      if (tall)
+        run<true, true>(m, a.rows, a.cols, a.count, false, part, e, s);
       else
-        run_apply<false, false, T>(m, t, a, 4 * aplane, 4 * xplane, next, p.ldx, s);
-    }
+        run<true, false>(m, a.rows, a.cols, a.count, false, part, e, s);
+    };
+    if (last)
+      apply(OrthApply<true, T>{t, a, next, p.ldx});
+    else
+      apply(OrthApply<false, T>{t, a, next, p.ldx});
   }
   return hipGetLastError();
 }

@@ -102,15 +102,17 @@ def test_orthogonalize_matches_oracle(dtype, shape):
         for k, (a, b) in enumerate(zip(got, mats)):
             ref = orc.orthogonalize(host(b), steps)
             _near(host(a), ref, _bound(host(b), steps, dtype), dtype, f"matrix {k}, {steps} steps")
-    # one matrix alone, in place, into rows with gaps: the same bits
+    # one matrix alone (the order of its sums depends on the number of matrices in a call); in
+    # place and into rows with gaps the same bits
+    alone = sn.sn_orthogonalize(mats[1], steps=6)
+    _near(host(alone), orc.orthogonalize(host(mats[1]), 6), _bound(host(mats[1]), 6, dtype), dtype, "alone")
     one = mats[1].clone()
     sn.sn_orthogonalize([one], steps=6, out=[one])
-    alone = sn.sn_orthogonalize(mats[1], steps=6)
-    assert torch.equal(one, got[1]) and torch.equal(alone, got[1])
+    assert torch.equal(one, alone)
     r, c = shape
     wide = torch.zeros(r, c + 7, dtype=DT[dtype], device="cuda")
-    sn.sn_orthogonalize(mats[0], steps=6, out=wide[:, :c])
-    assert torch.equal(wide[:, :c], got[0]) and float(wide[:, c:].abs().max()) == 0.0
+    sn.sn_orthogonalize(mats[1], steps=6, out=wide[:, :c])
+    assert torch.equal(wide[:, :c], alone) and float(wide[:, c:].abs().max()) == 0.0
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -158,7 +160,6 @@ def test_more_matrices_than_a_launch_takes():
     mats = [_mat(k, 20, 33, "f32") for k in range(70)]
     got = sn.sn_orthogonalize(mats)
     for k in (0, 31, 32, 63, 64, 69):
-        assert torch.equal(got[k], sn.sn_orthogonalize(mats[k]))
         _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, "f32"), "f32", f"matrix {k}")
 
 
@@ -182,10 +183,11 @@ def test_special_matrices():
     mats[1].zero_()
     mats[2][3, 4] = float("nan")
     mats[3][7, 8] = float("inf")
+    good = sn.sn_orthogonalize([mats[0]] * 4, out=[torch.empty(50, 70, device="cuda") for _ in range(4)])
     got = sn.sn_orthogonalize(mats)
     assert float(got[1].abs().max()) == 0.0
     assert bool(got[2].isnan().all()) and bool(got[3].isnan().all())
-    assert torch.equal(got[0], sn.sn_orthogonalize(mats[0]))
+    assert torch.equal(got[0], good[0])
 
 
 def test_the_update_stays_in_the_subspace():
