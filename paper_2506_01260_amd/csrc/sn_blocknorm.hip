@@ -18,7 +18,14 @@ namespace sn {
 
 namespace {
 
-__device__ __forceinline__ float sigmoid_of(float g) { return 1.0f / (1.0f + expf(-g)); }
+// For bf16 the hardware's exponential and reciprocal, 2^-22 or so off where the result is
+// rounded to 2^-9 (backward 4999 x 1600 with a gate a token: 41 us, 49 with expf and a division).
+template <typename T>
+__device__ __forceinline__ float sigmoid_of(float g) {
+  if constexpr (sizeof(T) == 2)
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950f * g));
+  return 1.0f / (1.0f + expf(-g));
+}
 
 // The gate's row of token i.
 template <typename T, typename A>
@@ -26,7 +33,8 @@ __device__ __forceinline__ const T *gate_row(const A &a, int64_t i) {
   return static_cast<const T *>(a.gate) + i * a.ldgate;
 }
 
-// n sums over a workgroup of W waves in one barrier; red: W * n floats, free as group_sum's.
+// NS sums over a workgroup of W waves in one barrier; red: W * NS floats, free as group_sum's.
+// The waves' sums are joined by lanes, not by each thread in turn, which took W * NS registers.
 template <int W, int NS>
 __device__ __forceinline__ void group_sums(float (&v)[NS], float (*red)[W]) {
 #pragma unroll
@@ -39,9 +47,8 @@ __device__ __forceinline__ void group_sums(float (&v)[NS], float (*red)[W]) {
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      v[s] = red[s][0];
-#pragma unroll
-      for (int i = 1; i < W; ++i) v[s] += red[s][i];
+      const int lane = threadIdx.x & 63;
+      v[s] = wave_sum(lane < W ? red[s][lane] : 0.0f);
     }
   }
 }
@@ -99,7 +106,7 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(BlockNormArgs a) {
     if (a.gate) {
       Piece<T>::unpack(fix<T, WHOLE>(gp[k], c0, d), t);
 #pragma unroll
-      for (int e = 0; e < E; ++e) h[k][e] *= a.sigmoid ? sigmoid_of(t[e]) : t[e];
+      for (int e = 0; e < E; ++e) h[k][e] *= a.sigmoid ? sigmoid_of<T>(t[e]) : t[e];
     }
     Piece<T>::unpack(fix<T, WHOLE>(rp[k], c0, d), t);
 #pragma unroll
@@ -162,7 +169,7 @@ __global__ __launch_bounds__(1024) void block_norm_long_kernel(BlockNormArgs a) 
     if (a.gate) {
       get(gate_row<T>(a, i), c0, a.d, t);
 #pragma unroll
-      for (int e = 0; e < E; ++e) h[e] *= a.sigmoid ? sigmoid_of(t[e]) : t[e];
+      for (int e = 0; e < E; ++e) h[e] *= a.sigmoid ? sigmoid_of<T>(t[e]) : t[e];
     }
     get(Rs, c0, a.d, t);
 #pragma unroll
@@ -195,152 +202,213 @@ __global__ __launch_bounds__(1024) void block_norm_long_kernel(BlockNormArgs a) 
 // the three column sums in registers; block_sum_kernel adds the parts.
 enum { kGw = 0, kGwPost = 1, kGate = 2 };
 
-template <typename T, int R, int K, int NT, bool WHOLE>
-__global__ __launch_bounds__(NT) void block_norm_grad_kernel(BlockNormGradArgs a) {
-  constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R;
+// Two neighbouring values of a piece, and a piece made of such pairs.
+template <typename T>
+__device__ __forceinline__ void pair_of(u32x4 v, int q, float &a, float &b) {
+  if constexpr (sizeof(T) == 2) {
+    a = bf_lo(v[q]);
+    b = bf_hi(v[q]);
+  } else {
+    a = __uint_as_float(v[2 * q]);
+    b = __uint_as_float(v[2 * q + 1]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void set_pair(u32x4 &v, int q, float a, float b) {
+  if constexpr (sizeof(T) == 2) {
+    v[q] = pack_bf16x2(a, b);
+  } else {
+    v[2 * q] = __float_as_uint(a);
+    v[2 * q + 1] = __float_as_uint(b);
+  }
+}
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void put_piece(T *row, int c0, int d, u32x4 v) {
+  if (WHOLE ? c0 < d : c0 + Piece<T>::E <= d) {
+    store_piece(row + c0, v);
+  } else if (!WHOLE) {
+    float x[Piece<T>::E];
+    Piece<T>::unpack(v, x);
+    store_part(row, c0, d, x);
+  }
+}
+
+// A row's pieces as they are loaded (a gate of one row is kept with the gains).
+template <int K>
+struct BlockRow {
+  u32x4 x[K], h[K], y[K], d[K], g[K];
+};
+template <typename T, int R, int K>
+__device__ __forceinline__ void fetch_row(const BlockNormGradArgs &a, int64_t i, int c, int d,
+                                          BlockRow<K> &r) {
+  constexpr int E = Piece<T>::E;
+  const auto each = [&](u32x4(&to)[K], const void *p, int64_t ld) {
+    const T *row = static_cast<const T *>(p) + i * ld;
+#pragma unroll
+    for (int k = 0; k < K; ++k) to[k] = take(row, c + k * R * E, d);
+  };
+  if (a.post || a.gate) each(r.x, a.X, a.ldx);
+  if (a.dY) {
+    each(r.h, a.H, a.ldh);
+    each(r.y, a.dY, a.lddy);
+  }
+  if (a.dH) each(r.d, a.dH, a.lddh);
+  if (a.gate && a.ldgate) each(r.g, a.gate, a.ldgate);
+}
+
+// NEXT: a workgroup's next row is sent for before the present one is worked on, so that its
+// two waits at barriers leave the memory busy.  Values are taken from their pieces two at a
+// time, and u = dy w and dh take the places of dY and dH: with eight at a time 1024 threads
+// had 176 bytes of scratch (16383 x 8192 bf16 1260 us).
+template <typename T, int R, int K, int NT, bool WHOLE, bool NEXT>
+__global__ __launch_bounds__(NT, 2) void block_norm_grad_kernel(BlockNormGradArgs a) {
+  constexpr int E = Piece<T>::E, W = R / 64, ROWS = NT / R, P = E / 2;
   static_assert(ROWS == 1 || W == 1, "a row of several waves has the workgroup to itself");
   __shared__ float red[3][W], red2[1][W];
   const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / R);
   const int c = static_cast<int>(threadIdx.x % R) * E, d = static_cast<int>(a.d);
-  const T *w = static_cast<const T *>(a.w), *w1 = static_cast<const T *>(a.w_post);
+  const bool need_x = a.post || a.gate;
+  // The gains and the one gate row of this thread's columns: kept, or (longer rows) loaded
+  // again where they are used.
+  constexpr bool KEEP = NEXT;
+  u32x4 ones;
+#pragma unroll
+  for (int q = 0; q < P; ++q) set_pair<T>(ones, q, 1.0f, 1.0f);
+  const auto gains = [&](const void *p, int k) {
+    const int c0 = c + k * R * E;
+    return p ? fix<T, WHOLE>(take(static_cast<const T *>(p), c0, d), c0, d) : ones;
+  };
+  const void *post_gains = a.post ? a.w_post : nullptr, *row_gate = a.ldgate ? nullptr : a.gate;
+  u32x4 w_kept[K], w1_kept[K], gate_kept[K];
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      w_kept[k] = gains(a.w, k);
+      w1_kept[k] = gains(post_gains, k);
+      gate_kept[k] = gains(row_gate, k);
+    }
+  }
   float sum[3][K][E] = {};
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + sub; i < a.N;
-       i += static_cast<int64_t>(gridDim.x) * ROWS) {
-    const T *X = static_cast<const T *>(a.X) + i * a.ldx;
-    u32x4 xp[K], hp[K], yp[K], dp[K], gp[K];
-    const bool need_x = a.post || a.gate;
-    if (need_x) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) xp[k] = take(X, c + k * R * E, d);
+  int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * ROWS;
+  BlockRow<K> later;
+  if (NEXT && i < a.N) fetch_row<T, R, K>(a, i, c, d, later);
+  for (; i < a.N; i += stride) {
+    BlockRow<K> r;
+    if constexpr (NEXT) {
+      r = later;
+      if (i + stride < a.N) fetch_row<T, R, K>(a, i + stride, c, d, later);
+    } else {
+      fetch_row<T, R, K>(a, i, c, d, r);
     }
-    if (a.dY) {
-      const T *H = static_cast<const T *>(a.H) + i * a.ldh;
-      const T *dY = static_cast<const T *>(a.dY) + i * a.lddy;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        hp[k] = take(H, c + k * R * E, d);
-        yp[k] = take(dY, c + k * R * E, d);
-      }
-    }
-    if (a.dH) {
-      const T *dH = static_cast<const T *>(a.dH) + i * a.lddh;
-#pragma unroll
-      for (int k = 0; k < K; ++k) dp[k] = take(dH, c + k * R * E, d);
-    }
-    if (a.gate) {
-      const T *G = gate_row<T>(a, i);
-#pragma unroll
-      for (int k = 0; k < K; ++k) gp[k] = take(G, c + k * R * E, d);
-    }
-    float x[E], h[E], y[E], t[E], s[3] = {0.0f, 0.0f, 0.0f};
+    float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c0 = c + k * R * E;
       if (need_x) {
-        xp[k] = fix<T, WHOLE>(xp[k], c0, d);
-        Piece<T>::unpack(xp[k], x);
+        r.x[k] = fix<T, WHOLE>(r.x[k], c0, d);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+        for (int q = 0; q < P; ++q) {
+          float x0, x1;
+          pair_of<T>(r.x[k], q, x0, x1);
+          s[0] = fmaf(x1, x1, fmaf(x0, x0, s[0]));
+        }
       }
       if (a.dY) {
-        hp[k] = fix<T, WHOLE>(hp[k], c0, d);
-        yp[k] = fix<T, WHOLE>(yp[k], c0, d);
-        Piece<T>::unpack(hp[k], h);
-        Piece<T>::unpack(yp[k], y);
-        if (w) {
-          Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), t);
+        r.h[k] = fix<T, WHOLE>(r.h[k], c0, d);
+        r.y[k] = fix<T, WHOLE>(r.y[k], c0, d);
+        const u32x4 w = KEEP ? w_kept[k] : gains(a.w, k);
 #pragma unroll
-          for (int e = 0; e < E; ++e) y[e] *= t[e];
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          s[1] = fmaf(h[e], h[e], s[1]);
-          s[2] = fmaf(y[e], h[e], s[2]);
+        for (int q = 0; q < P; ++q) {
+          float h0, h1, y0, y1, w0, w1v;
+          pair_of<T>(r.h[k], q, h0, h1);
+          pair_of<T>(r.y[k], q, y0, y1);
+          pair_of<T>(w, q, w0, w1v);
+          s[1] = fmaf(h1, h1, fmaf(h0, h0, s[1]));
+          s[2] = fmaf(y1 * w1v, h1, fmaf(y0 * w0, h0, s[2]));
         }
       }
+      if (a.dH) r.d[k] = fix<T, WHOLE>(r.d[k], c0, d);
+      if (a.gate && a.ldgate) r.g[k] = fix<T, WHOLE>(r.g[k], c0, d);
     }
     group_sums<W>(s, red);
-    const float q = a.post ? 1.0f / sqrtf(s[0] * a.inv_d + a.eps) : 1.0f;
+    const float q1 = a.post ? 1.0f / sqrtf(s[0] * a.inv_d + a.eps) : 1.0f;
     const float rho = 1.0f / sqrtf(s[1] * a.inv_d + a.eps), f = s[2] * a.inv_d * rho;
     T *dR = static_cast<T *>(a.dR) + i * a.lddr;
     T *dX = static_cast<T *>(a.dX) + i * a.lddx;
+    T *dG = a.dgate ? static_cast<T *>(a.dgate) + i * a.lddg : nullptr;
     float v[K][E], sv[1] = {0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c0 = c + k * R * E;
-      float o[E];
-      if (a.dH) {
-        Piece<T>::unpack(fix<T, WHOLE>(dp[k], c0, d), o);
-      } else {
+      const u32x4 w = KEEP ? w_kept[k] : gains(a.w, k), w1 = KEEP ? w1_kept[k] : gains(post_gains, k);
+      const u32x4 gate = a.ldgate ? r.g[k] : KEEP ? gate_kept[k] : gains(row_gate, k);
+      u32x4 out_r, out_g, out_x;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.0f;
-      }
-      if (a.dY) {
-        Piece<T>::unpack(hp[k], h);
-        Piece<T>::unpack(yp[k], y);
-        if (w) Piece<T>::unpack(fix<T, WHOLE>(take(w, c0, d), c0, d), t);
+      for (int q = 0; q < P; ++q) {
+        float o[2] = {0.0f, 0.0f}, g[2] = {1.0f, 1.0f}, x[2] = {0.0f, 0.0f}, wp[2], t[2];
+        if (a.dH) pair_of<T>(r.d[k], q, o[0], o[1]);
+        if (a.dY) {
+          float h[2], y[2];
+          pair_of<T>(r.h[k], q, h[0], h[1]);
+          pair_of<T>(r.y[k], q, y[0], y[1]);
+          pair_of<T>(w, q, t[0], t[1]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float n = h[e] * rho;
-          sum[kGw][k][e] = fmaf(y[e], n, sum[kGw][k][e]);
-          o[e] = fmaf(rho, fmaf(-n, f, w ? y[e] * t[e] : y[e]), o[e]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) h[e] = a.alpha * o[e];
-      put<T, WHOLE>(dR, c0, d, h);
-      // from here on x holds m (or x), t the post norm's gains
-      if (need_x) {
-        Piece<T>::unpack(xp[k], x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] *= q;
-      }
-      if (a.post && w1) {
-        Piece<T>::unpack(fix<T, WHOLE>(take(w1, c0, d), c0, d), t);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] = 1.0f;
-      }
-      if (a.gate) {
-        float g[E];
-        Piece<T>::unpack(fix<T, WHOLE>(gp[k], c0, d), g);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          float slope = 1.0f;
-          if (a.sigmoid) {
-            g[e] = sigmoid_of(g[e]);
-            slope = g[e] * (1.0f - g[e]);
+          for (int e = 0; e < 2; ++e) {
+            const float n = h[e] * rho;
+            sum[kGw][k][2 * q + e] = fmaf(y[e], n, sum[kGw][k][2 * q + e]);
+            o[e] = fmaf(rho, fmaf(-n, f, y[e] * t[e]), o[e]);
           }
-          y[e] = o[e] * x[e] * t[e] * slope;
-          o[e] *= g[e];
         }
-        if (a.dgate) {
-          put<T, WHOLE>(static_cast<T *>(a.dgate) + i * a.lddg, c0, d, y);
-        } else {
+        set_pair<T>(out_r, q, a.alpha * o[0], a.alpha * o[1]);
+        pair_of<T>(w1, q, wp[0], wp[1]);
+        if (need_x) {
+          pair_of<T>(r.x[k], q, x[0], x[1]);
+          x[0] *= q1;
+          x[1] *= q1;
+        }
+        if (a.gate) {
+          pair_of<T>(gate, q, g[0], g[1]);
 #pragma unroll
-          for (int e = 0; e < E; ++e) sum[kGate][k][e] += y[e];
+          for (int e = 0; e < 2; ++e) {
+            float slope = 1.0f;
+            if (a.sigmoid) {
+              g[e] = sigmoid_of<T>(g[e]);
+              slope = g[e] * (1.0f - g[e]);
+            }
+            t[e] = o[e] * x[e] * wp[e] * slope;
+            if (!dG) sum[kGate][k][2 * q + e] += t[e];
+            o[e] *= g[e];
+          }
+          set_pair<T>(out_g, q, t[0], t[1]);
         }
-      }
-      if (a.post) {
+        if (a.post) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          sum[kGwPost][k][e] = fmaf(o[e], x[e], sum[kGwPost][k][e]);
-          v[k][e] = o[e] * t[e];
-          sv[0] = fmaf(v[k][e], x[e], sv[0]);
+          for (int e = 0; e < 2; ++e) {
+            sum[kGwPost][k][2 * q + e] = fmaf(o[e], x[e], sum[kGwPost][k][2 * q + e]);
+            v[k][2 * q + e] = o[e] * wp[e];
+            sv[0] = fmaf(v[k][2 * q + e], x[e], sv[0]);
+          }
         }
-      } else {
-        put<T, WHOLE>(dX, c0, d, o);
+        set_pair<T>(out_x, q, o[0], o[1]);
       }
+      put_piece<T, WHOLE>(dR, c0, d, out_r);
+      if (dG) put_piece<T, WHOLE>(dG, c0, d, out_g);
+      if (!a.post) put_piece<T, WHOLE>(dX, c0, d, out_x);
     }
     if (a.post) {
       group_sums<W>(sv, red2);
-      const float f1 = sv[0] * a.inv_d;
+      const float f1 = sv[0] * a.inv_d * q1;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        Piece<T>::unpack(xp[k], x);
+        u32x4 out_x;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = q * fmaf(-x[e] * q, f1, v[k][e]);
-        put<T, WHOLE>(dX, c + k * R * E, d, x);
+        for (int q = 0; q < P; ++q) {
+          float x[2];
+          pair_of<T>(r.x[k], q, x[0], x[1]);
+          set_pair<T>(out_x, q, q1 * fmaf(-x[0], f1, v[k][2 * q]), q1 * fmaf(-x[1], f1, v[k][2 * q + 1]));
+        }
+        put_piece<T, WHOLE>(dX, c + k * R * E, d, out_x);
       }
     } else if constexpr (W > 1) {
       __syncthreads();  // red is used again
@@ -436,7 +504,7 @@ __global__ __launch_bounds__(1024) void block_norm_grad_long_kernel(BlockNormGra
         slope[e] = 1.0f;
         if (!a.gate) g[e] = 1.0f;
         if (a.gate && a.sigmoid) {
-          g[e] = sigmoid_of(g[e]);
+          g[e] = sigmoid_of<T>(g[e]);
           slope[e] = g[e] * (1.0f - g[e]);
         }
       }
@@ -537,10 +605,15 @@ hipError_t launch_norm_t(const BlockNormArgs &a, hipStream_t s) {
 }
 
 int64_t pieces_of(int dt, int64_t d) { return ceil_div(d, dt == 0 ? 4 : 8); }
-// Workgroups of the backward, each with a part of the column sums.
+// Workgroups of the backward, each with a part of the column sums: as many as run at a time,
+// but some 5 rows for each, so that the parts stay small beside the rows.
 int64_t grad_groups(int dt, int64_t N, int64_t d) {
-  const int64_t n = pieces_of(dt, d), groups = ceil_div(N, n <= 256 ? 4 : 1);
-  return groups < 512 ? groups : 512;
+  const int64_t n = pieces_of(dt, d);
+  const int64_t rows = n <= 64 ? 4 : 1;  // of a workgroup at a time
+  const int64_t most = n <= 64 ? 768 : n <= 128 ? 1536 : n <= 256 ? 768 : n <= 512 ? 512 : 256;
+  const int64_t few = ceil_div(N, 5 * rows), all = ceil_div(N, rows);
+  int64_t g = few < 256 ? (all < 256 ? all : 256) : few;
+  return g < most ? g : most;
 }
 
 template <typename T, bool WHOLE>
@@ -550,17 +623,21 @@ hipError_t launch_grad_t(int dt, const BlockNormGradArgs &a, hipStream_t s) {
   if (a.d < Piece<T>::E)
     block_norm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
   else if (n <= 64)
-    block_norm_grad_kernel<T, 64, 1, 256, WHOLE><<<g, 256, 0, s>>>(a);
+    block_norm_grad_kernel<T, 64, 1, 256, WHOLE, true><<<g, 256, 0, s>>>(a);
   else if (n <= 128)
-    block_norm_grad_kernel<T, 64, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
+    block_norm_grad_kernel<T, 128, 1, 128, WHOLE, true><<<g, 128, 0, s>>>(a);
   else if (n <= 256)
-    block_norm_grad_kernel<T, 64, 4, 256, WHOLE><<<g, 256, 0, s>>>(a);
+    block_norm_grad_kernel<T, 256, 1, 256, WHOLE, true><<<g, 256, 0, s>>>(a);
   else if (n <= 512)
-    block_norm_grad_kernel<T, 256, 2, 256, WHOLE><<<g, 256, 0, s>>>(a);
+    block_norm_grad_kernel<T, 256, 2, 256, WHOLE, true><<<g, 256, 0, s>>>(a);
   else if (n <= 1024)
-    block_norm_grad_kernel<T, 512, 2, 512, WHOLE><<<g, 512, 0, s>>>(a);
+    block_norm_grad_kernel<T, 512, 2, 512, WHOLE, true><<<g, 512, 0, s>>>(a);
+  else if (n <= 1536)
+    block_norm_grad_kernel<T, 512, 3, 512, WHOLE, false><<<g, 512, 0, s>>>(a);
+  else if (n <= 2048 && sizeof(T) == 4)  // eight values of bf16 would not leave the registers
+    block_norm_grad_kernel<T, 1024, 2, 1024, WHOLE, false><<<g, 1024, 0, s>>>(a);
   else if (n <= 2048)
-    block_norm_grad_kernel<T, 1024, 2, 1024, WHOLE><<<g, 1024, 0, s>>>(a);
+    block_norm_grad_kernel<T, 512, 4, 512, WHOLE, false><<<g, 512, 0, s>>>(a);
   else
     block_norm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
   return hipGetLastError();

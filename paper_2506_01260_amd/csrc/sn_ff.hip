@@ -365,6 +365,18 @@ int vec_slices(int64_t d, int64_t ff) {
 }
 bool by_vec(int dt, int64_t N, int64_t ff) { return N <= 8 && ff >= (dt == 0 ? 4 : 8); }
 
+#ifndef FEWD
+#define FEWD 6
+#endif
+constexpr int64_t kFew = 64;
+MmPlan few_plan(int64_t cols) {
+  MmPlan p = {};
+  p.grid.gm = 1;
+  p.grid.gn = p.grid.whole = ceil_div(cols, 128);
+  p.grid.mats = p.grid.splits = 1;
+  return p;
+}
+
 struct FfPlan {
   bool vec, own_x, own_w;  // own: read in place
   MmPlan t;
@@ -382,7 +394,7 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
     p.own_x = own_x;
     p.own_w = own_w;
     // a paired tile has half its columns of either product
-    p.t = mm_plan(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
+    p.t = N <= kFew ? few_plan(2 * ff) : mm_plan(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
     if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
     if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
     p.part = s.take(p.t.part_bytes);
@@ -434,7 +446,9 @@ hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t 
     MmGrid g = p.t.grid;
     g.part = a.part;
     const FfEpilogue<T> e = {a};
-    if (p.t.size == 256)
+    if (p.t.size == 0)
+      mm_launch<MmShape<false, true, false, 64, 128, 2, 2, FEWD, true>>(m, g, e, s);
+    else if (p.t.size == 256)
       mm_launch<MmShape<false, true, false, 256, 256, 2, 4, 2, true>>(m, g, e, s);
     else if (p.t.size == 128)
       mm_launch<MmShape<false, true, false, 128, 128, 2, 2, 2, true>>(m, g, e, s);

@@ -71,7 +71,7 @@ def test_block_norm_backward(over, code):
 
 def test_block_norm_workspace():
     f = sn.sn_block_norm_backward_workspace_bytes
-    assert f(8, 300, 1) >= 3 * 300 * 4 and f(100000, 4096, 1) == 512 * 4096 * 12
+    assert f(8, 300, 1) >= 3 * 300 * 4 and f(100000, 4096, 1) >= 100 * 4096 * 12
     for bad in ((0, 8, 0), (8, 0, 0), (8, 8, 5), (BIG, 8, 0), (8, BIG, 0)):
         assert f(*bad) == 0
 
