@@ -1526,8 +1526,7 @@ size_t sn_gated_ff_workspace_bytes(int64_t N, int64_t d, int64_t ff, int64_t ldx
   a.ff = ff;
   a.ldx = ldx;
   a.ldw = ldw;
-  if (!aligned) a.X = a.Wg = reinterpret_cast<const void *>(uintptr_t(2));
-  return sn::ff_workspace_bytes(dt, a);
+  return sn::ff_workspace_bytes(dt, a, aligned != 0);
 }
 
 size_t sn_gated_ff_backward_workspace_bytes(int64_t N, int64_t d, int64_t ff, int64_t ldx,
@@ -1543,11 +1542,7 @@ size_t sn_gated_ff_backward_workspace_bytes(int64_t N, int64_t d, int64_t ff, in
   a.ldx = ldx;
   a.ldw = ldw;
   a.ldd = ldd;
-  if (!aligned) {
-    a.X = a.Wg = reinterpret_cast<const void *>(uintptr_t(2));
-    a.dG = reinterpret_cast<void *>(uintptr_t(2));
-  }
-  return sn::ff_grad_workspace_bytes(dt, a);
+  return sn::ff_grad_workspace_bytes(dt, a, aligned != 0);
 }
 
 int32_t sn_gated_ff(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, const void *Wg,
@@ -1580,7 +1575,7 @@ int32_t sn_gated_ff(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt
   a.U = U;
   a.ldh = ldh;
   a.ldg = ldg;
-  const size_t need = sn::ff_workspace_bytes(dt, a);
+  const size_t need = sn::ff_call_bytes(dt, a);
   Buffers b;
   if (need) {
     if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
@@ -1643,7 +1638,7 @@ int32_t sn_gated_ff_backward(const void *X, int64_t N, int64_t d, int64_t ldx, i
   a.ldgw = ldgw;
   a.gdt = gdt;
   a.add = accumulate != 0;
-  const size_t need = N ? sn::ff_grad_workspace_bytes(dt, a) : 0;
+  const size_t need = N ? sn::ff_grad_call_bytes(dt, a) : 0;
   Buffers b;
   if (need) {
     if ((st = check_workspace(workspace, workspace_bytes, need))) return st;

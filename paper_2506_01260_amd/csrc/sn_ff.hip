@@ -196,25 +196,25 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs a, int parts) {
 }
 
 // ---- forward of up to 8 tokens: the weights stream by -----------------------------------
-// A workgroup takes 64 columns of both weights and a slice of d; a lane takes 16 bytes of
-// a weight's row, the lanes beside it the rest of the row's 64 columns and further rows.
-// Columns past ff: the row's last piece, whose values are stored by two lanes alike.
-constexpr int kVecCols = 64, kVecSlice = 1024;
+// A workgroup of 16 waves (8 for more than 4 tokens) takes 64 columns of both weights and a slice of d (all of it where
+// there are enough columns for the CUs); a lane takes 16 bytes of a weight's row, the lanes
+// beside it the rest of the row's 64 columns and further rows.  Columns past ff: the row's
+// last piece, whose values are stored by two lanes alike.
+constexpr int kVecCols = 64;
+constexpr int vec_waves(int nb) { return nb <= 4 ? 16 : 8; }
+constexpr int vec_slice(int nb) { return nb <= 4 ? 4096 : 2048; }  // longest
 template <typename T, int NB>
-__global__ __launch_bounds__(256) void ff_vec_kernel(FfArgs a, int slices) {
-  constexpr int E = Piece<T>::E, LANES = kVecCols / E, ROWS = 64 / LANES, STEP = ROWS * 4, UN = 4;
-  __shared__ __attribute__((aligned(16))) float xs[kVecSlice * NB];
-  __shared__ float red[4][NB][2][kVecCols];
+__global__ __launch_bounds__(vec_waves(NB) * 64) void ff_vec_kernel(FfArgs a, int slices) {
+  constexpr int kVecWaves = vec_waves(NB);
+  constexpr int E = Piece<T>::E, LANES = kVecCols / E, ROWS = 64 / LANES, STEP = ROWS * kVecWaves;
+  constexpr int UN = NB <= 4 ? 4 : 2, NT = kVecWaves * 64;
+  __shared__ __attribute__((aligned(16))) float xs[vec_slice(NB) * NB];
+  __shared__ float red[kVecWaves][NB][2][kVecCols];
   const int64_t strips = (a.ff + kVecCols - 1) / kVecCols, id = group_number();
   if (id >= strips * slices) return;
   const int64_t slice = id / strips, strip = id - slice * strips;
   const int64_t k0 = slice * a.d / slices, k1 = (slice + 1) * a.d / slices;
   const int len = static_cast<int>(k1 - k0), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = threadIdx.x; i < len * NB; i += 256) {
-    const int t = i / len, k = i - t * len;
-    xs[k * NB + t] = t < a.N ? to_f32(static_cast<const T *>(a.X)[t * a.ldx + k0 + k]) : 0.0f;
-  }
-  __syncthreads();
   const int64_t c = strip * kVecCols + lane % LANES * E, cb = c < a.ff - E ? c : a.ff - E;
   const int row = wave * ROWS + lane / LANES;
   const T *wg = static_cast<const T *>(a.Wg) + (k0 + row) * a.ldw + cb;
@@ -234,17 +234,39 @@ __global__ __launch_bounds__(256) void ff_vec_kernel(FfArgs a, int slices) {
       }
     }
   };
+  // the first rows are on their way while the tokens are put into the LDS
+  u32x4 vg[UN], vu[UN];
   int k = row;
-  for (; k + (UN - 1) * STEP < len; k += UN * STEP, wg += UN * STEP * a.ldw) {
-    u32x4 vg[UN], vu[UN];
+  const bool any = k + (UN - 1) * STEP < len;
+  if (any) {
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
       vg[i] = load_piece(wg + i * STEP * a.ldw);
       vu[i] = load_piece(wg + i * STEP * a.ldw + twin);
     }
-#pragma unroll
-    for (int i = 0; i < UN; ++i) add(k + i * STEP, vg[i], vu[i]);
   }
+#pragma unroll 1
+  for (int t = 0; t < NB; ++t) {
+    const T *x = static_cast<const T *>(a.X) + t * a.ldx + k0;
+#pragma unroll 2
+    for (int q = threadIdx.x; q < len; q += NT) xs[q * NB + t] = t < a.N ? to_f32(x[q]) : 0.0f;
+  }
+  __syncthreads();
+  if (any) {
+#pragma unroll 1
+    for (; k + (UN - 1) * STEP < len; k += UN * STEP) {
+      // past the last rows these ones again, so that no branch parts the loads
+      const T *next = k + (2 * UN - 1) * STEP < len ? wg + UN * STEP * a.ldw : wg;
+      wg += UN * STEP * a.ldw;
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        add(k + i * STEP, vg[i], vu[i]);
+        vg[i] = load_piece(next + i * STEP * a.ldw);
+        vu[i] = load_piece(next + i * STEP * a.ldw + twin);
+      }
+    }
+  }
+#pragma unroll 1
   for (; k < len; k += STEP, wg += STEP * a.ldw) add(k, load_piece(wg), load_piece(wg + twin));
 #pragma unroll
   for (int t = 0; t < NB; ++t)
@@ -258,15 +280,17 @@ __global__ __launch_bounds__(256) void ff_vec_kernel(FfArgs a, int slices) {
         if (lane < LANES) red[wave][t][q][lane * E + e] = v;
       }
   __syncthreads();
-  for (int i = threadIdx.x; i < NB * kVecCols; i += 256) {
+  for (int i = threadIdx.x; i < NB * kVecCols; i += NT) {
     const int t = i / kVecCols, j = i % kVecCols;
     const int64_t c1 = strip * kVecCols + j / E * E;
     const int64_t col = (c1 < a.ff - E ? c1 : a.ff - E) + j % E;
     if (t >= a.N || c1 >= a.ff) continue;
-    float s[2];
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-      s[q] = ((red[0][t][q][j] + red[1][t][q][j]) + red[2][t][q][j]) + red[3][t][q][j];
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll 4
+    for (int w = 0; w < kVecWaves; ++w) {
+      s[0] += red[w][t][0][j];
+      s[1] += red[w][t][1][j];
+    }
     if (slices > 1) {
       float *p = a.part + (slice * 2 * a.N + t) * a.ff + col;
       p[0] = s[0];
@@ -357,13 +381,19 @@ void pack(const void *src, int64_t rows, int64_t cols, int64_t ld, uint16_t *dst
       static_cast<const T *>(src), rows, cols, ld, dst, up8(cols));
 }
 
-int vec_slices(int64_t d, int64_t ff) {
-  const int64_t strips = ceil_div(ff, kVecCols), least = ceil_div(d, kVecSlice);
-  const int64_t want = ceil_div(1024, strips), most = ceil_div(d, 64);
+// Slices of d: one where the columns alone fill most CUs, else enough for one and a half
+// workgroups to each, of 64 rows or more.
+int vec_slices(int64_t N, int64_t d, int64_t ff) {
+  const int64_t strips = ceil_div(ff, kVecCols), least = ceil_div(d, vec_slice(N <= 4 ? 4 : 8));
+  const int64_t want = strips >= 160 ? 1 : ceil_div(384, strips), most = ceil_div(d, 64);
   const int64_t n = want < most ? want : most;
   return static_cast<int>(n > least ? n : least);
 }
-bool by_vec(int dt, int64_t N, int64_t ff) { return N <= 8 && ff >= (dt == 0 ? 4 : 8); }
+// bf16 weights of whole pieces are as fast through the matrix cores from two tokens on
+// (4096 x 14336: one token 52 us, 16 tokens 54); others would have to be copied first.
+bool by_vec(int dt, int64_t N, int64_t ff) {
+  return N <= (dt == 1 && ff % 8 == 0 ? 1 : 8) && ff >= (dt == 0 ? 4 : 8);
+}
 
 #ifndef FEWD
 #define FEWD 6
@@ -388,7 +418,7 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
   Space s;
   if (by_vec(dt, N, ff)) {
     p.vec = true;
-    p.slices = vec_slices(d, ff);
+    p.slices = vec_slices(N, d, ff);
     if (p.slices > 1) p.part = s.take(sizeof(float) * p.slices * 2 * N * ff);
   } else {
     p.own_x = own_x;
@@ -409,13 +439,13 @@ hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t 
   if (p.vec) {
     const dim3 grid = groups_grid(ceil_div(a.ff, kVecCols) * p.slices);
     if (a.N == 1)
-      ff_vec_kernel<T, 1><<<grid, 256, 0, s>>>(a, p.slices);
+      ff_vec_kernel<T, 1><<<grid, 1024, 0, s>>>(a, p.slices);
     else if (a.N == 2)
-      ff_vec_kernel<T, 2><<<grid, 256, 0, s>>>(a, p.slices);
+      ff_vec_kernel<T, 2><<<grid, 1024, 0, s>>>(a, p.slices);
     else if (a.N <= 4)
-      ff_vec_kernel<T, 4><<<grid, 256, 0, s>>>(a, p.slices);
+      ff_vec_kernel<T, 4><<<grid, 1024, 0, s>>>(a, p.slices);
     else
-      ff_vec_kernel<T, 8><<<grid, 256, 0, s>>>(a, p.slices);
+      ff_vec_kernel<T, 8><<<grid, 512, 0, s>>>(a, p.slices);
     if (p.slices > 1)
       ff_join_kernel<T><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, p.slices);
   } else {
@@ -552,23 +582,53 @@ hipError_t launch_ff_grad_t(int dt, const FfGradArgs &a, const FfGradPlan &p, ch
   return hipGetLastError();
 }
 
-FfPlan plan_of(int dt, const FfArgs &a) {
-  return ff_plan(dt, a.N, a.d, a.ff, direct(dt, a.X, a.d, a.ldx),
-                 direct(dt, a.Wg, a.ff, a.ldw) && direct(dt, a.Wu, a.ff, a.ldw));
+// What may be read in place where every matrix starts on 16 bytes.
+struct Places {
+  bool x, w, g;
+};
+Places places_of(int dt, const FfArgs &a, bool pointers) {
+  const auto p = [&](const void *q) { return pointers ? q : nullptr; };
+  return {direct(dt, p(a.X), a.d, a.ldx),
+          direct(dt, p(a.Wg), a.ff, a.ldw) && direct(dt, p(a.Wu), a.ff, a.ldw), false};
 }
-FfGradPlan plan_of(int dt, const FfGradArgs &a) {
-  return ff_grad_plan(dt, a.N, a.d, a.ff, direct(dt, a.X, a.d, a.ldx),
-                      direct(dt, a.Wg, a.ff, a.ldw) && direct(dt, a.Wu, a.ff, a.ldw),
-                      direct(dt, a.dG, a.ff, a.ldd) && direct(dt, a.dU, a.ff, a.ldd));
+Places places_of(int dt, const FfGradArgs &a, bool pointers) {
+  const auto p = [&](const void *q) { return pointers ? q : nullptr; };
+  return {direct(dt, p(a.X), a.d, a.ldx),
+          direct(dt, p(a.Wg), a.ff, a.ldw) && direct(dt, p(a.Wu), a.ff, a.ldw),
+          direct(dt, p(a.dG), a.ff, a.ldd) && direct(dt, p(a.dU), a.ff, a.ldd)};
+}
+FfPlan plan_of(int dt, const FfArgs &a, const Places &own) {
+  return ff_plan(dt, a.N, a.d, a.ff, own.x, own.w);
+}
+FfGradPlan plan_of(int dt, const FfGradArgs &a, const Places &own) {
+  return ff_grad_plan(dt, a.N, a.d, a.ff, own.x, own.w, own.g);
+}
+// The bytes of a call whose matrices all start on 16 bytes, or of whichever starts take most.
+template <typename A>
+size_t most_bytes(int dt, const A &a, bool aligned) {
+  const Places best = places_of(dt, a, false);
+  size_t most = plan_of(dt, a, best).total;
+  for (int m = 0; m < 7 && !aligned; ++m) {
+    const size_t n =
+        plan_of(dt, a, Places{best.x && (m & 1), best.w && (m & 2), best.g && (m & 4)}).total;
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 }  // namespace
 
-size_t ff_workspace_bytes(int dt, const FfArgs &a) { return plan_of(dt, a).total; }
-size_t ff_grad_workspace_bytes(int dt, const FfGradArgs &a) { return plan_of(dt, a).total; }
+size_t ff_workspace_bytes(int dt, const FfArgs &a, bool aligned) { return most_bytes(dt, a, aligned); }
+size_t ff_grad_workspace_bytes(int dt, const FfGradArgs &a, bool aligned) {
+  return most_bytes(dt, a, aligned);
+}
+size_t ff_call_bytes(int dt, const FfArgs &a) { return plan_of(dt, a, places_of(dt, a, true)).total; }
+size_t ff_grad_call_bytes(int dt, const FfGradArgs &a) {
+  return plan_of(dt, a, places_of(dt, a, true)).total;
+}
 
 hipError_t launch_ff(int dt, const FfArgs &a, void *ws, hipStream_t s) {
-  const FfPlan p = plan_of(dt, a);
+  const FfPlan p = plan_of(dt, a, places_of(dt, a, true));
   return dt == 0 ? launch_ff_t<float>(dt, a, p, static_cast<char *>(ws), s)
                  : launch_ff_t<bf16_t>(dt, a, p, static_cast<char *>(ws), s);
 }
@@ -581,7 +641,7 @@ hipError_t launch_ff_grad(int dt, const FfGradArgs &a, void *ws, hipStream_t s) 
       ff_zero_kernel<<<grid, 256, 0, s>>>(out_of<bf16_t>(a));
     return hipGetLastError();
   }
-  const FfGradPlan p = plan_of(dt, a);
+  const FfGradPlan p = plan_of(dt, a, places_of(dt, a, true));
   return dt == 0 ? launch_ff_grad_t<float>(dt, a, p, static_cast<char *>(ws), s)
                  : launch_ff_grad_t<bf16_t>(dt, a, p, static_cast<char *>(ws), s);
 }

@@ -410,8 +410,11 @@ struct FfGradArgs {
   int64_t ldgw;
   int gdt, add;
 };
-size_t ff_workspace_bytes(int dt, const FfArgs &a);
-size_t ff_grad_workspace_bytes(int dt, const FfGradArgs &a);
+// Workspace by sizes and strides (pointers unread; aligned: all on 16 bytes), and of a call.
+size_t ff_workspace_bytes(int dt, const FfArgs &a, bool aligned);
+size_t ff_grad_workspace_bytes(int dt, const FfGradArgs &a, bool aligned);
+size_t ff_call_bytes(int dt, const FfArgs &a);
+size_t ff_grad_call_bytes(int dt, const FfGradArgs &a);
 hipError_t launch_ff(int dt, const FfArgs &a, void *ws, hipStream_t s);
 hipError_t launch_ff_grad(int dt, const FfGradArgs &a, void *ws, hipStream_t s);
 
