@@ -70,7 +70,7 @@ __device__ const u32x4 mm_zeros = {0, 0, 0, 0};
 __device__ __forceinline__ void lds_load_16(const void *src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
-               : "s"(dst), "v"(src)
+               : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(src)
                : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) {

@@ -227,6 +227,112 @@ struct OrthApply {
   }
 };
 
+// ---- products of small matrices ---------------------------------------------------------
+// Where a product has few tiles its time is that of its steps, one after the other.  Here a
+// workgroup holds 32 x 32 sums, a wave 16 x 16 of them, and has 256 k values of both planes of both
+// operands in the LDS: one wait for K <= 256 instead of twelve.  Five steps over six 256 x 256
+// float32 matrices take 108 us, 149 with tiles of 64 x 64; each of the 17 launches is
+// then bound by its own latency.  Layout: KC, piece p of a row's 32 lies at p ^ (row % 16); else
+// 64 bytes a k, the second of its two chunks first where k / 8 is odd.
+struct SmallShape {
+  static constexpr int BM = 32, BN = 32, WM = 2, WN = 2, TN = 1, PAIR = 0;
+};
+constexpr int kSmallK = 256, kSmallPlane = 32 * kSmallK * 2, kSmallBytes = 4 * kSmallPlane;
+
+// This lane's part of an operand's planes from k0 on, 16 loads of 1 KB a plane.
+template <bool KC>
+__device__ __forceinline__ void small_load(const uint16_t *p, int64_t ld, int64_t n, int64_t r0, int64_t k0,
+                                           int64_t K, uint32_t lds, int wave, int lane) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int idx = (j * 4 + wave) * 64 + lane;
+    const uint16_t *src;
+    bool there;
+    if constexpr (KC) {
+      const int r = idx >> 5, k = ((idx & 31) ^ (r & 15)) * 8;
+      src = p + min(r0 + r, n - 1) * ld + k0 + k;
+      there = k0 + k < K;
+    } else {
+      const int k = idx >> 2, slot = idx & 3;
+      const int c = (((slot >> 1) ^ (k >> 3 & 1)) << 4) | ((slot & 1) << 3);
+      src = p + (k0 + k) * ld + min(r0 + c, n - 8);
+      there = k0 + k < K;
+    }
+    lds_load_16(there ? static_cast<const void *>(src) : &mm_zeros, lds + (j * 4 + wave) * 1024);
+  }
+}
+// The fragment of 16 rows from `half` of the tile, k values 32 ks ..
+template <bool KC>
+__device__ __forceinline__ u32x4 small_read(const char *lds, int half, int ks, int lane) {
+  const int g = lane >> 4, n = lane & 15;
+  if constexpr (KC) {
+    return *reinterpret_cast<const u32x4 *>(lds + (half * 16 + n) * 512 + (((ks * 4 + g) ^ n) << 4));
+  } else {
+    u32x2 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char *q = lds + (ks * 32 + 8 * g + 4 * h + (n >> 2)) * 64 + ((half ^ (g & 1)) << 5) + (n & 3) * 8;
+      v[h] = __builtin_bit_cast(
+          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                     (__attribute__((address_space(3))) s16x4 *)(const_cast<char *>(q))));
+    }
+    return u32x4{v[0].x, v[0].y, v[1].x, v[1].y};
+  }
+}
+
+// low_a, low_b: bytes to the operands' low planes, 0 where those are left out.  STAGES: 1 where
+// K <= 256.
+template <bool AK, bool BK, int STAGES, class Epi>
+__global__ __launch_bounds__(256, 3 - STAGES) void orth_small_kernel(MmArgs m, int64_t low_a, int64_t low_b, MmGrid g,
+                                                            Epi e) {
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * kSmallBytes];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const MmPlace p = mm_where(g, blockIdx.x);
+  const uint16_t *a = m.a.p[0] + p.z * (m.a.batch / 2), *b = m.b.p[0] + p.z * (m.b.batch / 2);
+  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds));
+  const auto load = [&](int64_t k0, uint32_t to) {
+    small_load<AK>(a, m.a.ld, m.a.n, p.tm * 32, k0, m.k, to, wave, lane);
+    small_load<BK>(b, m.b.ld, m.b.n, p.tn * 32, k0, m.k, to + 2 * kSmallPlane, wave, lane);
+    if (low_a)
+      small_load<AK>(a + low_a / 2, m.a.ld, m.a.n, p.tm * 32, k0, m.k, to + kSmallPlane, wave, lane);
+    if (low_b)
+      small_load<BK>(b + low_b / 2, m.b.ld, m.b.n, p.tn * 32, k0, m.k, to + 3 * kSmallPlane, wave, lane);
+  };
+  f32x4 high = {0, 0, 0, 0}, low = {0, 0, 0, 0};
+  uint32_t cur = 0;
+  load(0, base);
+  for (int64_t k0 = 0; k0 < m.k; k0 += kSmallK) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    if (STAGES > 1 && k0 + kSmallK < m.k) load(k0 + kSmallK, base + (cur ^ kSmallBytes));
+    const char *at = lds + cur;
+    const int64_t left = m.k - k0;
+    const int steps = left < kSmallK ? static_cast<int>((left + 31) / 32) : kSmallK / 32;
+    for (int ks = 0; ks < steps; ++ks) {
+      const u32x4 ah = small_read<AK>(at, wave >> 1, ks, lane);
+      const u32x4 bh = small_read<BK>(at + 2 * kSmallPlane, wave & 1, ks, lane);
+      high = mm_mfma<true>(bh, ah, high);
+      if (low_b) low = mm_mfma<true>(small_read<BK>(at + 3 * kSmallPlane, wave & 1, ks, lane), ah, low);
+      if (low_a) low = mm_mfma<true>(bh, small_read<AK>(at + kSmallPlane, wave >> 1, ks, lane), low);
+    }
+    if constexpr (STAGES > 1) cur ^= kSmallBytes;
+  }
+  f32x4 acc[1];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[0][i] = fmaf(low[i], 1.0f / kUp, high[i]);
+  mm_row<SmallShape>(e, p, 0, acc);
+}
+
+// Whether a product of M x N is one of small matrices: no more workgroups of 32 x 32 than run at a
+// time, and k values for a few stages.  Whole calls, float32, all products in this way and all in
+// the other, us: 128 x 128 40 times 228 and 254, 256 x 256 6 times 108 and 149, 12 times 143 and
+// 157, 24 times 226 and 183; 512 x 512 once 121 and 203, 3 times 229 and 231; 729 x 729 266 and
+// 265; 256 x 1024 112 and 165; 64 x 4096 191 and 147.
+bool small_product(int64_t M, int64_t N, int64_t count, int64_t k, bool sym) {
+  const int64_t r = ceil_div(M, 32), c = ceil_div(N, 32);
+  return k <= 4 * kSmallK && (sym ? r * (r + 1) / 2 : r * c) * count <= (k <= kSmallK ? 512 : 256);
+}
+
 // Products of one, two or three segments are cut in their own way.
 MmPlan cut(int64_t M, int64_t N, int64_t count, int64_t k, int segs, bool sym) {
   return mm_plan(M, N, count, ceil_div(k, kMmK) * segs, sym);
@@ -285,7 +391,23 @@ void planes(MmArgs &m, const uint16_t *a, int64_t aplane, const uint16_t *b, int
 
 template <bool AK, bool BK, class Epi>
 void run(const MmArgs &m, int64_t M, int64_t N, int64_t count, bool sym, float *part, const Epi &e,
-         hipStream_t s) {
+         int64_t low_a, int64_t low_b, hipStream_t s) {
+  if (small_product(M, N, count, m.k, sym)) {
+    MmArgs h = m;  // the high planes: the last segment's
+    h.a.p[0] = m.a.p[m.segs - 1];
+    h.b.p[0] = m.b.p[m.segs - 1];
+    MmGrid g = {};
+    g.gm = ceil_div(M, 32);
+    g.gn = ceil_div(N, 32);
+    g.mats = count;
+    g.sym = sym;
+    const unsigned grid = static_cast<unsigned>((sym ? g.gm * (g.gm + 1) / 2 : g.gm * g.gn) * count);
+    if (m.k <= kSmallK)
+      orth_small_kernel<AK, BK, 1, Epi><<<grid, 256, 0, s>>>(h, low_a, low_b, g, e);
+    else
+      orth_small_kernel<AK, BK, 2, Epi><<<grid, 256, 0, s>>>(h, low_a, low_b, g, e);
+    return;
+  }
   const MmPlan p = cut(M, N, count, m.k, m.segs, sym);
   MmGrid g = p.grid;
   g.part = part;
@@ -320,16 +442,20 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
     m.a.batch = m.b.batch = 4 * xplane;
     planes(m, x, xplane, x, xplane, whole ? kAll : kHigh);
     const OrthSym<false> gram = {p.n, p.lda, nullptr, A, true};
+    const int64_t low_x = whole ? 2 * xplane : 0;
     if (tall)
-      run<false, false>(m, p.n, p.n, a.count, true, part, gram, s);
+      run<false, false>(m, p.n, p.n, a.count, true, part, gram, low_x, low_x, s);
     else
-      run<true, true>(m, p.n, p.n, a.count, true, part, gram, s);
+      run<true, true>(m, p.n, p.n, a.count, true, part, gram, low_x, low_x, s);
     m.k = p.n;
     m.a.ld = m.b.ld = p.lda;
     m.a.n = m.b.n = p.n;
     m.a.batch = m.b.batch = 4 * aplane;
-    planes(m, A, aplane, A, aplane, whole || i + 2 >= a.steps ? kAll : kHigh);
-    run<true, true>(m, p.n, p.n, a.count, true, part, OrthSym<true>{p.n, p.lda, A, Q, whole}, s);
+    const bool square = whole || i + 2 >= a.steps;
+    planes(m, A, aplane, A, aplane, square ? kAll : kHigh);
+    const int64_t low_A = square ? 2 * aplane : 0;
+    run<true, true>(m, p.n, p.n, a.count, true, part, OrthSym<true>{p.n, p.lda, A, Q, whole}, low_A, low_A,
+                    s);
     MmOperand &o = tall ? m.a : m.b;  // X's
     o.ld = p.ldx;
     o.n = tall ? a.rows : p.ldx;
@@ -338,11 +464,12 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
       planes(m, x, xplane, Q, aplane, whole ? kAll : last ? kHigh : kBothOfA);
     else
       planes(m, Q, aplane, x, xplane, whole ? kAll : last ? kHigh : kBothOfB);
+    const int64_t low_q = whole ? 2 * aplane : 0, last_x = whole || !last ? 2 * xplane : 0;
     const auto apply = [&](const auto &e) {
       if (tall)
-        run<true, true>(m, a.rows, a.cols, a.count, false, part, e, s);
+        run<true, true>(m, a.rows, a.cols, a.count, false, part, e, last_x, low_q, s);
       else
-        run<true, false>(m, a.rows, a.cols, a.count, false, part, e, s);
+        run<true, false>(m, a.rows, a.cols, a.count, false, part, e, low_q, last_x, s);
     };
     if (last)
       apply(OrthApply<true, T>{t, a, next, p.ldx});

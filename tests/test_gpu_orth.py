@@ -163,6 +163,20 @@ def test_more_matrices_than_a_launch_takes():
         _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, "f32"), "f32", f"matrix {k}")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count,shape", [(1, (256, 256)), (2, (257, 255)), (1, (31, 1024)), (1, (1024, 31)),
+                                         (1, (40, 1025)), (1, (264, 520)), (1, (519, 265)), (16, (63, 65)),
+                                         (17, (256, 64)), (9, (200, 250))], ids=str)
+def test_small_products(dtype, count, shape):
+    """Sides, lengths and numbers of matrices on both sides of where products are cut another way."""
+    log(f"[orthogonalize, small] {dtype} {count} of {shape}")
+    mats = [_mat(k, *shape, dtype, k % 3) for k in range(count)]
+    got = sn.sn_orthogonalize(mats)
+    for k in {0, count // 2, count - 1}:
+        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, dtype), dtype, f"matrix {k}")
+    assert all(torch.equal(a, b) for a, b in zip(got, sn.sn_orthogonalize(mats)))
+
+
 @pytest.mark.parametrize("count,shape", [(1, (1100, 2100)), (1, (2100, 1100)), (5, (700, 900)), (24, (520, 540))],
                          ids=lambda s: str(s))
 def test_large_tiles(count, shape):
