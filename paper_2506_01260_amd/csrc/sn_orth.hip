@@ -481,8 +481,13 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
 
 }  // namespace
 
+// Of the launches' groups of matrices: the whole ones', or the last one's, whose few matrices may
+// be cut into more parts.
 size_t orth_workspace_bytes(int64_t rows, int64_t cols, int64_t count) {
-  return orth_plan(rows, cols, count < OrthMats::kMost ? count : OrthMats::kMost).total;
+  const int64_t last = count % OrthMats::kMost;
+  const size_t whole = count < OrthMats::kMost ? 0 : orth_plan(rows, cols, OrthMats::kMost).total;
+  const size_t rest = last ? orth_plan(rows, cols, last).total : 0;
+  return whole > rest ? whole : rest;
 }
 
 hipError_t launch_orth(int dt, const OrthMats &t, const OrthArgs &a, void *ws, hipStream_t s) {

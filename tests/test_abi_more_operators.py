@@ -197,6 +197,18 @@ def test_muon_step(over, code):
         assert sn.lib().sn_last_error().decode() != ""
 
 
+def test_orthogonalize_workspace_covers_every_launch():
+    """A call makes its matrices 32 at a time: the bytes of 32 and of what is left, whose fewer
+    matrices may be cut into more parts."""
+    f = sn.sn_orthogonalize_workspace_bytes
+    sizes = [1, 7, 33, 64, 100, 256, 300, 512, 729, 1600, 4267, 20000]
+    for rows in sizes:
+        for cols in sizes:
+            whole = f(32, rows, cols)
+            for left in (1, 2, 3, 5, 11, 31):
+                assert f(32 + left, rows, cols) == f(64 + left, rows, cols) == max(whole, f(left, rows, cols))
+
+
 def test_binding_refuses_before_the_library():
     x, w = torch.zeros(4, 8), torch.zeros(8)
     for call, status in (

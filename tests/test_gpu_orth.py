@@ -163,6 +163,19 @@ def test_more_matrices_than_a_launch_takes():
         _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, "f32"), "f32", f"matrix {k}")
 
 
+@pytest.mark.parametrize("count,shape", [(33, (1, 300)), (40, (3, 2000)), (35, (150, 90))], ids=str)
+def test_the_last_launch_keeps_to_the_workspace(count, shape):
+    """Behind 32 matrices come a few, cut into more parts; what lies behind the workspace stays."""
+    log(f"[orthogonalize, workspace] {count} of {shape}")
+    need = sn.sn_orthogonalize_workspace_bytes(count, *shape)
+    room = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    mats = [_mat(k, *shape, "f32") for k in range(count)]
+    got = sn.sn_orthogonalize(mats, workspace=room[:need])
+    assert bool((room[need:] == 0x5A).all())
+    for k in (0, 31, count - 1):
+        _near(host(got[k]), orc.orthogonalize(host(mats[k])), _bound(host(mats[k]), 5, "f32"), "f32", f"matrix {k}")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("count,shape", [(1, (256, 256)), (2, (257, 255)), (1, (31, 1024)), (1, (1024, 31)),
                                          (1, (40, 1025)), (1, (264, 520)), (1, (519, 265)), (16, (63, 65)),
