@@ -413,8 +413,9 @@ __global__ __launch_bounds__(S::NT, S::NT / 256) void mm_kernel(MmArgs m, MmGrid
   if (id < g.whole) {
     tile = mm_order(id, g.whole);
   } else {
-    split = (id - g.whole) / g.rest;
-    tile = id - split * g.rest;
+    const int64_t o = mm_order(id - g.whole, g.rest * g.splits);
+    split = o / g.rest;
+    tile = g.whole + o - split * g.rest;
     t0 = split * steps / g.splits;
     t1 = (split + 1) * steps / g.splits;
   }
