@@ -399,8 +399,21 @@ constexpr int64_t kFew = 64;
 // Steps of weights on their way to the LDS while few tokens are multiplied: 48 tokens take 55 us
 // with 6, 77 with 2.
 constexpr int kFewDepth = 6;
-MmPlan few_plan(int64_t cols) {
+// bf16 tokens for one row of tiles of 256 x 128, on half to all of the CUs: long columns of the
+// weights come from memory, and two steps of them on their way outdo what smaller tiles share in
+// the L2.  us, so and in tiles by mm_plan: 4096 x 14336 with 130 tokens 74 and 91, with 256 86
+// and 104; 2048 x 8192 39 and 40, 39 and 45; 8192 x 14336 133 and 167, 155 and 191; of shorter
+// columns (1024 x 8192) 25 and 22, of fewer (1024 x 4096) 23 and 14, of more (8192 x 28672) 275
+// and 231.
+bool in_one(int dt, int64_t N, int64_t d, int64_t ff) {
+  const int64_t groups = ceil_div(2 * ff, 128);
+  return dt == 1 && N > 128 && N <= 256 && d >= 2048 && groups >= 128 && groups <= 256;
+}
+constexpr int kOneDepth = 3;
+enum { kFewTile = 0, kOneTile = 1 };  // MmPlan's size beside 64, 128 and 256
+MmPlan row_plan(int size, int64_t cols) {
   MmPlan p = {};
+  p.size = size;
   p.grid.gm = 1;
   p.grid.gn = p.grid.whole = ceil_div(cols, 128);
   p.grid.mats = p.grid.splits = 1;
@@ -424,7 +437,9 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
     p.own_x = own_x;
     p.own_w = own_w;
     // a paired tile has half its columns of either product
-    p.t = N <= kFew ? few_plan(2 * ff) : mm_plan(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
+    p.t = N <= kFew              ? row_plan(kFewTile, 2 * ff)
+          : in_one(dt, N, d, ff) ? row_plan(kOneTile, 2 * ff)
+                                 : mm_plan(N, 2 * ff, 1, ceil_div(d, kMmK) * segs_of(dt));
     if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
     if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
     p.part = s.take(p.t.part_bytes);
@@ -476,7 +491,13 @@ hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t 
     MmGrid g = p.t.grid;
     g.part = a.part;
     const FfEpilogue<T> e = {a};
-    if (p.t.size == 0)
+    if constexpr (sizeof(T) == 2) {
+      if (p.t.size == kOneTile) {
+        mm_launch<MmShape<false, true, false, 256, 128, 4, 2, kOneDepth, true>>(m, g, e, s);
+        return hipGetLastError();
+      }
+    }
+    if (p.t.size == kFewTile)
       mm_launch<MmShape<false, true, false, 64, 128, 2, 2, kFewDepth, true>>(m, g, e, s);
     else if (p.t.size == 256)
       mm_launch<MmShape<false, true, false, 256, 256, 2, 4, 2, true>>(m, g, e, s);

@@ -467,7 +467,7 @@ void mm_launch(const MmArgs &m, const MmGrid &g, const Epi &e, hipStream_t s) {
 // How a product of M x N sums over `steps` steps is cut (N: both twins' columns where they are
 // paired): the tile and the splits of the shortest time by this model, in us.  A step of a tile
 // takes what the kernels measured on full CUs; a CU holds one workgroup of 256 x 256, two of
-// 128 x 128 or 64 x 64; the parts are written and read at 4 TB/s, and adding them takes a launch.
+// 128 x 128 or 64 x 64; the parts are written and read at 6 TB/s, and adding them takes a launch.
 struct MmPlan {
   int size;
   MmGrid grid;
@@ -500,7 +500,7 @@ inline MmPlan mm_plan(int64_t M, int64_t N, int64_t mats, int64_t steps, bool sy
       const double bytes = static_cast<double>(g.rest) * s * k.size * k.size * sizeof(float);
       if (s > 1)
         us += static_cast<double>(ceil_div(g.rest * s, slots)) *
-                  (k.step * static_cast<double>(ceil_div(steps, s)) + 3.0) + 4.0 + 2.0 * bytes / 4e6;
+                  (k.step * static_cast<double>(ceil_div(steps, s)) + 3.0) + 4.0 + 2.0 * bytes / 6e6;
       if (least > 0.0 && us >= least) continue;
       least = us;
       best.size = k.size;

@@ -115,6 +115,18 @@ def test_forward_matches_oracle(dtype, shape):
         assert float(out[:, :, ff:].abs().max()) == 0.0
 
 
+@pytest.mark.parametrize("shape", [(129, 2048, 8192), (256, 2050, 8200), (200, 2048, 16384), (257, 2048, 8192),
+                                   (256, 2047, 8192), (128, 2048, 8192)], ids=lambda s: "x".join(map(str, s)))
+def test_tokens_of_one_row_of_tiles(shape):
+    """Both sides of where long weights meet one row of tall tiles."""
+    n, d, ff = shape
+    log(f"[gated ff] bf16 {shape}")
+    X = _mat(n, n, d, "bf16")
+    Wg, Wu = (_mat(s, d, ff, "bf16", 0, d ** -0.5) for s in (1, 2))
+    H, G, Ut = sn.sn_gated_ff(X, Wg, Wu, save=True)
+    _check_forward(H, G, Ut, X, Wg, Wu, "silu", "bf16", "silu")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
 def test_backward_matches_oracle(dtype, shape):
