@@ -11,6 +11,9 @@
 // Memory-bound: each operand passes once, the row staying in registers between its two
 // (backward: two joint) sums and its outputs.  R threads hold a row in K pieces each; with
 // R = 64 a wave has a row of its own and no barrier.
+// bf16 with one gate row: 32768 x 4096 190 us, 5.7 TB/s (add of two arrays: 6.2); backward
+// 16383 x 8192 308 us, 5.2 TB/s; with a gate and its gradient for each token 4999 x 1600 36 us,
+// of it 4 the second launch that joins the column sums; one token 3.5 us in the kernel.
 #include "sn_internal.h"
 #include "sn_rows.h"
 
