@@ -8,8 +8,8 @@
 // and writes H from the 32-bit sums.  Backward: dG and dU are made once, elementwise, and
 // rounded to dt, the operands' type of the three products that read them (dX as one
 // product over 2 ff, both weights' gradients in one launch).
-// float32 operands are split in three bf16 planes (24 bits together, hi + mid + lo) and
-// the six products down to 2^-24 of the largest are added up: at the peak rates 2.6 times
+// float32 operands (forward: of more than 128 tokens) are split in three bf16 planes (24 bits
+// together, hi + mid + lo) and the six products down to 2^-24 of the largest are added up: at the peak rates 2.6 times
 // what the float32 matrix instructions do.  Matrices that are not 16-byte aligned, or
 // whose rows are no multiple of 8 elements, are copied to padded rows first.
 //
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs a, int parts) {
   }
 }
 
-// ---- forward of up to 8 tokens: the weights stream by -----------------------------------
+// ---- forward of up to 8 bf16 tokens: the weights stream by ------------------------------
 // A workgroup of 16 waves (8 for more than 4 tokens) takes 64 columns of both weights and a
 // slice of d (all of it where there are enough columns for the CUs); a lane takes 16 bytes of
 // a weight's row, the lanes beside it the rest of the row's 64 columns and further rows.
@@ -208,8 +208,9 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs a, int parts) {
 constexpr int kVecCols = 64;
 constexpr int vec_waves(int nb) { return nb <= 4 ? 16 : 8; }
 constexpr int vec_slice(int nb) { return nb <= 4 ? 4096 : 2048; }  // longest
-template <typename T, int NB>
+template <int NB>
 __global__ __launch_bounds__(vec_waves(NB) * 64) void ff_vec_kernel(FfArgs a, int slices) {
+  using T = bf16_t;
   constexpr int kVecWaves = vec_waves(NB);
   constexpr int E = Piece<T>::E, LANES = kVecCols / E, ROWS = 64 / LANES, STEP = ROWS * kVecWaves;
   constexpr int UN = NB <= 4 ? 4 : 2, NT = kVecWaves * 64;
@@ -310,6 +311,129 @@ __global__ __launch_bounds__(vec_waves(NB) * 64) void ff_vec_kernel(FfArgs a, in
   }
 }
 
+// ---- forward of up to 128 float32 tokens: the weights as they are -----------------------------
+// A workgroup takes 64 columns of both weights and a slice of d, 128 of its k at a time, whose
+// part of the tokens lies in the LDS; a wave takes every eighth four of them.  In the float32 matrix
+// instruction 16 x 16 x 4 lane l = 16 g + n supplies k = g of row n of either operand: a lane's 16 bytes
+// of a weight's row are columns 4 n + e, so the products of its value e have rows n for columns
+// 4 n + e, and the sums of all four are 16 neighbouring columns of the token n.
+// Bound by the weights' reading up to 16 tokens (4096 x 14336 85 us, 5.5 TB/s), then by the
+// instruction (64 tokens 178 us; its rate alone would take 96).
+constexpr int kFourCols = 64, kFourWaves = 8, kFourK = 128;
+template <int TT>  // tiles of 16 tokens
+__global__ __launch_bounds__(kFourWaves * 64) void ff_four_kernel(FfArgs a, int slices) {
+  constexpr int NT = kFourWaves * 64, TOK = 16 * TT, UN = kFourK / 4 / kFourWaves;
+  // rows 16 banks apart: the four k that are read together lie in different ones
+  constexpr int STRIDE = TT == 1 ? 16 : TOK + 16, XS = kFourK * STRIDE;
+  constexpr int RED = 2 * kFourWaves * 16 * kFourCols;
+  __shared__ __attribute__((aligned(16))) float lds[2 * XS > RED ? 2 * XS : RED];
+  const int64_t strips = (a.ff + kFourCols - 1) / kFourCols, blocks = (a.N + TOK - 1) / TOK;
+  const int64_t id = group_number(), part = id / blocks;
+  if (part >= strips * slices) return;
+  const int64_t slice = part / strips, strip = part - slice * strips, first = (id - part * blocks) * TOK;
+  const int64_t k0 = slice * a.d / slices, len = (slice + 1) * a.d / slices - k0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
+  const int64_t c = strip * kFourCols + 4 * n, cb = c < a.ff - 4 ? c : a.ff - 4;
+  const float *wg = static_cast<const float *>(a.Wg) + k0 * a.ldw + cb;
+  const int64_t twin = static_cast<const float *>(a.Wu) - static_cast<const float *>(a.Wg);
+  const float *X = static_cast<const float *>(a.X) + first * a.ldx + k0;
+  const int64_t tokens = a.N - first;
+  // the tokens' share of a thread: four k of token t, TT times
+  const int tt = threadIdx.x & 15, tk = threadIdx.x >> 4 << 2;
+  f32x4 xr[TT], acc[2][TT][4];
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[q][t][e] = f32x4{0, 0, 0, 0};
+  const auto fetch = [&](int64_t at) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      xr[t] = f32x4{0, 0, 0, 0};
+      if (t * 16 + tt < tokens && at + tk < len) xr[t] = get4(X + (t * 16 + tt) * a.ldx + at + tk, len - at - tk);
+    }
+  };
+  const auto store = [&](float *xs) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) xs[(tk + e) * STRIDE + t * 16 + tt] = xr[t][e];
+  };
+  u32x4 vg[UN], vu[UN];
+  const auto weights = [&](int i, int64_t at) {  // rows past the slice: its last one, as zeros
+    const int64_t k = at + (i * kFourWaves + wave) * 4 + g;
+    const float *w = wg + (k < len ? k : len - 1) * a.ldw;
+    const uint32_t keep = k < len ? ~0u : 0u;
+    vg[i] = load_piece(w) & u32x4{keep, keep, keep, keep};
+    vu[i] = load_piece(w + twin) & u32x4{keep, keep, keep, keep};
+  };
+  fetch(0);
+#pragma unroll
+  for (int i = 0; i < UN; ++i) weights(i, 0);
+  store(lds);
+  lds_barrier();
+  int cur = 0;
+#pragma unroll 1
+  for (int64_t at = 0; at < len; at += kFourK) {
+    const bool more = at + kFourK < len;
+    if (more) fetch(at + kFourK);
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      float x[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+        x[t] = lds[cur + ((i * kFourWaves + wave) * 4 + g) * STRIDE + t * 16 + n];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          acc[0][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vg[i][e]), x[t], acc[0][t][e], 0, 0, 0);
+          acc[1][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vu[i][e]), x[t], acc[1][t][e], 0, 0, 0);
+        }
+      weights(i, more ? at + kFourK : at);  // behind the last ones, these again: no branch parts the loads
+    }
+    cur ^= XS;
+    if (more) store(lds + cur);
+    lds_barrier();
+  }
+  // the waves' sums are added in order, tile by tile
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4 *>(lds + ((q * kFourWaves + wave) * 16 + n) * kFourCols + 16 * g + 4 * r) =
+            f32x4{acc[q][t][0][r], acc[q][t][1][r], acc[q][t][2][r], acc[q][t][3][r]};
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * kFourCols; i += NT) {
+      const int64_t token = first + t * 16 + i / kFourCols;
+      const int j = i % kFourCols;
+      const int64_t c1 = strip * kFourCols + j / 4 * 4;
+      const int64_t col = (c1 < a.ff - 4 ? c1 : a.ff - 4) + j % 4;
+      float s[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < kFourWaves; ++w)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) s[q] += lds[(q * kFourWaves + w) * 16 * kFourCols + i];
+      if (token >= a.N || c1 >= a.ff) continue;
+      if (slices > 1) {
+        float *p = a.part + (slice * 2 * a.N + token) * a.ff + col;
+        p[0] = s[0];
+        p[a.N * a.ff] = s[1];
+      } else {
+        static_cast<float *>(a.H)[token * a.ldh + col] = ff_act(a.act, s[0]) * s[1];
+        if (a.G) {
+          static_cast<float *>(a.G)[token * a.ldg + col] = s[0];
+          static_cast<float *>(a.U)[token * a.ldg + col] = s[1];
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
 // ---- products of the backward -----------------------------------------------------------
 // C (M x N; C2 for the second matrix) = the product, added to what is there with `add`.
 template <typename T>
@@ -396,8 +520,25 @@ int vec_slices(int64_t N, int64_t d, int64_t ff) {
 }
 // bf16 weights of whole pieces are as fast through the matrix cores from two tokens on
 // (4096 x 14336: one token 52 us, 16 tokens 54); others would have to be copied first.
-bool by_vec(int dt, int64_t N, int64_t ff) {
-  return N <= (dt == 1 && ff % 8 == 0 ? 1 : 8) && ff >= (dt == 0 ? 4 : 8);
+bool by_vec(int dt, int64_t N, int64_t ff) { return dt == 1 && N <= (ff % 8 == 0 ? 1 : 8) && ff >= 8; }
+
+// float32 weights read as they are, or copied into planes first: 4096 x 14336 with 16 tokens 86
+// and 515 us, 48 175 and 519, 100 340 and 515; 1024 x 4096 17, 23, 48 and 64, 66, 52; with more
+// tokens the planes' products gain (4096 x 14336, 256 tokens: 672 and 550).
+bool by_four(int dt, int64_t N, int64_t ff) { return dt == 0 && N <= 128 && ff >= 4; }
+// Tiles of 16 tokens of a workgroup.  Where the columns are half the CUs' or more, so many that
+// the weights pass once (2048 x 8192, 64 tokens: 61 us, 86 with a tile each); else one, the
+// weights coming from the caches again (1600 x 4267, 48 tokens: 39 us, 69 with four).
+int four_tiles(int64_t N, int64_t ff) {
+  return N <= 16 || ceil_div(ff, kFourCols) < 128 ? 1 : N <= 32 ? 2 : 4;
+}
+// Slices of d: as many as give each CU a workgroup at most (4096 x 14336, one token: 85 us; in
+// two slices, of which a CU holds two, 95), of a round of k or more, 16 at most.
+int four_slices(int64_t N, int64_t d, int64_t ff) {
+  const int64_t groups = ceil_div(ff, kFourCols) * ceil_div(N, 16 * four_tiles(N, ff));
+  const int64_t fit = 256 / groups, most = ceil_div(d, kFourK);
+  const int64_t n = fit < 1 ? 1 : fit < most ? fit : most;
+  return static_cast<int>(n < 16 ? n : 16);
 }
 
 constexpr int64_t kFew = 64;
@@ -426,7 +567,7 @@ MmPlan row_plan(int size, int64_t cols) {
 }
 
 struct FfPlan {
-  bool vec, own_x, own_w;  // own: read in place
+  bool vec, four, own_x, own_w;  // own: read in place
   MmPlan t;
   int slices;
   size_t x, w, part, total;
@@ -437,6 +578,10 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
   if (by_vec(dt, N, ff)) {
     p.vec = true;
     p.slices = vec_slices(N, d, ff);
+    if (p.slices > 1) p.part = s.take(sizeof(float) * p.slices * 2 * N * ff);
+  } else if (by_four(dt, N, ff)) {
+    p.four = true;
+    p.slices = four_slices(N, d, ff);
     if (p.slices > 1) p.part = s.take(sizeof(float) * p.slices * 2 * N * ff);
   } else {
     p.own_x = own_x;
@@ -453,21 +598,37 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
   return p;
 }
 
+void launch_vec(const FfArgs &a, int slices, hipStream_t s) {
+  const dim3 grid = groups_grid(ceil_div(a.ff, kVecCols) * slices);
+  if (a.N == 1)
+    ff_vec_kernel<1><<<grid, 1024, 0, s>>>(a, slices);
+  else if (a.N <= 4)  // two tokens alone would take scratch memory
+    ff_vec_kernel<4><<<grid, 1024, 0, s>>>(a, slices);
+  else
+    ff_vec_kernel<8><<<grid, 512, 0, s>>>(a, slices);
+  if (slices > 1)
+    ff_join_kernel<bf16_t><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, slices);
+}
+void launch_four(const FfArgs &a, int slices, hipStream_t s) {
+  const int tt = four_tiles(a.N, a.ff);
+  const dim3 grid = groups_grid(ceil_div(a.ff, kFourCols) * slices * ceil_div(a.N, 16 * tt));
+  if (tt == 1)
+    ff_four_kernel<1><<<grid, kFourWaves * 64, 0, s>>>(a, slices);
+  else if (tt == 2)
+    ff_four_kernel<2><<<grid, kFourWaves * 64, 0, s>>>(a, slices);
+  else
+    ff_four_kernel<4><<<grid, kFourWaves * 64, 0, s>>>(a, slices);
+  if (slices > 1)
+    ff_join_kernel<float><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, slices);
+}
+
 template <typename T>
 hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t s) {
   a.part = reinterpret_cast<float *>(ws + p.part);
   if (p.vec) {
-    const dim3 grid = groups_grid(ceil_div(a.ff, kVecCols) * p.slices);
-    if (a.N == 1)
-      ff_vec_kernel<T, 1><<<grid, 1024, 0, s>>>(a, p.slices);
-    else if (a.N == 2)
-      ff_vec_kernel<T, 2><<<grid, 1024, 0, s>>>(a, p.slices);
-    else if (a.N <= 4)
-      ff_vec_kernel<T, 4><<<grid, 1024, 0, s>>>(a, p.slices);
-    else
-      ff_vec_kernel<T, 8><<<grid, 512, 0, s>>>(a, p.slices);
-    if (p.slices > 1)
-      ff_join_kernel<T><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, p.slices);
+    launch_vec(a, p.slices, s);
+  } else if (p.four) {
+    launch_four(a, p.slices, s);
   } else {
     MmArgs m = {};
     m.k = a.d;

@@ -3,8 +3,9 @@
 Tolerances (u = 2^-24).  A product of K terms is summed in float32 by instructions of 32 terms:
 its error is at most u (p K / 32 + 44) S, S the sum of the terms' sizes and p the number of
 products that are added up, 1 for bf16 and 6 for float32 (12 in dX, which adds two products),
-whose operands in three parts leave out 2 u S more.  With up to 8 tokens a sum is a chain of at
-most 32 terms, a tree of 7 levels and d / 64 slices, which that covers.
+whose operands in three parts leave out 2 u S more.  With up to 8 bf16 tokens a sum is a chain of at
+most 32 terms, a tree of 7 levels and d / 64 slices; with up to 128 float32 ones it is eight chains of
+K / 8 terms and at most 16 slices, K / 8 + 24 roundings: that covers both.
   * H:   act' < 1.13, so 1.2 tol(G) (|U| + tol(U)) + |act| tol(U), and |H| u (16 + 2 G^2) for the
          exponential of a rounded argument
   * dG, dU:   |value| u (32 + 2 G^2), and 4 u |dH U| where terms of act' cancel
@@ -113,6 +114,24 @@ def test_forward_matches_oracle(dtype, shape):
                            out_g=out[1, :, :ff], out_u=out[2, :, :ff])
         assert all(torch.equal(a, b) for a, b in zip(r, (H, G, Ut)))
         assert float(out[:, :, ff:].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("shape", [(17, 300, 8200), (33, 129, 8195), (100, 700, 8192), (128, 257, 500), (129, 257, 500),
+                                   (16, 1000, 40), (64, 2000, 100), (9, 5, 4), (20, 64, 5), (30, 1, 8192),
+                                   (1, 3000, 9001), (65, 4100, 70), (12, 40, 3)], ids=lambda s: "x".join(map(str, s)))
+def test_few_float32_tokens(shape):
+    """Tiles of one, two and four times 16 tokens, several of them, slices of d and the least columns."""
+    n, d, ff = shape
+    log(f"[gated ff, few] f32 {shape}")
+    for k, (pad, shift) in enumerate(((0, 0), (1, 1))):
+        act = ("silu", "gelu")[k]
+        X = _mat(n, n, d, "f32", pad, 1.0, shift)
+        Wg, Wu = (_mat(s, d, ff, "f32", pad, d ** -0.5, shift) for s in (1, 2))
+        out = torch.zeros(3, n, ff + 5, device="cuda")
+        H, G, Ut = sn.sn_gated_ff(X, Wg, Wu, act=act, out=out[0, :, :ff], out_g=out[1, :, :ff], out_u=out[2, :, :ff])
+        _check_forward(H, G, Ut, X, Wg, Wu, act, "f32", f"{act} pad={pad}")
+        assert float(out[:, :, ff:].abs().max()) == 0.0
+        assert torch.equal(sn.sn_gated_ff(X, Wg, Wu, act=act), H)
 
 
 @pytest.mark.parametrize("shape", [(129, 2048, 8192), (256, 2050, 8200), (200, 2048, 16384), (257, 2048, 8192),
