@@ -785,11 +785,9 @@ int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out
 /* (X Q with A = X^T X where there are more rows than columns), a, b, c =     */
 /* 3.4445, -4.7750, 2.0315: five steps take singular values from 1 / 300 to 1 */
 /* into [0.68, 1.21].  The result has B's row and column space: an update of  */
-/* columns that lie in the subspace lies there too.  Sums are float32.  Of    */
-/* float32 matrices (muon: weights) products are made from operands of 22     */
-/* bits; of bf16 ones from as few as keep the result's error below what its   */
-/* rounding to bf16 adds, about 1e-3 of its norm.  B = 0 gives 0; a NaN or an */
-/* infinity in B makes the result NaN.                                        */
+/* columns that lie in the subspace lies there too.  Sums are float32, and    */
+/* products are made from operands of 22 bits, whatever the dtype.  B = 0     */
+/* gives 0; a NaN or an infinity in B makes the result NaN.                   */
 /* ------------------------------------------------------------------------ */
 
 /* Largest number of steps. */

@@ -13,22 +13,17 @@
 // 1.45 and 3.45, each is stored times a power of two that keeps it below 65504, and lo
 // times 2^11, as large as hi at most, so that what fp16's least normal number, 2^-14, cuts
 // off lies below 2^-28 in hi and 2^-39 in all.
-// Where the result is rounded to bf16, products are left out whose part of it is small beside
-// that rounding (1.7e-3 of the result's norm): A is made of hi hi, A^2 too but in the last
-// two steps, and Q X of Q's hi with both planes of X but in the last step: 16 products of
-// m x m x n, a symmetric one for half, where 30 make five whole steps.  The error is
-// 0.7e-3 to 1.6e-3 of the result's norm (Gaussian matrices, few strong directions, singular
-// values over four decades, rank 20 of 384).  What must not go is X's lo: with hi alone
-// it is 7e-3 over four decades and 4e-2 in rank 20, where the rounded-off part of X grows
-// into directions that X does not have.
+// A result of bf16 needs the same: roundings to 11 bits average out in random matrices (1e-3 of the
+// result's norm with hi hi alone for A and A^2), but are all alike in matrices of equal or few
+// distinct values, where they add up: 5e-3 to 8e-3 for constant matrices, one-hot rows and
+// diagonal blocks, whose rounding to bf16 is 1.6e-3 to 3.1e-3.
 // A and Q are symmetric: the tiles on and below the diagonal are computed and mirrored.
 // Matrices of one shape share every launch.
 //
 // Bounds and times of a whole update: the matrix cores in large matrices (four of 4096 x 4096
-// bf16 8.7 to 9.2 ms, 960 to 1020 TFLOP/s, of it 0.27 the two passes over gradient and momentum
-// at 5 TB/s), how whole tiles fit the matrix in middling ones (two of 1600 x 4267 float32
-// 1.6 ms), the launches of three products a step in small ones (six of 256 x 256 float32
-// 106 us).
+// bf16 15.6 ms, 1060 TFLOP/s, of it 0.27 the two passes over gradient and momentum at 5 TB/s), how
+// whole tiles fit the matrix in middling ones (two of 1600 x 4267 float32 1.6 ms, one of
+// 1024 x 4096 0.51), the launches of three products a step in small ones (six of 256 x 256 102 us).
 #include "sn_internal.h"
 #include "sn_mm.h"
 #include "sn_rows.h"
@@ -98,8 +93,8 @@ __device__ __forceinline__ float f16_value(uint16_t v) {
 __device__ __forceinline__ uint16_t f16_bits(float v) {
   return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
 }
-// fp16 planes of four values (low: both of them)
-__device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v, bool low = true) {
+// fp16 planes of four values
+__device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v) {
   uint16_t h[4], l[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -108,7 +103,6 @@ __device__ __forceinline__ void orth_put(uint16_t *to, int64_t plane, f32x4 v, b
   }
   *reinterpret_cast<u32x2 *>(to) =
       u32x2{h[0] | static_cast<uint32_t>(h[1]) << 16, h[2] | static_cast<uint32_t>(h[3]) << 16};
-  if (!low) return;
   *reinterpret_cast<u32x2 *>(to + plane) =
       u32x2{l[0] | static_cast<uint32_t>(l[1]) << 16, l[2] | static_cast<uint32_t>(l[3]) << 16};
 }
@@ -157,7 +151,6 @@ struct OrthSym {
   int64_t n, ldp;
   const uint16_t *A;
   uint16_t *to;
-  bool low;
   template <class S>
   __device__ __forceinline__ void row(const MmPlace &p, int64_t row, int64_t col0,
                                       f32x4 (&acc)[S::TN]) const {
@@ -182,14 +175,14 @@ struct OrthSym {
         }
         if (!inside) v[e] = 0.0f;
       }
-      if (row < n) orth_put(out + row * ldp + col, plane, v, low);
+      if (row < n) orth_put(out + row * ldp + col, plane, v);
       if (p.tm == p.tn) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (col + e >= n) continue;
         uint16_t *q = out + (col + e) * ldp + row;
         q[0] = f16_bits(v[e]);
-        if (low) q[plane] = f16_bits((v[e] - f16_value(f16_bits(v[e]))) * kUp);
+        q[plane] = f16_bits((v[e] - f16_value(f16_bits(v[e]))) * kUp);
       }
     }
   }
@@ -286,8 +279,7 @@ __device__ __forceinline__ u32x4 small_read(const char *lds, int half, int ks, i
   }
 }
 
-// low_a, low_b: bytes to the operands' low planes, 0 where those are left out.  STAGES: 1 where
-// K <= 256.
+// low_a, low_b: elements to the operands' low planes.  STAGES: 1 where K <= 256.
 template <bool AK, bool BK, int STAGES, class Epi>
 __global__ __launch_bounds__(256, 3 - STAGES) void orth_small_kernel(MmArgs m, int64_t low_a, int64_t low_b, MmGrid g,
                                                             Epi e) {
@@ -299,10 +291,8 @@ __global__ __launch_bounds__(256, 3 - STAGES) void orth_small_kernel(MmArgs m, i
   const auto load = [&](int64_t k0, uint32_t to) {
     small_load<AK>(a, m.a.ld, m.a.n, p.tm * 32, k0, m.k, to, wave, lane);
     small_load<BK>(b, m.b.ld, m.b.n, p.tn * 32, k0, m.k, to + 2 * kSmallPlane, wave, lane);
-    if (low_a)
-      small_load<AK>(a + low_a / 2, m.a.ld, m.a.n, p.tm * 32, k0, m.k, to + kSmallPlane, wave, lane);
-    if (low_b)
-      small_load<BK>(b + low_b / 2, m.b.ld, m.b.n, p.tn * 32, k0, m.k, to + 3 * kSmallPlane, wave, lane);
+    small_load<AK>(a + low_a, m.a.ld, m.a.n, p.tm * 32, k0, m.k, to + kSmallPlane, wave, lane);
+    small_load<BK>(b + low_b, m.b.ld, m.b.n, p.tn * 32, k0, m.k, to + 3 * kSmallPlane, wave, lane);
   };
   f32x4 high = {0, 0, 0, 0}, low = {0, 0, 0, 0};
   uint32_t cur = 0;
@@ -318,8 +308,8 @@ __global__ __launch_bounds__(256, 3 - STAGES) void orth_small_kernel(MmArgs m, i
       const u32x4 ah = small_read<AK>(at, wave >> 1, ks, lane);
       const u32x4 bh = small_read<BK>(at + 2 * kSmallPlane, wave & 1, ks, lane);
       high = mm_mfma<true>(bh, ah, high);
-      if (low_b) low = mm_mfma<true>(small_read<BK>(at + 3 * kSmallPlane, wave & 1, ks, lane), ah, low);
-      if (low_a) low = mm_mfma<true>(bh, small_read<AK>(at + kSmallPlane, wave >> 1, ks, lane), low);
+      low = mm_mfma<true>(small_read<BK>(at + 3 * kSmallPlane, wave & 1, ks, lane), ah, low);
+      low = mm_mfma<true>(bh, small_read<AK>(at + kSmallPlane, wave >> 1, ks, lane), low);
     }
     if constexpr (STAGES > 1) cur ^= kSmallBytes;
   }
@@ -339,9 +329,9 @@ bool small_product(int64_t M, int64_t N, int64_t count, int64_t k, bool sym) {
   return k <= 4 * kSmallK && (sym ? r * (r + 1) / 2 : r * c) * count <= (k <= kSmallK ? 512 : 256);
 }
 
-// Products of one, two or three segments are cut in their own way.
-MmPlan cut(int64_t M, int64_t N, int64_t count, int64_t k, int segs, bool sym) {
-  return mm_plan(M, N, count, ceil_div(k, kMmK) * segs, sym);
+constexpr int kSegs = 3;  // hi lo, lo hi and hi hi
+MmPlan cut(int64_t M, int64_t N, int64_t count, int64_t k, bool sym) {
+  return mm_plan(M, N, count, ceil_div(k, kMmK) * kSegs, sym);
 }
 struct OrthPlan {
   int64_t n, ldx, lda;  // the smaller side; the planes' strides
@@ -367,41 +357,32 @@ OrthPlan orth_plan(int64_t rows, int64_t cols, int64_t count) {
   p.q = take(a);
   p.sums_at = take(sizeof(double) * count * p.sums);
   size_t part = 0;
-  for (int segs = 1; segs <= 3; ++segs)
-    for (const MmPlan &m : {cut(p.n, p.n, count, rows < cols ? cols : rows, segs, true),
-                            cut(p.n, p.n, count, p.n, segs, true),
-                            cut(rows, cols, count, p.n, segs, false)})
-      part = m.part_bytes > part ? m.part_bytes : part;
+  for (const MmPlan &m : {cut(p.n, p.n, count, rows < cols ? cols : rows, true),
+                          cut(p.n, p.n, count, p.n, true), cut(rows, cols, count, p.n, false)})
+    part = m.part_bytes > part ? m.part_bytes : part;
   p.part = take(part);
   p.total = at;
   return p;
 }
 
-// The products that are added up: hi lo, lo hi and hi hi; hi hi alone; with both planes of
-// one operand.
-enum Products { kAll, kHigh, kBothOfA, kBothOfB };
-void planes(MmArgs &m, const uint16_t *a, int64_t aplane, const uint16_t *b, int64_t bplane,
-            Products which) {
-  m.segs = 0;
+void planes(MmArgs &m, const uint16_t *a, int64_t aplane, const uint16_t *b, int64_t bplane) {
+  m.segs = kSegs;
   m.factor = 1.0f / kUp;
-  const auto add = [&](int pa, int pb) {
-    m.a.p[m.segs] = a + pa * aplane;
-    m.b.p[m.segs++] = b + pb * bplane;
-  };
-  if (which == kAll || which == kBothOfB) add(0, 1);
-  if (which == kAll || which == kBothOfA) add(1, 0);
-  m.run[0] = m.segs ? m.segs : 1;
-  add(0, 0);
-  m.run[1] = m.segs;
+  m.run[0] = 2;
+  m.run[1] = 3;
+  m.a.p[0] = m.a.p[2] = a;
+  m.a.p[1] = a + aplane;
+  m.b.p[0] = b + bplane;
+  m.b.p[1] = m.b.p[2] = b;
 }
 
 template <bool AK, bool BK, class Epi>
 void run(const MmArgs &m, int64_t M, int64_t N, int64_t count, bool sym, float *part, const Epi &e,
-         int64_t low_a, int64_t low_b, hipStream_t s) {
+         hipStream_t s) {
   if (small_product(M, N, count, m.k, sym)) {
-    MmArgs h = m;  // the high planes: the last segment's
-    h.a.p[0] = m.a.p[m.segs - 1];
-    h.b.p[0] = m.b.p[m.segs - 1];
+    MmArgs h = m;
+    h.b.p[0] = m.b.p[2];
+    const int64_t low_a = m.a.p[1] - m.a.p[0], low_b = m.b.p[0] - m.b.p[2];
     MmGrid g = {};
     g.gm = ceil_div(M, 32);
     g.gn = ceil_div(N, 32);
@@ -414,7 +395,7 @@ void run(const MmArgs &m, int64_t M, int64_t N, int64_t count, bool sym, float *
       orth_small_kernel<AK, BK, 2, Epi><<<grid, 256, 0, s>>>(h, low_a, low_b, g, e);
     return;
   }
-  const MmPlan p = cut(M, N, count, m.k, m.segs, sym);
+  const MmPlan p = cut(M, N, count, m.k, sym);
   MmGrid g = p.grid;
   g.part = part;
   if (p.size == 256)
@@ -440,44 +421,38 @@ hipError_t launch_orth_t(const OrthMats &t, const OrthArgs &a, char *ws, hipStre
   const int64_t xplane = a.rows * p.ldx, aplane = p.n * p.lda;
   for (int i = 0; i < a.steps; ++i) {
     uint16_t *x = X[i & 1], *next = X[~i & 1];
-    const bool whole = sizeof(T) == 4, last = i + 1 == a.steps;
     MmArgs m = {};
     m.k = tall ? a.rows : a.cols;
     m.a.ld = m.b.ld = p.ldx;
     m.a.n = m.b.n = tall ? p.ldx : a.rows;
     m.a.batch = m.b.batch = 4 * xplane;
-    planes(m, x, xplane, x, xplane, whole ? kAll : kHigh);
-    const OrthSym<false> gram = {p.n, p.lda, nullptr, A, true};
-    const int64_t low_x = whole ? 2 * xplane : 0;
+    planes(m, x, xplane, x, xplane);
+    const OrthSym<false> gram = {p.n, p.lda, nullptr, A};
     if (tall)
-      run<false, false>(m, p.n, p.n, a.count, true, part, gram, low_x, low_x, s);
+      run<false, false>(m, p.n, p.n, a.count, true, part, gram, s);
     else
-      run<true, true>(m, p.n, p.n, a.count, true, part, gram, low_x, low_x, s);
+      run<true, true>(m, p.n, p.n, a.count, true, part, gram, s);
     m.k = p.n;
     m.a.ld = m.b.ld = p.lda;
     m.a.n = m.b.n = p.n;
     m.a.batch = m.b.batch = 4 * aplane;
-    const bool square = whole || i + 2 >= a.steps;
-    planes(m, A, aplane, A, aplane, square ? kAll : kHigh);
-    const int64_t low_A = square ? 2 * aplane : 0;
-    run<true, true>(m, p.n, p.n, a.count, true, part, OrthSym<true>{p.n, p.lda, A, Q, whole}, low_A, low_A,
-                    s);
+    planes(m, A, aplane, A, aplane);
+    run<true, true>(m, p.n, p.n, a.count, true, part, OrthSym<true>{p.n, p.lda, A, Q}, s);
     MmOperand &o = tall ? m.a : m.b;  // X's
     o.ld = p.ldx;
     o.n = tall ? a.rows : p.ldx;
     o.batch = 4 * xplane;
     if (tall)
-      planes(m, x, xplane, Q, aplane, whole ? kAll : last ? kHigh : kBothOfA);
+      planes(m, x, xplane, Q, aplane);
     else
-      planes(m, Q, aplane, x, xplane, whole ? kAll : last ? kHigh : kBothOfB);
-    const int64_t low_q = whole ? 2 * aplane : 0, last_x = whole || !last ? 2 * xplane : 0;
+      planes(m, Q, aplane, x, xplane);
     const auto apply = [&](const auto &e) {
       if (tall)
-        run<true, true>(m, a.rows, a.cols, a.count, false, part, e, last_x, low_q, s);
+        run<true, true>(m, a.rows, a.cols, a.count, false, part, e, s);
       else
-        run<true, false>(m, a.rows, a.cols, a.count, false, part, e, low_q, last_x, s);
+        run<true, false>(m, a.rows, a.cols, a.count, false, part, e, s);
     };
-    if (last)
+    if (i + 1 == a.steps)
       apply(OrthApply<true, T>{t, a, next, p.ldx});
     else
       apply(OrthApply<false, T>{t, a, next, p.ldx});
