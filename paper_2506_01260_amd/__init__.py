@@ -1397,7 +1397,7 @@ def _orth_workspace(mats, workspace):
 
 def sn_orthogonalize(mats, steps: int = 5, out=None, workspace=None, stream=None):
     """The matrices of the list (or the one matrix) with their singular values taken towards 1 by
-    `steps` Newton-Schulz steps; all of one shape and dtype.  out: a list of as many (or one); each
+    `steps` Newton-Schulz steps (1 to 8); all of one shape and dtype.  out: a list of as many (or one); each
     may be the matrix itself."""
     one = isinstance(mats, torch.Tensor)
     native = _native()

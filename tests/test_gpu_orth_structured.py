@@ -65,3 +65,21 @@ def test_results_are_exact_to_their_rounding(dtype, kind):
         off = np.linalg.norm(host(sn.sn_orthogonalize(a, steps=steps)) - ref) / norm
         log(f"  {steps} steps: {off:.2e} of the norm, its rounding {own:.2e}, at most {tol:.2e}")
         assert off <= tol
+
+
+@pytest.mark.parametrize("steps", [5, 8])
+def test_updates_stay_in_the_subspace(steps):
+    """Gradients whose columns lie in 24 of 256 dimensions: what the update leaves outside is the bound
+    above, and the rounding of W and G to float32, 2^-24, which grows alike."""
+    log(f"[muon step, subspace] {steps} steps")
+    r, k, c = 256, 24, 600
+    g = torch.Generator().manual_seed(1)
+    Q = torch.linalg.qr(torch.randn(r, k, dtype=torch.float64, generator=g))[0]
+    W, G = ((Q @ torch.randn(k, c, dtype=torch.float64, generator=g)).float().cuda() for _ in range(2))
+    w0 = host(W)
+    sn.sn_muon_step(W, G, torch.zeros(r, c, device="cuda"), 0.1, steps=steps)
+    step, q = host(W) - w0, Q.numpy()
+    outside, norm = np.linalg.norm(step - q @ (q.T @ step)), np.linalg.norm(step)
+    most = (5 * 2.0 ** -22 + 2 * 2.0 ** -24) * 3.4445 ** steps * norm + 2 * 2.0 ** -24 * np.linalg.norm(w0)
+    log(f"  {outside:.3g} outside, at most {most:.3g}; the step {norm:.3g}")
+    assert outside <= most and norm > 0.1
