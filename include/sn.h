@@ -672,8 +672,9 @@ int32_t sn_block_norm_backward(const void *X, int64_t N, int64_t d, int64_t ldx,
 /* float32 matrices are multiplied in parts of 24 bits together, exact to     */
 /* 2^-24 of the products' sizes, but for what lies below 2^-126, which counts */
 /* as 0; there a NaN or an infinity makes the results that it enters NaN or   */
-/* infinite, not always the infinity itself.  sn_gated_ff of up to 128 tokens */
-/* (ff of 4 or more) multiplies them as they are, without such limits.        */
+/* infinite, not always the infinity itself.  sn_gated_ff of up to 384 tokens */
+/* (ff of 4 or more) and the dX of as many multiply them as they are, without */
+/* such limits.                                                               */
 /* ------------------------------------------------------------------------ */
 
 typedef enum sn_act { SN_ACT_SILU = 0, SN_ACT_GELU = 1, SN_ACT_RELU = 2 } sn_act;

@@ -8,9 +8,10 @@
 // and writes H from the 32-bit sums.  Backward: dG and dU are made once, elementwise, and
 // rounded to dt, the operands' type of the three products that read them (dX as one
 // product over 2 ff, both weights' gradients in one launch).
-// float32 operands (forward: of more than 128 tokens) are split in three bf16 planes (24 bits
-// together, hi + mid + lo) and the six products down to 2^-24 of the largest are added up: at the peak rates 2.6 times
-// what the float32 matrix instructions do.  Matrices that are not 16-byte aligned, or
+// float32 operands are split in three bf16 planes (24 bits together, hi + mid + lo) and the six products
+// down to 2^-24 of the largest are added up: at the peak rates 2.6 times what the float32 matrix
+// instructions do.  Up to 384 tokens copying the weights' planes would take longer than that gains: the
+// forward and dX multiply them as they are.  Matrices that are not 16-byte aligned, or
 // whose rows are no multiple of 8 elements, are copied to padded rows first.
 //
 // Bounds and times: many tokens the matrix cores (32768 x 4096 x 14336 with G and U kept
@@ -311,126 +312,191 @@ __global__ __launch_bounds__(vec_waves(NB) * 64) void ff_vec_kernel(FfArgs a, in
   }
 }
 
-// ---- forward of up to 128 float32 tokens: the weights as they are -----------------------------
-// A workgroup takes 64 columns of both weights and a slice of d, 128 of its k at a time, whose
-// part of the tokens lies in the LDS; a wave takes every eighth four of them.  In the float32 matrix
-// instruction 16 x 16 x 4 lane l = 16 g + n supplies k = g of row n of either operand: a lane's 16 bytes
-// of a weight's row are columns 4 n + e, so the products of its value e have rows n for columns
-// 4 n + e, and the sums of all four are 16 neighbouring columns of the token n.
-// Bound by the weights' reading up to 16 tokens (4096 x 14336 85 us, 5.5 TB/s), then by the
-// instruction (64 tokens 178 us; its rate alone would take 96).
-constexpr int kFourCols = 64, kFourWaves = 8, kFourK = 128;
-template <int TT>  // tiles of 16 tokens
-__global__ __launch_bounds__(kFourWaves * 64) void ff_four_kernel(FfArgs a, int slices) {
-  constexpr int NT = kFourWaves * 64, TOK = 16 * TT, UN = kFourK / 4 / kFourWaves;
-  // rows 16 banks apart: the four k that are read together lie in different ones
-  constexpr int STRIDE = TT == 1 ? 16 : TOK + 16, XS = kFourK * STRIDE;
-  constexpr int RED = 2 * kFourWaves * 16 * kFourCols;
+// ---- products of up to 384 float32 tokens: the weights as they are -----------------------------------
+// Of A (tokens, k contiguous) and a weight: forward X Wg and X Wu (KC false: a weight's rows are k), or
+// dX's dG Wg^T and dU Wu^T (KC: its rows are the output's columns).  A workgroup takes 16 TT tokens, a
+// slice of k and 64 columns of both weights (KC: 128 of one); every other wave has one half of the
+// columns, each pair of waves 16 of the 64 k of a round.  The tokens' part of a round lies in the LDS, in
+// two places in turn; weights come straight to registers, D - 1 rounds ahead.  In the float32 matrix
+// instruction 16 x 16 x 4 lane l = 16 g + n supplies k = g of row n of either operand; here instruction s
+// of 16 k values takes k = 4 g + s, so that a lane's four values of a token are one 16-byte read, and
+// of a weight's row (KC) one load.  Where rows are k, a lane's 16 bytes are columns 4 n + e, so the
+// products of its value e have rows n for columns 4 n + e, and the sums of all four are 16
+// neighbouring columns of the token n.  A sum is four chains of a quarter of the slice's k.
+// Piece p of a token's row lies at p ^ (token % 16): the 16 rows of a read are in different banks.
+// Bound by the weights' reading up to 32 tokens (4096 x 14336: one token 84 us, 5.6 TB/s, 32 tokens 93), then
+// by the instruction (64 tokens 149, 128 253, 256 501: 120 TFLOP/s, 137 on the 224 CUs that have work; the
+// same of tiles whose weights go through the LDS too 185, 315, 530).
+struct FewArgs {
+  const float *A[2], *B[2];  // KC: one for each segment; else A[0], and both weights
+  int64_t lda, ldb, N, k, cols;
+  int slices;  // of k; KC: those of a segment, behind each other
+  float *part;
+  FfArgs out;  // not KC, one slice
+};
+constexpr int kFewK = 64, kFewWaves = 8;
+template <bool KC, int TT>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void ff_few_kernel(FewArgs a) {
+  // (of an odd TT the last load's upper half has no tokens, and lies behind them in the LDS)
+  constexpr int NT = kFewWaves * 64, TOK = 16 * TT, L = (TT + 1) / 2, XS = 32 * L * kFewK, D = TT <= 4 ? 4 : 2;
+  constexpr int RED = kFewWaves * 16 * 64, BN = KC ? 128 : 64;
   __shared__ __attribute__((aligned(16))) float lds[2 * XS > RED ? 2 * XS : RED];
-  const int64_t strips = (a.ff + kFourCols - 1) / kFourCols, blocks = (a.N + TOK - 1) / TOK;
-  const int64_t id = group_number(), part = id / blocks;
-  if (part >= strips * slices) return;
-  const int64_t slice = part / strips, strip = part - slice * strips, first = (id - part * blocks) * TOK;
-  const int64_t k0 = slice * a.d / slices, len = (slice + 1) * a.d / slices - k0;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
-  const int64_t c = strip * kFourCols + 4 * n, cb = c < a.ff - 4 ? c : a.ff - 4;
-  const float *wg = static_cast<const float *>(a.Wg) + k0 * a.ldw + cb;
-  const int64_t twin = static_cast<const float *>(a.Wu) - static_cast<const float *>(a.Wg);
-  const float *X = static_cast<const float *>(a.X) + first * a.ldx + k0;
-  const int64_t tokens = a.N - first;
-  // the tokens' share of a thread: four k of token t, TT times
-  const int tt = threadIdx.x & 15, tk = threadIdx.x >> 4 << 2;
-  f32x4 xr[TT], acc[2][TT][4];
+  const int64_t strips = (a.cols + BN - 1) / BN, blocks = (a.N + TOK - 1) / TOK;
+  const int64_t all = strips * blocks * a.slices * (KC ? 2 : 1), id = group_number();
+  if (id >= all) return;
+  const int64_t number = mm_order(id, all), part = number / blocks;
+  const int64_t slice = part / strips, strip = part - slice * strips, first = (number - part * blocks) * TOK;
+  const int seg = slice >= a.slices ? 1 : 0;
+  const int64_t rounds = (a.k + kFewK - 1) / kFewK, sl = slice - seg * a.slices;
+  const int64_t k0 = sl * rounds / a.slices * kFewK, k1 = min((sl + 1) * rounds / a.slices * kFewK, a.k);
+  const int64_t full = (k1 - k0) / kFewK, tail = k1 - k0 - full * kFewK;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, n = lane & 15, half = wave & 1, kw = 16 * (wave >> 1) + 4 * g;
+  // tokens: piece p of row r, L of them (past the last token that one again: nothing is made of it)
+  const int p = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+  const float *A = a.A[seg] + k0;
+  int64_t at[L];
 #pragma unroll
-  for (int q = 0; q < 2; ++q)
+  for (int j = 0; j < L; ++j) at[j] = min(first + r0 + j * (NT / 16), a.N - 1) * a.lda + 4 * p;
+  f32x4 xr[L];
+  const auto store = [&](float *to) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[q][t][e] = f32x4{0, 0, 0, 0};
-  const auto fetch = [&](int64_t at) {
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      xr[t] = f32x4{0, 0, 0, 0};
-      if (t * 16 + tt < tokens && at + tk < len) xr[t] = get4(X + (t * 16 + tt) * a.ldx + at + tk, len - at - tk);
+    for (int j = 0; j < L; ++j) {
+      const int r = r0 + j * (NT / 16);
+      *reinterpret_cast<f32x4 *>(to + r * kFewK + ((p ^ (r & 15)) << 2)) = xr[j];
     }
   };
-  const auto store = [&](float *xs) {
+  const auto fetch = [&](int64_t round) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) xs[(tk + e) * STRIDE + t * 16 + tt] = xr[t][e];
+    for (int j = 0; j < L; ++j) xr[j] = get4(A + round * kFewK + at[j], 4);
   };
-  u32x4 vg[UN], vu[UN];
-  const auto weights = [&](int i, int64_t at) {  // rows past the slice: its last one, as zeros
-    const int64_t k = at + (i * kFourWaves + wave) * 4 + g;
-    const float *w = wg + (k < len ? k : len - 1) * a.ldw;
-    const uint32_t keep = k < len ? ~0u : 0u;
-    vg[i] = load_piece(w) & u32x4{keep, keep, keep, keep};
-    vu[i] = load_piece(w + twin) & u32x4{keep, keep, keep, keep};
+  const auto token = [&](const float *from, int i) {
+    return *reinterpret_cast<const f32x4 *>(from + (16 * i + n) * kFewK + (((wave >> 1) * 4 + g) ^ n) * 4);
   };
-  fetch(0);
+  // weights: KC rows c0 + 16 f + n at k = kw .., else rows kw + s at columns c0 + 4 n ..
+  const int64_t c0 = strip * BN + (KC ? 64 * half : 0), cn = c0 + 4 * n;
+  const float *B = a.B[KC ? seg : half] + (KC ? k0 : k0 * a.ldb);
+  const float *bp[4];
 #pragma unroll
-  for (int i = 0; i < UN; ++i) weights(i, 0);
-  store(lds);
-  lds_barrier();
-  int cur = 0;
-#pragma unroll 1
-  for (int64_t at = 0; at < len; at += kFourK) {
-    const bool more = at + kFourK < len;
-    if (more) fetch(at + kFourK);
+  for (int s = 0; s < 4; ++s)
+    bp[s] = KC ? B + min(c0 + 16 * s + n, a.cols - 1) * a.ldb + kw : B + (kw + s) * a.ldb + min(cn, a.cols - 4);
+  f32x4 w[D][4], acc[TT][4];
+  const auto weights = [&](f32x4(&to)[4], int64_t round) {
+    const int64_t by = KC ? round * kFewK : round * kFewK * a.ldb;
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      float x[TT];
+    for (int s = 0; s < 4; ++s) to[s] = get4(bp[s] + by, 4);
+  };
 #pragma unroll
-      for (int t = 0; t < TT; ++t)
-        x[t] = lds[cur + ((i * kFourWaves + wave) * 4 + g) * STRIDE + t * 16 + n];
+  for (int i = 0; i < TT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[i][e] = f32x4{0, 0, 0, 0};
+  // value e of the sums: KC fragment e, else columns 4 n + e
+  const auto multiply = [&](int i, const f32x4 &x, const f32x4(&v)[4]) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
+        acc[i][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(KC ? v[e][s] : v[s][e], x[s], acc[i][e], 0, 0, 0);
+  };
+  if (full > 0) {
+    fetch(0);
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-          acc[0][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vg[i][e]), x[t], acc[0][t][e], 0, 0, 0);
-          acc[1][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vu[i][e]), x[t], acc[1][t][e], 0, 0, 0);
-        }
-      weights(i, more ? at + kFourK : at);  // behind the last ones, these again: no branch parts the loads
-    }
-    cur ^= XS;
-    if (more) store(lds + cur);
+    for (int d = 0; d < D - 1; ++d) weights(w[d], min(static_cast<int64_t>(d), full - 1));
+    store(lds);
+    fetch(full > 1 ? 1 : 0);
     lds_barrier();
-  }
-  // the waves' sums are added in order, tile by tile
+    f32x4 x = token(lds, 0);
+    int cur = 0;
+#pragma unroll 1
+    for (int64_t r = 0; r < full; r += D) {
 #pragma unroll
-  for (int t = 0; t < TT; ++t) {
+      for (int u = 0; u < D; ++u) {
+        if (r + u >= full) break;
+        const int64_t now = r + u, last = full - 1;
+        store(lds + (XS - cur));
+        fetch(now + 2 < last ? now + 2 : last);
+        weights(w[(u + D - 1) % D], now + D - 1 < last ? now + D - 1 : last);
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+        for (int i = 0; i < TT; ++i) {
+          if (i == TT - 1) {
+            lds_barrier();
+            cur = XS - cur;
+          }
+          const f32x4 now_x = x;
+          x = token(lds + cur, (i + 1) % TT);  // behind the last round, what nothing uses
+          multiply(i, now_x, w[u]);
+          // other work between the products, which run for 32 cycles each
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *reinterpret_cast<f32x4 *>(lds + ((q * kFourWaves + wave) * 16 + n) * kFourCols + 16 * g + 4 * r) =
-            f32x4{acc[q][t][0][r], acc[q][t][1][r], acc[q][t][2][r], acc[q][t][3][r]};
-    __syncthreads();
-    for (int i = threadIdx.x; i < 16 * kFourCols; i += NT) {
-      const int64_t token = first + t * 16 + i / kFourCols;
-      const int j = i % kFourCols;
-      const int64_t c1 = strip * kFourCols + j / 4 * 4;
-      const int64_t col = (c1 < a.ff - 4 ? c1 : a.ff - 4) + j % 4;
-      float s[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int w = 0; w < kFourWaves; ++w)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) s[q] += lds[(q * kFourWaves + w) * 16 * kFourCols + i];
-      if (token >= a.N || c1 >= a.ff) continue;
-      if (slices > 1) {
-        float *p = a.part + (slice * 2 * a.N + token) * a.ff + col;
-        p[0] = s[0];
-        p[a.N * a.ff] = s[1];
-      } else {
-        static_cast<float *>(a.H)[token * a.ldh + col] = ff_act(a.act, s[0]) * s[1];
-        if (a.G) {
-          static_cast<float *>(a.G)[token * a.ldg + col] = s[0];
-          static_cast<float *>(a.U)[token * a.ldg + col] = s[1];
+          for (int m = 0; m < 16; ++m) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+          }
+          if (i == TT - 1 || i == TT - 2) __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
+  }
+  if (tail > 0) {
+    lds_barrier();
+    const float *from = A + full * kFewK;
+#pragma unroll
+    for (int j = 0; j < L; ++j) xr[j] = 4 * p < tail ? get4(from + at[j], tail - 4 * p) : f32x4{0, 0, 0, 0};
+    store(lds);
+    const int64_t by = KC ? full * kFewK : full * kFewK * a.ldb;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int64_t left = tail - kw - (KC ? 0 : s);
+      w[0][s] = left > 0 ? get4(bp[s] + by, KC ? left : 4) : f32x4{0, 0, 0, 0};
+    }
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < TT; ++i) multiply(i, token(lds, i), w[0]);
+  }
+  // the waves' sums are added in order, 16 tokens at a time
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
     __syncthreads();
+    float *to = lds + (wave * 16 + n) * 64;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<f32x4 *>(to + (((KC ? 4 * e + g : 4 * g + e) ^ n) << 2)) =
+          KC ? acc[i][e] : f32x4{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+    __syncthreads();
+    // four columns of both halves' sums: of both weights, or neighbours
+    if (threadIdx.x >= 256) continue;
+    const int t = threadIdx.x >> 4, j = (threadIdx.x & 15) * 4;
+    const int64_t row = first + 16 * i + t;
+    if (row >= a.N) continue;
+    f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+    for (int v = 0; v < kFewWaves; ++v) s[v & 1] += *reinterpret_cast<const f32x4 *>(lds + (v * 16 + t) * 64 + (j ^ t << 2));
+    if constexpr (KC) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t col = strip * BN + 64 * h + j;
+        if (col < a.cols) put4(a.part + (slice * a.N + row) * a.cols + col, a.cols - col, s[h]);
+      }
+    } else {
+      if (strip * BN + j >= a.cols) continue;
+      const int64_t col = min(strip * BN + j, a.cols - 4);
+      if (a.slices > 1) {
+        float *q = a.part + (slice * 2 * a.N + row) * a.cols + col;
+        put4(q, 4, s[0]);
+        put4(q + a.N * a.cols, 4, s[1]);
+      } else {
+        f32x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = ff_act(a.out.act, s[0][e]) * s[1][e];
+        put4(static_cast<float *>(a.out.H) + row * a.out.ldh + col, 4, h);
+        if (a.out.G) {
+          put4(static_cast<float *>(a.out.G) + row * a.out.ldg + col, 4, s[0]);
+          put4(static_cast<float *>(a.out.U) + row * a.out.ldg + col, 4, s[1]);
+        }
+      }
+    }
   }
 }
 
@@ -462,6 +528,17 @@ __global__ __launch_bounds__(256) void ff_zero_kernel(FfOut<T> o) {
   const int64_t r = id / per, c = (id - r * per) * 4;
   if (r >= 2 * o.M) return;
   put4((r < o.M ? o.C + r * o.ldc : o.C2 + (r - o.M) * o.ldc) + c, o.N - c, f32x4{0, 0, 0, 0});
+}
+
+// dX: the parts of its sums, in order.
+__global__ __launch_bounds__(256) void ff_sum_kernel(const float *part, int parts, FfOut<float> o) {
+  const int64_t id = group_number() * 256 + threadIdx.x, per = (o.N + 3) / 4;
+  const int64_t r = id / per, c = (id - r * per) * 4, left = o.N - c;
+  if (r >= o.M) return;
+  f32x4 v = {0, 0, 0, 0};
+  const float *p = part + r * o.N + c;
+  for (int q = 0; q < parts; ++q, p += o.M * o.N) v += get4(p, left);
+  put4(o.C + r * o.ldc + c, left, v);
 }
 
 // ---- plans --------------------------------------------------------------------------------
@@ -522,23 +599,30 @@ int vec_slices(int64_t N, int64_t d, int64_t ff) {
 // (4096 x 14336: one token 52 us, 16 tokens 54); others would have to be copied first.
 bool by_vec(int dt, int64_t N, int64_t ff) { return dt == 1 && N <= (ff % 8 == 0 ? 1 : 8) && ff >= 8; }
 
-// float32 weights read as they are, or copied into planes first: 4096 x 14336 with 16 tokens 86
-// and 515 us, 48 175 and 519, 100 340 and 515; 1024 x 4096 17, 23, 48 and 64, 66, 52; with more
-// tokens the planes' products gain (4096 x 14336, 256 tokens: 672 and 550).
-bool by_four(int dt, int64_t N, int64_t ff) { return dt == 0 && N <= 128 && ff >= 4; }
-// Tiles of 16 tokens of a workgroup.  Where the columns are half the CUs' or more, so many that
-// the weights pass once (2048 x 8192, 64 tokens: 61 us, 86 with a tile each); else one, the
-// weights coming from the caches again (1600 x 4267, 48 tokens: 39 us, 69 with four).
-int four_tiles(int64_t N, int64_t ff) {
-  return N <= 16 || ceil_div(ff, kFourCols) < 128 ? 1 : N <= 32 ? 2 : 4;
-}
-// Slices of d: as many as give each CU a workgroup at most (4096 x 14336, one token: 85 us; in
-// two slices, of which a CU holds two, 95), of a round of k or more, 16 at most.
-int four_slices(int64_t N, int64_t d, int64_t ff) {
-  const int64_t groups = ceil_div(ff, kFourCols) * ceil_div(N, 16 * four_tiles(N, ff));
-  const int64_t fit = 256 / groups, most = ceil_div(d, kFourK);
-  const int64_t n = fit < 1 ? 1 : fit < most ? fit : most;
-  return static_cast<int>(n < 16 ? n : 16);
+// float32 weights as they are, or copied into planes first.  us, so, in planes, and of elementary float32
+// products: forward 4096 x 14336 with 160 tokens 337, 557, 345, with 320 681, 768, 747, with 384 759,
+// 774, 883, with 512 915, 832, 1020; 1600 x 4267 with 384 106, 115, 130, with 448 158, 127, 144; backward
+// (dX so, or all in planes) 4096 x 14336 with 128 484, 768, 597, with 384 1287, 1369, 1532, with 512 1612,
+// 1545, 1888.
+constexpr int64_t kFewFloats = 384;
+bool by_few(int dt, int64_t N) { return dt == 0 && N <= kFewFloats; }
+// Tiles of 16 tokens of a workgroup: up to 8 (more would not leave the registers), and as many as the
+// fewest blocks of tokens need.
+int few_tiles(int64_t N) { return static_cast<int>(ceil_div(N, 16 * ceil_div(N, 128))); }
+// Slices of k by the time of as many rounds of workgroups as 256 CUs take, one each: 0.47 us for 64 k of 16
+// tokens, 5 for a workgroup's start and end, and where there are parts, writing and adding them.
+int few_slices(int64_t N, int64_t strips, int64_t segs, int64_t k, int64_t cols) {
+  const int64_t tt = few_tiles(N), groups = strips * ceil_div(N, 16 * tt) * segs, rounds = ceil_div(k, kFewK);
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= 16 && (s == 1 || rounds / s >= 2); ++s) {
+    double us = static_cast<double>(ceil_div(groups * s, 256)) * (static_cast<double>(ceil_div(rounds, s)) * 0.47 * static_cast<double>(tt < 2 ? 2 : tt) + 5.0);
+    if (s * segs > 1) us += 4.0 + 2.0 * sizeof(float) * static_cast<double>(s * segs * N * cols) / 5e6;
+    if (s > 1 && us >= least) continue;
+    least = us;
+    best = s;
+  }
+  return best;
 }
 
 constexpr int64_t kFew = 64;
@@ -567,7 +651,7 @@ MmPlan row_plan(int size, int64_t cols) {
 }
 
 struct FfPlan {
-  bool vec, four, own_x, own_w;  // own: read in place
+  bool vec, few, own_x, own_w;  // own: read in place
   MmPlan t;
   int slices;
   size_t x, w, part, total;
@@ -579,9 +663,9 @@ FfPlan ff_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bool own_w)
     p.vec = true;
     p.slices = vec_slices(N, d, ff);
     if (p.slices > 1) p.part = s.take(sizeof(float) * p.slices * 2 * N * ff);
-  } else if (by_four(dt, N, ff)) {
-    p.four = true;
-    p.slices = four_slices(N, d, ff);
+  } else if (by_few(dt, N) && ff >= 4) {
+    p.few = true;
+    p.slices = few_slices(N, ceil_div(ff, 64), 1, d, 2 * ff);
     if (p.slices > 1) p.part = s.take(sizeof(float) * p.slices * 2 * N * ff);
   } else {
     p.own_x = own_x;
@@ -609,26 +693,33 @@ void launch_vec(const FfArgs &a, int slices, hipStream_t s) {
   if (slices > 1)
     ff_join_kernel<bf16_t><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, slices);
 }
-void launch_four(const FfArgs &a, int slices, hipStream_t s) {
-  const int tt = four_tiles(a.N, a.ff);
-  const dim3 grid = groups_grid(ceil_div(a.ff, kFourCols) * slices * ceil_div(a.N, 16 * tt));
-  if (tt == 1)
-    ff_four_kernel<1><<<grid, kFourWaves * 64, 0, s>>>(a, slices);
-  else if (tt == 2)
-    ff_four_kernel<2><<<grid, kFourWaves * 64, 0, s>>>(a, slices);
-  else
-    ff_four_kernel<4><<<grid, kFourWaves * 64, 0, s>>>(a, slices);
-  if (slices > 1)
-    ff_join_kernel<float><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, slices);
+template <bool KC>
+void launch_few(const FewArgs &a, hipStream_t s) {
+  const int tt = few_tiles(a.N);
+  const dim3 grid = groups_grid(ceil_div(a.cols, KC ? 128 : 64) * a.slices * (KC ? 2 : 1) * ceil_div(a.N, 16 * tt));
+  const auto run = [&](auto *kernel) { kernel<<<grid, kFewWaves * 64, 0, s>>>(a); };
+  switch (tt) {
+    case 1: return run(ff_few_kernel<KC, 1>);
+    case 2: return run(ff_few_kernel<KC, 2>);
+    case 3: return run(ff_few_kernel<KC, 3>);
+    case 4: return run(ff_few_kernel<KC, 4>);
+    case 5: return run(ff_few_kernel<KC, 5>);
+    case 6: return run(ff_few_kernel<KC, 6>);
+    case 7: return run(ff_few_kernel<KC, 7>);
+    default: return run(ff_few_kernel<KC, 8>);
+  }
 }
+const float *f32(const void *p) { return static_cast<const float *>(p); }
 
 template <typename T>
 hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t s) {
   a.part = reinterpret_cast<float *>(ws + p.part);
   if (p.vec) {
     launch_vec(a, p.slices, s);
-  } else if (p.four) {
-    launch_four(a, p.slices, s);
+  } else if (p.few) {
+    launch_few<false>(FewArgs{{f32(a.X)}, {f32(a.Wg), f32(a.Wu)}, a.ldx, a.ldw, a.N, a.d, a.ff, p.slices, a.part, a}, s);
+    if (p.slices > 1)
+      ff_join_kernel<float><<<pieces_grid(a.N, ceil_div(a.ff, 4)), 256, 0, s>>>(a, p.slices);
   } else {
     MmArgs m = {};
     m.k = a.d;
@@ -676,7 +767,8 @@ hipError_t launch_ff_t(int dt, FfArgs a, const FfPlan &p, char *ws, hipStream_t 
 }
 
 struct FfGradPlan {
-  bool own_x, own_w, own_g;
+  bool few, own_x, own_w, own_g;  // few: dX by it
+  int slices;
   MmPlan tx, tw;
   size_t x, w, g, part, total;
 };
@@ -686,10 +778,16 @@ FfGradPlan ff_grad_plan(int dt, int64_t N, int64_t d, int64_t ff, bool own_x, bo
   p.own_x = own_x;
   p.own_w = own_w;
   p.own_g = own_g;
-  p.tx = mm_plan(N, d, 1, ceil_div(ff, kMmK) * 2 * segs_of(dt));
+  p.few = by_few(dt, N);
   p.tw = mm_plan(d, ff, 2, ceil_div(N, kMmK) * segs_of(dt));
   if (!own_x) p.x = s.take(2 * kPlanes[dt] * N * up8(d));
-  if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
+  if (p.few) {
+    p.slices = few_slices(N, ceil_div(d, 128), 2, ff, d);
+    p.tx.part_bytes = sizeof(float) * 2 * p.slices * N * d;
+  } else {
+    p.tx = mm_plan(N, d, 1, ceil_div(ff, kMmK) * 2 * segs_of(dt));
+    if (!own_w) p.w = s.take(2 * 2 * kPlanes[dt] * d * up8(ff));
+  }
   if (!own_g) p.g = s.take(2 * 2 * kPlanes[dt] * N * up8(ff));
   p.part = s.take(p.tx.part_bytes > p.tw.part_bytes ? p.tx.part_bytes : p.tw.part_bytes);
   p.total = s.at;
@@ -733,7 +831,7 @@ hipError_t launch_ff_grad_t(int dt, const FfGradArgs &a, const FfGradPlan &p, ch
     x = to;
     ldx = up8(a.d);
   }
-  if (!p.own_w && a.dX) {
+  if (!p.own_w && !p.few && a.dX) {
     uint16_t *to = reinterpret_cast<uint16_t *>(ws + p.w), *to2 = to + planes * a.d * ff8;
     pack<T>(a.Wg, a.d, a.ff, a.ldw, to, s);
     pack<T>(a.Wu, a.d, a.ff, a.ldw, to2, s);
@@ -742,7 +840,13 @@ hipError_t launch_ff_grad_t(int dt, const FfGradArgs &a, const FfGradPlan &p, ch
     ldw = ff8;
   }
   float *part = reinterpret_cast<float *>(ws + p.part);
-  if (a.dX) {
+  if (a.dX && p.few) {
+    if constexpr (sizeof(T) == 4) {
+      launch_few<true>(FewArgs{{f32(a.dG), f32(a.dU)}, {f32(a.Wg), f32(a.Wu)}, a.ldd, a.ldw, a.N, a.ff, a.d, p.slices, part, {}}, s);
+      ff_sum_kernel<<<pieces_grid(a.N, ceil_div(a.d, 4)), 256, 0, s>>>(
+          part, 2 * p.slices, FfOut<float>{static_cast<float *>(a.dX), nullptr, a.N, a.d, a.lddx, 0});
+    }
+  } else if (a.dX) {
     MmArgs m = {};
     m.k = a.ff;
     m.a.ld = ldd;

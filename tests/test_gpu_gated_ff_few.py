@@ -1,0 +1,75 @@
+"""Up to 384 float32 tokens of the gated feed-forward block and its dX, whose weights are multiplied as
+they are, against the float64 oracle: both sides of every limit between the kernel's forms, lengths
+shorter than a round of 64 and with every rest, columns at the edges of strips, slices.
+
+Tolerance (u = 2^-24, K terms of sizes S): a sum is four chains of K / 4 terms at most, which are added,
+and the slices after them, 16 (dX: 32) at most: u (K / 4 + 4 + 32) S.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01260_amd as sn
+from gpu_helpers import host, log
+from oracle import gated_ff as orc
+from test_gpu_gated_ff import U, _mat, _near
+
+pytestmark = pytest.mark.gpu
+
+TOKENS = [1, 15, 16, 17, 32, 33, 48, 49, 80, 81, 96, 112, 113, 128, 129, 161, 256, 257, 273, 384]
+LENGTHS = [(1, 4), (3, 5), (4, 63), (61, 64), (63, 65), (64, 66), (65, 127), (66, 128), (67, 129), (127, 130),
+           (128, 257), (190, 1030), (512, 100), (1000, 12), (2049, 61), (4100, 36)]
+
+
+def _tol(k, size):
+    return U * (k / 4 + 36) * size
+
+
+def _check(n, d, ff, pad, shift, act="silu"):
+    X = _mat(n, n, d, "f32", pad, 1.0, shift)
+    Wg, Wu = (_mat(s, d, ff, "f32", 2 * pad, d ** -0.5, shift) for s in (1, 2))
+    out = torch.full((3, n, ff + 5), 7.0, device="cuda")
+    H, G, Ut = sn.sn_gated_ff(X, Wg, Wu, act=act, out=out[0, :, :ff], out_g=out[1, :, :ff], out_u=out[2, :, :ff])
+    x, wg, wu = host(X), host(Wg), host(Wu)
+    h, g, u = orc.gated_ff(x, wg, wu, act)
+    tg, tu = _tol(d, np.abs(x) @ np.abs(wg)), _tol(d, np.abs(x) @ np.abs(wu))
+    _near(host(G), g, tg, "G")
+    _near(host(Ut), u, tu, "U")
+    th = 1.2 * tg * (np.abs(u) + tu) + np.abs(orc.act(act, g)[0]) * tu + np.abs(h) * U * (16 + 2 * g * g)
+    _near(host(H), h, th, "H")
+    assert bool((out[:, :, ff:] == 7.0).all())
+    assert torch.equal(sn.sn_gated_ff(X, Wg, Wu, act=act), H)
+    dH = _mat(5, n, ff, "f32", pad, 0.1, shift)
+    dG, dU = (torch.empty(n, ff + pad, device="cuda")[:, :ff] for _ in range(2))
+    room = torch.full((n, d + 3), 7.0, device="cuda")
+    dX, _, _ = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, act=act, dG=dG, dU=dU, out=room[:, :d], want_gw=False)
+    dg, du = host(dG), host(dU)
+    ref, _, _ = orc.products_backward(x, wg, wu, dg, du)
+    _near(host(dX), ref, _tol(ff, np.abs(dg) @ np.abs(wg).T + np.abs(du) @ np.abs(wu).T), "dX")
+    assert bool((room[:, d:] == 7.0).all())
+    again, _, _ = sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, dH, act=act, dG=dG, dU=dU)
+    assert torch.equal(again, dX)
+
+
+@pytest.mark.parametrize("n", TOKENS)
+def test_tokens(n):
+    log(f"[gated ff, f32] {n} tokens")
+    _check(n, 200, 260, 0, 0)
+    _check(n, 131, 197, 1, 3, "gelu")
+
+
+@pytest.mark.parametrize("n", [5, 100, 200])
+@pytest.mark.parametrize("d,ff", LENGTHS, ids=str)
+def test_lengths(n, d, ff):
+    log(f"[gated ff, f32] {n} x {d} x {ff}")
+    _check(n, d, ff, 0, 0)
+    _check(n, d, ff, 3, 1, "relu")
+
+
+@pytest.mark.parametrize("n,d,ff", [(130, 520, 8200), (384, 2050, 4100), (20, 4097, 8195)], ids=str)
+def test_large(n, d, ff):
+    """More workgroups than CUs, and slices of both products."""
+    log(f"[gated ff, f32] {n} x {d} x {ff}")
+    _check(n, d, ff, 1, 1)
