@@ -1122,6 +1122,12 @@ _GATE_FN = {"none": 0, "sigmoid": 1}
 _ACT = {"silu": 0, "gelu": 1, "relu": 2}
 
 
+def _required(**operands):
+    for name, t in operands.items():
+        if t is None:
+            raise SnError(1, f"{name} is required")
+
+
 def _choice(table, name, what):
     if name not in table:
         raise SnError(8, f"{what} must be one of {', '.join(table)}, got {name!r}")
@@ -1157,8 +1163,7 @@ def sn_block_norm(X: torch.Tensor, residual: torch.Tensor, w=None, w_post=None, 
                               stream)
         if r is not None:
             return r
-    if residual is None:
-        raise SnError(1, "residual is required")
+    _required(X=X, residual=residual)
     xp, N, d, ldx = _mat(X, "X")
     dt = _dt(X)
     with _on(stream, X, residual, w, w_post, gate, out, resid_out):
@@ -1200,6 +1205,7 @@ def sn_block_norm_backward(X: torch.Tensor, H: torch.Tensor, dY, w=None, w_post=
                                        gw_post, dgate, out, resid_out, workspace, stream)
         if r is not None:
             return r
+    _required(X=X, H=H)
     xp, N, d, ldx = _mat(X, "X")
     dt = _dt(X)
     with _on(stream, X, H, dY, w, w_post, gate, dH, gw, gw_post, dgate, out, resid_out, workspace):
@@ -1297,6 +1303,7 @@ def sn_gated_ff(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, act: str = 
         r = native.gated_ff(X, Wg, Wu, fn, save, out, out_g, out_u, workspace, stream)
         if r is not None:
             return r
+    _required(X=X, Wg=Wg, Wu=Wu)
     with _on(stream, X, Wg, Wu, out, out_g, out_u, workspace):
         (xp, N, d, ldx, dt), (wg, wu, ff, ldw) = _ff_inputs(X, Wg, Wu)
         if out is None:
@@ -1340,6 +1347,7 @@ def sn_gated_ff_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G:
                                      want_dx, want_gw, workspace, stream)
         if r is not None:
             return r
+    _required(X=X, Wg=Wg, Wu=Wu, G=G, U=U, dH=dH)
     with _on(stream, X, Wg, Wu, G, U, dH, dG, dU, out, gWg, gWu, workspace):
         (xp, N, d, ldx, dt), (wg, wu, ff, ldw) = _ff_inputs(X, Wg, Wu)
         gp, up, ldg = _pair(G, U, ("G", "U"), (N, ff), X.dtype)
@@ -1379,6 +1387,11 @@ def sn_orthogonalize_workspace_bytes(count: int, rows: int, cols: int) -> int:
     return lib().sn_orthogonalize_workspace_bytes(count, rows, cols)
 
 
+def _all_there(**lists):
+    for name, ts in lists.items():
+        _required(**{f"{name}[{i}]": t for i, t in enumerate(ts)})
+
+
 def _matrices(ts, name):
     """sn_tensor array of a list of row-major device matrices."""
     arr = (_Tensor * max(1, len(ts)))()
@@ -1405,8 +1418,10 @@ def sn_orthogonalize(mats, steps: int = 5, out=None, workspace=None, stream=None
         r = native.orthogonalize(mats, steps, out, workspace, stream)
         if r is not None:
             return r
+    _required(mats=mats)
     src = [mats] if one else list(mats)
     dst = None if out is None else [out] if one else list(out)
+    _all_there(mats=src, out=dst or ())
     with _on(stream, *src, *(dst or ()), workspace):
         a = _matrices(src, "mats")
         if dst is None:
@@ -1430,10 +1445,12 @@ def sn_muon_step(W, G, M, lr: float, momentum: float = 0.95, nesterov: bool = Tr
     if native is not None and native.muon_step(W, G, M, lr, momentum, nesterov, weight_decay, scale,
                                                steps, workspace, stream) is not None:
         return W
+    _required(W=W, G=G, M=M)
     one = isinstance(W, torch.Tensor)
     ws_, gs, ms = ([W], [G], [M]) if one else (list(W), list(G), list(M))
     if len(gs) != len(ws_) or len(ms) != len(ws_):
         raise SnError(2, f"{len(ws_)} weights, {len(gs)} gradients, {len(ms)} momenta")
+    _all_there(W=ws_, G=gs, M=ms)
     with _on(stream, *ws_, *gs, *ms, workspace):
         w, g, m = _matrices(ws_, "W"), _matrices(gs, "G"), _matrices(ms, "M")
         buf, have = _orth_workspace(ws_, workspace)

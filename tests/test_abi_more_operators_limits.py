@@ -1,6 +1,7 @@
 """Limits and refusals of the block norm, the gated feed-forward block and the orthogonalised
 updates that no GPU is needed for."""
 import pytest
+import torch
 
 import paper_2506_01260_amd as sn
 from test_abi_more_operators import P, _mats, _orth
@@ -14,3 +15,28 @@ def test_orthogonalising_steps(steps, code):
     st = sn.lib().sn_muon_step(1, _mats(empty), _mats(empty), _mats((None, 0, 60, 60, 0)), 0.1, 0.9, 1, 0.0, 1.0,
                                steps, P[15], 1 << 30, None)
     assert st == code
+
+
+def test_missing_operands():
+    """What a call cannot do without is refused by name, not by an attribute of None."""
+    x = torch.zeros(4, 8)
+    calls = {
+        "X": [lambda: sn.sn_block_norm(None, x), lambda: sn.sn_block_norm_backward(None, x, x),
+              lambda: sn.sn_gated_ff(None, x, x), lambda: sn.sn_gated_ff_backward(None, x, x, x, x, x)],
+        "residual": [lambda: sn.sn_block_norm(x, None)],
+        "H": [lambda: sn.sn_block_norm_backward(x, None, x)],
+        "Wg": [lambda: sn.sn_gated_ff(x, None, x), lambda: sn.sn_gated_ff_backward(x, None, x, x, x, x)],
+        "Wu": [lambda: sn.sn_gated_ff(x, x, None), lambda: sn.sn_gated_ff_backward(x, x, None, x, x, x)],
+        "G": [lambda: sn.sn_gated_ff_backward(x, x, x, None, x, x), lambda: sn.sn_muon_step([x], None, [x], 0.1),
+              lambda: sn.sn_muon_step(x, None, x, 0.1)],
+        "U": [lambda: sn.sn_gated_ff_backward(x, x, x, x, None, x)],
+        "dH": [lambda: sn.sn_gated_ff_backward(x, x, x, x, x, None)],
+        "mats": [lambda: sn.sn_orthogonalize(None), lambda: sn.sn_orthogonalize([x, None])],
+        "W": [lambda: sn.sn_muon_step(None, [x], [x], 0.1), lambda: sn.sn_muon_step([None], [x], [x], 0.1)],
+        "M": [lambda: sn.sn_muon_step([x], [x], None, 0.1), lambda: sn.sn_muon_step([x], [x], [None], 0.1)],
+    }
+    for name, group in calls.items():
+        for k, call in enumerate(group):
+            with pytest.raises(sn.SnError) as e:
+                call()
+            assert e.value.status == 1 and f"{name}" in str(e.value), (name, k, str(e.value))
