@@ -1230,8 +1230,8 @@ int32_t sn_grad_clip(int32_t count, const sn_tensor *grads, const sn_tensor *out
 
 namespace {
 
-// What both calls of the block norm share; gate_cols: 0 for one row.
-int32_t check_block(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt, int32_t post,
+// What both calls of the block norm share; w_post: NULL without the post norm.
+int32_t check_block(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt,
                     const void *w_post, const void *gate, int64_t ldgate, int32_t gate_fn,
                     double alpha, const void *w, double eps) {
   if (!dtype_ok(dt)) return fail(SN_ERR_DTYPE, "unknown dtype %d", dt);
@@ -1246,7 +1246,6 @@ int32_t check_block(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t dt
   if (!elem_aligned(X, dt) || !elem_aligned(gate, dt) || !elem_aligned(w, dt) ||
       !elem_aligned(w_post, dt))
     return fail(SN_ERR_ALIGN, "X, the gate or a gain vector is not aligned to its element size");
-  (void)post;
   return SN_OK;
 }
 
@@ -1385,7 +1384,8 @@ int32_t sn_block_norm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t 
                       int64_t ldr, int32_t post, const void *w_post, const void *gate,
                       int64_t ldgate, int32_t gate_fn, double alpha, const void *w, double eps,
                       void *H, int64_t ldh, void *Y, int64_t ldy, sn_stream stream) {
-  int32_t st = check_block(X, N, d, ldx, dt, post, w_post, gate, ldgate, gate_fn, alpha, w, eps);
+  if (!post) w_post = nullptr;
+  int32_t st = check_block(X, N, d, ldx, dt, w_post, gate, ldgate, gate_fn, alpha, w, eps);
   if (st || (st = check_rows("R", N, d, ldr)) || (st = check_rows("H", N, d, ldh)) ||
       (Y && (st = check_rows("Y", N, d, ldy))))
     return st;
@@ -1400,7 +1400,7 @@ int32_t sn_block_norm(const void *X, int64_t N, int64_t d, int64_t ldx, int32_t 
   if (H != R || ldh != ldr) b.read(span(R, N, d, ldr, es));
   b.read(gate_span(gate, N, d, ldgate, es));
   b.read(span(w, 1, d, d, es));
-  if (post) b.read(span(w_post, 1, d, d, es));
+  b.read(span(w_post, 1, d, d, es));
   b.write(span(Y, N, d, ldy, es));
   if ((st = b.check("sn_block_norm"))) return st;
   sn::BlockNormArgs a = {};
@@ -1440,7 +1440,8 @@ int32_t sn_block_norm_backward(const void *X, int64_t N, int64_t d, int64_t ldx,
                                int64_t lddr, void *dgate, int64_t lddgate, float *dgate_row,
                                float *gw, float *gw_post, void *workspace, size_t workspace_bytes,
                                sn_stream stream) {
-  int32_t st = check_block(X, N, d, ldx, dt, post, w_post, gate, ldgate, gate_fn, alpha, w, eps);
+  if (!post) w_post = nullptr;
+  int32_t st = check_block(X, N, d, ldx, dt, w_post, gate, ldgate, gate_fn, alpha, w, eps);
   if (st || (st = check_rows("H", N, d, ldh)) || (dY && (st = check_rows("dY", N, d, lddy))) ||
       (dH && (st = check_rows("dH", N, d, lddh))) || (st = check_rows("dX", N, d, lddx)) ||
       (st = check_rows("dR", N, d, lddr)) ||
@@ -1473,7 +1474,7 @@ int32_t sn_block_norm_backward(const void *X, int64_t N, int64_t d, int64_t ldx,
   if (dH && !on_h) b.read(span(dH, N, d, lddh, es));
   if (!dgate || !same(dgate, lddgate, gate, ldgate)) b.read(gate_span(gate, N, d, ldgate, es));
   b.read(span(w, 1, d, d, es));
-  if (post) b.read(span(w_post, 1, d, d, es));
+  b.read(span(w_post, 1, d, d, es));
   b.write(span(gw, 1, d, d, 4));
   b.write(span(gw_post, 1, d, d, 4));
   b.write(span(dgate_row, 1, d, d, 4));

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2506_01260_amd as sn
-from test_abi_more_operators import P, _mats, _orth
+from test_abi_more_operators import BLOCK, BLOCK_BASE, BLOCK_BWD, P, _call, _mats, _orth
 
 
 @pytest.mark.parametrize("steps,code", [(1, 0), (8, 0), (9, 2), (16, 2)])
@@ -40,3 +40,16 @@ def test_missing_operands():
             with pytest.raises(sn.SnError) as e:
                 call()
             assert e.value.status == 1 and f"{name}" in str(e.value), (name, k, str(e.value))
+
+
+def test_gains_without_the_post_norm_are_not_looked_at():
+    """w_post is read only with the post norm: without it any pointer goes, whatever its alignment.
+    (Each call is refused for another reason, behind that check, so that nothing runs.)"""
+    fwd = dict(BLOCK_BASE, post=0, w_post=P[2] + 1)
+    assert _call("sn_block_norm", BLOCK, fwd, dict(Y=P[5])) == 5
+    assert _call("sn_block_norm", BLOCK, fwd, dict(Y=P[5], post=1)) == 4
+    bwd = {k: v for k, v in fwd.items() if k not in ("R", "ldr", "H", "ldh", "Y", "ldy")}
+    bwd.update(H=P[1], ldh=300, dY=P[5], lddy=300, dH=P[6], lddh=300, dX=P[7], lddx=300, dR=P[8], lddr=300,
+               dgate=None, lddgate=0, dgate_row=None, gw=P[9], gw_post=None, ws=None, ws_bytes=0)
+    assert _call("sn_block_norm_backward", BLOCK_BWD, bwd, {}) == 1
+    assert _call("sn_block_norm_backward", BLOCK_BWD, bwd, dict(post=1)) == 4
