@@ -73,12 +73,17 @@ __device__ const u32x4 mm_zeros = {0, 0, 0, 0};
 // assembly, as the compiler would wait for every such load before the first transposed
 // read after it (22 percent of the time of an 8192 x 8192 x 8192 product); it has no output
 // register, and the tile loop waits for it.
+// (The compiler keeps m0 for itself and warns of its name among the clobbered: it must not place this
+// between its own write of m0 and what that is for.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void lds_load_16(const void *src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(src)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
   return static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)(p)));
