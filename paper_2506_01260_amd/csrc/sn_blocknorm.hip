@@ -12,7 +12,7 @@
 // (backward: two joint) sums and its outputs.  R threads hold a row in K pieces each; with
 // R = 64 a wave has a row of its own and no barrier.
 // bf16 with one gate row: 32768 x 4096 190 us, 5.7 TB/s (add of two arrays: 6.2); backward
-// 16383 x 8192 308 us, 5.2 TB/s; with a gate and its gradient for each token 4999 x 1600 36 us,
+// 16383 x 8192 308 us, 5.2 TB/s; with a gate and its gradient for each token 4999 x 1600 37 us,
 // of it 4 the second launch that joins the column sums; one token 3.5 us in the kernel.
 #include "sn_internal.h"
 #include "sn_rows.h"
@@ -643,14 +643,19 @@ hipError_t launch_grad_t(int dt, const BlockNormGradArgs &a, hipStream_t s) {
     block_norm_grad_kernel<T, 256, 2, 256, WHOLE, true><<<g, 256, 0, s>>>(a);
   else if (n <= 1024)
     block_norm_grad_kernel<T, 512, 2, 512, WHOLE, true><<<g, 512, 0, s>>>(a);
-  else if (n <= 1536)
+  else if (n <= 1536)  // (ragged bf16 rows: 12 registers in scratch memory)
     block_norm_grad_kernel<T, 512, 3, 512, WHOLE, false><<<g, 512, 0, s>>>(a);
-  else if (n <= 2048 && sizeof(T) == 4)  // eight values of bf16 would not leave the registers
-    block_norm_grad_kernel<T, 1024, 2, 1024, WHOLE, false><<<g, 1024, 0, s>>>(a);
-  else if (n <= 2048)
-    block_norm_grad_kernel<T, 512, 4, 512, WHOLE, false><<<g, 512, 0, s>>>(a);
-  else
+  else if (n <= 2048) {
+    // Such rows and their three column sums do not fit the registers: of float32 2 go to scratch memory
+    // (ragged rows 8), of bf16 60 (119; of 1024 x 2, whose threads have half as many, 80 and 103).
+    // bf16 4096 x 16000 takes 390 us, 2.0 TB/s, 4096 x 13001 515.
+    if constexpr (sizeof(T) == 4)
+      block_norm_grad_kernel<T, 1024, 2, 1024, WHOLE, false><<<g, 1024, 0, s>>>(a);
+    else
+      block_norm_grad_kernel<T, 512, 4, 512, WHOLE, false><<<g, 512, 0, s>>>(a);
+  } else {
     block_norm_grad_long_kernel<T><<<g, 1024, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -85,8 +85,9 @@ __device__ __forceinline__ float bf16_near(float v) {
   return fabsf(r) == INFINITY ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : r;
 }
 // The planes of eight values: bf16 as it is, float32 as three bf16 that add up to it
-// exactly (8 bits each, signed), the second times 2^7 and the third times 2^14: at most a
-// quarter of the first, so that their products do not overflow before it does, and no
+// exactly (8 bits each, signed), the second times 2^7 and the third times 2^14: at most a half and
+// a quarter of the first (near the largest value, where the first is cut and not rounded, the
+// second is as large), so that their products do not overflow before it does, and no
 // smaller than it by more than their leading zeros.  An infinity or a NaN has nothing left
 // after the first.
 constexpr float kUp = 128.0f;
