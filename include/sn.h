@@ -601,6 +601,11 @@ int32_t sn_rmsnorm_backward(const void *H, int64_t N, int64_t d, int64_t ldh, in
 /* over rows of d columns, in float32; g is the gate or its sigmoid.  h is    */
 /* rounded to dt where it is stored, and y is made from the sum before that.  */
 /* Squares are summed as sn_rmsnorm sums them, with its limits.               */
+/* A residual stream that the codec carries without loss (table + subspace)   */
+/* stays one with alpha = 1, no gate and no w_post: the norm itself scales    */
+/* whole rows.  A gate or gains scale columns, and another alpha the table's  */
+/* part too: what such a block leaves crosses a stage boundary with loss.     */
+/* (w is free: y stays in the stage.)                                         */
 /* ------------------------------------------------------------------------ */
 
 /* The gate's function. */

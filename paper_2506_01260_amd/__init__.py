@@ -1153,7 +1153,8 @@ def sn_block_norm(X: torch.Tensor, residual: torch.Tensor, w=None, w_post=None, 
     """(Y, H): a block's end and the next one's norm, H = alpha residual + g Z with Z = X w_post /
     rms(X) (X itself with post=False), and Y = H w / rms(H) (None with next_norm=False).  gate:
     None, d values for all tokens, or a row for each; g is the gate or (gate_fn "sigmoid") its
-    sigmoid.  resid_out may be X or residual."""
+    sigmoid.  resid_out may be X or residual.  Where H crosses a stage boundary, only alpha = 1, no
+    gate and no w_post keep it free of loss."""
     fn = _choice(_GATE_FN, gate_fn, "gate_fn")
     if not next_norm and out is not None:
         raise SnError(2, "out belongs to the next norm")

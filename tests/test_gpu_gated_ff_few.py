@@ -73,3 +73,24 @@ def test_large(n, d, ff):
     """More workgroups than CUs, and slices of both products."""
     log(f"[gated ff, f32] {n} x {d} x {ff}")
     _check(n, d, ff, 1, 1)
+
+
+@pytest.mark.parametrize("which", ["X", "weights"])
+def test_offsets_past_32_bits(which):
+    """Rows so far apart that their elements' numbers pass 2^31."""
+    log(f"[gated ff, f32] far rows of {which}")
+    n, d, ff = 300, 2100, 96
+    far = 1 << 23 if which == "X" else 0
+    room = torch.empty(n * (far or d), device="cuda")
+    X = room.view(n, far or d)[:, :d]
+    X.copy_(_mat(1, n, d, "f32"))
+    ld = (1 << 20) + 40 if which == "weights" else 2 * ff
+    W = torch.empty(d * ld, device="cuda").view(d, ld)[:, :2 * ff]
+    W.copy_(_mat(2, d, 2 * ff, "f32", 0, d ** -0.5))
+    H, G, Ut = sn.sn_gated_ff(X, W[:, :ff], W[:, ff:], save=True)
+    near = sn.sn_gated_ff(X.clone(), W[:, :ff].clone(), W[:, ff:].clone(), save=True)
+    assert all(torch.equal(a, b) for a, b in zip((H, G, Ut), near))
+    dH = _mat(3, n, ff, "f32", 0, 0.1)
+    a = sn.sn_gated_ff_backward(X, W[:, :ff], W[:, ff:], G, Ut, dH)
+    b = sn.sn_gated_ff_backward(X.clone(), W[:, :ff].clone(), W[:, ff:].clone(), G, Ut, dH)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
