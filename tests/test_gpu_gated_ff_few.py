@@ -94,3 +94,39 @@ def test_offsets_past_32_bits(which):
     a = sn.sn_gated_ff_backward(X, W[:, :ff], W[:, ff:], G, Ut, dH)
     b = sn.sn_gated_ff_backward(X.clone(), W[:, :ff].clone(), W[:, ff:].clone(), G, Ut, dH)
     assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
+@pytest.mark.parametrize("n,d,ff", [(20, 2000, 70), (130, 1300, 200), (384, 640, 1000)], ids=str)
+def test_calls_keep_to_their_workspace(n, d, ff):
+    """Slices' parts lie in the workspace; behind it nothing is written."""
+    log(f"[gated ff, f32, workspace] {n} x {d} x {ff}")
+    X, Wg, Wu = _mat(1, n, d, "f32"), _mat(2, d, ff, "f32", 0, d ** -0.5), _mat(3, d, ff, "f32", 0, d ** -0.5)
+    f = sn.sn_gated_ff_workspace_bytes(n, d, ff, d, ff, 0, True)
+    b = sn.sn_gated_ff_backward_workspace_bytes(n, d, ff, d, ff, ff, 0, True)
+    assert f > 0 and b > 0
+    H, G, Ut = sn.sn_gated_ff(X, Wg, Wu, save=True)
+    for need, call, want in ((f, lambda ws: sn.sn_gated_ff(X, Wg, Wu, save=True, workspace=ws), (H, G, Ut)),
+                             (b, lambda ws: sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, H, workspace=ws),
+                              sn.sn_gated_ff_backward(X, Wg, Wu, G, Ut, H))):
+        room = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+        got = call(room[:need])
+        assert bool((room[need:] == 0x5A).all()) and all(torch.equal(s, t) for s, t in zip(got, want))
+
+
+def test_two_streams_at_once():
+    log("[gated ff, f32, streams]")
+    n, d, ff = 200, 512, 1100
+    Wg, Wu = _mat(2, d, ff, "f32", 0, d ** -0.5), _mat(3, d, ff, "f32", 0, d ** -0.5)
+    X = [_mat(k, n, d, "f32") for k in (4, 5)]
+
+    def calls(x, stream=None):
+        H, G, Ut = sn.sn_gated_ff(x, Wg, Wu, save=True, stream=stream)
+        return (H, G, Ut, *sn.sn_gated_ff_backward(x, Wg, Wu, G, Ut, H, stream=stream))
+    want = [calls(x) for x in X]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        got = [calls(x, s) for x, s in zip(X, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(s, t) for s, t in zip(a, b))
